@@ -511,6 +511,191 @@ int vda_readout(const void* q, const float* S_fwd, const float* S_rev,
                 const float* gate, int F, int N, int H, int d_k, int d_v,
                 int is_f32, void* out, hipStream_t stream);
 
+/* ------------------------------------------------------------------------- */
+/* The token-wise gated delta rule (Eq. 2)                                    */
+/* ------------------------------------------------------------------------- */
+
+/* Layouts of the tensors below. */
+typedef enum {
+  VDA_LAYOUT_HEADS = 0, /* [heads][tokens][d], as vda_prep writes              */
+  VDA_LAYOUT_TOKENS = 1 /* [tokens][heads][d], as the projections are          */
+} vda_layout;
+
+/*
+ * One problem of the token-wise rule (Sec. 2.4, Eq. 2), with one decay per
+ * token and head.  Each sequence and value head has a state S (d_v x d_k,
+ * fp32); its tokens, in order, give
+ *     Sbar = exp(g_t) S,   e_t = v_t - Sbar k_t,
+ *     S = Sbar + beta_t e_t k_t^T,   o_t = scale * S q_t.
+ *  - T tokens in n_seqs sequences: with cu_seqlens NULL, n_seqs sequences of
+ *    T / n_seqs consecutive tokens each (VDA_ERR_SIZE if that is no whole
+ *    number); otherwise cu_seqlens is a DEVICE pointer to n_seqs + 1 int32
+ *    offsets, not decreasing, sequence i being tokens cu_seqlens[i] ..
+ *    cu_seqlens[i + 1] - 1.  Sequences may be empty.  Outputs of tokens before
+ *    the first and behind the last sequence are left as they are.  The host
+ *    does not see the offsets: ones outside [0, T] are taken as the nearest
+ *    bound, and a list that decreases gives undefined values, but nothing
+ *    outside the tensors is read or written.
+ *  - H_k heads of q and k, H_v = G * H_k heads of v, g, beta, states and
+ *    output: value head h reads key head h / G.  d_k, d_v in {32, 64, 128}.
+ *  - layout (a vda_layout): heads: q, k [H_k][T][d_k], v, out [H_v][T][d_v],
+ *    g, beta [H_v][T]; tokens: q, k [T][H_k][d_k], v, out [T][H_v][d_v], g,
+ *    beta [T][H_v].  A batch [B][H][L][d] of equal clips in the heads layout is
+ *    H_k = B * heads, n_seqs = 1, T = L.
+ *  - storage of q, k, v, out and their gradients: bf16 (is_f32 == 0) or fp32.
+ *    g (log decay, <= 0; -inf resets the state; positive values are not
+ *    checked, and grow it) and beta (write strength, any sign; the rule is stable for
+ *    beta |k|^2 in [0, 2]) are fp32.
+ * A NaN or infinity in a token's q, k, v, g or beta (but g = -inf) makes the
+ * outputs of its aligned group of 64 tokens of its sequence and head undefined,
+ * and those of all later ones; other sequences and heads are not touched.
+ * bf16 storage: products run on bf16 matrix cores with fp32 accumulation;
+ * the state, what is written to it and the triangular inverses are carried as
+ * two bf16 parts (about 16 mantissa bits) where they enter a product, once
+ * rounded only where the product reaches a bf16 output alone.  fp32 storage: fp32
+ * throughout.
+ */
+typedef struct vda_delta_problem {
+  int T;
+  int n_seqs;
+  const int* cu_seqlens;
+  int H_k, H_v;
+  int d_k, d_v;
+  int layout;
+  int is_f32;
+  float scale;
+} vda_delta_problem;
+
+/*
+ * vda_delta_forward -- the rule over whole sequences, in chunks of 64 tokens.
+ *  - S_in: the states the sequences start from, [n_seqs][H_v][d_v][d_k] fp32,
+ *    or NULL (zero).  S_out: the states behind them, likewise, or NULL.  An
+ *    empty sequence's state passes through.
+ *  - work: a caller-owned DEVICE buffer of vda_delta_forward_workspace(p)
+ *    bytes, queried with the call's device current; its contents need not be
+ *    kept.  Calls that may run at the same time (other streams, graphs
+ *    replayed side by side) need buffers of their own.
+ * Long sequences of few heads are cut into segments whose maps are scanned
+ * side by side and joined (fp32), so results depend on the sizes, but not on
+ * timing: equal calls on equal devices give equal bits.
+ * q, k, v, out, states and work 16-byte aligned, g, beta and cu_seqlens 4-byte
+ * aligned; no output or work buffer may overlap an input or another output
+ * (S_out is not S_in).  Nothing is allocated or copied: the call can be
+ * captured into a graph.  Errors: VDA_ERR_NULL, VDA_ERR_SIZE,
+ * VDA_ERR_UNSUPPORTED (head dimensions, layout), VDA_ERR_ALIGN,
+ * VDA_ERR_OVERLAP, VDA_ERR_HIP.
+ */
+int vda_delta_forward(const vda_delta_problem* p, const void* q, const void* k, const void* v,
+                      const float* g, const float* beta, const float* S_in, void* out,
+                      float* S_out, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_delta_forward on the current device (0 for
+ * an invalid problem). */
+size_t vda_delta_forward_workspace(const vda_delta_problem* p);
+
+/*
+ * vda_delta_backward -- the gradients of vda_delta_forward: given dout (of
+ * out) and dS_out (of S_out, or NULL: zero), those of q, k, v, g, beta and
+ * S_in.  Nothing is kept from the forward call: states are computed again.
+ *  - dq, dk, dv as q, k, v (dq and dk summed over the value heads that share
+ *    them), dg, dbeta as g, beta, fp32; dS_in [n_seqs][H_v][d_v][d_k] fp32 or
+ *    NULL.  dg is the gradient of the log decay; where g < -200 (a decay of
+ *    zero in fp32) it is 0.
+ *  - work: vda_delta_backward_workspace(p) bytes, as above: mostly the states
+ *    at every 64th token and their gradients, 16 d_k d_v bytes per 64 tokens
+ *    of a head.
+ * Deterministic; otherwise as vda_delta_forward.
+ */
+int vda_delta_backward(const vda_delta_problem* p, const void* dout, const void* q, const void* k,
+                       const void* v, const float* g, const float* beta, const float* S_in,
+                       const float* dS_out, void* dq, void* dk, void* dv, float* dg, float* dbeta,
+                       float* dS_in, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_delta_backward on the current device (0 for
+ * an invalid problem). */
+size_t vda_delta_backward_workspace(const vda_delta_problem* p);
+
+/*
+ * vda_delta_step -- the rule's recurrent form: `tokens` further tokens of each
+ * of n sequences, whose states live in a pool and are updated in place.
+ *  - q, k [n][tokens][H_k][d_k], v, out [n][tokens][H_v][d_v] (bf16 or fp32
+ *    by is_f32), g, beta [n][tokens][H_v] fp32; scale, heads and dimensions as
+ *    above.
+ *  - state [n_slots][H_v][d_v][d_k] fp32.  slots: DEVICE pointer to n int32,
+ *    sequence i's slot of the pool, or NULL (slot i; then n <= n_slots).  A
+ *    slot outside [0, n_slots) marks padding: nothing of that row is read or
+ *    written, its part of out included.  Slots must be distinct: a slot given
+ *    twice has undefined contents afterwards.
+ * fp32 arithmetic; bound by reading and writing the states, 8 d_v d_k H_v
+ * bytes a sequence.  Needs no workspace.  Alignment, overlap (of out and of
+ * the whole pool) and errors as vda_delta_forward.
+ */
+int vda_delta_step(const void* q, const void* k, const void* v, const float* g, const float* beta,
+                   int n, int tokens, int H_k, int H_v, int d_k, int d_v, int is_f32, float scale,
+                   const int* slots, int n_slots, float* state, void* out, hipStream_t stream);
+
+/* ------------------------------------------------------------------------- */
+/* Rotary positions over time, height and width                               */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * Options of vda_rope.
+ *  - pairs_t, pairs_h, pairs_w: channel pairs of a head that each axis turns,
+ *    in this order: pair p < pairs_t by the token's time, the next pairs_h by
+ *    its height, the next pairs_w by its width.  Their sum R is at least 1, at
+ *    most d / 2 (VDA_ERR_SIZE) and a multiple of 8 (VDA_ERR_UNSUPPORTED);
+ *    channels from 2 R on are not turned.
+ *  - interleaved: pair p is channels 2 p and 2 p + 1; otherwise p and R + p.
+ *  - l2: each token of each head is divided by sqrt(sum of its d squared
+ *    channels + 1e-6) first (the feature map of Sec. 2.3; the rotation keeps
+ *    the length).
+ *  - layout (a vda_layout) of the output: heads [B * H][L][d] (index b * H +
+ *    h, as vda_prep writes), tokens [B * L][H * d].
+ *  - grid_h, grid_w, frame_offset: the tokens' positions where no list is
+ *    given: token n of a clip is at time frame_offset + n / (grid_h * grid_w),
+ *    height (n / grid_w) % grid_h, width n % grid_w.  All >= 0, the grid >= 1.
+ *  - x_row_stride, dx_row_stride: elements from one token's row of x (of dx)
+ *    to the next, 0 for H * d; larger where x is a slice of a fused
+ *    projection.  A multiple of 16 bytes.
+ */
+typedef struct vda_rope_options {
+  int pairs_t, pairs_h, pairs_w;
+  int interleaved;
+  int l2;
+  int layout;
+  int grid_h, grid_w, frame_offset;
+  int x_row_stride, dx_row_stride;
+} vda_rope_options;
+
+/*
+ * vda_rope -- rotary positions from the token-major projection to the heads:
+ * pair (x0, x1) of a head becomes (x0 cos a - x1 sin a, x0 sin a + x1 cos a)
+ * with a = position * inv_freq[p].
+ *  - x [B * L][H * d] (rows x_row_stride apart), bf16 or fp32 (is_f32); out of
+ *    the same type.  Neighbouring slices (q and k of a fused projection) are one
+ *    call over the heads of both.
+ *  - inv_freq: DEVICE, [R] fp32.  positions: DEVICE, [B * L][3] int32 (time,
+ *    height, width; any value), or NULL (the grid).
+ *  - d in {16, 32, 64, 128}; B, L, H >= 1.
+ * The angle is formed in 64 bits and reduced to one turn before the fp32
+ * cosine and sine, so far positions keep their accuracy; the rotation is fp32
+ * and rounded to the storage type once.  x and out 16-byte, the lists 4-byte
+ * aligned; out must not overlap the inputs.  Errors: VDA_ERR_NULL,
+ * VDA_ERR_SIZE, VDA_ERR_UNSUPPORTED, VDA_ERR_ALIGN, VDA_ERR_OVERLAP,
+ * VDA_ERR_HIP.
+ */
+int vda_rope(const void* x, const float* inv_freq, const int* positions, int B, int L, int H, int d,
+             const vda_rope_options* opts, int is_f32, void* out, hipStream_t stream);
+
+/*
+ * vda_rope_backward -- the gradient of vda_rope: dout in the output's layout
+ * to dx [B * L][H * d] (rows dx_row_stride apart).  x is the forward input,
+ * read with l2 only (otherwise it may be NULL).  Otherwise as vda_rope.
+ */
+int vda_rope_backward(const void* dout, const void* x, const float* inv_freq, const int* positions,
+                      int B, int L, int H, int d, const vda_rope_options* opts, int is_f32, void* dx,
+                      hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

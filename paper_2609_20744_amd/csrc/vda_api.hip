@@ -11,34 +11,26 @@
 
 #include "../../include/vda.h"
 #include "vda_common.h"
+#include "vda_host.h"
 #include "vda_launch.h"
 
 namespace {
 
-constexpr int kMaxDevices = 64;
-
-bool supported_dim(int d) { return d == 32 || d == 64 || d == 128; }
+using vda::aligned;
+using vda::current_device_cus;
+using vda::hip_status;
+using vda::kMaxDevices;
+using vda::overlaps;
+using vda::Range;
+using vda::range_of;
+using vda::round_up;
+using vda::supported_dim;
 
 // The whole forward also takes 16-channel heads, run as zero-padded 32-channel
 // heads (the stage entry points take only the kernels' own widths).
 bool forward_dim(int d) { return d == 16 || supported_dim(d); }
 
 int padded_dim(int d) { return d < 32 ? 32 : d; }
-
-size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-struct Range {
-  uintptr_t lo, hi;  // [lo, hi)
-};
-
-Range range_of(const void* p, size_t bytes) {
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return Range{lo, lo + bytes};
-}
-
-bool overlaps(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
 
 // Shape checks shared by every entry point.  Grids are one-dimensional with
 // one workgroup per (frame, head, split/chunk), so H*F*64 must fit 31 bits.
@@ -54,21 +46,6 @@ int check_shape(int F, int N, int H, int d_k, int d_v, bool forward = false) {
   if ((long long)N * dmax * 4 > 0x7fffffffLL) return VDA_ERR_SIZE;
   if ((long long)F * dmax * dmax * 4 > 0x7fffffffLL) return VDA_ERR_SIZE;
   return VDA_OK;
-}
-
-int hip_status(hipError_t e) { return e == hipSuccess ? VDA_OK : VDA_ERR_HIP; }
-
-int current_device_cus() {
-  static int cus[kMaxDevices] = {0};
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 256;
-  if (cus[dev] == 0) {
-    int c = 0;
-    if (hipDeviceGetAttribute(&c, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || c <= 0)
-      c = 256;
-    cus[dev] = c;
-  }
-  return cus[dev];
 }
 
 // Library-owned workspace cache per device.  Buffers come from hipMalloc

@@ -1,0 +1,415 @@
+// Internal definitions of the token-wise gated delta rule (Eq. 2), shared by
+// its kernels and its host code.
+//
+// Tokens are taken in chunks of 64.  With S the state entering a chunk
+// (d_v x d_k), G_i the sum of the chunk's log decays up to token i,
+// D_ij = e^(G_i - G_j), gam_i = e^(G_i), eta_i = e^(G_63 - G_i):
+//     L_ij = D_ij k_i.k_j (i > j),   T = (I + diag(beta) L)^-1,
+//     P_ij = scale D_ij q_i.k_j (i >= j),
+//     N = T diag(beta) (V - diag(gam) K S^T)   N_i = beta_i e_i, what token i writes
+//     O = scale diag(gam) Q S^T + P N
+//     S <- gam_63 S + N^T diag(eta) K
+// T and P do not depend on the state; the chunk-preparation kernel makes them
+// for all chunks at once, and the scans carry the state.
+#pragma once
+
+#include "vda_common.h"
+
+namespace vda {
+
+constexpr int kChunk = 64;  // tokens of a chunk
+
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------
+// Matrix operands.  A product contracts 32 indices a step; lane (li, lg) =
+// (lane % 16, lane / 16) holds, of the operand's row (or column) li, the
+// indices 4 lg + e and 16 + 4 lg + e, e < 4.  That is the order in which a
+// lane holds the rows of two 16 x 16 results, so a result whose rows are the
+// next product's contraction goes into it from registers.
+//
+// bf16 storage: an exact operand X is one bf16 vector (inputs, which are
+// bf16); a wide operand W is two, hi = bf16(x) and lo = bf16(x - hi), about
+// 16 mantissa bits, for values that exist in fp32 only: states, writes and
+// the triangular inverse go through such products (lo * lo is left out), so
+// that the state and the gates' gradients keep fp32-like accuracy (2^-17 a
+// factor); products that only reach a bf16 output take `head`, one rounding.
+// fp32 storage: both are fp32 vectors, on the fp32 matrix cores.
+// ---------------------------------------------------------------------------
+template <bool F32>
+struct Op;
+
+template <>
+struct Op<false> {
+  typedef uint16_t Elem;
+  typedef bf16x8 X;
+  struct W {
+    bf16x8 hi, lo;
+  };
+  static __device__ __forceinline__ X narrow(floatx4 a, floatx4 b) {
+    X x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = (__bf16)a[e], x[4 + e] = (__bf16)b[e];
+    return x;
+  }
+  static __device__ __forceinline__ W wide(floatx4 a, floatx4 b) {
+    W w;
+    w.hi = narrow(a, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w.lo[e] = (__bf16)(a[e] - (float)w.hi[e]);
+      w.lo[4 + e] = (__bf16)(b[e] - (float)w.hi[4 + e]);
+    }
+    return w;
+  }
+  static __device__ __forceinline__ X head(const W& w) { return w.hi; }
+  static __device__ __forceinline__ floatx4 mma(X a, X b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ floatx4 mma(X a, const W& b, floatx4 c) {
+    return mma(a, b.hi, mma(a, b.lo, c));
+  }
+  static __device__ __forceinline__ floatx4 mma(const W& a, X b, floatx4 c) {
+    return mma(a.hi, b, mma(a.lo, b, c));
+  }
+  static __device__ __forceinline__ floatx4 mma(const W& a, const W& b, floatx4 c) {
+    return mma(a.hi, b.hi, mma(a.hi, b.lo, mma(a.lo, b.hi, c)));
+  }
+  static __device__ __forceinline__ float value(X x, int e) { return (float)x[e]; }
+  static __device__ __forceinline__ float value(const W& w, int e) {
+    return (float)w.hi[e] + (float)w.lo[e];
+  }
+};
+
+template <>
+struct Op<true> {
+  typedef float Elem;
+  typedef floatx8 X;
+  struct W {
+    floatx8 v;
+  };
+  static __device__ __forceinline__ X narrow(floatx4 a, floatx4 b) {
+    return floatx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+  static __device__ __forceinline__ W wide(floatx4 a, floatx4 b) { return W{narrow(a, b)}; }
+  static __device__ __forceinline__ X head(const W& w) { return w.v; }
+  static __device__ __forceinline__ floatx4 mma(X a, X b, floatx4 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ floatx4 mma(X a, const W& b, floatx4 c) { return mma(a, b.v, c); }
+  static __device__ __forceinline__ floatx4 mma(const W& a, X b, floatx4 c) { return mma(a.v, b, c); }
+  static __device__ __forceinline__ floatx4 mma(const W& a, const W& b, floatx4 c) {
+    return mma(a.v, b.v, c);
+  }
+  static __device__ __forceinline__ float value(X x, int e) { return x[e]; }
+  static __device__ __forceinline__ float value(const W& w, int e) { return w.v[e]; }
+};
+
+// ---------------------------------------------------------------------------
+// Tiles in LDS: rows of 2^lu 16-byte units, unit u of row r at position
+// u ^ swizzle(r), so that both ways of reading an operand (16 rows at one
+// column, and columns of a few rows) spread over the banks with no padding:
+// tiles are filled by loads that go straight to LDS, 64 consecutive units an
+// instruction.
+// ---------------------------------------------------------------------------
+template <bool F32>
+__device__ __forceinline__ int swizzle(int r, int lu) {
+  if (F32) return lu >= 4 ? (r & 15) : (r & 7);
+  if (lu >= 4) return ((r & 7) << 1) | ((r >> 3) & 1);
+  if (lu == 3) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
+  return (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+
+// Row `r` of a tile as an operand, contraction step s along the row.
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X row_op(const char* tile, int lu, int r, int s, int lg) {
+  const int sw = swizzle<F32>(r, lu);
+  const char* row = tile + ((size_t)r << (lu + 4));
+  if constexpr (F32) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(row + (((8 * s + lg) ^ sw) << 4));
+    const floatx4 b = *reinterpret_cast<const floatx4*>(row + (((8 * s + 4 + lg) ^ sw) << 4));
+    return Op<true>::narrow(a, b);
+  } else {
+    const int u = 4 * s + (lg >> 1), h = (lg & 1) * 8;
+    const uint2 a = *reinterpret_cast<const uint2*>(row + ((u ^ sw) << 4) + h);
+    const uint2 b = *reinterpret_cast<const uint2*>(row + (((u + 2) ^ sw) << 4) + h);
+    return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
+  }
+}
+
+// Four rows r0 + 4 lg .. + 3 of column c0 + li.  bf16: ds_read_b64_tr_b16,
+// in which lane i of 16 receives element i % 4 of the 8-byte pieces that
+// lanes i / 4 + 4 e address.
+__device__ __forceinline__ shortx4 tr_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
+  const int r = r0 + 4 * lg + (li >> 2);
+  const int u = (c0 >> 3) + ((li & 3) >> 1);
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_shortx4*)(tile + ((size_t)r << (lu + 4)) + ((u ^ swizzle<false>(r, lu)) << 4) + (li & 1) * 8));
+}
+
+__device__ __forceinline__ floatx4 f32_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int r = r0 + 4 * lg + e;
+    v[e] = *reinterpret_cast<const float*>(tile + ((size_t)r << (lu + 4)) +
+                                           ((((c0 + li) >> 2) ^ swizzle<true>(r, lu)) << 4) +
+                                           (li & 3) * 4);
+  }
+  return v;
+}
+
+// Column c0 + li of a tile as an operand, contraction over rows r0 .. r0 + 31.
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X col_op(const char* tile, int lu, int r0, int c0, int li,
+                                                      int lg) {
+  if constexpr (F32) {
+    return Op<true>::narrow(f32_rows(tile, lu, r0, c0, li, lg), f32_rows(tile, lu, r0 + 16, c0, li, lg));
+  } else {
+    const shortx4 a = tr_rows(tile, lu, r0, c0, li, lg), b = tr_rows(tile, lu, r0 + 16, c0, li, lg);
+    typedef short shortx8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(bf16x8, shortx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+  }
+}
+
+// Rows r0 + 4 lg .. + 3 of column c0 + li as fp32 (where a result has them).
+template <bool F32>
+__device__ __forceinline__ floatx4 result_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
+  if constexpr (F32) {
+    return f32_rows(tile, lu, r0, c0, li, lg);
+  } else {
+    const shortx4 a = tr_rows(tile, lu, r0, c0, li, lg);
+    floatx4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16);
+    return v;
+  }
+}
+
+// Copies `units` (a multiple of 64) 16-byte units of a tile, `rows` rows of
+// 2^lu units taken at row_bytes apart, into LDS with the swizzle; the waves
+// share the instructions.  A row at or past `len` repeats row len - 1, so
+// that every address is the sequence's own (what such rows meet is zero:
+// their writes, their strengths, their stores).
+template <bool F32>
+__device__ __forceinline__ void copy_rows(__amdgpu_buffer_rsrc_t src, char* tile, int lu, int rows,
+                                          int len, uint32_t row_bytes, int wave, int waves, int lane) {
+  const int pieces = (rows << lu) >> 6;
+  for (int p = wave; p < pieces; p += waves) {
+    const int u = p * 64 + lane;
+    const int r = u >> lu;
+    const int from = (u & ((1 << lu) - 1)) ^ swizzle<F32>(r, lu);
+    const uint32_t off = (uint32_t)(r < len ? r : len - 1) * row_bytes + (uint32_t)from * 16u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16, off, 0, 0, 0);
+  }
+}
+
+// Copies `bytes` (a multiple of 1024) of contiguous memory into LDS as it is.
+__device__ __forceinline__ void copy_flat(const void* from, char* tile, int bytes, int wave, int waves,
+                                          int lane) {
+  const __amdgpu_buffer_rsrc_t src = make_rsrc(from, (uint32_t)bytes);
+  for (int p = wave; p < bytes >> 10; p += waves)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
+                                             (uint32_t)p * 1024u + (uint32_t)lane * 16u, 0, 0, 0);
+}
+
+// Barrier behind which copies into LDS issued before it, by any wave, are
+// visible: each wave first waits for its own loads and LDS operations.
+__device__ __forceinline__ void copy_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+  __syncthreads();
+}
+
+// ---------------------------------------------------------------------------
+// Triangular 64 x 64 matrices as operand tiles: six 16 x 32 tiles each, those
+// on or below the diagonal (transposed: on or above).  A tile holds each
+// lane's operand contiguously: bf16 1 KB (hi), then, for a wide matrix, the
+// lo tiles in a second plane; fp32 two 1 KB halves.
+// ---------------------------------------------------------------------------
+__host__ __device__ constexpr int tri_tile(int t, int s) { return s == 0 ? t : 2 + t; }
+__host__ __device__ constexpr int tri_tile_t(int t, int s) { return s == 1 ? t : 4 + t; }
+constexpr int kTriTiles = 6;
+constexpr int kWideTri = kTriTiles * 2048;  // bytes of a wide (or fp32) matrix
+
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X tile_x(const char* m, int tile, int lane) {
+  if constexpr (F32) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(m + tile * 2048 + lane * 16);
+    const floatx4 b = *reinterpret_cast<const floatx4*>(m + tile * 2048 + 1024 + lane * 16);
+    return Op<true>::narrow(a, b);
+  } else {
+    return *reinterpret_cast<const bf16x8*>(m + tile * 1024 + lane * 16);
+  }
+}
+
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::W tile_w(const char* m, int tile, int lane) {
+  if constexpr (F32) {
+    return typename Op<true>::W{tile_x<true>(m, tile, lane)};
+  } else {
+    return typename Op<false>::W{tile_x<false>(m, tile, lane),
+                                 tile_x<false>(m + kTriTiles * 1024, tile, lane)};
+  }
+}
+
+template <bool F32>
+__device__ __forceinline__ void store_tile_x(char* m, int tile, int lane, typename Op<F32>::X x) {
+  if constexpr (F32) {
+    *reinterpret_cast<floatx4*>(m + tile * 2048 + lane * 16) = floatx4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<floatx4*>(m + tile * 2048 + 1024 + lane * 16) = floatx4{x[4], x[5], x[6], x[7]};
+  } else {
+    *reinterpret_cast<bf16x8*>(m + tile * 1024 + lane * 16) = x;
+  }
+}
+
+template <bool F32>
+__device__ __forceinline__ void store_tile_w(char* m, int tile, int lane, const typename Op<F32>::W& w) {
+  if constexpr (F32) {
+    store_tile_x<true>(m, tile, lane, w.v);
+  } else {
+    store_tile_x<false>(m, tile, lane, w.hi);
+    store_tile_x<false>(m + kTriTiles * 1024, tile, lane, w.lo);
+  }
+}
+
+// What the preparation writes for a chunk of a value head: T (wide; beta stays
+// outside it, as a rounded beta would be an error of a whole row of N), gam,
+// eta and beta (fp32[64] each), and P (the forward pass: one part), or the wide
+// transposes of T and P (the backward pass).
+struct ChunkRecord {
+  static constexpr int kT = 0, kVec = kWideTri, kP = kWideTri + 1024, kTt = kP, kPt = kP + kWideTri;
+  static constexpr int kPBytes[2] = {kTriTiles * 1024, kTriTiles * 2048};  // bf16, fp32
+  __host__ __device__ static constexpr int bytes(bool f32, bool backward) {
+    return backward ? kPt + kWideTri : kP + (f32 ? kTriTiles * 2048 : kTriTiles * 1024);
+  }
+};
+
+// A value kept in the workspace for another kernel's wide operand, natural
+// row order: bf16 hi and lo planes, or one fp32 plane.
+template <bool F32>
+__device__ __forceinline__ void store_wide4(char* base, size_t elem, size_t plane_elems, floatx4 x) {
+  if constexpr (F32) {
+    *reinterpret_cast<floatx4*>(base + elem * 4) = x;
+  } else {
+    bf16x2 h0 = {(__bf16)x[0], (__bf16)x[1]}, h1 = {(__bf16)x[2], (__bf16)x[3]};
+    *reinterpret_cast<uint2*>(base + elem * 2) =
+        make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
+    *reinterpret_cast<uint2*>(base + (plane_elems + elem) * 2) =
+        make_uint2(pack_bf16x2(x[0] - (float)h0[0], x[1] - (float)h0[1]),
+                   pack_bf16x2(x[2] - (float)h1[0], x[3] - (float)h1[1]));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Sequences, chunks and segments
+// ---------------------------------------------------------------------------
+
+// A chunk: first token, tokens (1..64), sequence.  A segment: consecutive
+// chunks of one sequence that one workgroup (per head) scans.
+struct ChunkInfo {
+  int tok, len, seq;  // len 0: there is no such chunk
+};
+struct SegmentInfo {
+  int chunk, chunks, seq;  // chunks < 0: there is no such segment
+  int ends;                // bit 0: the sequence's first, bit 1: its last
+};
+
+struct DeltaArgs {
+  const void *q, *k, *v, *dout;
+  const float *g, *beta;
+  int Hk, Hv, group, d_v;
+  // Element strides between tokens and between heads.
+  size_t qk_tok, qk_head, v_tok, v_head, gate_tok, gate_head;
+  float scale;
+  // Sequences: n of length L each (cu null), or by table.
+  int n_seqs, L, seg_chunks, max_chunks, max_segs;
+  const int4 *chunk_tab, *seg_tab;
+  const int* counts;  // chunks, segments (by table)
+  const float *S_in, *dS_out;    // [n][Hv][d_v][d_k] or null
+  float *S_out, *dS_in;
+  void *out, *dq, *dk, *dv;
+  float *dg, *dbeta;
+  // Workspace.
+  char* rec;          // [chunk][Hv] ChunkRecord
+  float *segJ, *segM, *segMt;   // [segment][Hv] maps; entering states replace segJ
+  float* segdJ;
+  char *keepS, *keepN, *keepdS, *keepdv;  // [chunk][Hv] what the gradient kernel reads
+};
+
+__device__ __forceinline__ int chunks_of(int len) { return (len + kChunk - 1) / kChunk; }
+
+__device__ __forceinline__ ChunkInfo chunk_info(const DeltaArgs& a, int c) {
+  if (a.chunk_tab != nullptr) {
+    if (c >= a.counts[0]) return ChunkInfo{0, 0, 0};
+    const int4 t = a.chunk_tab[c];
+    return ChunkInfo{uniform(t.x), uniform(t.y), uniform(t.z)};
+  }
+  const int per = chunks_of(a.L);
+  const int seq = uniform(c / per), at = c - seq * per;
+  if (seq >= a.n_seqs) return ChunkInfo{0, 0, 0};
+  const int left = a.L - at * kChunk;
+  return ChunkInfo{uniform(seq * a.L + at * kChunk), uniform(left < kChunk ? left : kChunk), seq};
+}
+
+__device__ __forceinline__ SegmentInfo segment_info(const DeltaArgs& a, int s) {
+  if (a.seg_tab != nullptr) {
+    if (s >= a.counts[1]) return SegmentInfo{0, -1, 0, 0};
+    const int4 t = a.seg_tab[s];
+    return SegmentInfo{uniform(t.x), uniform(t.y), uniform(t.z), uniform(t.w)};
+  }
+  const int per = chunks_of(a.L);
+  const int segs = (per + a.seg_chunks - 1) / a.seg_chunks;
+  const int seq = uniform(s / segs), at = s - seq * segs;
+  if (seq >= a.n_seqs) return SegmentInfo{0, -1, 0, 0};
+  const int left = per - at * a.seg_chunks;
+  return SegmentInfo{uniform(seq * per + at * a.seg_chunks), uniform(left < a.seg_chunks ? left : a.seg_chunks),
+                     seq, uniform((at == 0 ? 1 : 0) | (at == segs - 1 ? 2 : 0))};
+}
+
+// Log decays below this are taken as this: e^-200 is 0 in fp32, and sums of
+// them stay finite (a decay of exactly 0, log decay -inf, among them).
+constexpr float kMinLogDecay = -200.f;
+// Write strengths below this in magnitude are taken as this with their sign:
+// what such a token writes is below fp32's resolution of the state by 2^-36,
+// and the gradients can divide by the strength.
+constexpr float kMinBeta = 0x1p-60f;
+
+__device__ __forceinline__ float strength(float b) {
+  return fabsf(b) < kMinBeta ? copysignf(kMinBeta, b) : b;
+}
+
+// Inclusive prefix sums over a wave's 64 lanes of g in units of log2, in 64
+// bits: differences of far prefixes keep their decay's accuracy.
+__device__ __forceinline__ double decay_prefix(float g, int lane) {
+  double x = (double)(g < kMinLogDecay ? kMinLogDecay : g) * 1.4426950408889634;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const double y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Host-side launchers (arguments validated).
+struct DeltaPlan {
+  bool split;        // sequences are cut into segments that run side by side
+  int seg_chunks;    // chunks of a segment
+  int max_chunks, max_segs;
+  size_t tabs, rec, segs, keep, total;  // workspace offsets
+};
+hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, int seg_chunks, int max_chunks,
+                             int max_segs, int* tabs, hipStream_t stream);
+hipError_t launch_delta_prepare(bool f32, int d_k, bool backward, const DeltaArgs& a, hipStream_t stream);
+// what: 0 the segments' maps, 1 the outputs, 2 the states and writes for the gradient kernel.
+hipError_t launch_delta_scan(bool f32, int d_k, int what, const DeltaArgs& a, hipStream_t stream);
+hipError_t launch_delta_join(int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream);
+hipError_t launch_delta_reverse(bool f32, int d_k, bool map, const DeltaArgs& a, hipStream_t stream);
+hipError_t launch_delta_grad(bool f32, int d_k, const DeltaArgs& a, hipStream_t stream);
+
+}  // namespace vda

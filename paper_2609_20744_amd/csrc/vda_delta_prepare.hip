@@ -1,0 +1,358 @@
+// Token-wise gated delta rule: the sequences' tables, and what each chunk's
+// products need that does not depend on the state (vda_delta.h): the
+// triangular inverse T and the decayed scores P, as operand tiles, and the
+// decays gam and eta.
+//
+// One workgroup of four waves per chunk and value head.  The scores k.k and
+// q.k come from the matrix cores with operands loaded straight from memory
+// (a lane takes 16 bytes of one token's row); wave w makes row block w.  The
+// decays multiply the fp32 results.  I + diag(beta) L is unit lower triangular
+// and is inverted in fp32, in LDS: its four 16 x 16 diagonal blocks by
+// forward substitution (a lane per column; a series of powers would be all
+// products, but its terms grow with repeated keys before they cancel), then
+// the blocks below by products with the blocks already inverted,
+// T21 = -T22 M21 T11, first in pairs of 16, then of 32, on the fp32 matrix
+// cores.
+#include "vda_delta.h"
+
+namespace vda {
+namespace {
+
+constexpr int kLd = 68;  // floats per row of the matrix in LDS
+
+__device__ __forceinline__ floatx4 mfma_f32(floatx4 a, floatx4 b, floatx4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
+// Operand of 16 rows of a [64][kLd] matrix: row r0 + li, columns c0 + 4 lg ..
+__device__ __forceinline__ floatx4 mat_row(const float* m, int r0, int c0, int li, int lg) {
+  return *reinterpret_cast<const floatx4*>(m + (r0 + li) * kLd + c0 + 4 * lg);
+}
+// Column c0 + li, rows r0 + 4 lg ..
+__device__ __forceinline__ floatx4 mat_col(const float* m, int r0, int c0, int li, int lg) {
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = m[(r0 + 4 * lg + e) * kLd + c0 + li];
+  return v;
+}
+
+// Inverse of the unit lower triangular I + M in place; M's strict lower part
+// is in m, the rest is not read.  Leaves the 16 x 16 blocks on and below the
+// diagonal (zeros above within the diagonal blocks).  256 threads.
+__device__ __forceinline__ void invert_unit_lower(float* m, int wave, int li, int lg) {
+  {
+    const int r0 = 16 * wave;
+    float row[16][16];
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+#pragma unroll
+      for (int c = 0; c < (i + 3) / 4; ++c) {
+        const floatx4 t = *reinterpret_cast<const floatx4*>(m + (r0 + i) * kLd + r0 + 4 * c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) row[i][4 * c + e] = t[e];
+      }
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = li == i ? 1.f : 0.f;
+#pragma unroll
+      for (int l = 0; l < i; ++l) x[i] -= row[i][l] * x[l];
+    }
+    // Every lane of the wave has read the block before it is overwritten: the
+    // values above are used.
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if ((i >> 2) == lg) m[(r0 + i) * kLd + r0 + li] = x[i];
+  }
+  lds_barrier();
+  if (wave < 2) {
+    const int r0 = 32 * wave + 16, c0 = 32 * wave;
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    const floatx4 y = mfma_f32(mat_row(m, r0, c0, li, lg), mat_col(m, c0, c0, li, lg), zero);
+    const floatx4 t = mfma_f32(mat_row(m, r0, r0, li, lg), y, zero);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m[(r0 + 4 * lg + e) * kLd + c0 + li] = -t[e];
+  }
+  lds_barrier();
+  const int c = wave & 1, rr = wave >> 1;
+  floatx4 y[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      if (b >= c) y[t] = mfma_f32(mat_row(m, 32 + 16 * t, 16 * b, li, lg), mat_col(m, 16 * b, 16 * c, li, lg), y[t]);
+  floatx4 t = mfma_f32(mat_row(m, 32 + 16 * rr, 32, li, lg), y[0], floatx4{0.f, 0.f, 0.f, 0.f});
+  if (rr == 1) t = mfma_f32(mat_row(m, 48, 48, li, lg), y[1], t);
+  lds_barrier();  // every wave has read M21
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m[(32 + 16 * rr + 4 * lg + e) * kLd + 16 * c + li] = -t[e];
+  lds_barrier();
+}
+
+// A token row as an operand, channels in memory order (the same in both
+// operands of a score): 8 consecutive channels a lane.
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X token_op(__amdgpu_buffer_rsrc_t r, uint32_t row_off, int s,
+                                                        int lg) {
+  if constexpr (F32) {
+    const uint32_t o = row_off + (uint32_t)(32 * s + 8 * lg) * 4u;
+    const uint4 a = load_b128(r, o), b = load_b128(r, o + 16u);
+    return floatx8{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                   __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+  } else {
+    return __builtin_bit_cast(bf16x8, load_b128(r, row_off + (uint32_t)(32 * s + 8 * lg) * 2u));
+  }
+}
+
+template <bool F32, int DK, bool BACKWARD>
+__global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
+  typedef Op<F32> O;
+  typedef typename O::X X;
+  constexpr int KS = DK / 32, ES = F32 ? 4 : 2;
+  __shared__ __align__(16) float m[kChunk * kLd];
+  __shared__ double pre[kChunk];
+  __shared__ float strengths[kChunk];
+  const int h = blockIdx.x % (unsigned)a.Hv;
+  const int chunk = blockIdx.x / (unsigned)a.Hv;
+  const ChunkInfo ci = chunk_info(a, chunk);
+  if (ci.len == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
+  const int wave = uniform(tid >> 6);
+  char* rec = a.rec + ((size_t)chunk * a.Hv + h) * ChunkRecord::bytes(F32, BACKWARD);
+
+  // Token rows: past the chunk's end they are out of the buffers' range and
+  // read as zero.
+  const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head;
+  const uint32_t row_bytes = (uint32_t)a.qk_tok * ES;
+  const uint32_t span = (uint32_t)(ci.len - 1) * row_bytes + DK * ES;
+  const __amdgpu_buffer_rsrc_t kr = make_rsrc((const char*)a.k + qk * ES, span);
+  const __amdgpu_buffer_rsrc_t qr = make_rsrc((const char*)a.q + qk * ES, span);
+  // All row blocks of k, and of q in the backward pass; the wave's own block
+  // once more (k; forward: q), because registers cannot be indexed by it.
+  constexpr int QT = BACKWARD ? 4 : 1;
+  X kt[4][KS], qt[QT][KS], kw[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    kw[s] = token_op<F32>(kr, (uint32_t)(16 * wave + li) * row_bytes, s, lg);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) kt[t][s] = token_op<F32>(kr, (uint32_t)(16 * t + li) * row_bytes, s, lg);
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+      qt[t][s] = token_op<F32>(qr, (uint32_t)(16 * (BACKWARD ? t : wave) + li) * row_bytes, s, lg);
+  }
+  if (wave == 0) {
+    const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
+    const bool real = lane < ci.len;
+    const double G = decay_prefix(real ? a.g[at] : 0.f, lane);
+    pre[lane] = G;
+    strengths[lane] = real ? strength(a.beta[at]) : 0.f;
+    const double last = __shfl(G, 63);
+    float* vec = reinterpret_cast<float*>(rec + ChunkRecord::kVec);
+    vec[lane] = exp2f((float)G);
+    vec[64 + lane] = exp2f((float)(last - G));
+    vec[128 + lane] = strengths[lane];
+  }
+  lds_barrier();
+
+  const int r0 = 16 * wave;
+  double gi[4];
+  float bi[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) gi[e] = pre[r0 + 4 * lg + e], bi[e] = strengths[r0 + 4 * lg + e];
+
+  // M = diag(beta) L, rows of this wave.
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    if (t > wave) continue;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = O::mma(kw[s], kt[t][s], acc);
+    const int j = 16 * t + li;
+    const double gj = pre[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = r0 + 4 * lg + e;
+      m[i * kLd + j] = i > j ? bi[e] * exp2f((float)(gi[e] - gj)) * acc[e] : 0.f;
+    }
+  }
+
+  // P, row block `wave`, as operand tiles: the product's rows are the columns j of P.
+  if constexpr (!BACKWARD) {
+    const double gq = pre[r0 + li];
+    const int i = r0 + li;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (32 * s > r0 + 15) continue;
+      floatx4 p[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = 2 * s + u;
+        p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < KS; ++c) p[u] = O::mma(kt[t][c], qt[0][c], p[u]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = 16 * t + 4 * lg + e;
+          p[u][e] = i >= j ? a.scale * exp2f((float)(gq - pre[j])) * p[u][e] : 0.f;
+        }
+      }
+      store_tile_x<F32>(rec + ChunkRecord::kP, tri_tile(wave, s), lane, O::narrow(p[0], p[1]));
+    }
+  } else {
+    // P transposed, row block j of `wave`: the product's rows are the rows i of P.
+    const int j = r0 + li;
+    const double gj = pre[j];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (32 * s + 31 < r0) continue;
+      floatx4 p[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = 2 * s + u;
+        p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < KS; ++c) p[u] = O::mma(qt[t][c], kw[c], p[u]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = 16 * t + 4 * lg + e;
+          p[u][e] = i >= j ? a.scale * exp2f((float)(pre[i] - gj)) * p[u][e] : 0.f;
+        }
+      }
+      store_tile_w<F32>(rec + ChunkRecord::kPt, tri_tile_t(wave, s), lane, O::wide(p[0], p[1]));
+    }
+  }
+  lds_barrier();
+  invert_unit_lower(m, wave, li, lg);
+
+  // T, row block `wave`.
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (32 * s > r0 + 15) continue;
+    floatx4 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int t = 2 * s + u;
+      x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (t <= wave) x[u] = mat_row(m, r0, 16 * t, li, lg);
+    }
+    store_tile_w<F32>(rec + ChunkRecord::kT, tri_tile(wave, s), lane, O::wide(x[0], x[1]));
+  }
+  if constexpr (BACKWARD) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (32 * s + 31 < r0) continue;
+      floatx4 x[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = 2 * s + u;
+        x[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (t >= wave) x[u] = mat_col(m, 16 * t, r0, li, lg);
+      }
+      store_tile_w<F32>(rec + ChunkRecord::kTt, tri_tile_t(wave, s), lane, O::wide(x[0], x[1]));
+    }
+  }
+}
+
+// Tables of the chunks and segments of sequences [cu[i], cu[i + 1]): tabs
+// holds counts[2] (and padding to 4), prefix sums of chunks and segments
+// [n + 1] each, then the int4 tables.  Offsets are clamped to [0, T] and the
+// tables to their sizes, so that no malformed list can address anything else.
+constexpr int kPlanThreads = 1024;
+
+__global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu, int n, int T, int seg_chunks,
+                                                                 int max_chunks, int max_segs, int* tabs) {
+  __shared__ int sum[2][kPlanThreads];
+  int* counts = tabs;
+  int* cpre = tabs + 4;
+  int* spre = cpre + n + 1;
+  int4* chunk_tab = reinterpret_cast<int4*>(tabs + (4 + 2 * (n + 1) + 3) / 4 * 4);
+  int4* seg_tab = chunk_tab + max_chunks;
+  const int tid = threadIdx.x;
+  auto clamp = [&](int x) { return x < 0 ? 0 : x > T ? T : x; };
+  int cbase = 0, sbase = 0;
+  for (int at = 0; at < n; at += kPlanThreads) {
+    const int i = at + tid;
+    int c = 0, s = 0;
+    if (i < n) {
+      const int len = clamp(cu[i + 1]) - clamp(cu[i]);
+      c = len > 0 ? chunks_of(len) : 0;
+      s = c > seg_chunks ? (c + seg_chunks - 1) / seg_chunks : 1;
+    }
+    sum[0][tid] = c, sum[1][tid] = s;
+    __syncthreads();
+    for (int d = 1; d < kPlanThreads; d <<= 1) {
+      const int x = tid >= d ? sum[0][tid - d] : 0, y = tid >= d ? sum[1][tid - d] : 0;
+      __syncthreads();
+      sum[0][tid] += x, sum[1][tid] += y;
+      __syncthreads();
+    }
+    if (i < n) cpre[i] = cbase + sum[0][tid] - c, spre[i] = sbase + sum[1][tid] - s;
+    cbase += sum[0][kPlanThreads - 1], sbase += sum[1][kPlanThreads - 1];
+    __syncthreads();
+  }
+  if (tid == 0) {
+    cpre[n] = cbase, spre[n] = sbase;
+    counts[0] = cbase < max_chunks ? cbase : max_chunks;
+    counts[1] = sbase < max_segs ? sbase : max_segs;
+  }
+  __threadfence_block();
+  __syncthreads();
+  // The sequence that entry x belongs to: the last whose prefix is <= x.
+  auto find = [&](const int* p, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (p[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+  };
+  const int nc = cbase < max_chunks ? cbase : max_chunks;
+  for (int c = tid; c < nc; c += kPlanThreads) {
+    const int seq = find(cpre, c);
+    const int b = clamp(cu[seq]), len = clamp(cu[seq + 1]) - b, at = (c - cpre[seq]) * kChunk;
+    chunk_tab[c] = make_int4(b + at, len - at < kChunk ? len - at : kChunk, seq, 0);
+  }
+  const int ns = sbase < max_segs ? sbase : max_segs;
+  for (int s = tid; s < ns; s += kPlanThreads) {
+    const int seq = find(spre, s);
+    const int at = s - spre[seq], chunks = cpre[seq + 1] - cpre[seq];
+    const int first = cpre[seq] + at * seg_chunks;
+    int count = chunks - at * seg_chunks;
+    count = count < seg_chunks ? count : seg_chunks;
+    if (first + count > nc) count = nc - first;
+    const bool last = s + 1 >= spre[seq + 1];
+    seg_tab[s] = make_int4(first, count > 0 ? count : 0, seq, (at == 0 ? 1 : 0) | (last ? 2 : 0));
+  }
+}
+
+template <bool F32, int DK>
+hipError_t run(bool backward, const DeltaArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)a.max_chunks * (unsigned)a.Hv;
+  if (backward)
+    delta_prepare_kernel<F32, DK, true><<<grid, kThreads, 0, stream>>>(a);
+  else
+    delta_prepare_kernel<F32, DK, false><<<grid, kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, int seg_chunks, int max_chunks, int max_segs,
+                             int* tabs, hipStream_t stream) {
+  delta_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu, n_seqs, T, seg_chunks, max_chunks, max_segs, tabs);
+  return hipGetLastError();
+}
+
+hipError_t launch_delta_prepare(bool f32, int d_k, bool backward, const DeltaArgs& a, hipStream_t stream) {
+  if (a.max_chunks == 0) return hipSuccess;
+  switch (d_k) {
+    case 32: return f32 ? run<true, 32>(backward, a, stream) : run<false, 32>(backward, a, stream);
+    case 64: return f32 ? run<true, 64>(backward, a, stream) : run<false, 64>(backward, a, stream);
+    default: return f32 ? run<true, 128>(backward, a, stream) : run<false, 128>(backward, a, stream);
+  }
+}
+
+}  // namespace vda

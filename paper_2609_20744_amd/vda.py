@@ -45,7 +45,23 @@ class VdaOptions(ctypes.Structure):
                 ("q_heads", ctypes.c_int)]
 
 
+class VdaDeltaProblem(ctypes.Structure):
+    """struct vda_delta_problem (include/vda.h)."""
+    _fields_ = [("T", ctypes.c_int), ("n_seqs", ctypes.c_int), ("cu_seqlens", ctypes.c_void_p),
+                ("H_k", ctypes.c_int), ("H_v", ctypes.c_int), ("d_k", ctypes.c_int),
+                ("d_v", ctypes.c_int), ("layout", ctypes.c_int), ("is_f32", ctypes.c_int),
+                ("scale", ctypes.c_float)]
+
+
+class VdaRopeOptions(ctypes.Structure):
+    """struct vda_rope_options (include/vda.h)."""
+    _fields_ = [(n, ctypes.c_int) for n in (
+        "pairs_t", "pairs_h", "pairs_w", "interleaved", "l2", "layout", "grid_h", "grid_w",
+        "frame_offset", "x_row_stride", "dx_row_stride")]
+
+
 RULES = {"joint": 0, "frozen": 1}
+LAYOUTS = {"heads": 0, "tokens": 1}
 
 _SIGNATURES = {
     "vda_status_string": (ctypes.c_char_p, [_I]),
@@ -65,6 +81,13 @@ _SIGNATURES = {
     "vda_state_scan_chunked_workspace": (ctypes.c_size_t, [_I, _I, _I, _I, _I, _I]),
     "vda_prep": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P]),
     "vda_readout": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P]),
+    "vda_delta_forward": (_I, [_P] * 11),
+    "vda_delta_forward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_delta_backward": (_I, [_P] * 17),
+    "vda_delta_backward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_delta_step": (_I, [_P] * 5 + [_I] * 7 + [ctypes.c_float, _P, _I, _P, _P, _P]),
+    "vda_rope": (_I, [_P, _P, _P, _I, _I, _I, _I, _P, _I, _P, _P]),
+    "vda_rope_backward": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _P, _I, _P, _P]),
     "vda_release_workspace": (_I, [_I, _P]),
     "vda_workspace_bytes": (_I, [_I, _P]),
 }
@@ -549,4 +572,302 @@ def readout(q, S_fwd, S_rev, gate, d_v=None, out=None, stream=None):
                gate.data_ptr(), F, N, H, d_k, d_v, int(q.dtype == torch.float32), out.data_ptr(),
                _stream_ptr(dev, stream))
     _check(st, "vda_readout")
+    return out
+
+
+# ----------------------------------------------------------------------------
+# The token-wise gated delta rule and rotary positions
+# ----------------------------------------------------------------------------
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _new(shape, dtype, dev, stream):
+    """An empty tensor that belongs to the stream the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _expect(t, name, shape, dtype, dev):
+    _require(t, name, dtype, dev)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} shape {tuple(t.shape)} must be {tuple(shape)}")
+
+
+def _storage(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name} dtype {t.dtype} must be bfloat16 or float32")
+    if t.device.type != "cuda":
+        raise ValueError("VDA runs on the GPU only; tensors must be on a cuda device")
+    return t.dtype, t.device
+
+
+def _delta_problem(q, k, v, g, beta, cu_seqlens, layout, scale):
+    """The problem, and the shape of its states."""
+    dt, dev = _storage(q, "q")
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _require(t, n, dt, dev)
+    _require(g, "g", torch.float32, dev)
+    _require(beta, "beta", torch.float32, dev)
+    if layout not in LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(LAYOUTS)}")
+    if q.dim() < 3 or v.dim() != q.dim():
+        raise ValueError("q, k, v must be [..., H, L, d] (heads) or [..., L, H, d] (tokens)")
+    if k.shape != q.shape:
+        raise ValueError(f"k shape {tuple(k.shape)} != q shape {tuple(q.shape)}")
+    lead, heads = tuple(q.shape[:-3]), layout == "heads"
+    H_k, L = (q.shape[-3], q.shape[-2]) if heads else (q.shape[-2], q.shape[-3])
+    H_v = v.shape[-3] if heads else v.shape[-2]
+    d_k, d_v = q.shape[-1], v.shape[-1]
+    gates = lead + ((H_v, L) if heads else (L, H_v))
+    if tuple(v.shape) != gates + (d_v,):
+        raise ValueError(f"v shape {tuple(v.shape)} does not match q")
+    for t, n in ((g, "g"), (beta, "beta")):
+        if tuple(t.shape) != gates:
+            raise ValueError(f"{n} shape {tuple(t.shape)} must be {gates}")
+    if H_k < 1 or H_v % H_k:
+        raise ValueError(f"{H_v} value heads must be a multiple of {H_k} key heads")
+    B = math.prod(lead)
+    if cu_seqlens is not None:
+        if lead:
+            raise ValueError("with cu_seqlens, q, k, v have three dimensions (one packed batch)")
+        _require(cu_seqlens, "cu_seqlens", torch.int32, dev)
+        if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens must hold one more offset than there are sequences")
+        n, states = cu_seqlens.numel() - 1, (cu_seqlens.numel() - 1, H_v, d_v, d_k)
+        T, Hk, Hv = L, H_k, H_v
+    elif heads:  # every leading index and head is a head problem of its own
+        n, T, Hk, Hv = 1, L, B * H_k, B * H_v
+        states = lead + (H_v, d_v, d_k)
+    else:
+        n, T, Hk, Hv = B, B * L, H_k, H_v
+        states = lead + (H_v, d_v, d_k)
+    p = VdaDeltaProblem(T, n, _ptr(cu_seqlens), Hk, Hv, d_k, d_v, LAYOUTS[layout],
+                        int(dt == torch.float32), 1.0 if scale is None else float(scale))
+    return p, states, dt, dev
+
+
+def _delta_workspace(fn, p, dev, stream):
+    nbytes = _call(fn, dev, ctypes.byref(p))
+    return _new((max(int(nbytes), 16),), torch.uint8, dev, stream)
+
+
+def delta_forward(q, k, v, g, beta, cu_seqlens=None, layout="heads", scale=None, state=None,
+                  return_state=False, out=None, state_out=None, work=None, stream=None):
+    """The token-wise gated delta rule over whole sequences (vda_delta_forward).
+
+    layout 'heads': q, k [..., H_k, L, d_k], v [..., H_v, L, d_v], g, beta
+    [..., H_v, L]; 'tokens': q, k [..., L, H_k, d_k], v [..., L, H_v, d_v], g,
+    beta [..., L, H_v]; H_v a multiple of H_k; q, k, v bfloat16 or float32,
+    g (log decay) and beta float32.  Each leading index is a sequence; with
+    cu_seqlens (int32 [n + 1]) there is none, and the L tokens are n packed
+    sequences.  state: the states to start from, [..., H_v, d_v, d_k] float32
+    ([n, H_v, d_v, d_k] with cu_seqlens), or None (zero).  scale defaults to 1.
+    Returns the output (v's shape), or (output, last states) with
+    return_state.  work: a device buffer of delta_workspace(...) bytes
+    (allocated if None); calls that may run at the same time need their own.
+    Packed rows outside every sequence are left as they are in `out` (a new
+    output holds anything there)."""
+    p, states, dt, dev = _delta_problem(q, k, v, g, beta, cu_seqlens, layout, scale)
+    if state is not None:
+        _expect(state, "state", states, torch.float32, dev)
+    if out is None:
+        out = _new(v.shape, dt, dev, stream)
+    else:
+        _expect(out, "out", v.shape, dt, dev)
+    if state_out is not None:
+        _expect(state_out, "state_out", states, torch.float32, dev)
+    elif return_state:
+        state_out = _new(states, torch.float32, dev, stream)
+    if work is None:
+        work = _delta_workspace(lib.vda_delta_forward_workspace, p, dev, stream)
+    else:
+        _delta_work(work, p, lib.vda_delta_forward_workspace, dev)
+    st = _call(lib.vda_delta_forward, dev, ctypes.byref(p), q.data_ptr(), k.data_ptr(),
+               v.data_ptr(), g.data_ptr(), beta.data_ptr(), _ptr(state), out.data_ptr(),
+               _ptr(state_out), work.data_ptr(), _stream_ptr(dev, stream))
+    _check(st, "vda_delta_forward")
+    return (out, state_out) if return_state else out
+
+
+def _delta_work(work, p, fn, dev):
+    _require(work, "work", torch.uint8, dev)
+    need = int(_call(fn, dev, ctypes.byref(p)))
+    if work.numel() < need:
+        raise ValueError(f"work holds {work.numel()} bytes, {need} are needed")
+
+
+def delta_workspace(q, k, v, g, beta, cu_seqlens=None, layout="heads", backward=False):
+    """Bytes of the work buffer of delta_forward (or delta_backward) for these arguments."""
+    p, _, _, dev = _delta_problem(q, k, v, g, beta, cu_seqlens, layout, None)
+    fn = lib.vda_delta_backward_workspace if backward else lib.vda_delta_forward_workspace
+    return int(_call(fn, dev, ctypes.byref(p)))
+
+
+def delta_backward(dout, q, k, v, g, beta, cu_seqlens=None, layout="heads", scale=None, state=None,
+                   dstate=None, outs=None, work=None, stream=None):
+    """The gradients of delta_forward (vda_delta_backward): dout of the
+    output, dstate of the last states (or None: zero); the other arguments as
+    there.  Returns (dq, dk, dv, dg, dbeta, dstate_in), dstate_in None where
+    state is None; `outs`, such a tuple, is filled instead of new tensors."""
+    p, states, dt, dev = _delta_problem(q, k, v, g, beta, cu_seqlens, layout, scale)
+    _expect(dout, "dout", v.shape, dt, dev)
+    for t, n in ((state, "state"), (dstate, "dstate")):
+        if t is not None:
+            _expect(t, n, states, torch.float32, dev)
+    shapes = ((q.shape, dt), (k.shape, dt), (v.shape, dt), (g.shape, torch.float32),
+              (beta.shape, torch.float32), (states, torch.float32))
+    names = ("dq", "dk", "dv", "dg", "dbeta", "dstate_in")
+    if outs is None:
+        outs = tuple(_new(s, d, dev, stream) if n != "dstate_in" or state is not None else None
+                     for n, (s, d) in zip(names, shapes))
+    else:
+        if len(outs) != 6:
+            raise ValueError("outs must be (dq, dk, dv, dg, dbeta, dstate_in)")
+        for t, n, (s, d) in zip(outs, names, shapes):
+            if t is not None or n != "dstate_in":
+                _expect(t, n, s, d, dev)
+    if work is None:
+        work = _delta_workspace(lib.vda_delta_backward_workspace, p, dev, stream)
+    else:
+        _delta_work(work, p, lib.vda_delta_backward_workspace, dev)
+    st = _call(lib.vda_delta_backward, dev, ctypes.byref(p), dout.data_ptr(), q.data_ptr(),
+               k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), _ptr(state),
+               _ptr(dstate), *(_ptr(t) for t in outs), work.data_ptr(), _stream_ptr(dev, stream))
+    _check(st, "vda_delta_backward")
+    return tuple(outs)
+
+
+def delta_step(q, k, v, g, beta, state, slots=None, scale=None, out=None, stream=None):
+    """A few tokens of each of n sequences (vda_delta_step): q, k [n, t, H_k,
+    d_k], v [n, t, H_v, d_v] bfloat16 or float32, g, beta [n, t, H_v]
+    float32; state [n_slots, H_v, d_v, d_k] float32, updated in place.  slots:
+    int32 [n], the sequences' slots (distinct; one outside the pool marks a
+    row of padding, whose output is left as it is), or None (slot i for
+    sequence i).  Returns the output [n, t, H_v, d_v]."""
+    dt, dev = _storage(q, "q")
+    if q.dim() != 4 or not isinstance(v, torch.Tensor) or v.dim() != 4:
+        raise ValueError("q, k must be [n, t, H_k, d_k] and v [n, t, H_v, d_v]")
+    n, t, H_k, d_k = q.shape
+    H_v, d_v = v.shape[2:]
+    _require(q, "q", dt, dev)
+    _expect(k, "k", q.shape, dt, dev)
+    _expect(v, "v", (n, t, H_v, d_v), dt, dev)
+    _expect(g, "g", (n, t, H_v), torch.float32, dev)
+    _expect(beta, "beta", (n, t, H_v), torch.float32, dev)
+    _require(state, "state", torch.float32, dev)
+    if state.dim() != 4 or tuple(state.shape[1:]) != (H_v, d_v, d_k):
+        raise ValueError(f"state shape {tuple(state.shape)} must be [n_slots, {H_v}, {d_v}, {d_k}]")
+    if slots is not None:
+        _expect(slots, "slots", (n,), torch.int32, dev)
+    if out is None:
+        out = _new(v.shape, dt, dev, stream)
+    else:
+        _expect(out, "out", v.shape, dt, dev)
+    st = _call(lib.vda_delta_step, dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(),
+               beta.data_ptr(), n, t, H_k, H_v, d_k, d_v, int(dt == torch.float32),
+               1.0 if scale is None else float(scale), _ptr(slots), state.shape[0],
+               state.data_ptr(), out.data_ptr(), _stream_ptr(dev, stream))
+    _check(st, "vda_delta_step")
+    return out
+
+
+def _token_rows(t, name, H):
+    """Row stride of a [B, L, H * d] tensor whose token rows are equally far apart."""
+    if t.dim() != 3 or t.shape[2] % H:
+        raise ValueError(f"{name} must be [B, L, H * d]")
+    B, L, C = t.shape
+    row = t.stride(1) if L > 1 else t.stride(0) if B > 1 else C
+    if t.stride(2) != 1 or row < C or (B > 1 and t.stride(0) != L * row):
+        raise ValueError(f"{name} must have contiguous rows at one stride over the batch and tokens")
+    return row
+
+
+def _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interleaved, l2, layout,
+               dev):
+    if layout not in LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(LAYOUTS)}")
+    pt, ph, pw = (int(a) for a in axes)
+    _expect(inv_freq, "inv_freq", (pt + ph + pw,), torch.float32, dev)
+    if positions is not None:
+        if grid is not None:
+            raise ValueError("give positions or a grid, not both")
+        _expect(positions, "positions", (B, L, 3), torch.int32, dev)
+        gh = gw = 1
+    elif grid is None:
+        raise ValueError("positions or a grid (height, width) is needed")
+    else:
+        gh, gw = (int(x) for x in grid)
+    return VdaRopeOptions(pt, ph, pw, int(bool(interleaved)), int(bool(l2)), LAYOUTS[layout], gh, gw,
+                          int(frame_offset), 0, 0)
+
+
+def rope(x, inv_freq, axes, H, positions=None, grid=None, frame_offset=0, interleaved=True,
+         l2=False, layout="heads", out=None, stream=None):
+    """Rotary positions over time, height and width (vda_rope): x [B, L, H*d]
+    bfloat16 or float32 (a slice of a fused projection's channels is fine),
+    axes = (pairs of time, of height, of width), inv_freq float32 [sum of
+    axes].  The tokens' positions: `positions` int32 [B, L, 3], or grid =
+    (height, width) with the first frame at frame_offset.  l2 divides each
+    token of each head by its length first.  Returns [B * H, L, d] (layout
+    'heads', as prep) or [B, L, H * d] ('tokens')."""
+    dt, dev = _storage(x, "x")
+    row = _token_rows(x, "x", H)
+    B, L, C = x.shape
+    d = C // H
+    o = _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interleaved, l2,
+                   layout, dev)
+    o.x_row_stride = row
+    shape = (B * H, L, d) if layout == "heads" else (B, L, C)
+    if out is None:
+        out = _new(shape, dt, dev, stream)
+    else:
+        _expect(out, "out", shape, dt, dev)
+    st = _call(lib.vda_rope, dev, x.data_ptr(), inv_freq.data_ptr(), _ptr(positions), B, L, H, d,
+               ctypes.byref(o), int(dt == torch.float32), out.data_ptr(), _stream_ptr(dev, stream))
+    _check(st, "vda_rope")
+    return out
+
+
+def rope_backward(dout, inv_freq, axes, H, x=None, positions=None, grid=None, frame_offset=0,
+                  interleaved=True, l2=False, layout="heads", out=None, stream=None):
+    """The gradient of rope (vda_rope_backward): dout in the output's layout,
+    x the forward input (needed with l2 only); the other arguments as there.
+    Returns dx [B, L, H * d] (`out` may be a slice of a fused gradient)."""
+    dt, dev = _storage(dout, "dout")
+    if layout == "heads":
+        if dout.dim() != 3 or dout.shape[0] % H:
+            raise ValueError("dout must be [B * H, L, d]")
+        B, L, d = dout.shape[0] // H, dout.shape[1], dout.shape[2]
+    else:
+        if dout.dim() != 3 or dout.shape[2] % H:
+            raise ValueError("dout must be [B, L, H * d]")
+        B, L, d = dout.shape[0], dout.shape[1], dout.shape[2] // H
+    _require(dout, "dout", dt, dev)
+    o = _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interleaved, l2,
+                   layout, dev)
+    if l2 and x is None:
+        raise ValueError("x is needed with l2")
+    for t, n in ((x, "x"), (out, "out")):
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or t.dtype is not dt or t.device != dev or \
+                tuple(t.shape) != (B, L, H * d):
+            raise ValueError(f"{n} must be {dt} [{B}, {L}, {H * d}] on {dev}")
+        row = _token_rows(t, n, H)
+        if n == "x":
+            o.x_row_stride = row
+        else:
+            o.dx_row_stride = row
+    if out is None:
+        out = _new((B, L, H * d), dt, dev, stream)
+    st = _call(lib.vda_rope_backward, dev, dout.data_ptr(), _ptr(x), inv_freq.data_ptr(),
+               _ptr(positions), B, L, H, d, ctypes.byref(o), int(dt == torch.float32),
+               out.data_ptr(), _stream_ptr(dev, stream))
+    _check(st, "vda_rope_backward")
     return out
