@@ -40,6 +40,20 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 template <bool F32>
 struct Op;
 
+// What the pair x, y leaves of itself beside its rounding `hi`, rounded: each
+// remainder in one instruction, a dot product of hi with (-1, 0) or (0, -1)
+// added to the value, exact (1 M values over all exponents compared with the
+// subtraction).  The constants pass through registers: as immediates the
+// compiler encodes the first like the second.
+__device__ __forceinline__ uint32_t rest_bf16x2(float x, float y, uint32_t hi) {
+  uint32_t first = 0x0000bf80u, second = 0xbf800000u;
+  asm("" : "+s"(first));
+  asm("" : "+s"(second));
+  const bf16x2 h = __builtin_bit_cast(bf16x2, hi);
+  return pack_bf16x2(__builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, first), x, false),
+                     __builtin_amdgcn_fdot2_f32_bf16(h, __builtin_bit_cast(bf16x2, second), y, false));
+}
+
 template <>
 struct Op<false> {
   typedef uint16_t Elem;
@@ -48,20 +62,18 @@ struct Op<false> {
     bf16x8 hi, lo;
   };
   static __device__ __forceinline__ X narrow(floatx4 a, floatx4 b) {
-    X x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = (__bf16)a[e], x[4 + e] = (__bf16)b[e];
-    return x;
+    return __builtin_bit_cast(
+        X, u32x4{pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])});
   }
   static __device__ __forceinline__ W wide(floatx4 a, floatx4 b) {
-    W w;
-    w.hi = narrow(a, b);
+    u32x4 hi, lo;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w.lo[e] = (__bf16)(a[e] - (float)w.hi[e]);
-      w.lo[4 + e] = (__bf16)(b[e] - (float)w.hi[4 + e]);
+    for (int p = 0; p < 4; ++p) {
+      const float x = p < 2 ? a[2 * p] : b[2 * p - 4], y = p < 2 ? a[2 * p + 1] : b[2 * p - 3];
+      hi[p] = pack_bf16x2(x, y);
+      lo[p] = rest_bf16x2(x, y, hi[p]);
     }
-    return w;
+    return W{__builtin_bit_cast(X, hi), __builtin_bit_cast(X, lo)};
   }
   static __device__ __forceinline__ X head(const W& w) { return w.hi; }
   static __device__ __forceinline__ floatx4 mma(X a, X b, floatx4 c) {
@@ -210,6 +222,195 @@ __device__ __forceinline__ void copy_rows(__amdgpu_buffer_rsrc_t src, char* tile
   }
 }
 
+// ---------------------------------------------------------------------------
+// Row tiles in LDS: 16 tokens x 32 channels, each lane's 16 bytes (eight
+// consecutive channels 8 lg .. of token li; fp32: four, in two halves of 1 KB)
+// in one place, so that an operand of the rows is one read at a lane's own
+// offset plus a constant: no address is computed in a loop.  Columns are
+// read across lanes' places (ds_read_b64_tr_b16, or four words in fp32), for
+// which the places of a unit column lg are permuted, which spreads them over the
+// banks (bf16: two accesses a bank, the least when half of each 16 bytes is read).
+//
+// Channels are paired with results by this order: operand element e of lane
+// lg, step s, is channel 32 s + 8 lg + e; so a result whose rows are such a
+// contraction comes in halves o = 0, 1 whose row 4 lg + r is channel
+// 32 s + 8 lg + 4 o + r.
+// ---------------------------------------------------------------------------
+template <bool F32>
+__host__ __device__ constexpr int row_tile_bytes() { return F32 ? 2048 : 1024; }
+
+template <bool F32>
+__device__ __forceinline__ int tile_place(int row, int lg) {
+  return (16 * lg + (row ^ (F32 ? lg : (lg & 1) << 3))) * 16;
+}
+
+// Row of place `row` of tile t in paired order.
+__device__ __forceinline__ int paired_row(int t, int row) {
+  return 32 * (t >> 1) + 8 * (row >> 2) + 4 * (t & 1) + (row & 3);
+}
+
+// ... and in twisted order: a tile read by columns in that order (twisted_cols)
+// takes both halves of its 16-byte places, and so all banks.
+__device__ __forceinline__ int twisted_row(int t, int row) {
+  return 32 * (t >> 1) + 8 * (row >> 2) + 4 * ((t ^ (row >> 3)) & 1) + (row & 3);
+}
+
+// Offsets of a lane: its row operand, and the columns that it reads.
+struct TileLane {
+  int row, col[4];
+};
+template <bool F32>
+__device__ __forceinline__ TileLane tile_lane(int li, int lg) {
+  TileLane l;
+  l.row = tile_place<F32>(li, lg);
+  if constexpr (F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l.col[e] = tile_place<true>(4 * lg + e, li >> 2) + (li & 3) * 4;
+  } else {
+    l.col[0] = tile_place<false>(4 * lg + (li >> 2), li & 3);
+    l.col[1] = l.col[2] = l.col[3] = 0;
+  }
+  return l;
+}
+
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X tile_row(const char* tile, const TileLane& l) {
+  if constexpr (F32) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(tile + l.row);
+    const floatx4 b = *reinterpret_cast<const floatx4*>(tile + 1024 + l.row);
+    return Op<true>::narrow(a, b);
+  } else {
+    return *reinterpret_cast<const bf16x8*>(tile + l.row);
+  }
+}
+
+// Channel 8 (li / 4) + 4 o + li % 4 of the tile at tokens 4 lg .. + 3.
+__device__ __forceinline__ shortx4 tile_col_bf16(const char* tile, int o, const TileLane& l) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + 8 * o + l.col[0]));
+}
+__device__ __forceinline__ floatx4 tile_col_f32(const char* tile, int o, const TileLane& l) {
+  floatx4 v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float*>(tile + 1024 * o + l.col[e]);
+  return v;
+}
+
+// The same channel of two tiles (tokens t0 .. and t1 ..) as an operand.
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X tile_cols(const char* t0, const char* t1, int o, const TileLane& l) {
+  if constexpr (F32) {
+    return Op<true>::narrow(tile_col_f32(t0, o, l), tile_col_f32(t1, o, l));
+  } else {
+    const shortx4 a = tile_col_bf16(t0, o, l), b = tile_col_bf16(t1, o, l);
+    typedef short shortx8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(bf16x8, shortx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+  }
+}
+
+// Offsets of a lane for columns in twisted order: channel 8 (li / 4) + 4 (o ^
+// li / 8) + li % 4 of a tile.
+struct TwistedLane {
+  int row, col[2][4];
+};
+template <bool F32>
+__device__ __forceinline__ TwistedLane twisted_lane(int li, int lg) {
+  TwistedLane l;
+  l.row = tile_place<F32>(li, lg);
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      l.col[o][e] = F32 ? tile_place<true>(4 * lg + e, li >> 2) + (li & 3) * 4 + 1024 * (o ^ (li >> 3))
+                        : tile_place<false>(4 * lg + (li >> 2), li & 3) + 8 * (o ^ ((li >> 1) & 1));
+  return l;
+}
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::X twisted_cols(const char* t0, const char* t1, const int (&col)[4]) {
+  if constexpr (F32) {
+    floatx4 a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = *reinterpret_cast<const float*>(t0 + col[e]);
+      b[e] = *reinterpret_cast<const float*>(t1 + col[e]);
+    }
+    return Op<true>::narrow(a, b);
+  } else {
+    const shortx4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(t0 + col[0]));
+    const shortx4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(t1 + col[0]));
+    typedef short shortx8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(bf16x8, shortx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+  }
+}
+
+// ... of one tile as fp32.
+template <bool F32>
+__device__ __forceinline__ floatx4 tile_values(const char* tile, int o, const TileLane& l) {
+  if constexpr (F32) {
+    return tile_col_f32(tile, o, l);
+  } else {
+    const shortx4 a = tile_col_bf16(tile, o, l);
+    floatx4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16);
+    return v;
+  }
+}
+
+// Copies ROWS rows of 32 BLOCKS channels, row_bytes apart, into row tiles
+// [block][row tile], by the first COPIERS waves (a power of two).  A row at or
+// past `len` repeats row len - 1, so that every address is the sequence's own
+// (what such rows meet is zero: their writes, their strengths, their stores).
+// ORDER: which row a place holds.
+enum class RowOrder {
+  kPlain,   // place r of tile t is row 16 t + r
+  kPaired,  // place 4 a + b of tiles 2 t and 2 t + 1 is row 32 t + 8 a + b and
+            // 32 t + 8 a + 4 + b: the order that channels have (above), for rows
+            // that are contracted with channels
+  kTwisted  // the same with the two tiles' rows exchanged for a >= 2
+};
+template <bool F32, int ROWS, int BLOCKS, int COPIERS, RowOrder ORDER = RowOrder::kPlain>
+__device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* tiles, int len, uint32_t row_bytes,
+                                           int wave, int lane, uint32_t from = 0) {
+  constexpr int kHalves = F32 ? 2 : 1, kBlock = F32 ? 128 : 64, kRow = row_tile_bytes<F32>(), kPer = ROWS / 16;
+  constexpr int kTiles = kPer * BLOCKS, kSteps = (kTiles + COPIERS - 1) / COPIERS;
+  const int lg = lane >> 4, row = (lane & 15) ^ (F32 ? lg : (lg & 1) << 3);
+  const uint32_t chan = (uint32_t)lg * (F32 ? 32u : 16u);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int p = wave + i * COPIERS;  // tile p % kPer of block p / kPer
+    if (kTiles % COPIERS != 0 && p >= kTiles) break;
+    const int t = p % kPer;
+    const int r = ORDER == RowOrder::kPaired ? paired_row(t, row) : ORDER == RowOrder::kTwisted ? twisted_row(t, row)
+                                                                                              : 16 * t + row;
+    const uint32_t at = __umul24((uint32_t)(r < len ? r : len - 1), row_bytes) + chan;
+#pragma unroll
+    for (int half = 0; half < kHalves; ++half)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tiles + p * kRow + half * 1024), 16, at,
+                                               from + (p / kPer) * kBlock + half * 16, 0, 0);
+  }
+}
+
+// Copies BYTES (a multiple of 1024) of contiguous memory into LDS as it is.
+template <int BYTES, int COPIERS>
+__device__ __forceinline__ void copy_flat(const void* from, char* to, int wave, int lane) {
+  constexpr int kPieces = BYTES / 1024, kSteps = (kPieces + COPIERS - 1) / COPIERS;
+  const __amdgpu_buffer_rsrc_t src = make_rsrc(from, (uint32_t)BYTES);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int p = wave + i * COPIERS;
+    if (kPieces % COPIERS != 0 && p >= kPieces) break;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(to + p * 1024), 16, (uint32_t)lane * 16u, p * 1024, 0,
+                                             0);
+  }
+}
+
+// No instruction is moved across (bf16 storage; fp32 operands take twice the
+// registers, and there the order is left to the compiler).
+template <bool F32>
+__device__ __forceinline__ void fence() {
+  if constexpr (!F32) __builtin_amdgcn_sched_barrier(0);
+}
+
 // Copies `bytes` (a multiple of 1024) of contiguous memory into LDS as it is.
 __device__ __forceinline__ void copy_flat(const void* from, char* tile, int bytes, int wave, int waves,
                                           int lane) {
@@ -221,8 +422,14 @@ __device__ __forceinline__ void copy_flat(const void* from, char* tile, int byte
 
 // Barrier behind which copies into LDS issued before it, by any wave, are
 // visible: each wave first waits for its own loads and LDS operations.
+// LATER: so many of the wave's memory operations at least were issued after
+// the copies (stores of the step between) and need not have ended: they end
+// in the order of issue.  Waiting for a step's stores as well cost about a
+// microsecond of each step.
+template <int LATER = 0>
 __device__ __forceinline__ void copy_barrier() {
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((LATER & 15) | 0x0070 | (LATER >> 4 << 14));  // vmcnt LATER, lgkmcnt 0
   __syncthreads();
 }
 
@@ -281,12 +488,13 @@ __device__ __forceinline__ void store_tile_w(char* m, int tile, int lane, const 
 // What the preparation writes for a chunk of a value head: T (wide; beta stays
 // outside it, as a rounded beta would be an error of a whole row of N), gam,
 // eta and beta (fp32[64] each), and P (the forward pass: one part), or the wide
-// transposes of T and P (the backward pass).
+// transposes of T and P and G in units of log2 (64 bits) (the backward pass).
 struct ChunkRecord {
-  static constexpr int kT = 0, kVec = kWideTri, kP = kWideTri + 1024, kTt = kP, kPt = kP + kWideTri;
+  static constexpr int kT = 0, kVec = kWideTri, kP = kWideTri + 1024, kTt = kP, kPt = kP + kWideTri,
+                       kPre = kPt + kWideTri;
   static constexpr int kPBytes[2] = {kTriTiles * 1024, kTriTiles * 2048};  // bf16, fp32
   __host__ __device__ static constexpr int bytes(bool f32, bool backward) {
-    return backward ? kPt + kWideTri : kP + (f32 ? kTriTiles * 2048 : kTriTiles * 1024);
+    return backward ? kPre + 1024 : kP + (f32 ? kTriTiles * 2048 : kTriTiles * 1024);
   }
 };
 
@@ -297,13 +505,43 @@ __device__ __forceinline__ void store_wide4(char* base, size_t elem, size_t plan
   if constexpr (F32) {
     *reinterpret_cast<floatx4*>(base + elem * 4) = x;
   } else {
-    bf16x2 h0 = {(__bf16)x[0], (__bf16)x[1]}, h1 = {(__bf16)x[2], (__bf16)x[3]};
-    *reinterpret_cast<uint2*>(base + elem * 2) =
-        make_uint2(__builtin_bit_cast(uint32_t, h0), __builtin_bit_cast(uint32_t, h1));
+    const uint32_t h0 = pack_bf16x2(x[0], x[1]), h1 = pack_bf16x2(x[2], x[3]);
+    *reinterpret_cast<uint2*>(base + elem * 2) = make_uint2(h0, h1);
     *reinterpret_cast<uint2*>(base + (plane_elems + elem) * 2) =
-        make_uint2(pack_bf16x2(x[0] - (float)h0[0], x[1] - (float)h0[1]),
-                   pack_bf16x2(x[2] - (float)h1[0], x[3] - (float)h1[1]));
+        make_uint2(rest_bf16x2(x[0], x[1], h0), rest_bf16x2(x[2], x[3], h1));
   }
+}
+
+// Eight values along a row, already wide; and one of them.
+template <bool F32>
+__device__ __forceinline__ void store_wide8(char* base, size_t elem, size_t plane_elems,
+                                            const typename Op<F32>::W& w) {
+  if constexpr (F32) {
+    *reinterpret_cast<floatx4*>(base + elem * 4) = floatx4{w.v[0], w.v[1], w.v[2], w.v[3]};
+    *reinterpret_cast<floatx4*>(base + elem * 4 + 16) = floatx4{w.v[4], w.v[5], w.v[6], w.v[7]};
+  } else {
+    *reinterpret_cast<bf16x8*>(base + elem * 2) = w.hi;
+    *reinterpret_cast<bf16x8*>(base + (plane_elems + elem) * 2) = w.lo;
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void store_wide1(char* base, size_t elem, size_t plane_elems,
+                                            const typename Op<F32>::W& w, int e) {
+  if constexpr (F32) {
+    *reinterpret_cast<float*>(base + elem * 4) = w.v[e];
+  } else {
+    *reinterpret_cast<__bf16*>(base + elem * 2) = w.hi[e];
+    *reinterpret_cast<__bf16*>(base + (plane_elems + elem) * 2) = w.lo[e];
+  }
+}
+template <bool F32>
+__device__ __forceinline__ typename Op<F32>::W load_wide8(const char* base, size_t elem, size_t plane_elems) {
+  if constexpr (F32)
+    return typename Op<true>::W{Op<true>::narrow(*reinterpret_cast<const floatx4*>(base + elem * 4),
+                                                 *reinterpret_cast<const floatx4*>(base + elem * 4 + 16))};
+  else
+    return typename Op<false>::W{*reinterpret_cast<const bf16x8*>(base + elem * 2),
+                                 *reinterpret_cast<const bf16x8*>(base + (plane_elems + elem) * 2)};
 }
 
 // ---------------------------------------------------------------------------
@@ -316,8 +554,8 @@ struct ChunkInfo {
   int tok, len, seq;  // len 0: there is no such chunk
 };
 struct SegmentInfo {
-  int chunk, chunks, seq;  // chunks < 0: there is no such segment
-  int ends;                // bit 0: the sequence's first, bit 1: its last
+  int chunk, tok, len, seq;  // first chunk, first token, tokens; len < 0: there is no such segment
+  int ends;                  // bit 0: the sequence's first, bit 1: its last
 };
 
 struct DeltaArgs {
@@ -337,8 +575,8 @@ struct DeltaArgs {
   float *dg, *dbeta;
   // Workspace.
   char* rec;          // [chunk][Hv] ChunkRecord
-  float *segJ, *segM, *segMt;   // [segment][Hv] maps; entering states replace segJ
-  float* segdJ;
+  float *segJ, *segdJ;  // [segment][Hv] states that maps add; the entering states replace them
+  char* segM;           // [segment][Hv] map matrices, wide, by rows and by columns
   char *keepS, *keepN, *keepdS, *keepdv;  // [chunk][Hv] what the gradient kernel reads
 };
 
@@ -359,29 +597,48 @@ __device__ __forceinline__ ChunkInfo chunk_info(const DeltaArgs& a, int c) {
 
 __device__ __forceinline__ SegmentInfo segment_info(const DeltaArgs& a, int s) {
   if (a.seg_tab != nullptr) {
-    if (s >= a.counts[1]) return SegmentInfo{0, -1, 0, 0};
+    if (s >= a.counts[1]) return SegmentInfo{0, 0, -1, 0, 0};
     const int4 t = a.seg_tab[s];
-    return SegmentInfo{uniform(t.x), uniform(t.y), uniform(t.z), uniform(t.w)};
+    const int w = uniform(t.w);
+    return SegmentInfo{uniform(t.x), uniform(t.y), uniform(t.z), w >> 2, w & 3};
   }
   const int per = chunks_of(a.L);
   const int segs = (per + a.seg_chunks - 1) / a.seg_chunks;
   const int seq = uniform(s / segs), at = s - seq * segs;
-  if (seq >= a.n_seqs) return SegmentInfo{0, -1, 0, 0};
-  const int left = per - at * a.seg_chunks;
-  return SegmentInfo{uniform(seq * per + at * a.seg_chunks), uniform(left < a.seg_chunks ? left : a.seg_chunks),
-                     seq, uniform((at == 0 ? 1 : 0) | (at == segs - 1 ? 2 : 0))};
+  if (seq >= a.n_seqs) return SegmentInfo{0, 0, -1, 0, 0};
+  const int from = at * a.seg_chunks * kChunk, left = a.L - from, most = a.seg_chunks * kChunk;
+  return SegmentInfo{uniform(seq * per + at * a.seg_chunks), uniform(seq * a.L + from),
+                     uniform(left < most ? left : most), seq,
+                     uniform((at == 0 ? 1 : 0) | (at == segs - 1 ? 2 : 0))};
 }
 
 // Log decays below this are taken as this: e^-200 is 0 in fp32, and sums of
 // them stay finite (a decay of exactly 0, log decay -inf, among them).
 constexpr float kMinLogDecay = -200.f;
 // Write strengths below this in magnitude are taken as this with their sign:
-// what such a token writes is below fp32's resolution of the state by 2^-36,
+// what such a token writes is below fp32's resolution of the state by 2^-24,
 // and the gradients can divide by the strength.
-constexpr float kMinBeta = 0x1p-60f;
+constexpr float kMinBeta = 0x1p-48f;
 
 __device__ __forceinline__ float strength(float b) {
   return fabsf(b) < kMinBeta ? copysignf(kMinBeta, b) : b;
+}
+
+// 2^x of the matrix of decays: one instruction, results below 2^-126 are 0.
+__device__ __forceinline__ float pow2(double x) { return __builtin_amdgcn_exp2f((float)x); }
+
+// Sum over aligned groups of LANES lanes (4, 8 or 16), in every lane: DPP adds.
+template <int LANES>
+__device__ __forceinline__ float group_sum(float x) {
+  auto add = [](float v, int y) { return v + __int_as_float(y); };
+  const int all = 0xf;
+  x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xB1, all, all, false));  // quad_perm 1,0,3,2
+  x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4E, all, all, false));  // quad_perm 2,3,0,1
+  if constexpr (LANES >= 8)
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x141, all, all, false));  // row_half_mirror
+  if constexpr (LANES >= 16)
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x140, all, all, false));  // row_mirror
+  return x;
 }
 
 // Inclusive prefix sums over a wave's 64 lanes of g in units of log2, in 64
@@ -408,7 +665,7 @@ hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, int seg_chunks, i
 hipError_t launch_delta_prepare(bool f32, int d_k, bool backward, const DeltaArgs& a, hipStream_t stream);
 // what: 0 the segments' maps, 1 the outputs, 2 the states and writes for the gradient kernel.
 hipError_t launch_delta_scan(bool f32, int d_k, int what, const DeltaArgs& a, hipStream_t stream);
-hipError_t launch_delta_join(int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream);
+hipError_t launch_delta_join(bool f32, int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream);
 hipError_t launch_delta_reverse(bool f32, int d_k, bool map, const DeltaArgs& a, hipStream_t stream);
 hipError_t launch_delta_grad(bool f32, int d_k, const DeltaArgs& a, hipStream_t stream);
 

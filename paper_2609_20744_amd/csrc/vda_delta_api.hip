@@ -1,6 +1,8 @@
 // C ABI of the token-wise gated delta rule and of the rotary positions:
 // argument validation, workspace layout, launch order.  Declarations and
 // contracts are in include/vda.h.
+#include <stdlib.h>
+
 #include <algorithm>
 #include <initializer_list>
 
@@ -37,13 +39,13 @@ int check_problem(const vda_delta_problem* p) {
   if (st != VDA_OK) return st;
   if (p->layout != VDA_LAYOUT_HEADS && p->layout != VDA_LAYOUT_TOKENS) return VDA_ERR_UNSUPPORTED;
   if (!aligned(p->cu_seqlens, 4)) return VDA_ERR_ALIGN;
-  // Byte offsets within a chunk's rows are 32-bit, and a launch has one
+  // A token's row is addressed in 24 bits, a chunk's in 32, and a launch has one
   // workgroup of up to 512 threads per chunk (or two per segment) and head.
   const long long es = p->is_f32 ? 4 : 2;
   const long long row = p->layout == VDA_LAYOUT_TOKENS
                             ? es * std::max((long long)p->H_k * p->d_k, (long long)p->H_v * p->d_v)
                             : es * std::max(p->d_k, p->d_v);
-  if (row * vda::kChunk * 2 > 0x7fffffffLL) return VDA_ERR_SIZE;
+  if (row >= 1 << 24) return VDA_ERR_SIZE;
   const long long items = ((long long)p->T / vda::kChunk + p->n_seqs + 1) * p->H_v;
   if (items * 1024 > kMaxThreads || (long long)p->n_seqs * p->H_v * (p->d_v / 16) * 256 > kMaxThreads ||
       (long long)p->T + vda::kChunk > 0x7fffffffLL)
@@ -60,8 +62,9 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   d.max_chunks = (int)(table ? (T + (vda::kChunk - 1) * n) / vda::kChunk : per * n);
   // Segments.
   const long long cus = vda::current_device_cus();
-  const long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
-  d.split = longest > 4 * share;
+  const long long tgt = getenv("TGT") ? atoi(getenv("TGT")) : cus;
+  const long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + tgt - 1) / tgt);
+  d.split = longest > (getenv("FAC") ? atoi(getenv("FAC")) : 4) * share;
   d.seg_chunks = (int)(d.split ? share : std::max(longest, 1LL));
   d.max_segs = (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));
   // Workspace.
@@ -108,9 +111,8 @@ vda::DeltaArgs args_of(const vda_delta_problem* p, const vda::DeltaPlan& d, bool
   const size_t segs = (size_t)d.max_segs * p->H_v, chunks = (size_t)d.max_chunks * p->H_v;
   if (d.split) {
     a.segJ = reinterpret_cast<float*>(w + d.segs);
-    a.segM = a.segJ + segs * mat;
-    a.segMt = a.segM + segs * km;
-    if (backward) a.segdJ = a.segMt + segs * km;
+    a.segM = w + d.segs + segs * mat * 4;
+    if (backward) a.segdJ = reinterpret_cast<float*>(a.segM + segs * 2 * km * 4);
   }
   if (backward) {
     a.keepS = w + d.keep;
@@ -152,7 +154,7 @@ hipError_t plan_and_prepare(const vda_delta_problem* p, const vda::DeltaPlan& d,
   hipError_t e = vda::launch_delta_prepare(p->is_f32 != 0, p->d_k, backward, a, stream);
   if (e != hipSuccess || !d.split) return e;
   if ((e = vda::launch_delta_scan(p->is_f32 != 0, p->d_k, 0, a, stream)) != hipSuccess) return e;
-  return vda::launch_delta_join(p->d_k, false, a, stream);
+  return vda::launch_delta_join(p->is_f32 != 0, p->d_k, false, a, stream);
 }
 
 }  // namespace
@@ -220,7 +222,7 @@ int vda_delta_backward(const vda_delta_problem* p, const void* dout, const void*
   if (e == hipSuccess) e = vda::launch_delta_scan(f32, p->d_k, 2, a, stream);
   if (e == hipSuccess && d.split) {
     e = vda::launch_delta_reverse(f32, p->d_k, true, a, stream);
-    if (e == hipSuccess) e = vda::launch_delta_join(p->d_k, true, a, stream);
+    if (e == hipSuccess) e = vda::launch_delta_join(f32, p->d_k, true, a, stream);
   }
   if (e == hipSuccess) e = vda::launch_delta_reverse(f32, p->d_k, false, a, stream);
   if (e == hipSuccess) e = vda::launch_delta_grad(f32, p->d_k, a, stream);

@@ -28,148 +28,209 @@ namespace {
 // owns 16 value columns of dS, transposed, in registers.  MAP: only what a
 // segment adds to the gradient that enters it (its map's matrix is the
 // forward one's transpose).
-template <bool F32, int DK, bool MAP>
-__global__ __launch_bounds__(512) void delta_reverse_kernel(DeltaArgs a) {
+template <bool F32, int DK, int DV, bool MAP>
+__global__ __launch_bounds__(4 * DV) __attribute__((amdgpu_waves_per_eu(1, 2)))
+void delta_reverse_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
   typedef typename O::W W;
-  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, NC = DK / 16;
-  constexpr int kLuK = __builtin_ctz(DK * ES / 16);
+  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kWaves = DV / 16, kRow = row_tile_bytes<F32>();
   constexpr int kBufs = F32 ? 1 : 2;
   constexpr int kTileK = kChunk * DK * ES;
   constexpr int kOffQ = kTileK, kOffVec = 2 * kTileK, kOffTt = kOffVec + 1024, kOffPt = kOffTt + kWideTri,
-                kOffDo = kOffPt + kWideTri, kStage = kOffDo + kChunk * 128 * ES;
+                kOffDo = kOffPt + kWideTri, kStage = kOffDo + kChunk * DV * ES;
   static_assert(ChunkRecord::kTt == ChunkRecord::kVec + 1024 && ChunkRecord::kPt == ChunkRecord::kTt + kWideTri,
                 "copied together");
-  __shared__ __align__(16) char lds[kBufs * kStage];
+  __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
 
-  const int DV = a.d_v;
   const int h = uniform(blockIdx.x % (unsigned)a.Hv);
   const int seg = uniform(blockIdx.x / (unsigned)a.Hv);
   const SegmentInfo si = segment_info(a, seg);
-  if (si.chunks < 0) return;
+  if (si.len < 0) return;
   if (MAP && (si.ends & 1)) return;  // nothing takes the first segment's
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
-  const int wave = uniform(tid >> 6), waves = uniform(blockDim.x >> 6);
-  const int v0 = wave * 16, col = v0 + li;
-  const int luv = __builtin_ctz(DV * ES / 16);
-  const size_t mat = (size_t)DV * DK;
+  const int wave = uniform(tid >> 6);
+  const int vb = wave >> 1, n0 = wave & 1;
+  const int col = 32 * vb + 8 * (li >> 2) + 4 * n0 + (li & 3);  // this lane's column
+  const int chunks = chunks_of(si.len);
+  constexpr size_t mat = (size_t)DV * DK;
   const size_t rec_size = ChunkRecord::bytes(F32, true);
+  const TileLane tl = tile_lane<F32>(li, lg);
 
   const float* init = nullptr;
   if (si.ends & 2)
     init = a.dS_out ? a.dS_out + ((size_t)si.seq * a.Hv + h) * mat : nullptr;
   else if (!MAP)
     init = a.segdJ + ((size_t)seg * a.Hv + h) * mat;
-  floatx4 S[NC];
+  floatx4 S[KS][2];
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
-    S[c] = init != nullptr ? *reinterpret_cast<const floatx4*>(init + (size_t)col * DK + 16 * c + 4 * lg)
-                           : floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+      S[s][o] = init != nullptr
+                    ? *reinterpret_cast<const floatx4*>(init + (size_t)col * DK + 32 * s + 8 * lg + 4 * o)
+                    : floatx4{0.f, 0.f, 0.f, 0.f};
 
+  // The chunks' rows, from the last: each chunk's 64 rows back.
   const uint32_t k_row = (uint32_t)a.qk_tok * ES, v_row = (uint32_t)a.v_tok * ES;
-  auto stage = [&](int step) {
-    char* buf = lds + (kBufs == 2 && (step & 1) ? kStage : 0);
-    const int chunk = si.chunk + si.chunks - 1 - step;
-    const ChunkInfo ci = chunk_info(a, chunk);
-    const char* rec = a.rec + ((size_t)chunk * a.Hv + h) * rec_size;
-    const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head;
-    const size_t vo = (size_t)ci.tok * a.v_tok + (size_t)h * a.v_head;
-    const uint32_t k_span = (uint32_t)(ci.len - 1) * k_row + DK * ES;
-    copy_rows<F32>(make_rsrc((const char*)a.k + qk * ES, k_span), buf, kLuK, kChunk, ci.len, k_row, wave,
-                   waves, lane);
-    copy_rows<F32>(make_rsrc((const char*)a.q + qk * ES, k_span), buf + kOffQ, kLuK, kChunk, ci.len, k_row,
-                   wave, waves, lane);
-    copy_rows<F32>(make_rsrc((const char*)a.dout + vo * ES, (uint32_t)(ci.len - 1) * v_row + DV * ES),
-                   buf + kOffDo, luv, kChunk, ci.len, v_row, wave, waves, lane);
-    copy_flat(rec + ChunkRecord::kVec, buf + kOffVec, 1024 + 2 * kWideTri, wave, waves, lane);
+  const size_t last = (size_t)si.tok + (size_t)(chunks - 1) * kChunk;
+  const size_t qk = (last * a.qk_tok + (size_t)(h / a.group) * a.qk_head) * ES;
+  const char *kp = (const char*)a.k + qk, *qp = (const char*)a.q + qk;
+  const char* op = (const char*)a.dout + (last * a.v_tok + (size_t)h * a.v_head) * ES;
+  const char* rp = a.rec + ((size_t)(si.chunk + chunks - 1) * a.Hv + h) * rec_size + ChunkRecord::kVec;
+  auto stage = [&](int at, char* buf) __attribute__((always_inline)) {
+    const int len = min(kChunk, si.len - at * kChunk);
+    copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
+    copy_flat<1024 + 2 * kWideTri, kWaves>(rp, buf + kOffVec, wave, lane);
+    copy_tiles<F32, kChunk, DV / 32, kWaves>(make_rsrc(op, 64u * v_row), buf + kOffDo, len, v_row, wave, lane);
+    copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
+    kp -= 64u * k_row, qp -= 64u * k_row, op -= 64u * v_row, rp -= rec_size * a.Hv;
   };
 
-  if (si.chunks > 0) stage(0);
-  for (int step = 0; step < si.chunks; ++step) {
-    copy_barrier();
-    if (kBufs == 2 && step + 1 < si.chunks) stage(step + 1);
-    const char* buf = lds + (kBufs == 2 && (step & 1) ? kStage : 0);
-    const float* gam = reinterpret_cast<const float*>(buf + kOffVec);
+  const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+  auto step = [&](int at, const char* buf) __attribute__((always_inline)) {
+    const float* gam = reinterpret_cast<const float*>(buf + kOffVec) + 4 * lg;
     const float *eta = gam + 64, *beta = gam + 128;
-    const int chunk = si.chunk + si.chunks - 1 - step;
-    const int len = chunk_info(a, chunk).len;
+    const int chunk = si.chunk + at, len = si.len - at * kChunk;
 
-    W Sw[KS];
+    X kr[2][4], dO[2];
+    auto rows = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) Sw[s] = O::wide(S[2 * s], S[2 * s + 1]);
-    if constexpr (!MAP) {
-      char* ks = a.keepdS + ((size_t)chunk * a.Hv + h) * mat * 4;
+      for (int t = 0; t < 4; ++t) kr[s & 1][t] = tile_row<F32>(buf + (4 * s + t) * kRow, tl);
+    };
+    rows(0);
+    floatx4 ev[4];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) store_wide4<F32>(ks, (size_t)col * DK + 16 * c + 4 * lg, mat, S[c]);
-    }
+    for (int t = 0; t < 4; ++t) ev[t] = *reinterpret_cast<const floatx4*>(eta + 16 * t);
+    const char* otiles = buf + kOffDo + 4 * vb * kRow;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      dO[t] = tile_cols<F32>(otiles + 2 * t * kRow, otiles + (2 * t + 1) * kRow, n0, tl);
+    fence<F32>();
 
     // dN = diag(eta) K dS^T + P^T dO.
-    X dO[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) dO[s] = col_op<F32>(buf + kOffDo, luv, 32 * s, v0, li, lg);
     floatx4 dN[4];
+    W M[4];
+    char* ks = a.keepdS + ((size_t)chunk * a.Hv + h) * mat * 4;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      dN[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < KS; ++s) {
+      const W Sw = O::wide(S[s][0], S[s][1]);
+      if constexpr (!MAP) store_wide8<F32>(ks, (size_t)col * DK + 32 * s + 8 * lg, mat, Sw);
+      if (s + 1 < KS)
+        rows(s + 1);
+      else
 #pragma unroll
-      for (int s = 0; s < KS; ++s) dN[t] = O::mma(row_op<F32>(buf, kLuK, 16 * t + li, s, lg), Sw[s], dN[t]);
-      dN[t] *= *reinterpret_cast<const floatx4*>(eta + 16 * t + 4 * lg);
+        for (int t = 0; t < 4; ++t) M[t] = tile_w<F32>(buf + kOffPt, tri_tile_t(t, 1), lane);
+      fence<F32>();
 #pragma unroll
-      for (int s = t / 2; s < 2; ++s)
-        dN[t] = O::mma(tile_w<F32>(buf + kOffPt, tri_tile_t(t, s), lane), dO[s], dN[t]);
+      for (int t = 0; t < 4; ++t) dN[t] = O::mma(kr[s & 1][t], Sw, s == 0 ? zero : dN[t]);
     }
+    W M0[2], Tt[4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) M0[t] = tile_w<F32>(buf + kOffPt, tri_tile_t(t, 0), lane);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) dN[t] = O::mma(M[t], dO[1], dN[t] * ev[t]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) Tt[t] = tile_w<F32>(buf + kOffTt, tri_tile_t(t, 1), lane);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) dN[t] = O::mma(M0[t], dO[0], dN[t]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) M0[t] = tile_w<F32>(buf + kOffTt, tri_tile_t(t, 0), lane);
+    fence<F32>();
     W dNw[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) dNw[s] = O::wide(dN[2 * s], dN[2 * s + 1]);
 
     // dv = beta T^T dN.
-    floatx4 y[4];
+    floatx4 y[4], gv[4], bv[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      y[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int s = t / 2; s < 2; ++s)
-        y[t] = O::mma(tile_w<F32>(buf + kOffTt, tri_tile_t(t, s), lane), dNw[s], y[t]);
-      y[t] *= *reinterpret_cast<const floatx4*>(beta + 16 * t + 4 * lg);
+      gv[t] = *reinterpret_cast<const floatx4*>(gam + 16 * t);
+      bv[t] = *reinterpret_cast<const floatx4*>(beta + 16 * t);
     }
+    // Columns of Q, then of K, half u of the channels at a time.
+    X ct[KS][2];
+    auto columns = [&](const char* tiles, int u) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          ct[s][t] = tile_cols<F32>(tiles + (4 * s + 2 * t) * kRow, tiles + (4 * s + 2 * t + 1) * kRow, u, tl);
+    };
+    columns(buf + kOffQ, 0);
+    fence<F32>();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] = O::mma(Tt[t], dNw[1], zero);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) y[t] = O::mma(M0[t], dNw[0], y[t]);
+
+    // dS <- gam_63 dS + Q^T (scale gam dO) - K^T (gam dv); rows of dO behind
+    // the chunk's end are left out here (elsewhere P or T has zeros there).
+    W dOw[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      floatx4 o[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[u][e] = 32 * s + 16 * u + 4 * lg + e < len
+                        ? a.scale * gv[2 * s + u][e] * O::value(dO[s], 4 * u + e)
+                        : 0.f;
+      dOw[s] = O::wide(o[0], o[1]);
+    }
+    const float gl = reinterpret_cast<const float*>(buf + kOffVec)[63];
+    auto update = [&](int u, const W (&w)[2]) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) S[s][u] = O::mma(ct[s][t], w[t], S[s][u]);
+    };
+#pragma unroll
+    for (int s = 0; s < KS; ++s) S[s][0] *= gl, S[s][1] *= gl;
+    update(0, dOw);
+    columns(buf + kOffQ, 1);
+    update(1, dOw);
+    columns(buf, 0);
+    W yw[2];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) y[t] *= bv[t];
     if constexpr (!MAP) {
       char* kd = a.keepdv + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
         store_wide4<F32>(kd, (size_t)col * kChunk + 16 * t + 4 * lg, (size_t)DV * kChunk, y[t]);
     }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) yw[s] = O::wide(-gv[2 * s] * y[2 * s], -gv[2 * s + 1] * y[2 * s + 1]);
+    update(0, yw);
+    columns(buf, 1);
+    update(1, yw);
+  };
 
-    // dS <- gam_63 dS + Q^T (scale gam dO) - K^T (gam dv); rows of dO behind
-    // the chunk's end are left out here (elsewhere P or T has zeros there).
-    W dOw[2], yw[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      floatx4 o[2], g[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        g[u] = *reinterpret_cast<const floatx4*>(gam + 32 * s + 16 * u + 4 * lg);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[u][e] = 32 * s + 16 * u + 4 * lg + e < len ? a.scale * g[u][e] * O::value(dO[s], 4 * u + e) : 0.f;
-      }
-      dOw[s] = O::wide(o[0], o[1]);
-      yw[s] = O::wide(-g[0] * y[2 * s], -g[1] * y[2 * s + 1]);
+  int at = chunks - 1;
+  if constexpr (kBufs == 2) {
+    if (at >= 0) stage(at, buf0);
+    constexpr int kStores = MAP ? 0 : 2 * KS + 8;  // of a step
+    for (; at >= 0; at -= 2) {
+      if (at == chunks - 1)
+        copy_barrier();
+      else
+        copy_barrier<kStores>();
+      if (at >= 1) stage(at - 1, buf1);
+      step(at, buf0);
+      if (at < 1) break;
+      copy_barrier<kStores>();
+      if (at >= 2) stage(at - 2, buf0);
+      step(at - 1, buf1);
     }
-    const float gl = gam[63];
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      S[c] *= gl;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        S[c] = O::mma(col_op<F32>(buf + kOffQ, kLuK, 32 * s, 16 * c, li, lg), dOw[s], S[c]);
-        S[c] = O::mma(col_op<F32>(buf, kLuK, 32 * s, 16 * c, li, lg), yw[s], S[c]);
-      }
-    }
-    if (kBufs == 1 && step + 1 < si.chunks) {
-      lds_barrier();
-      stage(step + 1);
+  } else {
+    for (; at >= 0; --at) {
+      if (at < chunks - 1) lds_barrier();  // every wave is done with the chunk before
+      stage(at, buf0);
+      copy_barrier();
+      step(at, buf0);
     }
   }
 
@@ -180,282 +241,338 @@ __global__ __launch_bounds__(512) void delta_reverse_kernel(DeltaArgs a) {
     to = a.dS_in + ((size_t)si.seq * a.Hv + h) * mat;
   if (to != nullptr)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) *reinterpret_cast<floatx4*>(to + (size_t)col * DK + 16 * c + 4 * lg) = S[c];
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+        *reinterpret_cast<floatx4*>(to + (size_t)col * DK + 32 * s + 8 * lg + 4 * o) = S[s][o];
 }
 
-// Gradients of a chunk's inputs.  One workgroup of four waves per chunk and
+// Gradients of a chunk's inputs.  One workgroup of eight waves per chunk and
 // key head, over the value heads that share it in turn, whose dq and dk it
-// sums in registers in a fixed order; wave w makes the 16 tokens of block w,
-// transposed (channels x tokens), so a lane stores consecutive channels.  The
-// value channels come in steps of 32 (S, dS, N, dv and dO of those channels),
-// the next step's copied into LDS while this one's are used; all sums over
-// value channels stay in registers between steps.
-template <bool F32, int DK>
-__global__ __launch_bounds__(kThreads) void delta_grad_kernel(DeltaArgs a) {
+// sums in registers in a fixed order.  Wave w makes the 16 tokens of tile
+// w % 4, transposed (channels x tokens), of every other four channels; of the
+// scores between tokens it makes the rows of 32 tokens, and the other wave of
+// the tile the others, exchanged at a head's end.  The value channels come in
+// steps of 32 (S, dS, N, dv and dO of those channels), the next step's copied
+// into LDS while this one's are used; all sums over value channels stay in
+// registers between steps, <dS, S> and N.dv too, as the diagonals of products.
+// Chunks start with different steps: their matrices lie a power of two apart,
+// and in step they would load the memory's channels one after another.  Tokens
+// and key channels are taken in twisted order, value channels in paired order
+// (vda_delta.h).
+template <bool F32, int DK, int DV>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void delta_grad_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
   typedef typename O::W W;
-  constexpr int ES = F32 ? 4 : 2, NC = DK / 16, kPlanes = F32 ? 1 : 2;
-  constexpr int kLuK = __builtin_ctz(DK * ES / 16), kLuN = F32 ? 4 : 3, kLuO = F32 ? 3 : 2;
+  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kPlanes = F32 ? 1 : 2, kRow = row_tile_bytes<F32>();
   constexpr int kTileK = kChunk * DK * ES, kTileS = 32 * DK * ES, kTileN = 32 * kChunk * ES;
-  constexpr int kBufs = F32 ? 1 : 2;
+  // Two steps in turn: a head's are then a whole number of turns.
+  constexpr int steps = DV / 32, kBufs = F32 || steps == 1 ? 1 : 2;
   constexpr int kOffdS = kPlanes * kTileS, kOffN = 2 * kPlanes * kTileS, kOffdv = kOffN + kPlanes * kTileN,
-                kOffO = kOffdv + kPlanes * kTileN, kStage = kOffO + kTileN;
-  __shared__ __align__(16) char lds[2 * kTileK + kBufs * kStage];
+                kOffO = kOffdv + kPlanes * kTileN, kUsed = kOffO + kTileN;
+  // (A head's end exchanges six operands of four tiles there.)
+  constexpr int kSwap = 4 * 6 * 64 * (int)sizeof(X), kStage = kUsed > kSwap ? kUsed : kSwap;
+  constexpr size_t mat = (size_t)DV * DK, nmat = (size_t)DV * kChunk;
+  __shared__ __align__(16) char rowsKQ[2 * kTileK], buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
   __shared__ double pre[kChunk];
-  __shared__ float gam[kChunk], eta[kChunk], strengths[kChunk], suffix[kChunk], prefix[kChunk], rows[4][kChunk],
-      states[4];
+  __shared__ float suffix[2][kChunk], prefix[2][kChunk], passed[4][kChunk], states[8];
 
   const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
   const int chunk = uniform(blockIdx.x / (unsigned)a.Hk);
   const ChunkInfo ci = chunk_info(a, chunk);
   if (ci.len == 0) return;
-  const int DV = a.d_v, steps = DV / 32, len = ci.len;
+  const int len = ci.len;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave = uniform(tid >> 6);
-  const int j0 = 16 * wave, j = j0 + li;  // this lane's token
-  const size_t mat = (size_t)DV * DK, nmat = (size_t)DV * kChunk;
+  const int w = wave & 3, part = wave >> 2;  // token tile; the channels' half
+  const int j = twisted_row(w, li);          // this lane's token
+  const TwistedLane tl = twisted_lane<F32>(li, lg);
+  int mine[4], own[4];  // column offsets of this wave's channels, and of its tokens
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    mine[e] = part ? tl.col[1][e] : tl.col[0][e], own[e] = w & 1 ? tl.col[1][e] : tl.col[0][e];
 
   const uint32_t k_row = (uint32_t)a.qk_tok * ES, v_row = (uint32_t)a.v_tok * ES;
-  const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)hk * a.qk_head;
-  const uint32_t k_span = (uint32_t)(len - 1) * k_row + DK * ES;
-  const uint32_t v_span = (uint32_t)(len - 1) * v_row + DV * ES;
-  const char* const tileK = lds;
-  const char* const tileQ = lds + kTileK;
-  char* const ring = lds + 2 * kTileK;
-  copy_rows<F32>(make_rsrc((const char*)a.k + qk * ES, k_span), lds, kLuK, kChunk, len, k_row, wave, 4, lane);
-  copy_rows<F32>(make_rsrc((const char*)a.q + qk * ES, k_span), lds + kTileK, kLuK, kChunk, len, k_row, wave, 4,
-                 lane);
+  const size_t qk = ((size_t)ci.tok * a.qk_tok + (size_t)hk * a.qk_head) * ES;
+  const char* const tileK = rowsKQ;
+  const char* const tileQ = rowsKQ + kTileK;
+  copy_tiles<F32, kChunk, KS, 8, RowOrder::kTwisted>(make_rsrc((const char*)a.k + qk, 64u * k_row), rowsKQ, len,
+                                                     k_row, wave, lane);
+  copy_tiles<F32, kChunk, KS, 8, RowOrder::kTwisted>(make_rsrc((const char*)a.q + qk, 64u * k_row), rowsKQ + kTileK,
+                                                     len, k_row, wave, lane);
 
-  const int total = a.group * steps;
-  auto stage = [&](int n) {
-    char* buf = ring + (kBufs == 2 && (n & 1) ? kStage : 0);
-    const int h = hk * a.group + n / steps, s = n % steps;
-    const size_t at = (size_t)chunk * a.Hv + h;
+  const size_t first = (size_t)chunk * a.Hv + (size_t)hk * a.group;
+  const size_t vo = ((size_t)ci.tok * a.v_tok + (size_t)hk * a.group * a.v_head) * ES;
+  const int turned = uniform(chunk + hk);
+  auto channels = [&](int n) { return (n + turned) & (steps - 1); };  // step n's value channels, 32 s ..
+  // Step n: of head n / steps.  (A head's second plane is an offset.)
+  auto stage = [&](int n, char* buf) __attribute__((always_inline)) {
+    constexpr uint32_t kMat = mat * ES, kNmat = nmat * ES;
+    const int s = channels(n);
+    const size_t at = first + n / steps;
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.keepS + at * mat * 4, kPlanes * kMat),
+                                 dsr = make_rsrc(a.keepdS + at * mat * 4, kPlanes * kMat),
+                                 nr = make_rsrc(a.keepN + at * nmat * 4, kPlanes * kNmat),
+                                 dvr = make_rsrc(a.keepdv + at * nmat * 4, kPlanes * kNmat);
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-      const size_t so = at * mat * 4 + ((size_t)p * mat + (size_t)32 * s * DK) * ES;
-      const size_t no = at * nmat * 4 + ((size_t)p * nmat + (size_t)32 * s * kChunk) * ES;
-      copy_rows<F32>(make_rsrc(a.keepS + so, kTileS), buf + p * kTileS, kLuK, 32, 32, DK * ES, wave, 4, lane);
-      copy_rows<F32>(make_rsrc(a.keepdS + so, kTileS), buf + kOffdS + p * kTileS, kLuK, 32, 32, DK * ES, wave, 4,
-                     lane);
-      copy_rows<F32>(make_rsrc(a.keepN + no, kTileN), buf + kOffN + p * kTileN, kLuN, 32, 32, kChunk * ES, wave, 4,
-                     lane);
-      copy_rows<F32>(make_rsrc(a.keepdv + no, kTileN), buf + kOffdv + p * kTileN, kLuN, 32, 32, kChunk * ES, wave,
-                     4, lane);
+      const uint32_t so = p * kMat + s * kTileS, no = p * kNmat + s * kTileN;
+      copy_tiles<F32, 32, KS, 8, RowOrder::kPaired>(sr, buf + p * kTileS, 32, DK * ES, wave, lane, so);
+      copy_tiles<F32, 32, KS, 8, RowOrder::kPaired>(dsr, buf + kOffdS + p * kTileS, 32, DK * ES, wave, lane, so);
+      copy_tiles<F32, 32, 2, 8, RowOrder::kPaired>(nr, buf + kOffN + p * kTileN, 32, kChunk * ES, wave, lane, no);
+      copy_tiles<F32, 32, 2, 8, RowOrder::kPaired>(dvr, buf + kOffdv + p * kTileN, 32, kChunk * ES, wave, lane, no);
     }
-    const size_t vo = (size_t)ci.tok * a.v_tok + (size_t)h * a.v_head + 32 * s;
-    copy_rows<F32>(make_rsrc((const char*)a.dout + vo * ES, (uint32_t)(len - 1) * v_row + 32 * ES), buf + kOffO,
-                   kLuO, kChunk, len, v_row, wave, 4, lane);
+    copy_tiles<F32, kChunk, 1, 8, RowOrder::kTwisted>(
+        make_rsrc((const char*)a.dout + vo + (n / steps) * a.v_head * ES, 64u * v_row), buf + kOffO, len, v_row, wave,
+        lane, 32 * s * ES);
   };
-  // A wide operand from the planes of a tile.
-  auto wide_col = [&](const char* tile, int plane, int lu, int c0) {
+  // Columns of tile block b of 32 rows of value channels: an exact operand of
+  // one plane, or a wide one of all.
+  auto col_x = [&](const char* tiles, int b, const int(&col)[4]) {
+    return twisted_cols<F32>(tiles + 2 * b * kRow, tiles + (2 * b + 1) * kRow, col);
+  };
+  auto col_w = [&](const char* tiles, int plane, int b, const int(&col)[4]) {
     if constexpr (F32)
-      return W{col_op<true>(tile, lu, 0, c0, li, lg)};
+      return W{col_x(tiles, b, col)};
     else
-      return W{col_op<false>(tile, lu, 0, c0, li, lg), col_op<false>(tile + plane, lu, 0, c0, li, lg)};
+      return W{col_x(tiles, b, col), col_x(tiles + plane, b, col)};
+  };
+  auto rows = [&](const char* tile) {
+    if constexpr (F32)
+      return Op<true>::narrow(*reinterpret_cast<const floatx4*>(tile + tl.row),
+                              *reinterpret_cast<const floatx4*>(tile + 1024 + tl.row));
+    else
+      return *reinterpret_cast<const bf16x8*>(tile + tl.row);
   };
 
   const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-  floatx4 dq[NC], dk[NC];
+  floatx4 dq[KS], dk[KS];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) dq[c] = zero, dk[c] = zero;
-  stage(0);
-  for (int hv = 0; hv < a.group; ++hv) {
-    const int h = hk * a.group + hv;
-    // The head's decays and strengths (the barrier below comes before their use).
-    if (hv > 0) lds_barrier();
-    if (wave == 0) {
-      const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
-      const bool real = lane < len;
-      const double G = decay_prefix(real ? a.g[at] : 0.f, lane);
-      const double last = __shfl(G, 63);
-      pre[lane] = G;
-      gam[lane] = exp2f((float)G);
-      eta[lane] = exp2f((float)(last - G));
-      strengths[lane] = real ? strength(a.beta[at]) : 1.f;
-    }
-    floatx4 Wt[4], Wn[4], Xa[4], Xb[4], Q[NC], Ka[NC], Kb[NC];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) Wt[t] = Wn[t] = Xa[t] = Xb[t] = zero;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) Q[c] = Ka[c] = Kb[c] = zero;
-    float db = 0.f, ss = 0.f;
-    const size_t vo = (size_t)ci.tok * a.v_tok + (size_t)h * a.v_head;
-    const __amdgpu_buffer_rsrc_t dvr = make_rsrc((char*)a.dv + vo * ES, v_span);
-    for (int s = 0; s < steps; ++s) {
-      const int n = hv * steps + s;
-      copy_barrier();
-      if (kBufs == 2 && n + 1 < total) stage(n + 1);
-      const char* buf = ring + (kBufs == 2 && (n & 1) ? kStage : 0);
-      const char *tS = buf, *tdS = buf + kOffdS, *tN = buf + kOffN, *tdv = buf + kOffdv, *tO = buf + kOffO;
+  for (int s = 0; s < KS; ++s) dq[s] = zero, dk[s] = zero;
 
-      // Tokens of this wave.
-      const X Oj = row_op<F32>(tO, kLuO, j, 0, lg);
-      const W Nj = wide_col(tN, kTileN, kLuN, j0), vj = wide_col(tdv, kTileN, kLuN, j0);
-      // dv out, and its product with N.
-      {
-        const uint32_t off = (uint32_t)j * v_row + (uint32_t)(32 * s + 4 * lg) * ES;
-        const float ib = 1.f / strengths[j];
-        float x[8];
+  // Sums over a head's value channels; the scores' rows are tiles 2 part, 2 part + 1.
+  floatx4 Wt[2], Wn[2], Xa[2], Xb[2], Q[KS], Ka[KS], Kb[KS], SS, ND;
+  // Of a head: this lane's token's, and (wave 0) token `lane`'s G and g.
+  struct Gates {
+    float gam, eta, strength, ends, decay;
+    double pre;
+  };
+  auto step = [&](int n, const char* buf) __attribute__((always_inline)) {
+    const char *tS = buf, *tdS = buf + kOffdS, *tN = buf + kOffN, *tdv = buf + kOffdv, *tO = buf + kOffO;
+    const X Oj = rows(tO + w * kRow);
+    const W Nj = col_w(tN, kTileN, w >> 1, own), vj = col_w(tdv, kTileN, w >> 1, own);
+    // Products with the states, channels x tokens; operands one block ahead.
+    W Sc[2], dSc[2];
+    Sc[0] = col_w(tS, kTileS, 0, mine), dSc[0] = col_w(tdS, kTileS, 0, mine);
+    X Nt[2], Ot[2];
+    W vt[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = O::value(vj, e);
-          db += (O::value(Nj, e) * ib) * (x[e] * ib);
-        }
+    for (int c = 0; c < KS; ++c) {
+      if (c + 1 < KS) {
+        Sc[(c + 1) & 1] = col_w(tS, kTileS, c + 1, mine), dSc[(c + 1) & 1] = col_w(tdS, kTileS, c + 1, mine);
+      } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          if constexpr (F32)
-            store_b128(dvr, off + 64u * u,
-                       __builtin_bit_cast(u32x4, floatx4{x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]}));
-          else
-            store_b64(dvr, off + 32u * u,
-                      make_uint2(pack_bf16x2(x[4 * u], x[4 * u + 1]), pack_bf16x2(x[4 * u + 2], x[4 * u + 3])));
+          Nt[u] = col_x(tN, part, tl.col[u]);
+          vt[u] = col_w(tdv, kTileN, part, tl.col[u]);
+          Ot[u] = rows(tO + (2 * part + u) * kRow);
         }
       }
-      // Scores between tokens, columns of this wave.
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        if (t <= wave) {
-          const X Nt = col_op<F32>(tN, kLuN, 0, 16 * t, li, lg);
-          Wt[t] = O::mma(Nt, Oj, Wt[t]);             // dO_j.N_i, rows i <= j
-          Xb[t] = O::mma(Nt, O::head(vj), Xb[t]);    // dv_j.N_i
-        }
-        if (t >= wave) {
-          Wn[t] = O::mma(row_op<F32>(tO, kLuO, 16 * t + li, 0, lg), Nj, Wn[t]);  // dO_i.N_j, rows i >= j
-          Xa[t] = O::mma(wide_col(tdv, kTileN, kLuN, 16 * t), Nj, Xa[t]);       // dv_i.N_j
-        }
-      }
-      // Products with the states, channels x tokens.
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const W Sc = wide_col(tS, kTileS, kLuK, 16 * c), dSc = wide_col(tdS, kTileS, kLuK, 16 * c);
-        Q[c] = O::mma(Sc, Oj, Q[c]);
-        Ka[c] = O::mma(dSc, Nj, Ka[c]);
-        Kb[c] = O::mma(Sc, vj, Kb[c]);
-        if ((c & 3) == wave)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss += O::value(Sc, e) * O::value(dSc, e);
-      }
-      if (kBufs == 1 && n + 1 < total) {
-        lds_barrier();
-        stage(n + 1);
-      }
+      fence<F32>();
+      Q[c] = O::mma(Sc[c & 1], Oj, Q[c]);
+      Ka[c] = O::mma(dSc[c & 1], Nj, Ka[c]);
+      Kb[c] = O::mma(Sc[c & 1], vj, Kb[c]);
+      SS = O::mma(Sc[c & 1], dSc[c & 1], SS);
     }
+    ND = O::mma(Nj, vj, ND);
+    // Scores between tokens, columns of this wave (those that the order of
+    // tokens rules out are left out at the head's end).
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      Wt[u] = O::mma(Nt[u], Oj, Wt[u]);           // dO_j.N_i, for i <= j
+      Xb[u] = O::mma(Nt[u], O::head(vj), Xb[u]);  // dv_j.N_i
+      Wn[u] = O::mma(Ot[u], Nj, Wn[u]);           // dO_i.N_j, for i >= j
+      Xa[u] = O::mma(vt[u], Nj, Xa[u]);           // dv_i.N_j
+    }
+    // dv out: its rounding is its first part.  (Half of the waves store; the
+    // others' stores are out of the buffer's range, as rows behind the end are.)
+    const __amdgpu_buffer_rsrc_t dvr = make_rsrc((char*)a.dv + vo + (n / steps) * a.v_head * ES,
+                                                 (uint32_t)(len - 1) * v_row + (uint32_t)DV * ES);
+    const bool stores = part == (n & 1);
+    const uint32_t off = stores ? (uint32_t)j * v_row + (uint32_t)(32 * channels(n) + 8 * lg) * ES : kOutOfRange;
+    const X out = O::head(vj);
+    if constexpr (F32) {
+      store_b128(dvr, off, __builtin_bit_cast(u32x4, floatx4{out[0], out[1], out[2], out[3]}));
+      store_b128(dvr, stores ? off + 16u : kOutOfRange,
+                 __builtin_bit_cast(u32x4, floatx4{out[4], out[5], out[6], out[7]}));
+    } else {
+      store_b128(dvr, off, __builtin_bit_cast(u32x4, out));
+    }
+  };
 
+  auto gates = [&](int h) {
+    const char* rec = a.rec + ((size_t)chunk * a.Hv + h) * ChunkRecord::bytes(F32, true);
+    const float* vec = reinterpret_cast<const float*>(rec + ChunkRecord::kVec);
+    Gates g;
+    g.gam = vec[j], g.eta = vec[64 + j], g.ends = vec[63];
+    g.strength = j < len ? vec[128 + j] : 1.f;
+    g.pre = reinterpret_cast<const double*>(rec + ChunkRecord::kPre)[lane];
+    g.decay = wave == 0 && lane < len ? a.g[(size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head] : 0.f;
+    return g;
+  };
+  auto clear = [&]() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) Wt[u] = Wn[u] = Xa[u] = Xb[u] = zero;
+#pragma unroll
+    for (int c = 0; c < KS; ++c) Q[c] = Ka[c] = Kb[c] = zero;
+    SS = zero, ND = zero;
+  };
+
+  // The end of a head; `swap` is LDS that nothing else uses now.
+  auto finish = [&](int h, const Gates& g, char* swap) {
+    if (wave == 0) pre[lane] = g.pre;
+    lds_barrier();
     // Decays between tokens: columns j of this lane.  What passes from j to
     // i > j (A): its sums over i, for token j, and over j, for tokens i.
     const double gj = pre[j];
-    const float gamj = gam[j], etaj = eta[j];
-    floatx4 Xs[4];
+    floatx4 Xs[2];
     float below = 0.f;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int u = 0; u < 2; ++u) {
+      const int t = 2 * part + u;
       floatx4 qk = zero, kk = zero;
-      if (t >= wave)
 #pragma unroll
-        for (int s = 0; s < DK / 32; ++s) {
-          const X kj = row_op<F32>(tileK, kLuK, j, s, lg);
-          qk = O::mma(row_op<F32>(tileQ, kLuK, 16 * t + li, s, lg), kj, qk);
-          kk = O::mma(row_op<F32>(tileK, kLuK, 16 * t + li, s, lg), kj, kk);
-        }
+      for (int s = 0; s < KS; ++s) {
+        const X kj = rows(tileK + (4 * s + w) * kRow);
+        qk = O::mma(rows(tileQ + (4 * s + t) * kRow), kj, qk);
+        kk = O::mma(rows(tileK + (4 * s + t) * kRow), kj, kk);
+      }
       floatx4 A = zero;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = 16 * t + 4 * lg + e;
-        const double gi = pre[i];
-        const float down = i >= j ? exp2f((float)(gi - gj)) : 0.f, up = i <= j ? exp2f((float)(gj - gi)) : 0.f;
-        Wt[t][e] = i <= j ? a.scale * up * Wt[t][e] : 0.f;
-        Wn[t][e] = i >= j && i < len ? a.scale * down * Wn[t][e] : 0.f;
-        Xs[t][e] = i > j ? -down * Xa[t][e] : i < j ? -up * Xb[t][e] : 0.f;
-        A[e] = i > j && i < len ? Wn[t][e] * qk[e] + Xs[t][e] * kk[e] : 0.f;
+        const int i = twisted_row(t, 4 * lg + e);
+        const double apart = pre[i] - gj;
+        const float d = pow2(i >= j ? apart : -apart);
+        Wt[u][e] = i <= j ? a.scale * d * Wt[u][e] : 0.f;
+        Wn[u][e] = i >= j && i < len ? a.scale * d * Wn[u][e] : 0.f;
+        Xs[u][e] = i > j ? -d * Xa[u][e] : i < j ? -d * Xb[u][e] : 0.f;
+        A[e] = i > j && i < len ? Wn[u][e] * qk[e] + Xs[u][e] * kk[e] : 0.f;
         below += A[e];
-      }
-      // Sums over the 16 columns of this wave.
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) A[e] += __shfl_xor(A[e], m);
+        A[e] = group_sum<16>(A[e]);
       }
       if (li == 0)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) rows[wave][16 * t + 4 * lg + e] = A[e];
+        for (int e = 0; e < 4; ++e) passed[w][twisted_row(t, 4 * lg + e)] = A[e];
     }
+    // The tokens' operands of the two waves of a tile: [tile][tokens 32 b ..][which][lane].
+    X Wy[2], Wx[2], Xx[2];
+    X* const ex = reinterpret_cast<X*>(swap) + w * 6 * 64 + lane;
+    ex[part * 192] = O::narrow(Wt[0], Wt[1]);
+    ex[part * 192 + 64] = O::narrow(Wn[0], Wn[1]);
+    ex[part * 192 + 128] = O::narrow(Xs[0], Xs[1]);
+    lds_barrier();
+#pragma unroll
+    for (int b = 0; b < 2; ++b) Wy[b] = ex[b * 192], Wx[b] = ex[b * 192 + 64], Xx[b] = ex[b * 192 + 128];
     float in = 0.f, end = 0.f;
-    X Xx[2], Wx[2], Wy[2];
+    const bool second = part ^ (lg >> 1);  // this lane's half of eight channels
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      Xx[s] = O::narrow(Xs[2 * s], Xs[2 * s + 1]);
-      Wx[s] = O::narrow(Wn[2 * s], Wn[2 * s + 1]);
-      Wy[s] = O::narrow(Wt[2 * s], Wt[2 * s + 1]);
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      floatx4 x = (a.scale * gamj) * Q[c], y = etaj * Ka[c] - gamj * Kb[c];
+    for (int c = 0; c < KS; ++c) {
+      floatx4 x = (a.scale * g.gam) * Q[c], y = g.eta * Ka[c] - g.gam * Kb[c];
       // This lane's four channels of its token's q and k.
-      const int sw = swizzle<F32>(j, kLuK);
-      floatx4 qv, kv;
-      if constexpr (F32) {
-        const int at = (j << (kLuK + 4)) + (((4 * c + lg) ^ sw) << 4);
-        qv = *reinterpret_cast<const floatx4*>(tileQ + at);
-        kv = *reinterpret_cast<const floatx4*>(tileK + at);
-      } else {
-        const int at = (j << (kLuK + 4)) + (((2 * c + (lg >> 1)) ^ sw) << 4) + (lg & 1) * 8;
-        const uint2 q2 = *reinterpret_cast<const uint2*>(tileQ + at), k2 = *reinterpret_cast<const uint2*>(tileK + at);
-        qv = floatx4{bf16_lo(q2.x), bf16_hi(q2.x), bf16_lo(q2.y), bf16_hi(q2.y)};
-        kv = floatx4{bf16_lo(k2.x), bf16_hi(k2.x), bf16_lo(k2.y), bf16_hi(k2.y)};
+      const X qv = rows(tileQ + (4 * c + w) * kRow), kv = rows(tileK + (4 * c + w) * kRow);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float qe = second ? O::value(qv, 4 + e) : O::value(qv, e),
+                    ke = second ? O::value(kv, 4 + e) : O::value(kv, e);
+        in += qe * x[e] - g.gam * ke * Kb[c][e], end += ke * Ka[c][e];
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) in += qv[e] * x[e] - gamj * kv[e] * Kb[c][e], end += kv[e] * Ka[c][e];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const X kt = col_op<F32>(tileK, kLuK, 32 * s, 16 * c, li, lg);
-        const X qt = col_op<F32>(tileQ, kLuK, 32 * s, 16 * c, li, lg);
-        x = O::mma(kt, Wy[s], x);
-        y = O::mma(qt, Wx[s], y);
-        y = O::mma(kt, Xx[s], y);
+      for (int b = 0; b < 2; ++b) {
+        const X kt = twisted_cols<F32>(tileK + (4 * c + 2 * b) * kRow, tileK + (4 * c + 2 * b + 1) * kRow, mine);
+        const X qt = twisted_cols<F32>(tileQ + (4 * c + 2 * b) * kRow, tileQ + (4 * c + 2 * b + 1) * kRow, mine);
+        x = O::mma(kt, Wy[b], x);
+        y = O::mma(qt, Wx[b], y);
+        y = O::mma(kt, Xx[b], y);
       }
       dq[c] += x;
       dk[c] += y;
     }
-    // Sums over the lanes of a token (lg), then over the chunk.
-    float past = below + etaj * end;
+    // Diagonals: this lane's token's N.dv, and its share of <dS, S>.
+    float db = 0.f, ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) db += li == 4 * lg + e ? ND[e] : 0.f, ss += li == 4 * lg + e ? SS[e] : 0.f;
+    // Sums over the lanes of a token (lg), over the channels' halves, then over the chunk.
+    float past = below + g.eta * end;
     in += __shfl_xor(in, 16), in += __shfl_xor(in, 32);
     past += __shfl_xor(past, 16), past += __shfl_xor(past, 32);
     db += __shfl_xor(db, 16), db += __shfl_xor(db, 32);
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) ss += __shfl_xor(ss, m);
+    ss = group_sum<16>(ss);
+    ss += __shfl_xor(ss, 16), ss += __shfl_xor(ss, 32);
     if (lg == 0) {
-      suffix[j] = j < len ? in : 0.f;
-      prefix[j] = j < len ? past : 0.f;
-      if (j < len) a.dbeta[(size_t)(ci.tok + j) * a.gate_tok + (size_t)h * a.gate_head] = db;
+      suffix[part][j] = j < len ? in : 0.f;
+      prefix[part][j] = j < len ? past : 0.f;
+      if (part == 0 && j < len)
+        a.dbeta[(size_t)(ci.tok + j) * a.gate_tok + (size_t)h * a.gate_head] = db / g.strength / g.strength;
     }
     if (lane == 0) states[wave] = ss;
     lds_barrier();
     if (wave == 0) {
-      // Token t = lane: sums of suffix from t on, and of prefix less rows before t.
-      const float pass = prefix[lane] - ((rows[0][lane] + rows[1][lane]) + (rows[2][lane] + rows[3][lane]));
-      float x = suffix[lane], y = pass;
+      // Token t = lane: sums of suffix from t on, and of prefix less passed before t.
+      const float pass = (prefix[0][lane] + prefix[1][lane]) -
+                         ((passed[0][lane] + passed[1][lane]) + (passed[2][lane] + passed[3][lane]));
+      float x = suffix[0][lane] + suffix[1][lane], y = pass;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const float down = __shfl_down(x, d), up = __shfl_up(y, d);
         if (lane + d < 64) x += down;
         if (lane >= d) y += up;
       }
-      x += y - pass + gam[63] * ((states[0] + states[1]) + (states[2] + states[3]));
+      x += y - pass + g.ends * (states[0] + states[4]);  // (all waves of a half have the same sum)
       if (lane < len) {
         const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
         // A decay of zero: nothing of the state before reaches the token.
-        a.dg[at] = a.g[at] < kMinLogDecay ? 0.f : x;
+        a.dg[at] = g.decay < kMinLogDecay ? 0.f : x;
       }
     }
+  };
+
+  // Steps of all heads in turn.
+  const int total = a.group * steps;
+  Gates g = gates(hk * a.group);
+  if constexpr (kBufs == 2) stage(0, buf0);
+  for (int h = hk * a.group, n = 0; n < total; ++h) {
+    clear();
+    for (int s = 0; s < steps; s += kBufs, n += kBufs) {
+      if constexpr (kBufs == 2) {
+        if (n == 0)
+          copy_barrier();
+        else
+          copy_barrier<1>();  // (dv of the step between)
+        stage(n + 1, buf1);
+        step(n, buf0);
+        copy_barrier<1>();
+        if (n + 2 < total) stage(n + 2, buf0);
+        step(n + 1, buf1);
+      } else {
+        if (n > 0) lds_barrier();  // every wave is done with the step before
+        stage(n, buf0);
+        copy_barrier();
+        step(n, buf0);
+      }
+    }
+    const Gates next = n < total ? gates(h + 1) : g;
+    lds_barrier();  // every wave is done with the last step
+    finish(h, g, kBufs == 2 ? buf1 : buf0);
+    g = next;
   }
 
-  const __amdgpu_buffer_rsrc_t dqr = make_rsrc((char*)a.dq + qk * ES, k_span);
-  const __amdgpu_buffer_rsrc_t dkr = make_rsrc((char*)a.dk + qk * ES, k_span);
+  const uint32_t k_span = (uint32_t)(len - 1) * k_row + DK * ES;
+  const __amdgpu_buffer_rsrc_t dqr = make_rsrc((char*)a.dq + qk, k_span);
+  const __amdgpu_buffer_rsrc_t dkr = make_rsrc((char*)a.dk + qk, k_span);
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    const uint32_t off = (uint32_t)j * k_row + (uint32_t)(16 * c + 4 * lg) * ES;
+  for (int c = 0; c < KS; ++c) {
+    const uint32_t off = (uint32_t)j * k_row + (uint32_t)(32 * c + 8 * lg + 4 * (part ^ (lg >> 1))) * ES;
     if constexpr (F32) {
       store_b128(dqr, off, __builtin_bit_cast(u32x4, dq[c]));
       store_b128(dkr, off, __builtin_bit_cast(u32x4, dk[c]));
@@ -466,19 +583,33 @@ __global__ __launch_bounds__(kThreads) void delta_grad_kernel(DeltaArgs a) {
   }
 }
 
-template <bool F32, int DK>
+template <bool F32, int DK, int DV>
 hipError_t reverse(bool map, const DeltaArgs& a, hipStream_t stream) {
-  const unsigned items = (unsigned)a.max_segs * (unsigned)a.Hv, threads = 4u * a.d_v;
+  const unsigned items = (unsigned)a.max_segs * (unsigned)a.Hv;
   if (map)
-    delta_reverse_kernel<F32, DK, true><<<items, threads, 0, stream>>>(a);
+    delta_reverse_kernel<F32, DK, DV, true><<<items, 4 * DV, 0, stream>>>(a);
   else
-    delta_reverse_kernel<F32, DK, false><<<items, threads, 0, stream>>>(a);
+    delta_reverse_kernel<F32, DK, DV, false><<<items, 4 * DV, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <bool F32, int DK>
+hipError_t reverse(bool map, const DeltaArgs& a, hipStream_t stream) {
+  switch (a.d_v) {
+    case 32: return reverse<F32, DK, 32>(map, a, stream);
+    case 64: return reverse<F32, DK, 64>(map, a, stream);
+    default: return reverse<F32, DK, 128>(map, a, stream);
+  }
+}
+
+template <bool F32, int DK>
 hipError_t grad(const DeltaArgs& a, hipStream_t stream) {
-  delta_grad_kernel<F32, DK><<<(unsigned)a.max_chunks * (unsigned)a.Hk, kThreads, 0, stream>>>(a);
+  const unsigned grid = (unsigned)a.max_chunks * (unsigned)a.Hk;
+  switch (a.d_v) {
+    case 32: delta_grad_kernel<F32, DK, 32><<<grid, 512, 0, stream>>>(a); break;
+    case 64: delta_grad_kernel<F32, DK, 64><<<grid, 512, 0, stream>>>(a); break;
+    default: delta_grad_kernel<F32, DK, 128><<<grid, 512, 0, stream>>>(a); break;
+  }
   return hipGetLastError();
 }
 

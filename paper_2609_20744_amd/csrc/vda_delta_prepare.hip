@@ -151,9 +151,10 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
     strengths[lane] = real ? strength(a.beta[at]) : 0.f;
     const double last = __shfl(G, 63);
     float* vec = reinterpret_cast<float*>(rec + ChunkRecord::kVec);
-    vec[lane] = exp2f((float)G);
-    vec[64 + lane] = exp2f((float)(last - G));
+    vec[lane] = pow2(G);
+    vec[64 + lane] = pow2(last - G);
     vec[128 + lane] = strengths[lane];
+    if constexpr (BACKWARD) reinterpret_cast<double*>(rec + ChunkRecord::kPre)[lane] = G;
   }
   lds_barrier();
 
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = r0 + 4 * lg + e;
-      m[i * kLd + j] = i > j ? bi[e] * exp2f((float)(gi[e] - gj)) * acc[e] : 0.f;
+      m[i * kLd + j] = i > j ? bi[e] * pow2(gi[e] - gj) * acc[e] : 0.f;
     }
   }
 
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int j = 16 * t + 4 * lg + e;
-          p[u][e] = i >= j ? a.scale * exp2f((float)(gq - pre[j])) * p[u][e] : 0.f;
+          p[u][e] = i >= j ? a.scale * pow2(gq - pre[j]) * p[u][e] : 0.f;
         }
       }
       store_tile_x<F32>(rec + ChunkRecord::kP, tri_tile(wave, s), lane, O::narrow(p[0], p[1]));
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * t + 4 * lg + e;
-          p[u][e] = i >= j ? a.scale * exp2f((float)(pre[i] - gj)) * p[u][e] : 0.f;
+          p[u][e] = i >= j ? a.scale * pow2(pre[i] - gj) * p[u][e] : 0.f;
         }
       }
       store_tile_w<F32>(rec + ChunkRecord::kPt, tri_tile_t(wave, s), lane, O::wide(p[0], p[1]));
@@ -318,13 +319,13 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
   const int ns = sbase < max_segs ? sbase : max_segs;
   for (int s = tid; s < ns; s += kPlanThreads) {
     const int seq = find(spre, s);
-    const int at = s - spre[seq], chunks = cpre[seq + 1] - cpre[seq];
-    const int first = cpre[seq] + at * seg_chunks;
-    int count = chunks - at * seg_chunks;
-    count = count < seg_chunks ? count : seg_chunks;
-    if (first + count > nc) count = nc - first;
+    const int at = s - spre[seq], first = cpre[seq] + at * seg_chunks, from = at * seg_chunks * kChunk;
+    const int b = clamp(cu[seq]);
+    int len = clamp(cu[seq + 1]) - b - from;
+    if (len > seg_chunks * kChunk) len = seg_chunks * kChunk;
+    if (len > (nc - first) * kChunk) len = (nc - first) * kChunk;  // offsets that decrease: the table ends
     const bool last = s + 1 >= spre[seq + 1];
-    seg_tab[s] = make_int4(first, count > 0 ? count : 0, seq, (at == 0 ? 1 : 0) | (last ? 2 : 0));
+    seg_tab[s] = make_int4(first, b + from, len > 0 ? len : 0, seq << 2 | (at == 0 ? 1 : 0) | (last ? 2 : 0));
   }
 }
 

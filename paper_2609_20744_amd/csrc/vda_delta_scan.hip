@@ -2,7 +2,7 @@
 // (vda_delta.h), with the outputs, with what the gradient kernel reads, or as
 // the affine maps of segments; and the join of those maps.
 //
-// One workgroup per segment and value head; a wave owns 16 NV value columns of
+// One workgroup per segment and value head; a wave owns 32 value columns of
 // the state, transposed (key channels x value columns), in registers, and
 // nothing passes between waves: each product leaves its result with the rows
 // that the next one contracts,
@@ -11,7 +11,7 @@
 // matrices that all waves share (k, q and v rows, T, P) come through LDS, the
 // next chunk's copied by loads straight to LDS while this one's are used, one
 // barrier a chunk.  O^T = S Q^T + N^T P^T takes the same registers as left
-// operands, so a lane ends with consecutive channels of a token's output.
+// operands, so a lane ends with eight consecutive channels of a token's output.
 //
 // The chain of a chunk bounds a scan whose workgroups do not fill the device:
 // long sequences of few heads are cut into segments.  A segment's map
@@ -25,49 +25,58 @@ namespace {
 
 constexpr int kMap = 0, kOutput = 1, kKeep = 2;
 
-// Waves of a workgroup over `cols` state columns.
-template <int NV>
-constexpr int waves_of(int cols) {
-  return (cols + 16 * NV - 1) / (16 * NV);
-}
+// Waves of a workgroup, and 16-column blocks of a wave.  The map's workgroups
+// hold both parts, waves of J, then waves of M, of 32 columns each.
+template <int DK, int DV, int MODE>
+struct ScanShape {
+  static constexpr int kNV = MODE == kMap ? 2 : 1;
+  static constexpr int kJ = DV / (16 * kNV), kWaves = MODE == kMap ? kJ + DK / 32 : kJ;
+  static constexpr int kCopiers = kWaves >= 8 ? 8 : kWaves >= 4 ? 4 : kWaves >= 2 ? 2 : 1;
+};
 
-template <bool F32, int DK, int NV, int MODE>
-__global__ __launch_bounds__(64 * waves_of<NV>(128)) void delta_scan_kernel(DeltaArgs a) {
+template <bool F32, int DK, int DV, int MODE>
+__global__ __launch_bounds__((64 * ScanShape<DK, DV, MODE>::kWaves))
+__attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
   typedef typename O::W W;
-  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, NC = DK / 16;
-  constexpr int kLuK = __builtin_ctz(DK * ES / 16);
-  constexpr int kBufs = F32 ? 1 : 2;
-  constexpr int kTileK = kChunk * DK * ES;
-  // Stage: k rows, T, gam and eta, v rows, then (outputs) q rows and P.
-  constexpr int kOffT = kTileK, kOffVec = kOffT + kWideTri, kOffV = kOffVec + 1024,
-                kOffQ = kOffV + kChunk * 128 * ES, kOffP = kOffQ + kTileK,
-                kStage = MODE == kOutput ? kOffP + ChunkRecord::kPBytes[F32] : kOffQ;
-  __shared__ __align__(16) char lds[kBufs * kStage];
+  typedef ScanShape<DK, DV, MODE> Shape;
+  constexpr int NV = Shape::kNV, kCopiers = Shape::kCopiers;
+  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kRow = row_tile_bytes<F32>();
+  constexpr int kBufs = F32 ? 1 : 2;  // (two stages of fp32 do not fit)
+  constexpr int kTileK = kChunk * DK * ES, kTileV = kChunk * DV * ES;
+  // Stage: k rows, the chunk's record (T; gam, eta and beta; outputs: P), v
+  // rows, then (outputs) q rows.
+  constexpr int kRecord = ChunkRecord::kP + (MODE == kOutput ? ChunkRecord::kPBytes[F32] : 0);
+  constexpr int kOffT = kTileK, kOffVec = kOffT + ChunkRecord::kVec, kOffP = kOffT + ChunkRecord::kP,
+                kOffV = kOffT + kRecord, kOffQ = kOffV + kTileV, kStage = kOffQ + (MODE == kOutput ? kTileK : 0);
+  // Two arrays, each named where it is used: with one indexed by the step the
+  // compiler takes any read for one of what is still being copied, and waits.
+  __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
 
-  const int DV = a.d_v;
-  unsigned id = blockIdx.x;
-  bool matrix = false;  // this workgroup scans M's rows, not J's
-  if constexpr (MODE == kMap) matrix = id & 1, id >>= 1;
-  const int h = uniform(id % (unsigned)a.Hv);
-  const int seg = uniform(id / (unsigned)a.Hv);
+  const int h = uniform(blockIdx.x % (unsigned)a.Hv);
+  const int seg = uniform(blockIdx.x / (unsigned)a.Hv);
   const SegmentInfo si = segment_info(a, seg);
-  if (si.chunks < 0) return;
-  // The last segment's map is not needed, nor the first one's matrix.
-  if (MODE == kMap && ((si.ends & 2) || (matrix && (si.ends & 1)))) return;
+  if (si.len < 0) return;
+  if (MODE == kMap && (si.ends & 2)) return;  // nothing follows the last segment's map
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
-  const int wave = uniform(tid >> 6), waves = uniform(blockDim.x >> 6);
-  const int cols = matrix ? DK : DV;
-  const int v0 = wave * 16 * NV;
-  const bool active = v0 < cols;
-  const int luv = __builtin_ctz(DV * ES / 16);
+  const int wave = uniform(tid >> 6);
+  // The wave's columns: 32 of the state (NV 2), or one of the halves n0 of 32
+  // (four of every eight).
+  const bool matrix = MODE == kMap && wave >= Shape::kJ;
+  const int vw = matrix ? wave - Shape::kJ : wave;
+  const int vb = NV == 2 ? vw : vw >> 1, n0 = NV == 2 ? 0 : vw & 1;
+  // Nothing precedes the first segment: its M is not needed.
+  const bool active = !(matrix && (si.ends & 1));
+  const int chunks = chunks_of(si.len);
   const size_t rec_size = ChunkRecord::bytes(F32, MODE == kKeep || (MODE == kMap && a.dout != nullptr));
+  const TileLane tl = tile_lane<F32>(li, lg);
+  const int col = 32 * vb + 8 * (li >> 2) + 4 * n0 + (li & 3);  // + 4 n: this lane's columns
 
-  // The entering state.
-  floatx4 S[NC][NV];
-  const size_t mat = (size_t)DV * DK;
+  // The entering state: S[s][o][n] holds channels 32 s + 8 lg + 4 o + r of column col + 4 n.
+  floatx4 S[KS][2][NV];
+  constexpr size_t mat = (size_t)DV * DK;
   const float* init = nullptr;
   if (!matrix) {
     if (si.ends & 1)
@@ -76,236 +85,294 @@ __global__ __launch_bounds__(64 * waves_of<NV>(128)) void delta_scan_kernel(Delt
       init = a.segJ + ((size_t)seg * a.Hv + h) * mat;
   }
 #pragma unroll
-  for (int c = 0; c < NC; ++c)
+  for (int s = 0; s < KS; ++s)
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      S[c][n] = floatx4{0.f, 0.f, 0.f, 0.f};
-      const int col = v0 + 16 * n + li;
-      if (matrix) {
+    for (int o = 0; o < 2; ++o)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[c][n][e] = 16 * c + 4 * lg + e == col ? 1.f : 0.f;
-      } else if (init != nullptr && active && v0 + 16 * n < cols) {
-        S[c][n] = *reinterpret_cast<const floatx4*>(init + (size_t)col * DK + 16 * c + 4 * lg);
+      for (int n = 0; n < NV; ++n) {
+        const int ch = 32 * s + 8 * lg + 4 * o;
+        S[s][o][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (matrix) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[s][o][n][e] = ch + e == col + 4 * n ? 1.f : 0.f;
+        } else if (init != nullptr) {
+          S[s][o][n] = *reinterpret_cast<const floatx4*>(init + (size_t)(col + 4 * n) * DK + ch);
+        }
       }
-    }
 
   const uint32_t k_row = (uint32_t)a.qk_tok * ES, v_row = (uint32_t)a.v_tok * ES;
-  auto stage = [&](int c) {
-    char* buf = lds + (kBufs == 2 && (c & 1) ? kStage : 0);
-    const int chunk = si.chunk + c;
-    const ChunkInfo ci = chunk_info(a, chunk);
-    const char* rec = a.rec + ((size_t)chunk * a.Hv + h) * rec_size;
-    const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head;
-    const uint32_t k_span = (uint32_t)(ci.len - 1) * k_row + DK * ES;
-    copy_rows<F32>(make_rsrc((const char*)a.k + qk * ES, k_span), buf, kLuK, kChunk, ci.len, k_row, wave,
-                   waves, lane);
-    copy_flat(rec + ChunkRecord::kT, buf + kOffT, kWideTri + 1024, wave, waves, lane);
-    if (!matrix) {
-      const size_t vo = (size_t)ci.tok * a.v_tok + (size_t)h * a.v_head;
-      copy_rows<F32>(make_rsrc((const char*)a.v + vo * ES, (uint32_t)(ci.len - 1) * v_row + DV * ES),
-                     buf + kOffV, luv, kChunk, ci.len, v_row, wave, waves, lane);
+  // The chunks' rows: each chunk's 64 rows further.
+  const char* kp = (const char*)a.k + ((size_t)si.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head) * ES;
+  const char* qp = (const char*)a.q + ((size_t)si.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head) * ES;
+  const char* vp = (const char*)a.v + ((size_t)si.tok * a.v_tok + (size_t)h * a.v_head) * ES;
+  const char* rp = a.rec + ((size_t)si.chunk * a.Hv + h) * rec_size;
+  auto stage = [&](int c, char* buf) __attribute__((always_inline)) {
+    const int len = min(kChunk, si.len - c * kChunk);
+    if (Shape::kWaves == kCopiers || wave < kCopiers) {
+      copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
+      copy_flat<kRecord, kCopiers>(rp, buf + kOffT, wave, lane);
+      copy_tiles<F32, kChunk, DV / 32, kCopiers>(make_rsrc(vp, 64u * v_row), buf + kOffV, len, v_row, wave, lane);
+      if constexpr (MODE == kOutput)
+        copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
     }
-    if constexpr (MODE == kOutput) {
-      copy_rows<F32>(make_rsrc((const char*)a.q + qk * ES, k_span), buf + kOffQ, kLuK, kChunk, ci.len,
-                     k_row, wave, waves, lane);
-      copy_flat(rec + ChunkRecord::kP, buf + kOffP, ChunkRecord::kPBytes[F32], wave, waves, lane);
-    }
+    kp += 64u * k_row, vp += 64u * v_row, rp += rec_size * a.Hv;
+    if constexpr (MODE == kOutput) qp += 64u * k_row;
   };
 
   const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-  if (si.chunks > 0) stage(0);
-  for (int c = 0; c < si.chunks; ++c) {
-    copy_barrier();
-    if (kBufs == 2 && c + 1 < si.chunks) stage(c + 1);
-    const char* buf = lds + (kBufs == 2 && (c & 1) ? kStage : 0);
-    if (active) {
-      const float* gam = reinterpret_cast<const float*>(buf + kOffVec);
-      const float *eta = gam + 64, *beta = gam + 128;
-      const int chunk = si.chunk + c;
+  auto step = [&](int c, const char* buf) __attribute__((always_inline)) {
+    if (!active) return;
+    const float* gam = reinterpret_cast<const float*>(buf + kOffVec) + 4 * lg;
+    const float *eta = gam + 64, *beta = gam + 128;
+    const int chunk = si.chunk + c;
 
-      W Sw[KS][NV];
+    // Operands are read from LDS a group of products ahead; the fences keep
+    // the compiler from moving a group's reads down to its first use, where
+    // each product would wait for them.
+    X kr[2][4], qr[2][4];
+    auto rows = [&](int s) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        kr[s & 1][t] = tile_row<F32>(buf + (4 * s + t) * kRow, tl);
+        if constexpr (MODE == kOutput) qr[s & 1][t] = tile_row<F32>(buf + kOffQ + (4 * s + t) * kRow, tl);
+      }
+    };
+    rows(0);
+    fence<F32>();
+
+    // Z = K S^T, and the state's part of O^T = S Q^T.  With 16 columns a wave
+    // there are registers for what X takes, read ahead as well.
+    floatx4 z[4][NV], o[4][NV], gv[4], bv[4], vv[4][NV];
+    W T[4];
+    auto values = [&](int half) {
+#pragma unroll
+      for (int t = 2 * half; t < 2 * half + 2; ++t) {
+        gv[t] = *reinterpret_cast<const floatx4*>(gam + 16 * t);
+        bv[t] = *reinterpret_cast<const floatx4*>(beta + 16 * t);
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          vv[t][n] = zero;
+          if (!matrix) vv[t][n] = tile_values<F32>(buf + kOffV + (4 * vb + t) * kRow, n0 + n, tl);
+        }
+      }
+    };
+    auto inverse = [&]() {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) T[t] = tile_w<F32>(buf + kOffT, tri_tile(t, 0), lane);
+    };
+    char* ks = a.keepS + ((size_t)chunk * a.Hv + h) * mat * 4;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      W Sw[NV];
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        Sw[n] = O::wide(S[s][0][n], S[s][1][n]);
+        if constexpr (MODE == kKeep)
+          store_wide8<F32>(ks, (size_t)(col + 4 * n) * DK + 32 * s + 8 * lg, mat, Sw[n]);
+      }
+      if (s + 1 < KS) rows(s + 1);
+      if (NV == 1 && s + 1 == KS) {
+        values(0);
+        values(1);
+        inverse();
+      }
+      fence<F32>();
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          z[t][n] = O::mma(kr[s & 1][t], Sw[n], s == 0 ? zero : z[t][n]);
+          if constexpr (MODE == kOutput) o[t][n] = O::mma(O::head(Sw[n]), qr[s & 1][t], s == 0 ? zero : o[t][n]);
+        }
+    }
+
+    // X = beta (V - gam Z).
+    W Xw[2][NV];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (NV == 2) values(half);
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        floatx4 x[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int t = 2 * half + u;
+          x[u] = bv[t] * (vv[t][n] - gv[t] * z[t][n]);
+        }
+        Xw[half][n] = O::wide(x[0], x[1]);
+      }
+    }
+
+    // N = T X.
+    floatx4 N[4][NV];
+    if (NV == 2) inverse();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int n = 0; n < NV; ++n) N[t][n] = O::mma(T[t], Xw[0][n], zero);
+#pragma unroll
+    for (int t = 2; t < 4; ++t) T[t] = tile_w<F32>(buf + kOffT, tri_tile(t, 1), lane);
+#pragma unroll
+    for (int t = 2; t < 4; ++t)
+#pragma unroll
+      for (int n = 0; n < NV; ++n) N[t][n] = O::mma(T[t], Xw[1][n], N[t][n]);
+
+    // Columns of K for the update, half u of the channels at a time.
+    X kt[KS][2];
+    auto columns = [&](int u) {
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int n = 0; n < NV; ++n) Sw[s][n] = O::wide(S[2 * s][n], S[2 * s + 1][n]);
+        for (int t = 0; t < 2; ++t)
+          kt[s][t] = tile_cols<F32>(buf + (4 * s + 2 * t) * kRow, buf + (4 * s + 2 * t + 1) * kRow, u, tl);
+    };
 
-      if constexpr (MODE == kKeep) {
-        char* ks = a.keepS + ((size_t)chunk * a.Hv + h) * mat * 4;
-#pragma unroll
-        for (int cc = 0; cc < NC; ++cc)
-#pragma unroll
-          for (int n = 0; n < NV; ++n)
-            if (v0 + 16 * n < cols)
-              store_wide4<F32>(ks, (size_t)(v0 + 16 * n + li) * DK + 16 * cc + 4 * lg, mat, S[cc][n]);
-      }
-
-      // Z = K S^T, X = beta (V - gam Z).
-      W Xw[2][NV];
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2) {
-        floatx4 z[2][NV];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int t = 2 * s2 + u;
-#pragma unroll
-          for (int n = 0; n < NV; ++n) z[u][n] = zero;
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            const X kop = row_op<F32>(buf, kLuK, 16 * t + li, s, lg);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) z[u][n] = O::mma(kop, Sw[s][n], z[u][n]);
-          }
-          const floatx4 gv = *reinterpret_cast<const floatx4*>(gam + 16 * t + 4 * lg);
-          const floatx4 bv = *reinterpret_cast<const floatx4*>(beta + 16 * t + 4 * lg);
-#pragma unroll
-          for (int n = 0; n < NV; ++n) {
-            floatx4 vv = zero;
-            if (!matrix && v0 + 16 * n < cols)
-              vv = result_rows<F32>(buf + kOffV, luv, 16 * t, v0 + 16 * n, li, lg);
-            z[u][n] = bv * (vv - gv * z[u][n]);
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < NV; ++n) Xw[s2][n] = O::wide(z[0][n], z[1][n]);
-      }
-
-      // N = T X.
-      floatx4 N[4][NV];
+    if constexpr (MODE == kKeep) {
+      char* kn = a.keepN + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int n = 0; n < NV; ++n) N[t][n] = zero;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int s = 0; s <= t / 2; ++s) {
-          const W T = tile_w<F32>(buf + kOffT, tri_tile(t, s), lane);
-#pragma unroll
-          for (int n = 0; n < NV; ++n) N[t][n] = O::mma(T, Xw[s][n], N[t][n]);
-        }
-
-      if constexpr (MODE == kKeep) {
-        char* kn = a.keepN + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int n = 0; n < NV; ++n)
-            if (v0 + 16 * n < cols)
-              store_wide4<F32>(kn, (size_t)(v0 + 16 * n + li) * kChunk + 16 * t + 4 * lg,
-                               (size_t)DV * kChunk, N[t][n]);
-      }
-
-      if constexpr (MODE == kOutput) {
-        X Nx[2][NV];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int n = 0; n < NV; ++n) Nx[s][n] = O::narrow(N[2 * s][n], N[2 * s + 1][n]);
-        const ChunkInfo ci = chunk_info(a, chunk);
-        const size_t vo = (size_t)ci.tok * a.v_tok + (size_t)h * a.v_head;
-        const __amdgpu_buffer_rsrc_t orsrc =
-            make_rsrc((char*)a.out + vo * ES, (uint32_t)(ci.len - 1) * v_row + DV * ES);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          floatx4 o[NV];
-#pragma unroll
-          for (int n = 0; n < NV; ++n) o[n] = zero;
-#pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            const X qop = row_op<F32>(buf + kOffQ, kLuK, 16 * t + li, s, lg);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) o[n] = O::mma(O::head(Sw[s][n]), qop, o[n]);
-          }
-          const float gq = a.scale * gam[16 * t + li];
-#pragma unroll
-          for (int n = 0; n < NV; ++n) o[n] *= gq;
-#pragma unroll
-          for (int s = 0; s <= t / 2; ++s) {
-            const X P = tile_x<F32>(buf + kOffP, tri_tile(t, s), lane);
-#pragma unroll
-            for (int n = 0; n < NV; ++n) o[n] = O::mma(Nx[s][n], P, o[n]);
-          }
-#pragma unroll
-          for (int n = 0; n < NV; ++n) {
-            if (v0 + 16 * n >= cols) continue;
-            const uint32_t off = (uint32_t)(16 * t + li) * v_row + (uint32_t)(v0 + 16 * n + 4 * lg) * ES;
-            if constexpr (F32)
-              store_b128(orsrc, off, __builtin_bit_cast(u32x4, o[n]));
-            else
-              store_b64(orsrc, off, make_uint2(pack_bf16x2(o[n][0], o[n][1]), pack_bf16x2(o[n][2], o[n][3])));
-          }
-        }
-      }
-
-      // S <- gam_63 S + N^T diag(eta) K.
-      W Nw[2][NV];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const floatx4 e0 = *reinterpret_cast<const floatx4*>(eta + 32 * s + 4 * lg);
-        const floatx4 e1 = *reinterpret_cast<const floatx4*>(eta + 32 * s + 16 + 4 * lg);
-#pragma unroll
-        for (int n = 0; n < NV; ++n) Nw[s][n] = O::wide(N[2 * s][n] * e0, N[2 * s + 1][n] * e1);
-      }
-      const float gl = gam[63];
-#pragma unroll
-      for (int cc = 0; cc < NC; ++cc) {
-#pragma unroll
-        for (int n = 0; n < NV; ++n) S[cc][n] *= gl;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const X kt = col_op<F32>(buf, kLuK, 32 * s, 16 * cc, li, lg);
-#pragma unroll
-          for (int n = 0; n < NV; ++n) S[cc][n] = O::mma(kt, Nw[s][n], S[cc][n]);
-        }
-      }
+        for (int n = 0; n < NV; ++n)
+          store_wide4<F32>(kn, (size_t)(col + 4 * n) * kChunk + 16 * t + 4 * lg, (size_t)DV * kChunk, N[t][n]);
     }
-    if (kBufs == 1 && c + 1 < si.chunks) {
-      lds_barrier();
-      stage(c + 1);
+
+    if constexpr (MODE == kOutput) {
+      X Nx[2][NV], P[kTriTiles];
+      float gq[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) gq[t] = reinterpret_cast<const float*>(buf + kOffVec)[16 * t + li];
+#pragma unroll
+      for (int i = 0; i < kTriTiles; ++i) P[i] = tile_x<F32>(buf + kOffP, i, lane);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int n = 0; n < NV; ++n) Nx[s][n] = O::narrow(N[2 * s][n], N[2 * s + 1][n]);
+      columns(0);
+      fence<F32>();
+      const int tok = si.tok + c * kChunk, len = min(kChunk, si.len - c * kChunk);
+      const size_t vo = (size_t)tok * a.v_tok + (size_t)h * a.v_head;
+      const __amdgpu_buffer_rsrc_t orsrc =
+          make_rsrc((char*)a.out + vo * ES, (uint32_t)(len - 1) * v_row + DV * ES);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          o[t][n] = O::mma(Nx[0][n], P[tri_tile(t, 0)], (a.scale * gq[t]) * o[t][n]);
+          if (t >= 2) o[t][n] = O::mma(Nx[1][n], P[tri_tile(t, 1)], o[t][n]);
+        }
+        // Rows behind the chunk's end are out of the buffer's range.
+        const uint32_t off = (uint32_t)(16 * t + li) * v_row + (uint32_t)(32 * vb + 8 * lg + 4 * n0) * ES;
+        if constexpr (F32) {
+#pragma unroll
+          for (int n = 0; n < NV; ++n) store_b128(orsrc, off + 16 * n, __builtin_bit_cast(u32x4, o[t][n]));
+        } else if constexpr (NV == 2) {
+          store_b128(orsrc, off, __builtin_bit_cast(u32x4, O::narrow(o[t][0], o[t][1])));
+        } else {
+          store_b64(orsrc, off,
+                    make_uint2(pack_bf16x2(o[t][0][0], o[t][0][1]), pack_bf16x2(o[t][0][2], o[t][0][3])));
+        }
+      }
+    } else {
+      columns(0);
+      fence<F32>();
+    }
+
+    // S <- gam_63 S + N^T diag(eta) K.
+    W Nw[2][NV];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        Nw[s][n] = O::wide(N[2 * s][n] * *reinterpret_cast<const floatx4*>(eta + 32 * s),
+                           N[2 * s + 1][n] * *reinterpret_cast<const floatx4*>(eta + 32 * s + 16));
+    const float gl = reinterpret_cast<const float*>(buf + kOffVec)[63];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (u == 1) columns(1);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int n = 0; n < NV; ++n) S[s][u][n] *= gl;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int n = 0; n < NV; ++n) S[s][u][n] = O::mma(kt[s][t], Nw[t][n], S[s][u][n]);
+    }
+  };
+
+  if constexpr (kBufs == 2) {
+    if (chunks > 0) stage(0, buf0);
+    // Stores of a step, all of them of every wave.
+    constexpr int kStores = MODE == kOutput ? 4 : MODE == kKeep ? 2 * KS + 8 : 0;
+    for (int c = 0; c < chunks; c += 2) {
+      if (c == 0)
+        copy_barrier();
+      else
+        copy_barrier<kStores>();
+      if (c + 1 < chunks) stage(c + 1, buf1);
+      step(c, buf0);
+      if (c + 1 >= chunks) break;
+      copy_barrier<kStores>();
+      if (c + 2 < chunks) stage(c + 2, buf0);
+      step(c + 1, buf1);
+    }
+  } else {
+    for (int c = 0; c < chunks; ++c) {
+      if (c > 0) lds_barrier();  // every wave is done with the chunk before
+      stage(c, buf0);
+      copy_barrier();
+      step(c, buf0);
     }
   }
 
   if (!active) return;
+  const size_t km = (size_t)DK * DK;
 #pragma unroll
-  for (int n = 0; n < NV; ++n) {
-    if (v0 + 16 * n >= cols) continue;
-    const int col = v0 + 16 * n + li;
+  for (int s = 0; s < KS; ++s)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const size_t at = (size_t)col * DK + 16 * c + 4 * lg;
-      if constexpr (MODE == kMap) {
-        if (matrix) {
-          const size_t base = ((size_t)seg * a.Hv + h) * DK * DK;
-          *reinterpret_cast<floatx4*>(a.segM + base + at) = S[c][n];
+    for (int n = 0; n < NV; ++n) {
+      const int u = col + 4 * n, ch = 32 * s + 8 * lg;
+      if (MODE == kMap && matrix) {
+        // M by rows and by columns, each a wide operand of the join.
+        char* m = a.segM + ((size_t)seg * a.Hv + h) * 2 * km * 4;
+        const W w = O::wide(S[s][0][n], S[s][1][n]);
+        store_wide8<F32>(m, (size_t)u * DK + ch, km, w);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) a.segMt[base + (size_t)(16 * c + 4 * lg + e) * DK + col] = S[c][n][e];
-        } else {
-          *reinterpret_cast<floatx4*>(a.segJ + ((size_t)seg * a.Hv + h) * mat + at) = S[c][n];
+        for (int e = 0; e < 8; ++e) store_wide1<F32>(m + km * 4, (size_t)(ch + e) * DK + u, km, w, e);
+      } else {
+        float* to = nullptr;
+        if (MODE == kMap)
+          to = a.segJ + ((size_t)seg * a.Hv + h) * mat;
+        else if ((si.ends & 2) && a.S_out != nullptr)
+          to = a.S_out + ((size_t)si.seq * a.Hv + h) * mat;
+        if (to != nullptr) {
+          *reinterpret_cast<floatx4*>(to + (size_t)u * DK + ch) = S[s][0][n];
+          *reinterpret_cast<floatx4*>(to + (size_t)u * DK + ch + 4) = S[s][1][n];
         }
-      } else if ((si.ends & 2) && a.S_out != nullptr) {
-        *reinterpret_cast<floatx4*>(a.S_out + ((size_t)si.seq * a.Hv + h) * mat + at) = S[c][n];
       }
     }
-  }
 }
 
 // The join: x <- x M_s + J_s over the segments of a sequence in order (or, in
 // reverse, x <- x M_s^T + J_s from the last), the state entering each segment
-// written over its J.  The recurrence of a state's rows is independent of the
-// others': one workgroup of four waves per sequence, head and 16 rows; a wave makes
-// d_k / 4 columns of the product (transposed, the matrix as left operand),
-// which it passes to the others as operands through LDS.  fp32 matrix cores:
-// a step's 16 x d_k x d_k product is small beside the chunks it stands for.
-template <int DK>
+// written over its J.  The rows of a state are independent of each other: one
+// workgroup of four waves per sequence, head and 16 rows; a wave makes d_k / 4
+// columns of the product (transposed, the matrix as left operand), which the
+// others get through LDS (two waves at d_k 32).  The matrices are read two
+// segments ahead.
+template <bool F32, int DK>
 __global__ __launch_bounds__(kThreads) void delta_join_kernel(DeltaArgs a, bool reverse) {
-  typedef Op<true> O;
+  typedef Op<F32> O;
+  typedef typename O::W W;
   constexpr int KS = DK / 32, NC = DK / 16, WT = (NC + 3) / 4;
   constexpr int kRow = DK + 4;
   __shared__ __align__(16) float x[2][16 * kRow];
   const int blocks = a.d_v / 16;
   const int rb = blockIdx.x % blocks;
-  const int h = (blockIdx.x / blocks) % a.Hv;
-  const int seq = blockIdx.x / (blocks * a.Hv);
+  const int h = uniform((blockIdx.x / blocks) % a.Hv);
+  const int seq = uniform(blockIdx.x / (blocks * a.Hv));
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave = uniform(tid >> 6);
   // The sequence's segments.
@@ -320,62 +387,89 @@ __global__ __launch_bounds__(kThreads) void delta_join_kernel(DeltaArgs a, bool 
   }
   if (count < 2) return;
   float* J = reverse ? a.segdJ : a.segJ;
-  const float* M = reverse ? a.segM : a.segMt;
-  const size_t mat = (size_t)a.d_v * DK;
+  const size_t mat = (size_t)a.d_v * DK, km = (size_t)DK * DK;
   const int row = rb * 16 + li;
   auto index = [&](int i) { return (size_t)(reverse ? first + count - 1 - i : first + i) * a.Hv + h; };
-
-  // After segment 0 the state is its own J (scanned from the sequence's state).
-  floatx4 y[WT];
-#pragma unroll
-  for (int w = 0; w < WT; ++w) {
-    const int c = wave * WT + w;
-    if (c < NC) y[w] = *reinterpret_cast<const floatx4*>(J + index(0) * mat + (size_t)row * DK + 16 * c + 4 * lg);
-  }
-  for (int i = 1; i < count; ++i) {
-    floatx4 add[WT];
-    const bool more = i + 1 < count;
-    float* Ji = J + index(i) * mat + (size_t)row * DK;
-    float* buf = x[i & 1];
+  // Result columns 16 c + 4 lg .. of this wave, c = wave WT + w; the matrix's
+  // operand rows 16 c + li.  Past the last segment its own place is read again
+  // (in bounds, and not used).
+  W m[2][WT][KS];
+  floatx4 y[WT], add[2][WT];
+  auto load = [&](int i, int slot) __attribute__((always_inline)) {
+    const size_t at = index(i < count ? i : count - 1);
+    const char* mi = a.segM + at * 2 * km * 4 + (reverse ? 0 : km * 4);
+    const float* Ji = J + at * mat + (size_t)row * DK;
 #pragma unroll
     for (int w = 0; w < WT; ++w) {
       const int c = wave * WT + w;
-      if (c >= NC) continue;
-      if (more) add[w] = *reinterpret_cast<const floatx4*>(Ji + 16 * c + 4 * lg);
+      add[slot][w] = *reinterpret_cast<const floatx4*>(Ji + 16 * c + 4 * lg);
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        m[slot][w][s] = load_wide8<F32>(mi, (size_t)(16 * c + li) * DK + 32 * s + 8 * lg, km);
+    }
+  };
+  // After segment 0 the state is its own J (scanned from the sequence's state).
+#pragma unroll
+  for (int w = 0; w < WT; ++w)
+    y[w] = *reinterpret_cast<const floatx4*>(J + index(0) * mat + (size_t)row * DK + 16 * (wave * WT + w) + 4 * lg);
+  // Segment i; false after the last.
+  auto join = [&](int i, int slot) __attribute__((always_inline)) {
+    float* buf = x[slot];
+    float* Ji = J + index(i) * mat + (size_t)row * DK;
+#pragma unroll
+    for (int w = 0; w < WT; ++w) {
+      const int c = wave * WT + w;
       *reinterpret_cast<floatx4*>(Ji + 16 * c + 4 * lg) = y[w];
       *reinterpret_cast<floatx4*>(buf + li * kRow + 16 * c + 4 * lg) = y[w];
     }
-    if (!more) return;
+    if (i + 1 == count) return false;
     lds_barrier();
-    const float* Mi = M + index(i) * DK * DK;
 #pragma unroll
-    for (int w = 0; w < WT; ++w) {
-      const int c = wave * WT + w;
-      if (c >= NC) continue;
-      y[w] = add[w];
+    for (int w = 0; w < WT; ++w) y[w] = add[slot][w];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const float* xr = buf + li * kRow + 32 * s + 4 * lg;
-        const float* mr = Mi + (size_t)(16 * c + li) * DK + 32 * s + 4 * lg;
-        const O::X xo = O::narrow(*reinterpret_cast<const floatx4*>(xr), *reinterpret_cast<const floatx4*>(xr + 16));
-        const O::X mo = O::narrow(*reinterpret_cast<const floatx4*>(mr), *reinterpret_cast<const floatx4*>(mr + 16));
-        y[w] = O::mma(mo, xo, y[w]);
-      }
+    for (int s = 0; s < KS; ++s) {
+      const float* xr = buf + li * kRow + 32 * s + 8 * lg;
+      const W xo = O::wide(*reinterpret_cast<const floatx4*>(xr), *reinterpret_cast<const floatx4*>(xr + 4));
+#pragma unroll
+      for (int w = 0; w < WT; ++w) y[w] = O::mma(m[slot][w][s], xo, y[w]);
     }
+    load(i + 2, slot);
+    return true;
+  };
+  load(1, 1);
+  load(2, 0);
+  for (int i = 1;; i += 2)
+    if (!join(i, 1) || !join(i + 1, 0)) return;
+}
+
+template <bool F32, int DK, int DV>
+hipError_t run(int what, const DeltaArgs& a, hipStream_t stream) {
+  const unsigned items = (unsigned)a.max_segs * (unsigned)a.Hv;
+  if (what == kMap)
+    delta_scan_kernel<F32, DK, DV, kMap><<<items, 64 * ScanShape<DK, DV, kMap>::kWaves, 0, stream>>>(a);
+  else if (what == kOutput)
+    delta_scan_kernel<F32, DK, DV, kOutput><<<items, 64 * ScanShape<DK, DV, kOutput>::kWaves, 0, stream>>>(a);
+  else
+    delta_scan_kernel<F32, DK, DV, kKeep><<<items, 64 * ScanShape<DK, DV, kKeep>::kWaves, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <bool F32, int DK>
+hipError_t run(int what, const DeltaArgs& a, hipStream_t stream) {
+  switch (a.d_v) {
+    case 32: return run<F32, DK, 32>(what, a, stream);
+    case 64: return run<F32, DK, 64>(what, a, stream);
+    default: return run<F32, DK, 128>(what, a, stream);
   }
 }
 
-template <bool F32, int DK, int NV>
-hipError_t run(int what, const DeltaArgs& a, hipStream_t stream) {
-  const unsigned items = (unsigned)a.max_segs * (unsigned)a.Hv;
-  const int waves = waves_of<NV>(a.d_v);
-  if (what == kMap) {
-    const int w = waves_of<NV>(a.d_v > DK ? a.d_v : DK);
-    delta_scan_kernel<F32, DK, NV, kMap><<<items * 2, 64 * w, 0, stream>>>(a);
-  } else if (what == kOutput) {
-    delta_scan_kernel<F32, DK, NV, kOutput><<<items, 64 * waves, 0, stream>>>(a);
-  } else {
-    delta_scan_kernel<F32, DK, NV, kKeep><<<items, 64 * waves, 0, stream>>>(a);
+template <bool F32>
+hipError_t join(int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream) {
+  const unsigned grid = (unsigned)a.n_seqs * (unsigned)a.Hv * (unsigned)(a.d_v / 16);
+  switch (d_k) {
+    case 32: delta_join_kernel<F32, 32><<<grid, 128, 0, stream>>>(a, reverse); break;
+    case 64: delta_join_kernel<F32, 64><<<grid, kThreads, 0, stream>>>(a, reverse); break;
+    default: delta_join_kernel<F32, 128><<<grid, kThreads, 0, stream>>>(a, reverse); break;
   }
   return hipGetLastError();
 }
@@ -384,20 +478,14 @@ hipError_t run(int what, const DeltaArgs& a, hipStream_t stream) {
 
 hipError_t launch_delta_scan(bool f32, int d_k, int what, const DeltaArgs& a, hipStream_t stream) {
   switch (d_k) {
-    case 32: return f32 ? run<true, 32, 1>(what, a, stream) : run<false, 32, 1>(what, a, stream);
-    case 64: return f32 ? run<true, 64, 1>(what, a, stream) : run<false, 64, 1>(what, a, stream);
-    default: return f32 ? run<true, 128, 1>(what, a, stream) : run<false, 128, 1>(what, a, stream);
+    case 32: return f32 ? run<true, 32>(what, a, stream) : run<false, 32>(what, a, stream);
+    case 64: return f32 ? run<true, 64>(what, a, stream) : run<false, 64>(what, a, stream);
+    default: return f32 ? run<true, 128>(what, a, stream) : run<false, 128>(what, a, stream);
   }
 }
 
-hipError_t launch_delta_join(int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)a.n_seqs * (unsigned)a.Hv * (unsigned)(a.d_v / 16);
-  switch (d_k) {
-    case 32: delta_join_kernel<32><<<grid, kThreads, 0, stream>>>(a, reverse); break;
-    case 64: delta_join_kernel<64><<<grid, kThreads, 0, stream>>>(a, reverse); break;
-    default: delta_join_kernel<128><<<grid, kThreads, 0, stream>>>(a, reverse); break;
-  }
-  return hipGetLastError();
+hipError_t launch_delta_join(bool f32, int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream) {
+  return f32 ? join<true>(d_k, reverse, a, stream) : join<false>(d_k, reverse, a, stream);
 }
 
 }  // namespace vda

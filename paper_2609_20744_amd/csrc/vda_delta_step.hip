@@ -16,19 +16,6 @@
 namespace vda {
 namespace {
 
-#define VDA_STEP_DPP_ADD(x, ctrl) \
-  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xf, 0xf, false))
-
-// Sum over aligned groups of LANES lanes (4, 8 or 16), in every lane.
-template <int LANES>
-__device__ __forceinline__ float group_sum(float x) {
-  VDA_STEP_DPP_ADD(x, 0xB1);                         // quad_perm 1,0,3,2
-  VDA_STEP_DPP_ADD(x, 0x4E);                         // quad_perm 2,3,0,1
-  if constexpr (LANES >= 8) VDA_STEP_DPP_ADD(x, 0x141);   // row_half_mirror
-  if constexpr (LANES >= 16) VDA_STEP_DPP_ADD(x, 0x140);  // row_mirror
-  return x;
-}
-
 __device__ __forceinline__ floatx4 load4(const float* p) { return *reinterpret_cast<const floatx4*>(p); }
 __device__ __forceinline__ floatx4 load4(const uint16_t* p) {
   const uint2 w = *reinterpret_cast<const uint2*>(p);
