@@ -1,8 +1,6 @@
 // C ABI of the token-wise gated delta rule and of the rotary positions:
 // argument validation, workspace layout, launch order.  Declarations and
 // contracts are in include/vda.h.
-#include <stdlib.h>
-
 #include <algorithm>
 #include <initializer_list>
 
@@ -60,11 +58,19 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   const long long per = (T / n + vda::kChunk - 1) / vda::kChunk;  // chunks of a sequence (equal lengths)
   const long long longest = table ? (T + vda::kChunk - 1) / vda::kChunk : per;
   d.max_chunks = (int)(table ? (T + (vda::kChunk - 1) * n) / vda::kChunk : per * n);
-  // Segments.
+  // Segments.  A sequence that is cut costs each of its chunks a second scan
+  // (the segment's map) and a step of the join per segment.  Where sequences
+  // and heads alone fill the compute units, only one that is far longer than
+  // the rest is cut: 24 uneven sequences of 16411 tokens with 16 heads take
+  // 233 us whole and 296 us cut into segments of 18 chunks.  Where they do not,
+  // every unit gets a segment: 9 such sequences take 1.08 ms forward and
+  // backward cut and 1.43 ms whole, one of 1560 tokens with 24 heads 88 and
+  // 116 us.  A segment has at least four chunks and a sequence more than four
+  // segments, or the join outweighs what running side by side saves.
   const long long cus = vda::current_device_cus();
-  const long long tgt = getenv("TGT") ? atoi(getenv("TGT")) : cus;
-  const long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + tgt - 1) / tgt);
-  d.split = longest > (getenv("FAC") ? atoi(getenv("FAC")) : 4) * share;
+  long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
+  if (n * p->H_v >= cus) share = std::max(share, 4 * ((d.max_chunks + n - 1) / n));
+  d.split = longest > 4 * share;
   d.seg_chunks = (int)(d.split ? share : std::max(longest, 1LL));
   d.max_segs = (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));
   // Workspace.

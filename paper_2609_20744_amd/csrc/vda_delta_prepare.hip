@@ -44,21 +44,25 @@ __device__ __forceinline__ floatx4 mat_col(const float* m, int r0, int c0, int l
 __device__ __forceinline__ void invert_unit_lower(float* m, int wave, int li, int lg) {
   {
     const int r0 = 16 * wave;
-    float row[16][16];
-#pragma unroll
-    for (int i = 1; i < 16; ++i)
-#pragma unroll
-      for (int c = 0; c < (i + 3) / 4; ++c) {
-        const floatx4 t = *reinterpret_cast<const floatx4*>(m + (r0 + i) * kLd + r0 + 4 * c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) row[i][4 * c + e] = t[e];
-      }
     float x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      x[i] = li == i ? 1.f : 0.f;
+    for (int b = 0; b < 4; ++b) {
+      floatx4 row[4][4];
 #pragma unroll
-      for (int l = 0; l < i; ++l) x[i] -= row[i][l] * x[l];
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c <= b; ++c)
+          row[i][c] = *reinterpret_cast<const floatx4*>(m + (r0 + 4 * b + i) * kLd + r0 + 4 * c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v = li == 4 * b + i ? 1.f : 0.f;
+#pragma unroll
+        for (int l = 0; l < 4 * b + i; ++l) v -= row[i][l >> 2][l & 3] * x[l];
+        x[4 * b + i] = v;
+      }
+      // Four rows at a time (the next rows are read after these are used): all
+      // at once would take 120 registers.
+      asm volatile("" : "+v"(x[4 * b + 3]) : : "memory");
     }
     // Every lane of the wave has read the block before it is overwritten: the
     // values above are used.
@@ -92,6 +96,24 @@ __device__ __forceinline__ void invert_unit_lower(float* m, int wave, int li, in
   lds_barrier();
 }
 
+// x where `keep`, else 0.  The mask is opaque to the compiler, which otherwise
+// jumps around the score's exponential: a score is cheaper than a jump.
+__device__ __forceinline__ float keep_if(bool keep, float x) {
+  uint32_t mask = keep ? 0xffffffffu : 0u;
+  asm("" : "+v"(mask));
+  return __uint_as_float(__float_as_uint(x) & mask);
+}
+
+// The prefixes of four tokens in a row.
+struct Prefix4 {
+  double x[4];
+};
+__device__ __forceinline__ Prefix4 prefix4(const double* pre) {
+  typedef double double2v __attribute__((ext_vector_type(2)));
+  const double2v a = *reinterpret_cast<const double2v*>(pre), b = *reinterpret_cast<const double2v*>(pre + 2);
+  return {{a[0], a[1], b[0], b[1]}};
+}
+
 // A token row as an operand, channels in memory order (the same in both
 // operands of a score): 8 consecutive channels a lane.
 template <bool F32>
@@ -108,13 +130,14 @@ __device__ __forceinline__ typename Op<F32>::X token_op(__amdgpu_buffer_rsrc_t r
 }
 
 template <bool F32, int DK, bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(F32 ? 1 : BACKWARD ? 3 : 4)))
+void delta_prepare_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
   constexpr int KS = DK / 32, ES = F32 ? 4 : 2;
   __shared__ __align__(16) float m[kChunk * kLd];
-  __shared__ double pre[kChunk];
-  __shared__ float strengths[kChunk];
+  __shared__ __align__(16) double pre[kChunk];
+  __shared__ __align__(16) float strengths[kChunk];
   const int h = blockIdx.x % (unsigned)a.Hv;
   const int chunk = blockIdx.x / (unsigned)a.Hv;
   const ChunkInfo ci = chunk_info(a, chunk);
@@ -123,6 +146,12 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
   const int wave = uniform(tid >> 6);
   char* rec = a.rec + ((size_t)chunk * a.Hv + h) * ChunkRecord::bytes(F32, BACKWARD);
 
+  // The gates first: the decays are summed while the rows are on their way.
+  float decay = 0.f, beta = 0.f;
+  if (wave == 0 && lane < ci.len) {
+    const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
+    decay = a.g[at], beta = strength(a.beta[at]);
+  }
   // Token rows: past the chunk's end they are out of the buffers' range and
   // read as zero.
   const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head;
@@ -144,11 +173,9 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
       qt[t][s] = token_op<F32>(qr, (uint32_t)(16 * (BACKWARD ? t : wave) + li) * row_bytes, s, lg);
   }
   if (wave == 0) {
-    const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
-    const bool real = lane < ci.len;
-    const double G = decay_prefix(real ? a.g[at] : 0.f, lane);
+    const double G = decay_prefix(decay, lane);
     pre[lane] = G;
-    strengths[lane] = real ? strength(a.beta[at]) : 0.f;
+    strengths[lane] = beta;
     const double last = __shfl(G, 63);
     float* vec = reinterpret_cast<float*>(rec + ChunkRecord::kVec);
     vec[lane] = pow2(G);
@@ -159,10 +186,8 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
   lds_barrier();
 
   const int r0 = 16 * wave;
-  double gi[4];
-  float bi[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) gi[e] = pre[r0 + 4 * lg + e], bi[e] = strengths[r0 + 4 * lg + e];
+  const Prefix4 gi = prefix4(pre + r0 + 4 * lg);
+  const floatx4 bi = *reinterpret_cast<const floatx4*>(strengths + r0 + 4 * lg);
 
   // M = diag(beta) L, rows of this wave.
 #pragma unroll
@@ -176,7 +201,7 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = r0 + 4 * lg + e;
-      m[i * kLd + j] = i > j ? bi[e] * pow2(gi[e] - gj) * acc[e] : 0.f;
+      m[i * kLd + j] = keep_if(i > j, bi[e] * pow2(gi.x[e] - gj) * acc[e]);
     }
   }
 
@@ -194,10 +219,11 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
         p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < KS; ++c) p[u] = O::mma(kt[t][c], qt[0][c], p[u]);
+        const Prefix4 gj = prefix4(pre + 16 * t + 4 * lg);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int j = 16 * t + 4 * lg + e;
-          p[u][e] = i >= j ? a.scale * pow2(gq - pre[j]) * p[u][e] : 0.f;
+          p[u][e] = keep_if(i >= j, a.scale * pow2(gq - gj.x[e]) * p[u][e]);
         }
       }
       store_tile_x<F32>(rec + ChunkRecord::kP, tri_tile(wave, s), lane, O::narrow(p[0], p[1]));
@@ -216,10 +242,11 @@ __global__ __launch_bounds__(kThreads) void delta_prepare_kernel(DeltaArgs a) {
         p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < KS; ++c) p[u] = O::mma(qt[t][c], kw[c], p[u]);
+        const Prefix4 gi = prefix4(pre + 16 * t + 4 * lg);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * t + 4 * lg + e;
-          p[u][e] = i >= j ? a.scale * pow2(pre[i] - gj) * p[u][e] : 0.f;
+          p[u][e] = keep_if(i >= j, a.scale * pow2(gi.x[e] - gj) * p[u][e]);
         }
       }
       store_tile_w<F32>(rec + ChunkRecord::kPt, tri_tile_t(wave, s), lane, O::wide(p[0], p[1]));
