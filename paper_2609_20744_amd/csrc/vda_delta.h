@@ -120,115 +120,17 @@ struct Op<true> {
   static __device__ __forceinline__ float value(const W& w, int e) { return w.v[e]; }
 };
 
-// ---------------------------------------------------------------------------
-// Tiles in LDS: rows of 2^lu 16-byte units, unit u of row r at position
-// u ^ swizzle(r), so that both ways of reading an operand (16 rows at one
-// column, and columns of a few rows) spread over the banks with no padding:
-// tiles are filled by loads that go straight to LDS, 64 consecutive units an
-// instruction.
-// ---------------------------------------------------------------------------
-template <bool F32>
-__device__ __forceinline__ int swizzle(int r, int lu) {
-  if (F32) return lu >= 4 ? (r & 15) : (r & 7);
-  if (lu >= 4) return ((r & 7) << 1) | ((r >> 3) & 1);
-  if (lu == 3) return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
-  return (((r >> 2) & 1) << 1) | ((r >> 3) & 1);
-}
-
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
-
-// Row `r` of a tile as an operand, contraction step s along the row.
-template <bool F32>
-__device__ __forceinline__ typename Op<F32>::X row_op(const char* tile, int lu, int r, int s, int lg) {
-  const int sw = swizzle<F32>(r, lu);
-  const char* row = tile + ((size_t)r << (lu + 4));
-  if constexpr (F32) {
-    const floatx4 a = *reinterpret_cast<const floatx4*>(row + (((8 * s + lg) ^ sw) << 4));
-    const floatx4 b = *reinterpret_cast<const floatx4*>(row + (((8 * s + 4 + lg) ^ sw) << 4));
-    return Op<true>::narrow(a, b);
-  } else {
-    const int u = 4 * s + (lg >> 1), h = (lg & 1) * 8;
-    const uint2 a = *reinterpret_cast<const uint2*>(row + ((u ^ sw) << 4) + h);
-    const uint2 b = *reinterpret_cast<const uint2*>(row + (((u + 2) ^ sw) << 4) + h);
-    return __builtin_bit_cast(bf16x8, u32x4{a.x, a.y, b.x, b.y});
-  }
-}
-
-// Four rows r0 + 4 lg .. + 3 of column c0 + li.  bf16: ds_read_b64_tr_b16,
-// in which lane i of 16 receives element i % 4 of the 8-byte pieces that
-// lanes i / 4 + 4 e address.
-__device__ __forceinline__ shortx4 tr_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
-  const int r = r0 + 4 * lg + (li >> 2);
-  const int u = (c0 >> 3) + ((li & 3) >> 1);
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_shortx4*)(tile + ((size_t)r << (lu + 4)) + ((u ^ swizzle<false>(r, lu)) << 4) + (li & 1) * 8));
-}
-
-__device__ __forceinline__ floatx4 f32_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
-  floatx4 v;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int r = r0 + 4 * lg + e;
-    v[e] = *reinterpret_cast<const float*>(tile + ((size_t)r << (lu + 4)) +
-                                           ((((c0 + li) >> 2) ^ swizzle<true>(r, lu)) << 4) +
-                                           (li & 3) * 4);
-  }
-  return v;
-}
-
-// Column c0 + li of a tile as an operand, contraction over rows r0 .. r0 + 31.
-template <bool F32>
-__device__ __forceinline__ typename Op<F32>::X col_op(const char* tile, int lu, int r0, int c0, int li,
-                                                      int lg) {
-  if constexpr (F32) {
-    return Op<true>::narrow(f32_rows(tile, lu, r0, c0, li, lg), f32_rows(tile, lu, r0 + 16, c0, li, lg));
-  } else {
-    const shortx4 a = tr_rows(tile, lu, r0, c0, li, lg), b = tr_rows(tile, lu, r0 + 16, c0, li, lg);
-    typedef short shortx8 __attribute__((ext_vector_type(8)));
-    return __builtin_bit_cast(bf16x8, shortx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
-  }
-}
-
-// Rows r0 + 4 lg .. + 3 of column c0 + li as fp32 (where a result has them).
-template <bool F32>
-__device__ __forceinline__ floatx4 result_rows(const char* tile, int lu, int r0, int c0, int li, int lg) {
-  if constexpr (F32) {
-    return f32_rows(tile, lu, r0, c0, li, lg);
-  } else {
-    const shortx4 a = tr_rows(tile, lu, r0, c0, li, lg);
-    floatx4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16);
-    return v;
-  }
-}
-
-// Copies `units` (a multiple of 64) 16-byte units of a tile, `rows` rows of
-// 2^lu units taken at row_bytes apart, into LDS with the swizzle; the waves
-// share the instructions.  A row at or past `len` repeats row len - 1, so
-// that every address is the sequence's own (what such rows meet is zero:
-// their writes, their strengths, their stores).
-template <bool F32>
-__device__ __forceinline__ void copy_rows(__amdgpu_buffer_rsrc_t src, char* tile, int lu, int rows,
-                                          int len, uint32_t row_bytes, int wave, int waves, int lane) {
-  const int pieces = (rows << lu) >> 6;
-  for (int p = wave; p < pieces; p += waves) {
-    const int u = p * 64 + lane;
-    const int r = u >> lu;
-    const int from = (u & ((1 << lu) - 1)) ^ swizzle<F32>(r, lu);
-    const uint32_t off = (uint32_t)(r < len ? r : len - 1) * row_bytes + (uint32_t)from * 16u;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16, off, 0, 0, 0);
-  }
-}
 
 // ---------------------------------------------------------------------------
 // Row tiles in LDS: 16 tokens x 32 channels, each lane's 16 bytes (eight
 // consecutive channels 8 lg .. of token li; fp32: four, in two halves of 1 KB)
 // in one place, so that an operand of the rows is one read at a lane's own
 // offset plus a constant: no address is computed in a loop.  Columns are
-// read across lanes' places (ds_read_b64_tr_b16, or four words in fp32), for
-// which the places of a unit column lg are permuted, which spreads them over the
+// read across lanes' places (ds_read_b64_tr_b16, in which lane i of 16 receives
+// element i % 4 of the 8-byte pieces that lanes i / 4 + 4 e address; or four
+// words in fp32), for which the places of a unit column lg are permuted, which spreads them over the
 // banks (bf16: two accesses a bank, the least when half of each 16 bytes is read).
 //
 // Channels are paired with results by this order: operand element e of lane
@@ -411,15 +313,6 @@ __device__ __forceinline__ void fence() {
   if constexpr (!F32) __builtin_amdgcn_sched_barrier(0);
 }
 
-// Copies `bytes` (a multiple of 1024) of contiguous memory into LDS as it is.
-__device__ __forceinline__ void copy_flat(const void* from, char* tile, int bytes, int wave, int waves,
-                                          int lane) {
-  const __amdgpu_buffer_rsrc_t src = make_rsrc(from, (uint32_t)bytes);
-  for (int p = wave; p < bytes >> 10; p += waves)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
-                                             (uint32_t)p * 1024u + (uint32_t)lane * 16u, 0, 0, 0);
-}
-
 // Barrier behind which copies into LDS issued before it, by any wave, are
 // visible: each wave first waits for its own loads and LDS operations.
 // LATER: so many of the wave's memory operations at least were issued after
@@ -512,7 +405,7 @@ __device__ __forceinline__ void store_wide4(char* base, size_t elem, size_t plan
   }
 }
 
-// Eight values along a row, already wide; and one of them.
+// Eight values along a row, already wide.
 template <bool F32>
 __device__ __forceinline__ void store_wide8(char* base, size_t elem, size_t plane_elems,
                                             const typename Op<F32>::W& w) {
@@ -522,16 +415,6 @@ __device__ __forceinline__ void store_wide8(char* base, size_t elem, size_t plan
   } else {
     *reinterpret_cast<bf16x8*>(base + elem * 2) = w.hi;
     *reinterpret_cast<bf16x8*>(base + (plane_elems + elem) * 2) = w.lo;
-  }
-}
-template <bool F32>
-__device__ __forceinline__ void store_wide1(char* base, size_t elem, size_t plane_elems,
-                                            const typename Op<F32>::W& w, int e) {
-  if constexpr (F32) {
-    *reinterpret_cast<float*>(base + elem * 4) = w.v[e];
-  } else {
-    *reinterpret_cast<__bf16*>(base + elem * 2) = w.hi[e];
-    *reinterpret_cast<__bf16*>(base + (plane_elems + elem) * 2) = w.lo[e];
   }
 }
 template <bool F32>

@@ -287,8 +287,9 @@ void delta_prepare_kernel(DeltaArgs a) {
 // Tables of the chunks and segments of sequences [cu[i], cu[i + 1]): tabs
 // holds counts[2] (and padding to 4), prefix sums of chunks and segments
 // [n + 1] each, then the int4 tables.  Offsets are clamped to [0, T] and the
-// tables to their sizes, so that no malformed list can address anything else.
-constexpr int kPlanThreads = 1024;
+// tables to their sizes, and sums stop at kMost, above any table's size, so that
+// no malformed list can address anything else.
+constexpr int kPlanThreads = 1024, kMost = 0x3fffffff;
 
 __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu, int n, int T, int seg_chunks,
                                                                  int max_chunks, int max_segs, int* tabs) {
@@ -300,6 +301,7 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
   int4* seg_tab = chunk_tab + max_chunks;
   const int tid = threadIdx.x;
   auto clamp = [&](int x) { return x < 0 ? 0 : x > T ? T : x; };
+  auto add = [](int x, int y) { return x + y < kMost ? x + y : kMost; };
   int cbase = 0, sbase = 0;
   for (int at = 0; at < n; at += kPlanThreads) {
     const int i = at + tid;
@@ -314,11 +316,14 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
     for (int d = 1; d < kPlanThreads; d <<= 1) {
       const int x = tid >= d ? sum[0][tid - d] : 0, y = tid >= d ? sum[1][tid - d] : 0;
       __syncthreads();
-      sum[0][tid] += x, sum[1][tid] += y;
+      sum[0][tid] = add(sum[0][tid], x), sum[1][tid] = add(sum[1][tid], y);
       __syncthreads();
     }
-    if (i < n) cpre[i] = cbase + sum[0][tid] - c, spre[i] = sbase + sum[1][tid] - s;
-    cbase += sum[0][kPlanThreads - 1], sbase += sum[1][kPlanThreads - 1];
+    if (i < n) {
+      cpre[i] = add(cbase, tid ? sum[0][tid - 1] : 0);
+      spre[i] = add(sbase, tid ? sum[1][tid - 1] : 0);
+    }
+    cbase = add(cbase, sum[0][kPlanThreads - 1]), sbase = add(sbase, sum[1][kPlanThreads - 1]);
     __syncthreads();
   }
   if (tid == 0) {
@@ -350,7 +355,8 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
     const int b = clamp(cu[seq]);
     int len = clamp(cu[seq + 1]) - b - from;
     if (len > seg_chunks * kChunk) len = seg_chunks * kChunk;
-    if (len > (nc - first) * kChunk) len = (nc - first) * kChunk;  // offsets that decrease: the table ends
+    const int room = nc > first ? nc - first : 0;  // offsets that decrease: the table of chunks ends
+    if (len > room * kChunk) len = room * kChunk;
     const bool last = s + 1 >= spre[seq + 1];
     seg_tab[s] = make_int4(first, b + from, len > 0 ? len : 0, seq << 2 | (at == 0 ? 1 : 0) | (last ? 2 : 0));
   }

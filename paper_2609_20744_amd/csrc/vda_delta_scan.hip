@@ -34,6 +34,31 @@ struct ScanShape {
   static constexpr int kCopiers = kWaves >= 8 ? 8 : kWaves >= 4 ? 4 : kWaves >= 2 ? 2 : 1;
 };
 
+// 4 x 4 values of four lanes, a column each, transposed: a row each.
+__device__ __forceinline__ floatx4 quad_transpose(floatx4 v) {
+  const int lane = threadIdx.x;
+#pragma unroll
+  for (int m = 1; m < 4; m <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e & m) continue;
+      const bool odd = lane & m;
+      const int send = __float_as_int(odd ? v[e] : v[e | m]);
+      const float got = __int_as_float(m == 1 ? __builtin_amdgcn_update_dpp(0, send, 0xB1, 0xf, 0xf, false)
+                                              : __builtin_amdgcn_update_dpp(0, send, 0x4E, 0xf, 0xf, false));
+      v[e] = odd ? got : v[e];
+      v[e | m] = odd ? v[e | m] : got;
+    }
+  return v;
+}
+
+// Where a map's matrix has the element (r, c): 16 x 32 tiles with each lane's
+// operand, eight consecutive columns of a row, in one place.
+template <int DK>
+__device__ __forceinline__ size_t map_elem(int r, int c) {
+  return ((size_t)((r >> 4) * (DK / 32) + (c >> 5)) * 64 + (c >> 3 & 3) * 16 + (r & 15)) * 8 + (c & 7);
+}
+
 template <bool F32, int DK, int DV, int MODE>
 __global__ __launch_bounds__((64 * ScanShape<DK, DV, MODE>::kWaves))
 __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
@@ -335,12 +360,15 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
     for (int n = 0; n < NV; ++n) {
       const int u = col + 4 * n, ch = 32 * s + 8 * lg;
       if (MODE == kMap && matrix) {
-        // M by rows and by columns, each a wide operand of the join.
+        // M by rows and by columns, each as wide operand tiles of the join.
         char* m = a.segM + ((size_t)seg * a.Hv + h) * 2 * km * 4;
-        const W w = O::wide(S[s][0][n], S[s][1][n]);
-        store_wide8<F32>(m, (size_t)u * DK + ch, km, w);
+        store_wide8<F32>(m, map_elem<DK>(u, ch), km, O::wide(S[s][0][n], S[s][1][n]));
+        if (n == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) store_wide1<F32>(m + km * 4, (size_t)(ch + e) * DK + u, km, w, e);
+          for (int o = 0; o < 2; ++o)
+            store_wide8<F32>(m + km * 4, map_elem<DK>(ch + 4 * o + (li & 3), 32 * vb + 8 * (li >> 2)), km,
+                             O::wide(quad_transpose(S[s][o][0]), quad_transpose(S[s][o][NV - 1])));
+        }
       } else {
         float* to = nullptr;
         if (MODE == kMap)
@@ -369,10 +397,13 @@ __global__ __launch_bounds__(kThreads) void delta_join_kernel(DeltaArgs a, bool 
   constexpr int KS = DK / 32, NC = DK / 16, WT = (NC + 3) / 4;
   constexpr int kRow = DK + 4;
   __shared__ __align__(16) float x[2][16 * kRow];
+  // Workgroups go round the eight dies: those of one sequence and head, which
+  // read the same matrices, to one of them.
   const int blocks = a.d_v / 16;
-  const int rb = blockIdx.x % blocks;
-  const int h = uniform((blockIdx.x / blocks) % a.Hv);
-  const int seq = uniform(blockIdx.x / (blocks * a.Hv));
+  const int rb = blockIdx.x / 8 % blocks;
+  const int item = uniform(blockIdx.x / (8 * blocks) * 8 + blockIdx.x % 8);
+  const int seq = uniform(item / a.Hv), h = item - seq * a.Hv;
+  if (seq >= a.n_seqs) return;
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
   const int wave = uniform(tid >> 6);
   // The sequence's segments.
@@ -405,7 +436,7 @@ __global__ __launch_bounds__(kThreads) void delta_join_kernel(DeltaArgs a, bool 
       add[slot][w] = *reinterpret_cast<const floatx4*>(Ji + 16 * c + 4 * lg);
 #pragma unroll
       for (int s = 0; s < KS; ++s)
-        m[slot][w][s] = load_wide8<F32>(mi, (size_t)(16 * c + li) * DK + 32 * s + 8 * lg, km);
+        m[slot][w][s] = load_wide8<F32>(mi, map_elem<DK>(16 * c + li, 32 * s + 8 * lg), km);
     }
   };
   // After segment 0 the state is its own J (scanned from the sequence's state).
@@ -465,7 +496,7 @@ hipError_t run(int what, const DeltaArgs& a, hipStream_t stream) {
 
 template <bool F32>
 hipError_t join(int d_k, bool reverse, const DeltaArgs& a, hipStream_t stream) {
-  const unsigned grid = (unsigned)a.n_seqs * (unsigned)a.Hv * (unsigned)(a.d_v / 16);
+  const unsigned grid = ((unsigned)a.n_seqs * (unsigned)a.Hv + 7) / 8 * 8 * (unsigned)(a.d_v / 16);
   switch (d_k) {
     case 32: delta_join_kernel<F32, 32><<<grid, 128, 0, stream>>>(a, reverse); break;
     case 64: delta_join_kernel<F32, 64><<<grid, kThreads, 0, stream>>>(a, reverse); break;
