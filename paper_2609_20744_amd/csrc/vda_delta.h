@@ -146,13 +146,9 @@ __device__ __forceinline__ int tile_place(int row, int lg) {
   return (16 * lg + (row ^ (F32 ? lg : (lg & 1) << 3))) * 16;
 }
 
-// Row of place `row` of tile t in paired order.
-__device__ __forceinline__ int paired_row(int t, int row) {
-  return 32 * (t >> 1) + 8 * (row >> 2) + 4 * (t & 1) + (row & 3);
-}
-
-// ... and in twisted order: a tile read by columns in that order (twisted_cols)
-// takes both halves of its 16-byte places, and so all banks.
+// Row of place `row` of tile t in twisted order: paired order (below) with the
+// two tiles' rows exchanged for row >= 8.  A tile read by columns in that order
+// (twisted_cols) takes both halves of its 16-byte places, and so all banks.
 __device__ __forceinline__ int twisted_row(int t, int row) {
   return 32 * (t >> 1) + 8 * (row >> 2) + 4 * ((t ^ (row >> 3)) & 1) + (row & 3);
 }
@@ -262,15 +258,8 @@ __device__ __forceinline__ floatx4 tile_values(const char* tile, int o, const Ti
 // [block][row tile], by the first COPIERS waves (a power of two).  A row at or
 // past `len` repeats row len - 1, so that every address is the sequence's own
 // (what such rows meet is zero: their writes, their strengths, their stores).
-// ORDER: which row a place holds.
-enum class RowOrder {
-  kPlain,   // place r of tile t is row 16 t + r
-  kPaired,  // place 4 a + b of tiles 2 t and 2 t + 1 is row 32 t + 8 a + b and
-            // 32 t + 8 a + 4 + b: the order that channels have (above), for rows
-            // that are contracted with channels
-  kTwisted  // the same with the two tiles' rows exchanged for a >= 2
-};
-template <bool F32, int ROWS, int BLOCKS, int COPIERS, RowOrder ORDER = RowOrder::kPlain>
+// Place r of tile t is row 16 t + r, or TWISTED.
+template <bool F32, int ROWS, int BLOCKS, int COPIERS, bool TWISTED = false>
 __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* tiles, int len, uint32_t row_bytes,
                                            int wave, int lane, uint32_t from = 0) {
   constexpr int kHalves = F32 ? 2 : 1, kBlock = F32 ? 128 : 64, kRow = row_tile_bytes<F32>(), kPer = ROWS / 16;
@@ -282,8 +271,7 @@ __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* til
     const int p = wave + i * COPIERS;  // tile p % kPer of block p / kPer
     if (kTiles % COPIERS != 0 && p >= kTiles) break;
     const int t = p % kPer;
-    const int r = ORDER == RowOrder::kPaired ? paired_row(t, row) : ORDER == RowOrder::kTwisted ? twisted_row(t, row)
-                                                                                              : 16 * t + row;
+    const int r = TWISTED ? twisted_row(t, row) : 16 * t + row;
     const uint32_t at = __umul24((uint32_t)(r < len ? r : len - 1), row_bytes) + chan;
 #pragma unroll
     for (int half = 0; half < kHalves; ++half)
@@ -292,17 +280,18 @@ __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* til
   }
 }
 
-// Copies BYTES (a multiple of 1024) of contiguous memory into LDS as it is.
+// Copies BYTES (a multiple of 1024) of contiguous memory, `from` bytes behind
+// src, into LDS as it is.
 template <int BYTES, int COPIERS>
-__device__ __forceinline__ void copy_flat(const void* from, char* to, int wave, int lane) {
+__device__ __forceinline__ void copy_flat(__amdgpu_buffer_rsrc_t src, char* to, int wave, int lane,
+                                          uint32_t from = 0) {
   constexpr int kPieces = BYTES / 1024, kSteps = (kPieces + COPIERS - 1) / COPIERS;
-  const __amdgpu_buffer_rsrc_t src = make_rsrc(from, (uint32_t)BYTES);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int p = wave + i * COPIERS;
     if (kPieces % COPIERS != 0 && p >= kPieces) break;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(to + p * 1024), 16, (uint32_t)lane * 16u, p * 1024, 0,
-                                             0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(to + p * 1024), 16, (uint32_t)lane * 16u,
+                                             from + p * 1024, 0, 0);
   }
 }
 
@@ -391,16 +380,41 @@ struct ChunkRecord {
   }
 };
 
-// A value kept in the workspace for another kernel's wide operand, natural
-// row order: bf16 hi and lo planes, or one fp32 plane.
+// What the scans keep for the gradient kernel (S and dS, value x key channels;
+// N and dv, value channels x tokens) lies as that kernel's row tiles, 32 value
+// channels after 32, in bf16 hi and lo planes or one of fp32, so that it copies
+// contiguous memory.  Place r of tile t of 32 rows is row 8 (r / 4) + 4 t + r % 4
+// (paired order: the order that channels have, above, for rows that are
+// contracted with channels), which a scan's lane r has of half t.
+// Tile: half t of rows 32 s .., block b of `blocks` of 32 columns.
+__device__ __forceinline__ int keep_tile(int s, int t, int b, int blocks) { return (s * blocks + b) * 2 + t; }
+
+// Eight channels of a state's row; place: TileLane::row.
 template <bool F32>
-__device__ __forceinline__ void store_wide4(char* base, size_t elem, size_t plane_elems, floatx4 x) {
+__device__ __forceinline__ void keep_state(char* base, int tile, int place, size_t plane_elems,
+                                           const typename Op<F32>::W& w) {
+  char* to = base + tile * row_tile_bytes<F32>() + place;
   if constexpr (F32) {
-    *reinterpret_cast<floatx4*>(base + elem * 4) = x;
+    *reinterpret_cast<floatx4*>(to) = floatx4{w.v[0], w.v[1], w.v[2], w.v[3]};
+    *reinterpret_cast<floatx4*>(to + 1024) = floatx4{w.v[4], w.v[5], w.v[6], w.v[7]};
+  } else {
+    *reinterpret_cast<bf16x8*>(to) = w.hi;
+    *reinterpret_cast<bf16x8*>(to + plane_elems * 2) = w.lo;
+  }
+}
+
+// Tokens 16 u + 4 lg .. + 3 of a block of 32, of the row of place li.
+template <bool F32>
+__device__ __forceinline__ void keep_tokens(char* base, int tile, int u, int li, int lg, size_t plane_elems,
+                                            floatx4 x) {
+  char* to = base + tile * row_tile_bytes<F32>() + tile_place<F32>(li, 2 * u + (lg >> 1));
+  if constexpr (F32) {
+    *reinterpret_cast<floatx4*>(to + (lg & 1) * 1024) = x;
   } else {
     const uint32_t h0 = pack_bf16x2(x[0], x[1]), h1 = pack_bf16x2(x[2], x[3]);
-    *reinterpret_cast<uint2*>(base + elem * 2) = make_uint2(h0, h1);
-    *reinterpret_cast<uint2*>(base + (plane_elems + elem) * 2) =
+    to += (lg & 1) * 8;
+    *reinterpret_cast<uint2*>(to) = make_uint2(h0, h1);
+    *reinterpret_cast<uint2*>(to + plane_elems * 2) =
         make_uint2(rest_bf16x2(x[0], x[1], h0), rest_bf16x2(x[2], x[3], h1));
   }
 }

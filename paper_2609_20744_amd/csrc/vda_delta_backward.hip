@@ -82,7 +82,7 @@ void delta_reverse_kernel(DeltaArgs a) {
   auto stage = [&](int at, char* buf) __attribute__((always_inline)) {
     const int len = min(kChunk, si.len - at * kChunk);
     copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
-    copy_flat<1024 + 2 * kWideTri, kWaves>(rp, buf + kOffVec, wave, lane);
+    copy_flat<1024 + 2 * kWideTri, kWaves>(make_rsrc(rp, 1024 + 2 * kWideTri), buf + kOffVec, wave, lane);
     copy_tiles<F32, kChunk, DV / 32, kWaves>(make_rsrc(op, 64u * v_row), buf + kOffDo, len, v_row, wave, lane);
     copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
     kp -= 64u * k_row, qp -= 64u * k_row, op -= 64u * v_row, rp -= rec_size * a.Hv;
@@ -116,7 +116,7 @@ void delta_reverse_kernel(DeltaArgs a) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const W Sw = O::wide(S[s][0], S[s][1]);
-      if constexpr (!MAP) store_wide8<F32>(ks, (size_t)col * DK + 32 * s + 8 * lg, mat, Sw);
+      if constexpr (!MAP) keep_state<F32>(ks, keep_tile(vb, n0, s, KS), tl.row, mat, Sw);
       if (s + 1 < KS)
         rows(s + 1);
       else
@@ -200,7 +200,7 @@ void delta_reverse_kernel(DeltaArgs a) {
       char* kd = a.keepdv + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        store_wide4<F32>(kd, (size_t)col * kChunk + 16 * t + 4 * lg, (size_t)DV * kChunk, y[t]);
+        keep_tokens<F32>(kd, keep_tile(vb, n0, t >> 1, 2), t & 1, li, lg, (size_t)DV * kChunk, y[t]);
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) yw[s] = O::wide(-gv[2 * s] * y[2 * s], -gv[2 * s + 1] * y[2 * s + 1]);
@@ -297,9 +297,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const size_t qk = ((size_t)ci.tok * a.qk_tok + (size_t)hk * a.qk_head) * ES;
   const char* const tileK = rowsKQ;
   const char* const tileQ = rowsKQ + kTileK;
-  copy_tiles<F32, kChunk, KS, 8, RowOrder::kTwisted>(make_rsrc((const char*)a.k + qk, 64u * k_row), rowsKQ, len,
+  copy_tiles<F32, kChunk, KS, 8, true>(make_rsrc((const char*)a.k + qk, 64u * k_row), rowsKQ, len,
                                                      k_row, wave, lane);
-  copy_tiles<F32, kChunk, KS, 8, RowOrder::kTwisted>(make_rsrc((const char*)a.q + qk, 64u * k_row), rowsKQ + kTileK,
+  copy_tiles<F32, kChunk, KS, 8, true>(make_rsrc((const char*)a.q + qk, 64u * k_row), rowsKQ + kTileK,
                                                      len, k_row, wave, lane);
 
   const size_t first = (size_t)chunk * a.Hv + (size_t)hk * a.group;
@@ -318,12 +318,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
       const uint32_t so = p * kMat + s * kTileS, no = p * kNmat + s * kTileN;
-      copy_tiles<F32, 32, KS, 8, RowOrder::kPaired>(sr, buf + p * kTileS, 32, DK * ES, wave, lane, so);
-      copy_tiles<F32, 32, KS, 8, RowOrder::kPaired>(dsr, buf + kOffdS + p * kTileS, 32, DK * ES, wave, lane, so);
-      copy_tiles<F32, 32, 2, 8, RowOrder::kPaired>(nr, buf + kOffN + p * kTileN, 32, kChunk * ES, wave, lane, no);
-      copy_tiles<F32, 32, 2, 8, RowOrder::kPaired>(dvr, buf + kOffdv + p * kTileN, 32, kChunk * ES, wave, lane, no);
+      copy_flat<kTileS, 8>(sr, buf + p * kTileS, wave, lane, so);
+      copy_flat<kTileS, 8>(dsr, buf + kOffdS + p * kTileS, wave, lane, so);
+      copy_flat<kTileN, 8>(nr, buf + kOffN + p * kTileN, wave, lane, no);
+      copy_flat<kTileN, 8>(dvr, buf + kOffdv + p * kTileN, wave, lane, no);
     }
-    copy_tiles<F32, kChunk, 1, 8, RowOrder::kTwisted>(
+    copy_tiles<F32, kChunk, 1, 8, true>(
         make_rsrc((const char*)a.dout + vo + (n / steps) * a.v_head * ES, 64u * v_row), buf + kOffO, len, v_row, wave,
         lane, 32 * s * ES);
   };

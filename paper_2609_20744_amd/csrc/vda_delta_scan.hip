@@ -135,7 +135,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
     const int len = min(kChunk, si.len - c * kChunk);
     if (Shape::kWaves == kCopiers || wave < kCopiers) {
       copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
-      copy_flat<kRecord, kCopiers>(rp, buf + kOffT, wave, lane);
+      copy_flat<kRecord, kCopiers>(make_rsrc(rp, kRecord), buf + kOffT, wave, lane);
       copy_tiles<F32, kChunk, DV / 32, kCopiers>(make_rsrc(vp, 64u * v_row), buf + kOffV, len, v_row, wave, lane);
       if constexpr (MODE == kOutput)
         copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
@@ -193,7 +193,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
       for (int n = 0; n < NV; ++n) {
         Sw[n] = O::wide(S[s][0][n], S[s][1][n]);
         if constexpr (MODE == kKeep)
-          store_wide8<F32>(ks, (size_t)(col + 4 * n) * DK + 32 * s + 8 * lg, mat, Sw[n]);
+          keep_state<F32>(ks, keep_tile(vb, n0 + n, s, KS), tl.row, mat, Sw[n]);
       }
       if (s + 1 < KS) rows(s + 1);
       if (NV == 1 && s + 1 == KS) {
@@ -258,7 +258,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int n = 0; n < NV; ++n)
-          store_wide4<F32>(kn, (size_t)(col + 4 * n) * kChunk + 16 * t + 4 * lg, (size_t)DV * kChunk, N[t][n]);
+          keep_tokens<F32>(kn, keep_tile(vb, n0 + n, t >> 1, 2), t & 1, li, lg, (size_t)DV * kChunk, N[t][n]);
     }
 
     if constexpr (MODE == kOutput) {
