@@ -143,7 +143,7 @@ __host__ __device__ constexpr int row_tile_bytes() { return F32 ? 2048 : 1024; }
 
 template <bool F32>
 __device__ __forceinline__ int tile_place(int row, int lg) {
-  return (16 * lg + (row ^ (F32 ? lg : (lg & 1) << 3))) * 16;
+  return F32 ? (16 * lg + (row ^ lg)) * 16 : (4 * row + (lg ^ (row >> 2))) * 16;
 }
 
 // Row of place `row` of tile t in twisted order: paired order (below) with the
@@ -264,7 +264,7 @@ __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* til
                                            int wave, int lane, uint32_t from = 0) {
   constexpr int kHalves = F32 ? 2 : 1, kBlock = F32 ? 128 : 64, kRow = row_tile_bytes<F32>(), kPer = ROWS / 16;
   constexpr int kTiles = kPer * BLOCKS, kSteps = (kTiles + COPIERS - 1) / COPIERS;
-  const int lg = lane >> 4, row = (lane & 15) ^ (F32 ? lg : (lg & 1) << 3);
+  const int row = F32 ? (lane & 15) ^ (lane >> 4) : lane >> 2, lg = F32 ? lane >> 4 : (lane & 3) ^ (row >> 2);
   const uint32_t chan = (uint32_t)lg * (F32 ? 32u : 16u);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
