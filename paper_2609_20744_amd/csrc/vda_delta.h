@@ -130,8 +130,15 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 // offset plus a constant: no address is computed in a loop.  Columns are
 // read across lanes' places (ds_read_b64_tr_b16, in which lane i of 16 receives
 // element i % 4 of the 8-byte pieces that lanes i / 4 + 4 e address; or four
-// words in fp32), for which the places of a unit column lg are permuted, which spreads them over the
-// banks (bf16: two accesses a bank, the least when half of each 16 bytes is read).
+// words in fp32).  Places are permuted so that 16 lanes that read together, by
+// rows or by columns, meet 16 different places of the 256 bytes of all banks.
+//
+// The 1 KB of a copy to LDS are consecutive places, so their order is also what
+// a copy reads from memory at a time: with a row's places 16 apart it was 16
+// bytes of each of 16 rows, then the next 16, and the reverse scan took 178 us
+// (16401 tokens, 16 heads); with four lanes on 64 bytes of a row 167 us.  Where
+// there are two tiles of a row, they share 2 KB, eight lanes take 128 bytes of
+// a row, a whole cache line (RowTiles::kPairs).
 //
 // Channels are paired with results by this order: operand element e of lane
 // lg, step s, is channel 32 s + 8 lg + e; so a result whose rows are such a
@@ -145,6 +152,20 @@ template <bool F32>
 __device__ __forceinline__ int tile_place(int row, int lg) {
   return F32 ? (16 * lg + (row ^ lg)) * 16 : (4 * row + (lg ^ (row >> 2))) * 16;
 }
+// ... of a pair of tiles (bf16), lg < 8.
+__device__ __forceinline__ int pair_unit(int row, int lg) { return lg ^ ((row & 2) << 1 | row >> 2); }
+__device__ __forceinline__ int pair_place(int row, int lg) { return (8 * row + pair_unit(row, lg)) * 16; }
+
+// 64 rows of 32 BLOCKS channels: where tile (block s, row tile t) is, and what
+// a lane's offsets in a block's tiles are changed by (the second of a pair).
+template <bool F32, int BLOCKS>
+struct RowTiles {
+  static constexpr bool kPairs = !F32 && BLOCKS % 2 == 0;
+  __device__ static constexpr int tile(int s, int t) {
+    return kPairs ? ((s >> 1) * 4 + t) * 2048 : (s * 4 + t) * row_tile_bytes<F32>();
+  }
+  __device__ static constexpr int odd(int s) { return kPairs ? (s & 1) * 64 : 0; }
+};
 
 // Row of place `row` of tile t in twisted order: paired order (below) with the
 // two tiles' rows exchanged for row >= 8.  A tile read by columns in that order
@@ -157,34 +178,35 @@ __device__ __forceinline__ int twisted_row(int t, int row) {
 struct TileLane {
   int row, col[4];
 };
-template <bool F32>
+template <bool F32, bool PAIRS>
 __device__ __forceinline__ TileLane tile_lane(int li, int lg) {
   TileLane l;
-  l.row = tile_place<F32>(li, lg);
+  l.row = PAIRS ? pair_place(li, lg) : tile_place<F32>(li, lg);
   if constexpr (F32) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) l.col[e] = tile_place<true>(4 * lg + e, li >> 2) + (li & 3) * 4;
   } else {
-    l.col[0] = tile_place<false>(4 * lg + (li >> 2), li & 3);
+    const int row = 4 * lg + (li >> 2), unit = li & 3;
+    l.col[0] = PAIRS ? pair_place(row, unit) : tile_place<false>(row, unit);
     l.col[1] = l.col[2] = l.col[3] = 0;
   }
   return l;
 }
 
 template <bool F32>
-__device__ __forceinline__ typename Op<F32>::X tile_row(const char* tile, const TileLane& l) {
+__device__ __forceinline__ typename Op<F32>::X tile_row(const char* tile, int odd, const TileLane& l) {
   if constexpr (F32) {
     const floatx4 a = *reinterpret_cast<const floatx4*>(tile + l.row);
     const floatx4 b = *reinterpret_cast<const floatx4*>(tile + 1024 + l.row);
     return Op<true>::narrow(a, b);
   } else {
-    return *reinterpret_cast<const bf16x8*>(tile + l.row);
+    return *reinterpret_cast<const bf16x8*>(tile + (l.row ^ odd));
   }
 }
 
 // Channel 8 (li / 4) + 4 o + li % 4 of the tile at tokens 4 lg .. + 3.
-__device__ __forceinline__ shortx4 tile_col_bf16(const char* tile, int o, const TileLane& l) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + 8 * o + l.col[0]));
+__device__ __forceinline__ shortx4 tile_col_bf16(const char* tile, int o, int odd, const TileLane& l) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + 8 * o + (l.col[0] ^ odd)));
 }
 __device__ __forceinline__ floatx4 tile_col_f32(const char* tile, int o, const TileLane& l) {
   floatx4 v;
@@ -195,13 +217,28 @@ __device__ __forceinline__ floatx4 tile_col_f32(const char* tile, int o, const T
 
 // The same channel of two tiles (tokens t0 .. and t1 ..) as an operand.
 template <bool F32>
-__device__ __forceinline__ typename Op<F32>::X tile_cols(const char* t0, const char* t1, int o, const TileLane& l) {
+__device__ __forceinline__ typename Op<F32>::X tile_cols(const char* t0, const char* t1, int o, int odd,
+                                                         const TileLane& l) {
   if constexpr (F32) {
     return Op<true>::narrow(tile_col_f32(t0, o, l), tile_col_f32(t1, o, l));
   } else {
-    const shortx4 a = tile_col_bf16(t0, o, l), b = tile_col_bf16(t1, o, l);
+    const shortx4 a = tile_col_bf16(t0, o, odd, l), b = tile_col_bf16(t1, o, odd, l);
     typedef short shortx8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8, shortx8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+  }
+}
+
+// ... of one tile as fp32.
+template <bool F32>
+__device__ __forceinline__ floatx4 tile_values(const char* tile, int o, int odd, const TileLane& l) {
+  if constexpr (F32) {
+    return tile_col_f32(tile, o, l);
+  } else {
+    const shortx4 a = tile_col_bf16(tile, o, odd, l);
+    floatx4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16);
+    return v;
   }
 }
 
@@ -240,43 +277,35 @@ __device__ __forceinline__ typename Op<F32>::X twisted_cols(const char* t0, cons
   }
 }
 
-// ... of one tile as fp32.
-template <bool F32>
-__device__ __forceinline__ floatx4 tile_values(const char* tile, int o, const TileLane& l) {
-  if constexpr (F32) {
-    return tile_col_f32(tile, o, l);
-  } else {
-    const shortx4 a = tile_col_bf16(tile, o, l);
-    floatx4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float((uint32_t)(uint16_t)a[e] << 16);
-    return v;
-  }
-}
-
-// Copies ROWS rows of 32 BLOCKS channels, row_bytes apart, into row tiles
-// [block][row tile], by the first COPIERS waves (a power of two).  A row at or
-// past `len` repeats row len - 1, so that every address is the sequence's own
-// (what such rows meet is zero: their writes, their strengths, their stores).
-// Place r of tile t is row 16 t + r, or TWISTED.
-template <bool F32, int ROWS, int BLOCKS, int COPIERS, bool TWISTED = false>
+// Copies 64 rows of 32 BLOCKS channels, row_bytes apart, into row tiles (as
+// RowTiles has them, or TWISTED: no pairs, twisted order) by the first COPIERS
+// waves (a power of two).  A row at or past `len` repeats row len - 1, so that
+// every address is the sequence's own (what such rows meet is zero: their
+// writes, their strengths, their stores).
+template <bool F32, int BLOCKS, int COPIERS, bool TWISTED = false>
 __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* tiles, int len, uint32_t row_bytes,
                                            int wave, int lane, uint32_t from = 0) {
-  constexpr int kHalves = F32 ? 2 : 1, kBlock = F32 ? 128 : 64, kRow = row_tile_bytes<F32>(), kPer = ROWS / 16;
-  constexpr int kTiles = kPer * BLOCKS, kSteps = (kTiles + COPIERS - 1) / COPIERS;
+  constexpr bool kPairs = !TWISTED && RowTiles<F32, BLOCKS>::kPairs;
+  constexpr int kHalves = F32 ? 2 : 1, kRow = row_tile_bytes<F32>();
+  constexpr int kTiles = 4 * BLOCKS, kSteps = (kTiles + COPIERS - 1) / COPIERS;
   const int row = F32 ? (lane & 15) ^ (lane >> 4) : lane >> 2, lg = F32 ? lane >> 4 : (lane & 3) ^ (row >> 2);
   const uint32_t chan = (uint32_t)lg * (F32 ? 32u : 16u);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int p = wave + i * COPIERS;  // tile p % kPer of block p / kPer
+    const int p = wave + i * COPIERS;  // tile p % 4 of block p / 4; or half of a pair
     if (kTiles % COPIERS != 0 && p >= kTiles) break;
-    const int t = p % kPer;
-    const int r = TWISTED ? twisted_row(t, row) : 16 * t + row;
-    const uint32_t at = __umul24((uint32_t)(r < len ? r : len - 1), row_bytes) + chan;
+    if constexpr (kPairs) {
+      const int in = 8 * (p & 1) + (lane >> 3), r = 16 * (p >> 1 & 3) + in;
+      const uint32_t at = __umul24((uint32_t)(r < len ? r : len - 1), row_bytes) + pair_unit(in, lane & 7) * 16u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tiles + p * 1024), 16, at, from + (p >> 3) * 128, 0, 0);
+    } else {
+      const int t = p & 3, r = TWISTED ? twisted_row(t, row) : 16 * t + row;
+      const uint32_t at = __umul24((uint32_t)(r < len ? r : len - 1), row_bytes) + chan;
 #pragma unroll
-    for (int half = 0; half < kHalves; ++half)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tiles + p * kRow + half * 1024), 16, at,
-                                               from + (p / kPer) * kBlock + half * 16, 0, 0);
+      for (int half = 0; half < kHalves; ++half)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tiles + p * kRow + half * 1024), 16, at,
+                                                 from + (p >> 2) * (F32 ? 128 : 64) + half * 16, 0, 0);
+    }
   }
 }
 
@@ -389,7 +418,7 @@ struct ChunkRecord {
 // Tile: half t of rows 32 s .., block b of `blocks` of 32 columns.
 __device__ __forceinline__ int keep_tile(int s, int t, int b, int blocks) { return (s * blocks + b) * 2 + t; }
 
-// Eight channels of a state's row; place: TileLane::row.
+// Eight channels of a state's row; place: tile_place(li, lg).
 template <bool F32>
 __device__ __forceinline__ void keep_state(char* base, int tile, int place, size_t plane_elems,
                                            const typename Op<F32>::W& w) {

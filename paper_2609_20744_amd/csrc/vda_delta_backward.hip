@@ -34,7 +34,7 @@ void delta_reverse_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
   typedef typename O::W W;
-  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kWaves = DV / 16, kRow = row_tile_bytes<F32>();
+  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kWaves = DV / 16;
   constexpr int kBufs = F32 ? 1 : 2;
   constexpr int kTileK = kChunk * DK * ES;
   constexpr int kOffQ = kTileK, kOffVec = 2 * kTileK, kOffTt = kOffVec + 1024, kOffPt = kOffTt + kWideTri,
@@ -56,7 +56,9 @@ void delta_reverse_kernel(DeltaArgs a) {
   const int chunks = chunks_of(si.len);
   constexpr size_t mat = (size_t)DV * DK;
   const size_t rec_size = ChunkRecord::bytes(F32, true);
-  const TileLane tl = tile_lane<F32>(li, lg);
+  typedef RowTiles<F32, KS> RowsK;
+  typedef RowTiles<F32, DV / 32> RowsV;
+  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg), vl = tile_lane<F32, RowsV::kPairs>(li, lg);
 
   const float* init = nullptr;
   if (si.ends & 2)
@@ -81,10 +83,10 @@ void delta_reverse_kernel(DeltaArgs a) {
   const char* rp = a.rec + ((size_t)(si.chunk + chunks - 1) * a.Hv + h) * rec_size + ChunkRecord::kVec;
   auto stage = [&](int at, char* buf) __attribute__((always_inline)) {
     const int len = min(kChunk, si.len - at * kChunk);
-    copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
+    copy_tiles<F32, KS, kWaves>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
     copy_flat<1024 + 2 * kWideTri, kWaves>(make_rsrc(rp, 1024 + 2 * kWideTri), buf + kOffVec, wave, lane);
-    copy_tiles<F32, kChunk, DV / 32, kWaves>(make_rsrc(op, 64u * v_row), buf + kOffDo, len, v_row, wave, lane);
-    copy_tiles<F32, kChunk, KS, kWaves>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
+    copy_tiles<F32, DV / 32, kWaves>(make_rsrc(op, 64u * v_row), buf + kOffDo, len, v_row, wave, lane);
+    copy_tiles<F32, KS, kWaves>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
     kp -= 64u * k_row, qp -= 64u * k_row, op -= 64u * v_row, rp -= rec_size * a.Hv;
   };
 
@@ -97,16 +99,16 @@ void delta_reverse_kernel(DeltaArgs a) {
     X kr[2][4], dO[2];
     auto rows = [&](int s) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) kr[s & 1][t] = tile_row<F32>(buf + (4 * s + t) * kRow, tl);
+      for (int t = 0; t < 4; ++t) kr[s & 1][t] = tile_row<F32>(buf + RowsK::tile(s, t), RowsK::odd(s), tl);
     };
     rows(0);
     floatx4 ev[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) ev[t] = *reinterpret_cast<const floatx4*>(eta + 16 * t);
-    const char* otiles = buf + kOffDo + 4 * vb * kRow;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
-      dO[t] = tile_cols<F32>(otiles + 2 * t * kRow, otiles + (2 * t + 1) * kRow, n0, tl);
+      dO[t] = tile_cols<F32>(buf + kOffDo + RowsV::tile(vb, 2 * t), buf + kOffDo + RowsV::tile(vb, 2 * t + 1), n0,
+                             RowsV::odd(vb), vl);
     fence<F32>();
 
     // dN = diag(eta) K dS^T + P^T dO.
@@ -116,7 +118,7 @@ void delta_reverse_kernel(DeltaArgs a) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const W Sw = O::wide(S[s][0], S[s][1]);
-      if constexpr (!MAP) keep_state<F32>(ks, keep_tile(vb, n0, s, KS), tl.row, mat, Sw);
+      if constexpr (!MAP) keep_state<F32>(ks, keep_tile(vb, n0, s, KS), tile_place<F32>(li, lg), mat, Sw);
       if (s + 1 < KS)
         rows(s + 1);
       else
@@ -156,7 +158,7 @@ void delta_reverse_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          ct[s][t] = tile_cols<F32>(tiles + (4 * s + 2 * t) * kRow, tiles + (4 * s + 2 * t + 1) * kRow, u, tl);
+          ct[s][t] = tile_cols<F32>(tiles + RowsK::tile(s, 2 * t), tiles + RowsK::tile(s, 2 * t + 1), u, RowsK::odd(s), tl);
     };
     columns(buf + kOffQ, 0);
     fence<F32>();
@@ -297,9 +299,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   const size_t qk = ((size_t)ci.tok * a.qk_tok + (size_t)hk * a.qk_head) * ES;
   const char* const tileK = rowsKQ;
   const char* const tileQ = rowsKQ + kTileK;
-  copy_tiles<F32, kChunk, KS, 8, true>(make_rsrc((const char*)a.k + qk, 64u * k_row), rowsKQ, len,
+  copy_tiles<F32, KS, 8, true>(make_rsrc((const char*)a.k + qk, 64u * k_row), rowsKQ, len,
                                                      k_row, wave, lane);
-  copy_tiles<F32, kChunk, KS, 8, true>(make_rsrc((const char*)a.q + qk, 64u * k_row), rowsKQ + kTileK,
+  copy_tiles<F32, KS, 8, true>(make_rsrc((const char*)a.q + qk, 64u * k_row), rowsKQ + kTileK,
                                                      len, k_row, wave, lane);
 
   const size_t first = (size_t)chunk * a.Hv + (size_t)hk * a.group;
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       copy_flat<kTileN, 8>(nr, buf + kOffN + p * kTileN, wave, lane, no);
       copy_flat<kTileN, 8>(dvr, buf + kOffdv + p * kTileN, wave, lane, no);
     }
-    copy_tiles<F32, kChunk, 1, 8, true>(
+    copy_tiles<F32, 1, 8, true>(
         make_rsrc((const char*)a.dout + vo + (n / steps) * a.v_head * ES, 64u * v_row), buf + kOffO, len, v_row, wave,
         lane, 32 * s * ES);
   };

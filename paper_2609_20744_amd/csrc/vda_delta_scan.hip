@@ -67,7 +67,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   typedef typename O::W W;
   typedef ScanShape<DK, DV, MODE> Shape;
   constexpr int NV = Shape::kNV, kCopiers = Shape::kCopiers;
-  constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kRow = row_tile_bytes<F32>();
+  constexpr int ES = F32 ? 4 : 2, KS = DK / 32;
   constexpr int kBufs = F32 ? 1 : 2;  // (two stages of fp32 do not fit)
   constexpr int kTileK = kChunk * DK * ES, kTileV = kChunk * DV * ES;
   // Stage: k rows, the chunk's record (T; gam, eta and beta; outputs: P), v
@@ -96,7 +96,9 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   const bool active = !(matrix && (si.ends & 1));
   const int chunks = chunks_of(si.len);
   const size_t rec_size = ChunkRecord::bytes(F32, MODE == kKeep || (MODE == kMap && a.dout != nullptr));
-  const TileLane tl = tile_lane<F32>(li, lg);
+  typedef RowTiles<F32, KS> RowsK;
+  typedef RowTiles<F32, DV / 32> RowsV;
+  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg), vl = tile_lane<F32, RowsV::kPairs>(li, lg);
   const int col = 32 * vb + 8 * (li >> 2) + 4 * n0 + (li & 3);  // + 4 n: this lane's columns
 
   // The entering state: S[s][o][n] holds channels 32 s + 8 lg + 4 o + r of column col + 4 n.
@@ -134,11 +136,11 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   auto stage = [&](int c, char* buf) __attribute__((always_inline)) {
     const int len = min(kChunk, si.len - c * kChunk);
     if (Shape::kWaves == kCopiers || wave < kCopiers) {
-      copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
+      copy_tiles<F32, KS, kCopiers>(make_rsrc(kp, 64u * k_row), buf, len, k_row, wave, lane);
       copy_flat<kRecord, kCopiers>(make_rsrc(rp, kRecord), buf + kOffT, wave, lane);
-      copy_tiles<F32, kChunk, DV / 32, kCopiers>(make_rsrc(vp, 64u * v_row), buf + kOffV, len, v_row, wave, lane);
+      copy_tiles<F32, DV / 32, kCopiers>(make_rsrc(vp, 64u * v_row), buf + kOffV, len, v_row, wave, lane);
       if constexpr (MODE == kOutput)
-        copy_tiles<F32, kChunk, KS, kCopiers>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
+        copy_tiles<F32, KS, kCopiers>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
     }
     kp += 64u * k_row, vp += 64u * v_row, rp += rec_size * a.Hv;
     if constexpr (MODE == kOutput) qp += 64u * k_row;
@@ -158,8 +160,8 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
     auto rows = [&](int s) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        kr[s & 1][t] = tile_row<F32>(buf + (4 * s + t) * kRow, tl);
-        if constexpr (MODE == kOutput) qr[s & 1][t] = tile_row<F32>(buf + kOffQ + (4 * s + t) * kRow, tl);
+        kr[s & 1][t] = tile_row<F32>(buf + RowsK::tile(s, t), RowsK::odd(s), tl);
+        if constexpr (MODE == kOutput) qr[s & 1][t] = tile_row<F32>(buf + kOffQ + RowsK::tile(s, t), RowsK::odd(s), tl);
       }
     };
     rows(0);
@@ -177,7 +179,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
           vv[t][n] = zero;
-          if (!matrix) vv[t][n] = tile_values<F32>(buf + kOffV + (4 * vb + t) * kRow, n0 + n, tl);
+          if (!matrix) vv[t][n] = tile_values<F32>(buf + kOffV + RowsV::tile(vb, t), n0 + n, RowsV::odd(vb), vl);
         }
       }
     };
@@ -193,7 +195,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
       for (int n = 0; n < NV; ++n) {
         Sw[n] = O::wide(S[s][0][n], S[s][1][n]);
         if constexpr (MODE == kKeep)
-          keep_state<F32>(ks, keep_tile(vb, n0 + n, s, KS), tl.row, mat, Sw[n]);
+          keep_state<F32>(ks, keep_tile(vb, n0 + n, s, KS), tile_place<F32>(li, lg), mat, Sw[n]);
       }
       if (s + 1 < KS) rows(s + 1);
       if (NV == 1 && s + 1 == KS) {
@@ -249,7 +251,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          kt[s][t] = tile_cols<F32>(buf + (4 * s + 2 * t) * kRow, buf + (4 * s + 2 * t + 1) * kRow, u, tl);
+          kt[s][t] = tile_cols<F32>(buf + RowsK::tile(s, 2 * t), buf + RowsK::tile(s, 2 * t + 1), u, RowsK::odd(s), tl);
     };
 
     if constexpr (MODE == kKeep) {
