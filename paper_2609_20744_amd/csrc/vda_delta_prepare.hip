@@ -4,8 +4,9 @@
 // decays gam and eta.
 //
 // One workgroup of four waves per chunk and value head.  The scores k.k and
-// q.k come from the matrix cores with operands loaded straight from memory
-// (a lane takes 16 bytes of one token's row); wave w makes row block w.  The
+// q.k come from the matrix cores, the rows copied to LDS as operand tiles (with
+// operands loaded straight from memory, 16 bytes of 16 rows at a time, the
+// kernel took 68 us where it now takes 49); wave w makes row block w.  The
 // decays multiply the fp32 results.  I + diag(beta) L is unit lower triangular
 // and is inverted in fp32, in LDS: its four 16 x 16 diagonal blocks by
 // forward substitution (a lane per column; a series of powers would be all
@@ -114,28 +115,17 @@ __device__ __forceinline__ Prefix4 prefix4(const double* pre) {
   return {{a[0], a[1], b[0], b[1]}};
 }
 
-// A token row as an operand, channels in memory order (the same in both
-// operands of a score): 8 consecutive channels a lane.
-template <bool F32>
-__device__ __forceinline__ typename Op<F32>::X token_op(__amdgpu_buffer_rsrc_t r, uint32_t row_off, int s,
-                                                        int lg) {
-  if constexpr (F32) {
-    const uint32_t o = row_off + (uint32_t)(32 * s + 8 * lg) * 4u;
-    const uint4 a = load_b128(r, o), b = load_b128(r, o + 16u);
-    return floatx8{__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                   __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-  } else {
-    return __builtin_bit_cast(bf16x8, load_b128(r, row_off + (uint32_t)(32 * s + 8 * lg) * 2u));
-  }
-}
-
 template <bool F32, int DK, bool BACKWARD>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(F32 ? 1 : BACKWARD ? 3 : 4)))
+__global__ __launch_bounds__(kThreads)
 void delta_prepare_kernel(DeltaArgs a) {
   typedef Op<F32> O;
   typedef typename O::X X;
-  constexpr int KS = DK / 32, ES = F32 ? 4 : 2;
-  __shared__ __align__(16) float m[kChunk * kLd];
+  constexpr int KS = DK / 32, ES = F32 ? 4 : 2, kTileK = kChunk * DK * ES;
+  typedef RowTiles<F32, KS> Rows;
+  // The matrix takes the place of q's rows, which makes four workgroups a compute unit.
+  constexpr int kMatrix = kChunk * kLd * (int)sizeof(float);
+  __shared__ __align__(16) char rowsK[kTileK], rowsQ[kTileK > kMatrix ? kTileK : kMatrix];
+  float* const m = reinterpret_cast<float*>(rowsQ);
   __shared__ __align__(16) double pre[kChunk];
   __shared__ __align__(16) float strengths[kChunk];
   const int h = blockIdx.x % (unsigned)a.Hv;
@@ -152,26 +142,17 @@ void delta_prepare_kernel(DeltaArgs a) {
     const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
     decay = a.g[at], beta = strength(a.beta[at]);
   }
-  // Token rows: past the chunk's end they are out of the buffers' range and
-  // read as zero.
-  const size_t qk = (size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head;
+  // The rows.  Those behind the chunk's end repeat its last: of T they reach
+  // nothing (such tokens have no strength), of P rows that only the backward
+  // pass reads, which are cleared there.
+  const size_t qk = ((size_t)ci.tok * a.qk_tok + (size_t)(h / a.group) * a.qk_head) * ES;
   const uint32_t row_bytes = (uint32_t)a.qk_tok * ES;
-  const uint32_t span = (uint32_t)(ci.len - 1) * row_bytes + DK * ES;
-  const __amdgpu_buffer_rsrc_t kr = make_rsrc((const char*)a.k + qk * ES, span);
-  const __amdgpu_buffer_rsrc_t qr = make_rsrc((const char*)a.q + qk * ES, span);
-  // All row blocks of k, and of q in the backward pass; the wave's own block
-  // once more (k; forward: q), because registers cannot be indexed by it.
-  constexpr int QT = BACKWARD ? 4 : 1;
-  X kt[4][KS], qt[QT][KS], kw[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    kw[s] = token_op<F32>(kr, (uint32_t)(16 * wave + li) * row_bytes, s, lg);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) kt[t][s] = token_op<F32>(kr, (uint32_t)(16 * t + li) * row_bytes, s, lg);
-#pragma unroll
-    for (int t = 0; t < QT; ++t)
-      qt[t][s] = token_op<F32>(qr, (uint32_t)(16 * (BACKWARD ? t : wave) + li) * row_bytes, s, lg);
-  }
+  copy_tiles<F32, KS, 4>(make_rsrc((const char*)a.k + qk, 64u * row_bytes), rowsK, ci.len, row_bytes, wave, lane);
+  copy_tiles<F32, KS, 4>(make_rsrc((const char*)a.q + qk, 64u * row_bytes), rowsQ, ci.len, row_bytes, wave, lane);
+  const TileLane tl = tile_lane<F32, Rows::kPairs>(li, lg);
+  auto row = [&](const char* rows, int t, int s) __attribute__((always_inline)) {
+    return tile_row<F32>(rows + Rows::tile(s, t), Rows::odd(s), tl);
+  };
   if (wave == 0) {
     const double G = decay_prefix(decay, lane);
     pre[lane] = G;
@@ -183,28 +164,19 @@ void delta_prepare_kernel(DeltaArgs a) {
     vec[128 + lane] = strengths[lane];
     if constexpr (BACKWARD) reinterpret_cast<double*>(rec + ChunkRecord::kPre)[lane] = G;
   }
-  lds_barrier();
+  copy_barrier();
 
   const int r0 = 16 * wave;
   const Prefix4 gi = prefix4(pre + r0 + 4 * lg);
   const floatx4 bi = *reinterpret_cast<const floatx4*>(strengths + r0 + 4 * lg);
 
-  // M = diag(beta) L, rows of this wave.
+  // The operands of this wave's rows: of k, and in the forward pass of q.
+  X kw[KS], qw[KS];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    if (t > wave) continue;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int s = 0; s < KS; ++s) acc = O::mma(kw[s], kt[t][s], acc);
-    const int j = 16 * t + li;
-    const double gj = pre[j];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = r0 + 4 * lg + e;
-      m[i * kLd + j] = keep_if(i > j, bi[e] * pow2(gi.x[e] - gj) * acc[e]);
-    }
+  for (int s = 0; s < KS; ++s) {
+    kw[s] = row(rowsK, wave, s);
+    if (!BACKWARD) qw[s] = row(rowsQ, wave, s);
   }
-
   // P, row block `wave`, as operand tiles: the product's rows are the columns j of P.
   if constexpr (!BACKWARD) {
     const double gq = pre[r0 + li];
@@ -218,7 +190,7 @@ void delta_prepare_kernel(DeltaArgs a) {
         const int t = 2 * s + u;
         p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < KS; ++c) p[u] = O::mma(kt[t][c], qt[0][c], p[u]);
+        for (int c = 0; c < KS; ++c) p[u] = O::mma(row(rowsK, t, c), qw[c], p[u]);
         const Prefix4 gj = prefix4(pre + 16 * t + 4 * lg);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -241,15 +213,32 @@ void delta_prepare_kernel(DeltaArgs a) {
         const int t = 2 * s + u;
         p[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < KS; ++c) p[u] = O::mma(qt[t][c], kw[c], p[u]);
+        for (int c = 0; c < KS; ++c) p[u] = O::mma(row(rowsQ, t, c), kw[c], p[u]);
         const Prefix4 gi = prefix4(pre + 16 * t + 4 * lg);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int i = 16 * t + 4 * lg + e;
-          p[u][e] = keep_if(i >= j, a.scale * pow2(gi.x[e] - gj) * p[u][e]);
+          p[u][e] = keep_if(i >= j && i < ci.len, a.scale * pow2(gi.x[e] - gj) * p[u][e]);
         }
       }
       store_tile_w<F32>(rec + ChunkRecord::kPt, tri_tile_t(wave, s), lane, O::wide(p[0], p[1]));
+    }
+  }
+  lds_barrier();  // every wave is done with q
+
+  // M = diag(beta) L, rows of this wave.
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    if (t > wave) continue;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = O::mma(kw[s], row(rowsK, t, s), acc);
+    const int j = 16 * t + li;
+    const double gj = pre[j];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = r0 + 4 * lg + e;
+      m[i * kLd + j] = keep_if(i > j, bi[e] * pow2(gi.x[e] - gj) * acc[e]);
     }
   }
   lds_barrier();
