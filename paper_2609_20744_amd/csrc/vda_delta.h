@@ -130,8 +130,9 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 // offset plus a constant: no address is computed in a loop.  Columns are
 // read across lanes' places (ds_read_b64_tr_b16, in which lane i of 16 receives
 // element i % 4 of the 8-byte pieces that lanes i / 4 + 4 e address; or four
-// words in fp32).  Places are permuted so that 16 lanes that read together, by
-// rows or by columns, meet 16 different places of the 256 bytes of all banks.
+// words in fp32).  Places are permuted (bf16: place_shift) so that the 16 lanes
+// whose 16 bytes are read together meet the 256 bytes of all banks; they are not
+// 16 in a row, but quads 0, 3, 5, 6 and 1, 2, 4, 7 of lanes of every 32.
 //
 // The 1 KB of a copy to LDS are consecutive places, so their order is also what
 // a copy reads from memory at a time: with a row's places 16 apart it was 16
@@ -148,12 +149,15 @@ typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 template <bool F32>
 __host__ __device__ constexpr int row_tile_bytes() { return F32 ? 2048 : 1024; }
 
+// 0, 2, 3, 1 of row / 4.
+__device__ __forceinline__ int place_shift(int row) { return ((row >> 1 ^ row >> 2) & 2) | row >> 3; }
+
 template <bool F32>
 __device__ __forceinline__ int tile_place(int row, int lg) {
-  return F32 ? (16 * lg + (row ^ lg)) * 16 : (4 * row + (lg ^ (row >> 2))) * 16;
+  return F32 ? (16 * lg + (row ^ lg)) * 16 : (4 * row + (lg ^ place_shift(row))) * 16;
 }
 // ... of a pair of tiles (bf16), lg < 8.
-__device__ __forceinline__ int pair_unit(int row, int lg) { return lg ^ ((row & 2) << 1 | row >> 2); }
+__device__ __forceinline__ int pair_unit(int row, int lg) { return lg ^ ((row & 2) << 1 | place_shift(row)); }
 __device__ __forceinline__ int pair_place(int row, int lg) { return (8 * row + pair_unit(row, lg)) * 16; }
 
 // 64 rows of 32 BLOCKS channels: where tile (block s, row tile t) is, and what
@@ -288,7 +292,7 @@ __device__ __forceinline__ void copy_tiles(__amdgpu_buffer_rsrc_t src, char* til
   constexpr bool kPairs = !TWISTED && RowTiles<F32, BLOCKS>::kPairs;
   constexpr int kHalves = F32 ? 2 : 1, kRow = row_tile_bytes<F32>();
   constexpr int kTiles = 4 * BLOCKS, kSteps = (kTiles + COPIERS - 1) / COPIERS;
-  const int row = F32 ? (lane & 15) ^ (lane >> 4) : lane >> 2, lg = F32 ? lane >> 4 : (lane & 3) ^ (row >> 2);
+  const int row = F32 ? (lane & 15) ^ (lane >> 4) : lane >> 2, lg = F32 ? lane >> 4 : (lane & 3) ^ place_shift(row);
   const uint32_t chan = (uint32_t)lg * (F32 ? 32u : 16u);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
