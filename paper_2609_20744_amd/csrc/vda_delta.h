@@ -484,7 +484,7 @@ struct ChunkInfo {
   int tok, len, seq;  // len 0: there is no such chunk
 };
 struct SegmentInfo {
-  int chunk, tok, len, seq;  // first chunk, first token, tokens; len < 0: there is no such segment
+  int id, chunk, tok, len, seq;  // first chunk, first token, tokens; len < 0: there is no such segment
   int ends;                  // bit 0: the sequence's first, bit 1: its last
 };
 
@@ -498,7 +498,7 @@ struct DeltaArgs {
   // Sequences: n of length L each (cu null), or by table.
   int n_seqs, L, seg_chunks, max_chunks, max_segs;
   const int4 *chunk_tab, *seg_tab;
-  const int* counts;  // chunks, segments (by table)
+  const int *counts, *seg_id;  // chunks, segments (by table); the table's segments' numbers in order
   const float *S_in, *dS_out;    // [n][Hv][d_v][d_k] or null
   float *S_out, *dS_in;
   void *out, *dq, *dk, *dv;
@@ -525,19 +525,20 @@ __device__ __forceinline__ ChunkInfo chunk_info(const DeltaArgs& a, int c) {
   return ChunkInfo{uniform(seq * a.L + at * kChunk), uniform(left < kChunk ? left : kChunk), seq};
 }
 
+// The s-th segment to scan.
 __device__ __forceinline__ SegmentInfo segment_info(const DeltaArgs& a, int s) {
   if (a.seg_tab != nullptr) {
-    if (s >= a.counts[1]) return SegmentInfo{0, 0, -1, 0, 0};
+    if (s >= a.counts[1]) return SegmentInfo{0, 0, 0, -1, 0, 0};
     const int4 t = a.seg_tab[s];
     const int w = uniform(t.w);
-    return SegmentInfo{uniform(t.x), uniform(t.y), uniform(t.z), w >> 2, w & 3};
+    return SegmentInfo{uniform(a.seg_id[s]), uniform(t.x), uniform(t.y), uniform(t.z), w >> 2, w & 3};
   }
   const int per = chunks_of(a.L);
   const int segs = (per + a.seg_chunks - 1) / a.seg_chunks;
   const int seq = uniform(s / segs), at = s - seq * segs;
-  if (seq >= a.n_seqs) return SegmentInfo{0, 0, -1, 0, 0};
+  if (seq >= a.n_seqs) return SegmentInfo{0, 0, 0, -1, 0, 0};
   const int from = at * a.seg_chunks * kChunk, left = a.L - from, most = a.seg_chunks * kChunk;
-  return SegmentInfo{uniform(seq * per + at * a.seg_chunks), uniform(seq * a.L + from),
+  return SegmentInfo{s, uniform(seq * per + at * a.seg_chunks), uniform(seq * a.L + from),
                      uniform(left < most ? left : most), seq,
                      uniform((at == 0 ? 1 : 0) | (at == segs - 1 ? 2 : 0))};
 }

@@ -82,7 +82,7 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   };
   const size_t mat = (size_t)p->d_v * p->d_k * 4, km = (size_t)p->d_k * p->d_k * 4;
   const size_t segs = (size_t)d.max_segs * p->H_v, chunks = (size_t)d.max_chunks * p->H_v;
-  d.tabs = take(table ? round_up((4 + 2 * (n + 1)) * 4, 16) + ((size_t)d.max_chunks + d.max_segs) * 16 : 0);
+  d.tabs = take(table ? round_up((4 + 2 * (n + 1)) * 4, 16) + ((size_t)d.max_chunks + d.max_segs) * 16 + (size_t)d.max_segs * 4 : 0);
   d.rec = take(chunks * vda::ChunkRecord::bytes(p->is_f32 != 0, backward));
   d.segs = take(d.split ? segs * (mat * (backward ? 2 : 1) + 2 * km) : 0);
   d.keep = take(backward ? chunks * 2 * (mat + (size_t)p->d_v * vda::kChunk * 4) : 0);
@@ -111,6 +111,7 @@ vda::DeltaArgs args_of(const vda_delta_problem* p, const vda::DeltaPlan& d, bool
     a.counts = tabs;
     a.chunk_tab = reinterpret_cast<int4*>(tabs + (4 + 2 * (p->n_seqs + 1) + 3) / 4 * 4);
     a.seg_tab = a.chunk_tab + d.max_chunks;
+    a.seg_id = reinterpret_cast<const int*>(a.seg_tab + d.max_segs);
   }
   a.rec = w + d.rec;
   const size_t mat = (size_t)p->d_v * p->d_k, km = (size_t)p->d_k * p->d_k;

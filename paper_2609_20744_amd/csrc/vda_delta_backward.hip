@@ -44,9 +44,9 @@ void delta_reverse_kernel(DeltaArgs a) {
   __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
 
   const int h = uniform(blockIdx.x % (unsigned)a.Hv);
-  const int seg = uniform(blockIdx.x / (unsigned)a.Hv);
-  const SegmentInfo si = segment_info(a, seg);
+  const SegmentInfo si = segment_info(a, uniform(blockIdx.x / (unsigned)a.Hv));
   if (si.len < 0) return;
+  const int seg = si.id;
   if (MAP && (si.ends & 1)) return;  // nothing takes the first segment's
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;

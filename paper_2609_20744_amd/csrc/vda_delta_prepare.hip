@@ -275,79 +275,116 @@ void delta_prepare_kernel(DeltaArgs a) {
 
 // Tables of the chunks and segments of sequences [cu[i], cu[i + 1]): tabs
 // holds counts[2] (and padding to 4), prefix sums of chunks and segments
-// [n + 1] each, then the int4 tables.  Offsets are clamped to [0, T] and the
-// tables to their sizes, and sums stop at kMost, above any table's size, so that
-// no malformed list can address anything else.
-constexpr int kPlanThreads = 1024, kMost = 0x3fffffff;
+// [n + 1] each, then the int4 tables and the segments' numbers.  Offsets are
+// clamped to [0, T] and the tables to their sizes, and sums stop at kMost,
+// above any table's size, so that no malformed list can address anything else.
+//
+// Segments are listed the longest first, by classes of 1/32 of the greatest
+// length (in any order within one: each is scanned by itself): the device then
+// ends with short ones.  9 uneven sequences of 16401 tokens with 16 heads,
+// backward: 910 us in the sequences' order, 887 us in this one.
+constexpr int kPlanThreads = 1024, kMost = 0x3fffffff, kClasses = 32;
 
 __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu, int n, int T, int seg_chunks,
                                                                  int max_chunks, int max_segs, int* tabs) {
-  __shared__ int sum[2][kPlanThreads];
+  __shared__ int pre[2][kPlanThreads], ends[2][kPlanThreads / 64], at_class[kClasses];
   int* counts = tabs;
   int* cpre = tabs + 4;
   int* spre = cpre + n + 1;
   int4* chunk_tab = reinterpret_cast<int4*>(tabs + (4 + 2 * (n + 1) + 3) / 4 * 4);
   int4* seg_tab = chunk_tab + max_chunks;
-  const int tid = threadIdx.x;
+  int* seg_id = reinterpret_cast<int*>(seg_tab + max_segs);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool small = n <= kPlanThreads;  // the prefixes are in LDS as well
   auto clamp = [&](int x) { return x < 0 ? 0 : x > T ? T : x; };
   auto add = [](int x, int y) { return x + y < kMost ? x + y : kMost; };
-  int cbase = 0, sbase = 0;
+  if (tid < kClasses) at_class[tid] = 0;
+  int base[2] = {0, 0};
   for (int at = 0; at < n; at += kPlanThreads) {
     const int i = at + tid;
-    int c = 0, s = 0;
+    int x[2] = {0, 0};  // chunks, segments
     if (i < n) {
       const int len = clamp(cu[i + 1]) - clamp(cu[i]);
-      c = len > 0 ? chunks_of(len) : 0;
-      s = c > seg_chunks ? (c + seg_chunks - 1) / seg_chunks : 1;
+      x[0] = len > 0 ? chunks_of(len) : 0;
+      x[1] = x[0] > seg_chunks ? (x[0] + seg_chunks - 1) / seg_chunks : 1;
     }
-    sum[0][tid] = c, sum[1][tid] = s;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x[w], d);
+        if (lane >= d) x[w] = add(x[w], y);
+      }
+      if (lane == 63) ends[w][wave] = x[w];
+    }
     __syncthreads();
-    for (int d = 1; d < kPlanThreads; d <<= 1) {
-      const int x = tid >= d ? sum[0][tid - d] : 0, y = tid >= d ? sum[1][tid - d] : 0;
-      __syncthreads();
-      sum[0][tid] = add(sum[0][tid], x), sum[1][tid] = add(sum[1][tid], y);
-      __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      int before = base[w];
+      for (int v = 0; v < kPlanThreads / 64; ++v) {
+        const int y = ends[w][v];
+        if (v < wave) before = add(before, y);
+        base[w] = add(base[w], y);
+      }
+      const int mine = __shfl_up(x[w], 1);
+      before = add(before, lane ? mine : 0);
+      if (i < n) (w ? spre : cpre)[i] = before;
+      if (small) pre[w][tid] = before;
     }
-    if (i < n) {
-      cpre[i] = add(cbase, tid ? sum[0][tid - 1] : 0);
-      spre[i] = add(sbase, tid ? sum[1][tid - 1] : 0);
-    }
-    cbase = add(cbase, sum[0][kPlanThreads - 1]), sbase = add(sbase, sum[1][kPlanThreads - 1]);
     __syncthreads();
   }
+  const int nc = base[0] < max_chunks ? base[0] : max_chunks, ns = base[1] < max_segs ? base[1] : max_segs;
   if (tid == 0) {
-    cpre[n] = cbase, spre[n] = sbase;
-    counts[0] = cbase < max_chunks ? cbase : max_chunks;
-    counts[1] = sbase < max_segs ? sbase : max_segs;
+    cpre[n] = base[0], spre[n] = base[1];
+    counts[0] = nc, counts[1] = ns;
   }
   __threadfence_block();
   __syncthreads();
+  auto prefix = [&](int w, int i) { return i == n ? base[w] : small ? pre[w][i] : (w ? spre : cpre)[i]; };
   // The sequence that entry x belongs to: the last whose prefix is <= x.
-  auto find = [&](const int* p, int x) {
+  auto find = [&](int w, int x) {
     int lo = 0, hi = n - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (p[mid] <= x) lo = mid; else hi = mid - 1;
+      if (prefix(w, mid) <= x) lo = mid; else hi = mid - 1;
     }
     return lo;
   };
-  const int nc = cbase < max_chunks ? cbase : max_chunks;
   for (int c = tid; c < nc; c += kPlanThreads) {
-    const int seq = find(cpre, c);
-    const int b = clamp(cu[seq]), len = clamp(cu[seq + 1]) - b, at = (c - cpre[seq]) * kChunk;
+    const int seq = find(0, c);
+    const int b = clamp(cu[seq]), len = clamp(cu[seq + 1]) - b, at = (c - prefix(0, seq)) * kChunk;
     chunk_tab[c] = make_int4(b + at, len - at < kChunk ? len - at : kChunk, seq, 0);
   }
-  const int ns = sbase < max_segs ? sbase : max_segs;
-  for (int s = tid; s < ns; s += kPlanThreads) {
-    const int seq = find(spre, s);
-    const int at = s - spre[seq], first = cpre[seq] + at * seg_chunks, from = at * seg_chunks * kChunk;
+  auto segment = [&](int s) {
+    const int seq = find(1, s);
+    const int at = s - prefix(1, seq), first = prefix(0, seq) + at * seg_chunks, from = at * seg_chunks * kChunk;
     const int b = clamp(cu[seq]);
     int len = clamp(cu[seq + 1]) - b - from;
     if (len > seg_chunks * kChunk) len = seg_chunks * kChunk;
     const int room = nc > first ? nc - first : 0;  // offsets that decrease: the table of chunks ends
     if (len > room * kChunk) len = room * kChunk;
-    const bool last = s + 1 >= spre[seq + 1];
-    seg_tab[s] = make_int4(first, b + from, len > 0 ? len : 0, seq << 2 | (at == 0 ? 1 : 0) | (last ? 2 : 0));
+    const bool last = s + 1 >= prefix(1, seq + 1);
+    return make_int4(first, b + from, len > 0 ? len : 0, seq << 2 | (at == 0 ? 1 : 0) | (last ? 2 : 0));
+  };
+  auto cls = [&](int len) { return kClasses - 1 - chunks_of(len) * kClasses / (seg_chunks + 1); };
+  int4 mine = make_int4(0, 0, 0, 0);
+  if (tid < ns) mine = segment(tid);
+  for (int s = tid; s < ns; s += kPlanThreads) atomicAdd(&at_class[cls(s == tid ? mine.z : segment(s).z)], 1);
+  __syncthreads();
+  if (wave == 0) {
+    int x = lane < kClasses ? at_class[lane] : 0;
+    const int count = x;
+    for (int d = 1; d < kClasses; d <<= 1) {
+      const int y = __shfl_up(x, d);
+      if (lane >= d) x += y;
+    }
+    if (lane < kClasses) at_class[lane] = x - count;
+  }
+  __syncthreads();
+  for (int s = tid; s < ns; s += kPlanThreads) {
+    const int4 e = s == tid ? mine : segment(s);
+    const int to = atomicAdd(&at_class[cls(e.z)], 1);
+    seg_tab[to] = e, seg_id[to] = s;
   }
 }
 

@@ -80,9 +80,9 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
 
   const int h = uniform(blockIdx.x % (unsigned)a.Hv);
-  const int seg = uniform(blockIdx.x / (unsigned)a.Hv);
-  const SegmentInfo si = segment_info(a, seg);
+  const SegmentInfo si = segment_info(a, uniform(blockIdx.x / (unsigned)a.Hv));
   if (si.len < 0) return;
+  const int seg = si.id;
   if (MODE == kMap && (si.ends & 2)) return;  // nothing follows the last segment's map
 
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
