@@ -329,6 +329,100 @@ def test_argument_errors(V):
 
 
 # ---------------------------------------------------------------------------------------------------------------------
+# Tables of many and uneven sequences; large tensors
+# ---------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_long_sequence_among_many(V, dtype):
+    """Sequences and heads that fill the device by themselves: the long one alone is cut into segments."""
+    lens = [int(x) for x in np.random.default_rng(3).integers(0, 40, 40)]
+    lens[17] = 64 * 40 + 3
+    c = Case(lens, Hk=4, group=2, dk=32, dv=32, dtype=dtype, layout="tokens", rough=True)
+    c.check_forward(*c.forward(V))
+    c.check_backward(c.backward(V))
+
+
+@pytest.mark.parametrize("n", [1024, 1100, 2050])
+def test_more_sequences_than_the_planning_threads(V, n):
+    lens = [int(x) for x in np.random.default_rng(n).integers(0, 4, n)]
+    lens[n - 20] = 64 * 17
+    c = Case(lens, Hk=1, dk=32, dv=32, layout="tokens")
+    c.check_forward(*c.forward(V))
+    c.check_backward(c.backward(V))
+
+
+def _guarded(t, value=7.0):
+    """A tensor like t within a buffer of `value`, and the buffer's parts outside it."""
+    import torch
+    pad = 4096
+    buf = torch.full((t.numel() + 2 * pad,), value, dtype=t.dtype, device="cuda")
+    return buf[pad:pad + t.numel()].view(t.shape), (buf[:pad], buf[pad + t.numel():])
+
+
+@pytest.mark.parametrize("offsets", [[0, 200, 100, 300], [300, 0, 300, 0, 300], [0, 300, 0, 300, 0, 300, 0, 300]])
+def test_decreasing_offsets_stay_inside(V, offsets):
+    """A malformed list: nothing outside the tensors and the workspace is written, and what only a first sequence
+    covers is right."""
+    import torch
+    c = Case(lens=[200, 100], Hk=2, dk=64, dv=64, state=False)
+    want = c.forward(V)
+    cu = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    d = c.dev
+    args = [d[x] for x in ("q", "k", "v", "g", "beta")]
+    out, guard = _guarded(d["v"])
+    need = [V.delta_workspace(*args, cu_seqlens=cu, backward=b) for b in (False, True)]
+    works = [_guarded(torch.empty(n, dtype=torch.uint8), 0x5a) for n in need]
+    V.delta_forward(*args, cu_seqlens=cu, scale=c.scale, out=out, work=works[0][0])
+    grads = [_guarded(t) for t in args]
+    dS, dS_guard = _guarded(torch.empty(len(offsets) - 1, 2, 64, 64))
+    V.delta_backward(d["do"], *args, cu_seqlens=cu, scale=c.scale, outs=[t for t, _ in grads] + [dS],
+                     work=works[1][0])
+    for parts in [guard, dS_guard] + [p for _, p in grads]:
+        assert all((p == 7).all() for p in parts)
+    assert all((p == 0x5a).all() for _, parts in works for p in parts)
+    if offsets[1] == 200:
+        assert torch.equal(out[:, :100], want[0][:, :100])
+
+
+def test_tensors_past_32_bits(V):
+    """The last sequence of tensors of more than 2^31 elements (heads layout), and of more than 2^31 bytes with a
+    workspace of tens of GiB in the backward pass (tokens layout)."""
+    import torch
+    T = (1 << 20) + 200
+    small = Case(lens=[200], Hk=1, dk=128, dv=128, seed=5)
+    for H, layout in ((16, "heads"), (8, "tokens")):
+        print(f"{H} heads of {T} tokens, {layout}", flush=True)
+        torch.cuda.empty_cache()
+        g = torch.Generator(device="cuda").manual_seed(2)
+        shape = (H, T) if layout == "heads" else (T, H)
+
+        def fill(d, last, scale):
+            x = torch.empty(*shape, *d, dtype=last.dtype, device="cuda").normal_(0, scale, generator=g)
+            part = x[:, -200:] if layout == "heads" else x[-200:].transpose(0, 1)
+            part.copy_(last.cuda().expand_as(part))
+            return x
+
+        h = small.host
+        q, k, v = fill((128,), h["q"], 128 ** -0.5), fill((128,), h["k"], 128 ** -0.5), fill((128,), h["v"], 1.0)
+        gate, beta = fill((), h["g"], 0.0).add_(0), fill((), h["beta"], 0.0)
+        cu = torch.tensor([0, T - 200, T], dtype=torch.int32, device="cuda")
+        kw = dict(cu_seqlens=cu, layout=layout, scale=small.scale)
+        tail = lambda x: (x[-1:, -200:] if layout == "heads" else x[-200:, -1:].transpose(0, 1))  # noqa: E731
+        S = torch.stack([torch.zeros(H, 128, 128), small.S[0].expand(H, 128, 128)]).cuda()
+        if layout == "heads":
+            out, last = V.delta_forward(q, k, v, gate, beta, state=S, return_state=True, **kw)
+            small.check_forward(tail(out).contiguous(), last[1:, -1:])
+        else:
+            dS = torch.stack([torch.zeros(H, 128, 128), small.dS[0].expand(H, 128, 128)]).cuda()
+            do = fill((128,), h["do"], 1.0)
+            grads = V.delta_backward(do, q, k, v, gate, beta, state=S, dstate=dS, **kw)
+            small.check_backward([tail(x).contiguous() for x in grads[:5]] + [grads[5][1:, -1:]])
+            del do, grads
+        del q, k, v, gate, beta, S
+    torch.cuda.empty_cache()
+
+
+# ---------------------------------------------------------------------------------------------------------------------
 # The recurrent form
 # ---------------------------------------------------------------------------------------------------------------------
 
@@ -401,6 +495,20 @@ def test_step_without_slots_and_errors(V):
                dict(out=torch.empty(2, 1, 1, 31, device="cuda"))):
         with pytest.raises(ValueError):
             V.delta_step(q, k, v, g, beta, **{"state": state, **kw})
+
+
+def test_step_far_into_the_pool(V):
+    """A slot whose state begins past 2^32 bytes."""
+    import torch
+    q, k, v, g, beta = (x.cuda() for x in _step_case(2, 1, 8, 2, 128, 128, "bf16"))
+    per = 16 * 128 * 128
+    n = (1 << 30) // per + 9
+    pool = torch.zeros(n, 16, 128, 128, device="cuda")
+    near = torch.randn(2, 16, 128, 128, device="cuda")
+    pool[-1], pool[3] = near[0], near[1]
+    out = V.delta_step(q, k, v, g, beta, pool, slots=torch.tensor([n - 1, 3], dtype=torch.int32, device="cuda"))
+    want = V.delta_step(q, k, v, g, beta, near)
+    assert torch.equal(out, want) and torch.equal(pool[-1], near[0]) and torch.equal(pool[3], near[1])
 
 
 def test_step_in_a_graph(V):

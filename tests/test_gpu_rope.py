@@ -119,6 +119,23 @@ def test_slices_of_a_fused_projection(V):
         V.rope(fused[:, :4, :H * d], f, (4, 6, 6), H, grid=(3, 3))
 
 
+def test_tensors_past_32_bits(V):
+    """The last tokens of more than 2^31 elements, as by themselves."""
+    import torch
+    H, d, L = 16, 128, (1 << 20) + 70
+    x = torch.empty(1, L, H * d, dtype=torch.bfloat16, device="cuda").normal_(0, 1)
+    f = torch.rand(64, device="cuda")
+    last = x[:, -70:].contiguous()
+    kw = dict(l2=True, layout="heads")
+    pos = torch.arange(L, dtype=torch.int32, device="cuda")[None, :, None].expand(1, L, 3).contiguous()
+    y = V.rope(x, f, (16, 24, 24), H, positions=pos, **kw)
+    want = V.rope(last, f, (16, 24, 24), H, positions=pos[:, -70:].contiguous(), **kw)
+    assert torch.equal(y[:, -70:], want)
+    dx = V.rope_backward(y, f, (16, 24, 24), H, x=x, positions=pos, **kw)
+    dlast = V.rope_backward(want, f, (16, 24, 24), H, x=last, positions=pos[:, -70:].contiguous(), **kw)
+    assert torch.equal(dx[:, -70:], dlast)
+
+
 def test_other_stream_and_graph(V):
     import torch
     x = torch.randn(1, 77, 4 * 64, device="cuda").bfloat16()
