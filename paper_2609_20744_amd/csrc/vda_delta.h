@@ -18,6 +18,7 @@
 namespace vda {
 
 constexpr int kChunk = 64;  // tokens of a chunk
+constexpr int kLds = 160 * 1024;  // bytes of LDS of a workgroup
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));

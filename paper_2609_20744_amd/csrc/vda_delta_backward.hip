@@ -35,10 +35,10 @@ void delta_reverse_kernel(DeltaArgs a) {
   typedef typename O::X X;
   typedef typename O::W W;
   constexpr int ES = F32 ? 4 : 2, KS = DK / 32, kWaves = DV / 16;
-  constexpr int kBufs = F32 ? 1 : 2;
   constexpr int kTileK = kChunk * DK * ES;
   constexpr int kOffQ = kTileK, kOffVec = 2 * kTileK, kOffTt = kOffVec + 1024, kOffPt = kOffTt + kWideTri,
                 kOffDo = kOffPt + kWideTri, kStage = kOffDo + kChunk * DV * ES;
+  constexpr int kBufs = 2 * kStage <= kLds ? 2 : 1;  // (two stages of 128 fp32 channels do not fit)
   static_assert(ChunkRecord::kTt == ChunkRecord::kVec + 1024 && ChunkRecord::kPt == ChunkRecord::kTt + kWideTri,
                 "copied together");
   __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
@@ -88,6 +88,7 @@ void delta_reverse_kernel(DeltaArgs a) {
     copy_tiles<F32, DV / 32, kWaves>(make_rsrc(op, 64u * v_row), buf + kOffDo, len, v_row, wave, lane);
     copy_tiles<F32, KS, kWaves>(make_rsrc(qp, 64u * k_row), buf + kOffQ, len, k_row, wave, lane);
     kp -= 64u * k_row, qp -= 64u * k_row, op -= 64u * v_row, rp -= rec_size * a.Hv;
+    __builtin_amdgcn_sched_barrier(0);  // the step's stores stay behind the copies (copy_barrier)
   };
 
   const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -214,7 +215,7 @@ void delta_reverse_kernel(DeltaArgs a) {
   int at = chunks - 1;
   if constexpr (kBufs == 2) {
     if (at >= 0) stage(at, buf0);
-    constexpr int kStores = MAP ? 0 : 2 * KS + 8;  // of a step
+    constexpr int kStores = MAP ? 0 : 2 * KS + (F32 ? 4 : 8);  // of a step
     for (; at >= 0; at -= 2) {
       if (at == chunks - 1)
         copy_barrier();

@@ -68,13 +68,13 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   typedef ScanShape<DK, DV, MODE> Shape;
   constexpr int NV = Shape::kNV, kCopiers = Shape::kCopiers;
   constexpr int ES = F32 ? 4 : 2, KS = DK / 32;
-  constexpr int kBufs = F32 ? 1 : 2;  // (two stages of fp32 do not fit)
   constexpr int kTileK = kChunk * DK * ES, kTileV = kChunk * DV * ES;
   // Stage: k rows, the chunk's record (T; gam, eta and beta; outputs: P), v
   // rows, then (outputs) q rows.
   constexpr int kRecord = ChunkRecord::kP + (MODE == kOutput ? ChunkRecord::kPBytes[F32] : 0);
   constexpr int kOffT = kTileK, kOffVec = kOffT + ChunkRecord::kVec, kOffP = kOffT + ChunkRecord::kP,
                 kOffV = kOffT + kRecord, kOffQ = kOffV + kTileV, kStage = kOffQ + (MODE == kOutput ? kTileK : 0);
+  constexpr int kBufs = 2 * kStage <= kLds ? 2 : 1;  // (two stages of 128 fp32 channels do not fit)
   // Two arrays, each named where it is used: with one indexed by the step the
   // compiler takes any read for one of what is still being copied, and waits.
   __shared__ __align__(16) char buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
@@ -144,6 +144,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
     }
     kp += 64u * k_row, vp += 64u * v_row, rp += rec_size * a.Hv;
     if constexpr (MODE == kOutput) qp += 64u * k_row;
+    __builtin_amdgcn_sched_barrier(0);  // the step's stores stay behind the copies (copy_barrier)
   };
 
   const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -332,7 +333,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   if constexpr (kBufs == 2) {
     if (chunks > 0) stage(0, buf0);
     // Stores of a step, all of them of every wave.
-    constexpr int kStores = MODE == kOutput ? 4 : MODE == kKeep ? 2 * KS + 8 : 0;
+    constexpr int kStores = MODE == kOutput ? 4 : MODE == kKeep ? 2 * KS + (F32 ? 4 : 8) : 0;
     for (int c = 0; c < chunks; c += 2) {
       if (c == 0)
         copy_barrier();
