@@ -544,10 +544,11 @@ typedef enum {
  *    H_k = B * heads, n_seqs = 1, T = L.
  *  - storage of q, k, v, out and their gradients: bf16 (is_f32 == 0) or fp32.
  *    g (log decay, <= 0; -inf resets the state; positive values are not
- *    checked, and grow it) and beta (write strength, any sign; the rule is stable for
- *    beta |k|^2 in [0, 2]) are fp32.
+ *    checked, and grow it) and beta (write strength, any sign, below 2^-48 in
+ *    magnitude taken as that; the rule is stable for beta |k|^2 in [0, 2]) are
+ *    fp32.
  * A NaN or infinity in a token's q, k, v, g or beta (but g = -inf) makes the
- * outputs of its aligned group of 64 tokens of its sequence and head undefined,
+ * outputs of its group of 64 tokens (counted from the sequence's first) of its head undefined,
  * and those of all later ones; other sequences and heads are not touched.
  * bf16 storage: products run on bf16 matrix cores with fp32 accumulation;
  * the state, what is written to it and the triangular inverses are carried as
@@ -602,8 +603,8 @@ size_t vda_delta_forward_workspace(const vda_delta_problem* p);
  *    NULL.  dg is the gradient of the log decay; where g < -200 (a decay of
  *    zero in fp32) it is 0.
  *  - work: vda_delta_backward_workspace(p) bytes, as above: mostly the states
- *    at every 64th token and their gradients, 16 d_k d_v bytes per 64 tokens
- *    of a head.
+ *    at every 64th token, what the tokens write, and the gradients of both,
+ *    8 d_v (d_k + 64) bytes per 64 tokens of a head.
  * Deterministic; otherwise as vda_delta_forward.
  */
 int vda_delta_backward(const vda_delta_problem* p, const void* dout, const void* q, const void* k,

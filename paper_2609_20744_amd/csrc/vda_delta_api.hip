@@ -61,11 +61,11 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   // Segments.  A sequence that is cut costs each of its chunks a second scan
   // (the segment's map) and a step of the join per segment.  Where sequences
   // and heads alone fill the compute units, only one that is far longer than
-  // the rest is cut: 24 uneven sequences of 16411 tokens with 16 heads take
+  // the rest is cut: 24 uneven sequences of 16411 tokens with 16 heads took
   // 233 us whole and 296 us cut into segments of 18 chunks.  Where they do not,
-  // every unit gets a segment: 9 such sequences take 1.08 ms forward and
-  // backward cut and 1.43 ms whole, one of 1560 tokens with 24 heads 88 and
-  // 116 us.  A segment has at least four chunks and a sequence more than four
+  // every unit gets a segment: the backward pass of 9 such sequences took 1.08 ms
+  // cut and 1.43 ms whole, one sequence of 1560 tokens with 24 heads takes 71 us
+  // cut and 97 whole.  A segment has at least four chunks and a sequence more than four
   // segments, or the join outweighs what running side by side saves.
   const long long cus = vda::current_device_cus();
   long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);

@@ -27,7 +27,9 @@ namespace {
 // The reverse scan, laid out as the forward scan (vda_delta_scan.hip): a wave
 // owns 16 value columns of dS, transposed, in registers.  MAP: only what a
 // segment adds to the gradient that enters it (its map's matrix is the
-// forward one's transpose).
+// forward one's transpose).  Bound by memory where its workgroups fill the
+// device: 135 us for 16401 tokens of 16 heads, 128 x 128, 5.4 TB/s; the map
+// 100 us.
 template <bool F32, int DK, int DV, bool MAP>
 __global__ __launch_bounds__(4 * DV) __attribute__((amdgpu_waves_per_eu(1, 2)))
 void delta_reverse_kernel(DeltaArgs a) {
@@ -263,6 +265,11 @@ void delta_reverse_kernel(DeltaArgs a) {
 // and in step they would load the memory's channels one after another.  Tokens
 // and key channels are taken in twisted order, value channels in paired order
 // (vda_delta.h).
+//
+// 309 us for 16401 tokens of 16 heads, 128 x 128, bf16: the copies alone take
+// 267 us (3.6 TB/s: with 142 KB of LDS one workgroup runs on a compute unit, one
+// step's 52 KB on the way); the heads' ends, short chains of reads, sums over
+// lanes and barriers, hide least of theirs.
 template <bool F32, int DK, int DV>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void delta_grad_kernel(DeltaArgs a) {
   typedef Op<F32> O;
@@ -435,10 +442,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   // The end of a head; `swap` is LDS that nothing else uses now.
   auto finish = [&](int h, const Gates& g, char* swap) {
     if (wave == 0) pre[lane] = g.pre;
+    // (Opaque: the comparisons below, kept from head to head, would take 100
+    // scalar registers, and the kernel 343 us instead of 309, of spilled ones.)
+    int jj = j, ll = lane;
+    asm volatile("" : "+v"(jj), "+v"(ll));
     lds_barrier();
     // Decays between tokens: columns j of this lane.  What passes from j to
     // i > j (A): its sums over i, for token j, and over j, for tokens i.
-    const double gj = pre[j];
+    const double gj = pre[jj];
     floatx4 Xs[2];
     float below = 0.f;
 #pragma unroll
@@ -454,13 +465,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       floatx4 A = zero;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = twisted_row(t, 4 * lg + e);
+        const int i = twisted_row(t, 4 * (ll >> 4) + e);
         const double apart = pre[i] - gj;
-        const float d = pow2(i >= j ? apart : -apart);
-        Wt[u][e] = i <= j ? a.scale * d * Wt[u][e] : 0.f;
-        Wn[u][e] = i >= j && i < len ? a.scale * d * Wn[u][e] : 0.f;
-        Xs[u][e] = i > j ? -d * Xa[u][e] : i < j ? -d * Xb[u][e] : 0.f;
-        A[e] = i > j && i < len ? Wn[u][e] * qk[e] + Xs[u][e] * kk[e] : 0.f;
+        const float d = pow2(i >= jj ? apart : -apart);
+        Wt[u][e] = i <= jj ? a.scale * d * Wt[u][e] : 0.f;
+        Wn[u][e] = i >= jj && i < len ? a.scale * d * Wn[u][e] : 0.f;
+        Xs[u][e] = i > jj ? -d * Xa[u][e] : i < jj ? -d * Xb[u][e] : 0.f;
+        A[e] = i > jj && i < len ? Wn[u][e] * qk[e] + Xs[u][e] * kk[e] : 0.f;
         below += A[e];
         A[e] = group_sum<16>(A[e]);
       }
@@ -504,7 +515,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     // Diagonals: this lane's token's N.dv, and its share of <dS, S>.
     float db = 0.f, ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) db += li == 4 * lg + e ? ND[e] : 0.f, ss += li == 4 * lg + e ? SS[e] : 0.f;
+    for (int e = 0; e < 4; ++e) db += (ll & 15) == 4 * (ll >> 4) + e ? ND[e] : 0.f, ss += (ll & 15) == 4 * (ll >> 4) + e ? SS[e] : 0.f;
     // Sums over the lanes of a token (lg), over the channels' halves, then over the chunk.
     float past = below + g.eta * end;
     in += __shfl_xor(in, 16), in += __shfl_xor(in, 32);
@@ -528,8 +539,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const float down = __shfl_down(x, d), up = __shfl_up(y, d);
-        if (lane + d < 64) x += down;
-        if (lane >= d) y += up;
+        if (ll + d < 64) x += down;
+        if (ll >= d) y += up;
       }
       x += y - pass + g.ends * (states[0] + states[4]);  // (all waves of a half have the same sum)
       if (lane < len) {

@@ -2,16 +2,27 @@
 // (vda_delta.h), with the outputs, with what the gradient kernel reads, or as
 // the affine maps of segments; and the join of those maps.
 //
-// One workgroup per segment and value head; a wave owns 32 value columns of
-// the state, transposed (key channels x value columns), in registers, and
-// nothing passes between waves: each product leaves its result with the rows
-// that the next one contracts,
+// One workgroup per segment and value head; a wave owns 16 value columns of
+// the state (32 in the maps), transposed (key channels x value columns), in
+// registers, and nothing passes between waves: each product leaves its result
+// with the rows that the next one contracts,
 //     Z = K S^T -> X = beta (V - gam Z) -> N = T X -> S^T <- gam_63 S^T + K^T (eta N),
 // so a step is three dependent products with no exchange through LDS.  The
 // matrices that all waves share (k, q and v rows, T, P) come through LDS, the
 // next chunk's copied by loads straight to LDS while this one's are used, one
 // barrier a chunk.  O^T = S Q^T + N^T P^T takes the same registers as left
 // operands, so a lane ends with eight consecutive channels of a token's output.
+//
+// Two waves a SIMD with 16 columns each, rather than one with 32, hide each
+// other's waits (with the rows as operand tiles in LDS and copies that no store
+// is waited for with, 40320 tokens of 7 heads went from 455 to 362 us).  What
+// bounds it, bf16, 128 x 128: where a workgroup runs alone the chain of a chunk,
+// 3.4 us (matrix cores, LDS and vector ALUs are busy a third of it each); with
+// one on every compute unit memory, 83 KB a chunk: 88 us for the outputs of
+// those 40320 tokens, 4.2 TB/s, and 108 us for what the gradient kernel reads
+// (16401 tokens, 16 heads), 5.7 TB/s.  The maps' 5.9 us a chunk are products and
+// vector operations, twice those of a scan.  Outputs that went through LDS to
+// be stored in whole lines were 2% slower than eight bytes a lane.
 //
 // The chain of a chunk bounds a scan whose workgroups do not fill the device:
 // long sequences of few heads are cut into segments.  A segment's map
@@ -392,7 +403,8 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
 // workgroup of four waves per sequence, head and 16 rows; a wave makes d_k / 4
 // columns of the product (transposed, the matrix as left operand), which the
 // others get through LDS (two waves at d_k 32).  The matrices are read two
-// segments ahead.
+// segments ahead, a KB of operands at a time (as rows, 16 bytes of 16 rows at a
+// time, a step took 2.1 us; now 1.1 us at d_k 128, of loads and their latency).
 template <bool F32, int DK>
 __global__ __launch_bounds__(kThreads) void delta_join_kernel(DeltaArgs a, bool reverse) {
   typedef Op<F32> O;
