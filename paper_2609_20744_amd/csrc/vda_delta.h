@@ -198,6 +198,20 @@ __device__ __forceinline__ TileLane tile_lane(int li, int lg) {
   return l;
 }
 
+// The column offsets of half o of block s, both runtime, from the tiles' begin
+// (read with o 0 and odd 0): an address that is one addition to a named array.
+// Of a longer chain the compiler does not see which array it is in, and waits
+// for all copies into LDS before the read (the reverse scan's map took 100 us
+// so, and takes 87: 16401 tokens, 16 heads).
+template <bool F32, int BLOCKS>
+__device__ __forceinline__ TileLane tile_block(const TileLane& l, int s, int o) {
+  typedef RowTiles<F32, BLOCKS> Rows;
+  TileLane b = l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) b.col[e] = (l.col[e] ^ Rows::odd(s)) + Rows::tile(s, 0) + o * (F32 ? 1024 : 8);
+  return b;
+}
+
 template <bool F32>
 __device__ __forceinline__ typename Op<F32>::X tile_row(const char* tile, int odd, const TileLane& l) {
   if constexpr (F32) {

@@ -29,7 +29,7 @@ namespace {
 // segment adds to the gradient that enters it (its map's matrix is the
 // forward one's transpose).  Bound by memory where its workgroups fill the
 // device: 135 us for 16401 tokens of 16 heads, 128 x 128, 5.4 TB/s; the map
-// 100 us.
+// 87 us.
 template <bool F32, int DK, int DV, bool MAP>
 __global__ __launch_bounds__(4 * DV) __attribute__((amdgpu_waves_per_eu(1, 2)))
 void delta_reverse_kernel(DeltaArgs a) {
@@ -60,7 +60,8 @@ void delta_reverse_kernel(DeltaArgs a) {
   const size_t rec_size = ChunkRecord::bytes(F32, true);
   typedef RowTiles<F32, KS> RowsK;
   typedef RowTiles<F32, DV / 32> RowsV;
-  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg), vl = tile_lane<F32, RowsV::kPairs>(li, lg);
+  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg);
+  const TileLane vl = tile_block<F32, DV / 32>(tile_lane<F32, RowsV::kPairs>(li, lg), vb, n0);
 
   const float* init = nullptr;
   if (si.ends & 2)
@@ -110,8 +111,7 @@ void delta_reverse_kernel(DeltaArgs a) {
     for (int t = 0; t < 4; ++t) ev[t] = *reinterpret_cast<const floatx4*>(eta + 16 * t);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
-      dO[t] = tile_cols<F32>(buf + kOffDo + RowsV::tile(vb, 2 * t), buf + kOffDo + RowsV::tile(vb, 2 * t + 1), n0,
-                             RowsV::odd(vb), vl);
+      dO[t] = tile_cols<F32>(buf + kOffDo + RowsV::tile(0, 2 * t), buf + kOffDo + RowsV::tile(0, 2 * t + 1), 0, 0, vl);
     fence<F32>();
 
     // dN = diag(eta) K dS^T + P^T dO.
@@ -327,12 +327,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                                  dvr = make_rsrc(a.keepdv + at * nmat * 4, kPlanes * kNmat);
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
-      const uint32_t so = p * kMat + s * kTileS, no = p * kNmat + s * kTileN;
+      const uint32_t so = p * kMat + s * kTileS;
       copy_flat<kTileS, 8>(sr, buf + p * kTileS, wave, lane, so);
       copy_flat<kTileS, 8>(dsr, buf + kOffdS + p * kTileS, wave, lane, so);
-      copy_flat<kTileN, 8>(nr, buf + kOffN + p * kTileN, wave, lane, no);
-      copy_flat<kTileN, 8>(dvr, buf + kOffdv + p * kTileN, wave, lane, no);
     }
+    // N and dv: the planes together are a piece for each wave.
+    constexpr int kPieces = kTileN / 1024;
+    static_assert(kPlanes * kPieces == 8, "a piece a wave");
+    const uint32_t no = wave / kPieces * kNmat + s * kTileN + wave % kPieces * 1024;
+    copy_flat<1024, 1>(nr, buf + kOffN + wave * 1024, 0, lane, no);
+    copy_flat<1024, 1>(dvr, buf + kOffdv + wave * 1024, 0, lane, no);
     copy_tiles<F32, 1, 8, true>(
         make_rsrc((const char*)a.dout + vo + (n / steps) * a.v_head * ES, 64u * v_row), buf + kOffO, len, v_row, wave,
         lane, 32 * s * ES);

@@ -18,8 +18,8 @@
 // is waited for with, 40320 tokens of 7 heads went from 455 to 362 us).  What
 // bounds it, bf16, 128 x 128: where a workgroup runs alone the chain of a chunk,
 // 3.4 us (matrix cores, LDS and vector ALUs are busy a third of it each); with
-// one on every compute unit memory, 83 KB a chunk: 88 us for the outputs of
-// those 40320 tokens, 4.2 TB/s, and 108 us for what the gradient kernel reads
+// one on every compute unit memory, 83 KB a chunk: 86 us for the outputs of
+// those 40320 tokens, 4.3 TB/s, and 108 us for what the gradient kernel reads
 // (16401 tokens, 16 heads), 5.7 TB/s.  The maps' 5.9 us a chunk are products and
 // vector operations, twice those of a scan.  Outputs that went through LDS to
 // be stored in whole lines were 2% slower than eight bytes a lane.
@@ -109,7 +109,8 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
   const size_t rec_size = ChunkRecord::bytes(F32, MODE == kKeep || (MODE == kMap && a.dout != nullptr));
   typedef RowTiles<F32, KS> RowsK;
   typedef RowTiles<F32, DV / 32> RowsV;
-  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg), vl = tile_lane<F32, RowsV::kPairs>(li, lg);
+  const TileLane tl = tile_lane<F32, RowsK::kPairs>(li, lg);
+  const TileLane vl = tile_block<F32, DV / 32>(tile_lane<F32, RowsV::kPairs>(li, lg), vb, n0);
   const int col = 32 * vb + 8 * (li >> 2) + 4 * n0 + (li & 3);  // + 4 n: this lane's columns
 
   // The entering state: S[s][o][n] holds channels 32 s + 8 lg + 4 o + r of column col + 4 n.
@@ -191,7 +192,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) {
           vv[t][n] = zero;
-          if (!matrix) vv[t][n] = tile_values<F32>(buf + kOffV + RowsV::tile(vb, t), n0 + n, RowsV::odd(vb), vl);
+          if (!matrix) vv[t][n] = tile_values<F32>(buf + kOffV + RowsV::tile(0, t), n, 0, vl);
         }
       }
     };

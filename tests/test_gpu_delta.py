@@ -359,6 +359,29 @@ def _guarded(t, value=7.0):
     return buf[pad:pad + t.numel()].view(t.shape), (buf[:pad], buf[pad + t.numel():])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", [dict(lens=[64 * 18], Hk=1, group=2, dk=128, dv=128),
+                                  dict(lens=[64 * 18 + 1, 0, 100], Hk=1, group=3, dk=32, dv=64, layout="tokens"),
+                                  dict(lens=[300, 70], Hk=4, dk=64, dv=128)], ids=["cut_128", "cut_32x64", "whole"])
+def test_nothing_else_is_written(V, case, dtype):
+    """Outputs and workspace within guarded buffers, inputs as they were."""
+    import torch
+    c = Case(dtype=dtype, **case)
+    d = c.dev
+    args = [d[x] for x in ("q", "k", "v", "g", "beta")]
+    inputs = args + [d["do"], c.cu_dev] + c.states
+    before = [t.clone() for t in inputs]
+    works = [_guarded(torch.empty(V.delta_workspace(*args, cu_seqlens=c.cu_dev, layout=c.layout, backward=b),
+                                  dtype=torch.uint8), 0x5a) for b in (False, True)]
+    out, S = _guarded(d["v"]), _guarded(c.states[0])
+    grads = [_guarded(t) for t in args + [c.states[0]]]
+    c.check_forward(*c.forward(V, out=out[0], state_out=S[0], work=works[0][0]))
+    c.check_backward(c.backward(V, outs=[t for t, _ in grads], work=works[1][0]))
+    assert all((p == 7).all() for _, parts in grads + [out, S] for p in parts)
+    assert all((p == 0x5a).all() for _, parts in works for p in parts)
+    assert all(torch.equal(x, y) for x, y in zip(inputs, before))
+
+
 @pytest.mark.parametrize("offsets", [[0, 200, 100, 300], [300, 0, 300, 0, 300], [0, 300, 0, 300, 0, 300, 0, 300]])
 def test_decreasing_offsets_stay_inside(V, offsets):
     """A malformed list: nothing outside the tensors and the workspace is written, and what only a first sequence
