@@ -45,7 +45,8 @@ int check_problem(const vda_delta_problem* p) {
                             : es * std::max(p->d_k, p->d_v);
   if (row >= 1 << 24) return VDA_ERR_SIZE;
   const long long items = ((long long)p->T / vda::kChunk + p->n_seqs + 1) * p->H_v;
-  if (items * 1024 > kMaxThreads || (long long)p->n_seqs * p->H_v * (p->d_v / 16) * 256 > kMaxThreads ||
+  const long long joined = ((long long)p->n_seqs * p->H_v + 7) / 8 * 8 * (p->d_v / 16);
+  if (items * 1024 > kMaxThreads || joined * 256 > kMaxThreads ||
       (long long)p->T + vda::kChunk > 0x7fffffffLL)
     return VDA_ERR_SIZE;
   return VDA_OK;
@@ -72,7 +73,8 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   if (n * p->H_v >= cus) share = std::max(share, 4 * ((d.max_chunks + n - 1) / n));
   d.split = longest > 4 * share;
   d.seg_chunks = (int)(d.split ? share : std::max(longest, 1LL));
-  d.max_segs = (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));
+  d.max_segs =
+      (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));
   // Workspace.
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -82,7 +84,8 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   };
   const size_t mat = (size_t)p->d_v * p->d_k * 4, km = (size_t)p->d_k * p->d_k * 4;
   const size_t segs = (size_t)d.max_segs * p->H_v, chunks = (size_t)d.max_chunks * p->H_v;
-  d.tabs = take(table ? round_up((4 + 2 * (n + 1)) * 4, 16) + ((size_t)d.max_chunks + d.max_segs) * 16 + (size_t)d.max_segs * 4 : 0);
+  const size_t entries = (size_t)d.max_chunks * 16 + (size_t)d.max_segs * (16 + 4);
+  d.tabs = take(table ? round_up((4 + 2 * (n + 1)) * 4, 16) + entries : 0);
   d.rec = take(chunks * vda::ChunkRecord::bytes(p->is_f32 != 0, backward));
   d.segs = take(d.split ? segs * (mat * (backward ? 2 : 1) + 2 * km) : 0);
   d.keep = take(backward ? chunks * 2 * (mat + (size_t)p->d_v * vda::kChunk * 4) : 0);

@@ -161,7 +161,8 @@ void delta_reverse_kernel(DeltaArgs a) {
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          ct[s][t] = tile_cols<F32>(tiles + RowsK::tile(s, 2 * t), tiles + RowsK::tile(s, 2 * t + 1), u, RowsK::odd(s), tl);
+          ct[s][t] = tile_cols<F32>(tiles + RowsK::tile(s, 2 * t), tiles + RowsK::tile(s, 2 * t + 1), u,
+                                    RowsK::odd(s), tl);
     };
     columns(buf + kOffQ, 0);
     fence<F32>();
@@ -519,7 +520,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     // Diagonals: this lane's token's N.dv, and its share of <dS, S>.
     float db = 0.f, ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) db += (ll & 15) == 4 * (ll >> 4) + e ? ND[e] : 0.f, ss += (ll & 15) == 4 * (ll >> 4) + e ? SS[e] : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      const bool diagonal = (ll & 15) == 4 * (ll >> 4) + e;
+      db += diagonal ? ND[e] : 0.f, ss += diagonal ? SS[e] : 0.f;
+    }
     // Sums over the lanes of a token (lg), over the channels' halves, then over the chunk.
     float past = below + g.eta * end;
     in += __shfl_xor(in, 16), in += __shfl_xor(in, 32);
