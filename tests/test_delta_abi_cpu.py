@@ -140,3 +140,13 @@ def test_binding_refuses_cpu_tensors():
     with pytest.raises(ValueError):
         vda.delta_step(*(torch.zeros(1, 1, 1, 32),) * 3, torch.zeros(1, 1, 1), torch.zeros(1, 1, 1),
                        torch.zeros(1, 1, 32, 32))
+
+
+def test_most_sequences():
+    """The join has a workgroup for 16 rows of every state, of a count that is rounded up to eight: below 2^32 threads."""
+    need = lambda **kw: vda.lib.vda_delta_forward_workspace(  # noqa: E731
+        ctypes.byref(_problem(T=64, cu_seqlens=BIG, H_k=1, H_v=1, **kw)))
+    assert need(n_seqs=(1 << 21) - 8, d_v=128) > 0
+    assert need(n_seqs=(1 << 21) - 1, d_v=128) == 0
+    assert need(n_seqs=(1 << 21) - 1, d_v=64) > 0
+    assert need(n_seqs=1 << 22, d_v=32) == 0
