@@ -18,6 +18,7 @@
 namespace vda {
 
 constexpr int kChunk = 64;  // tokens of a chunk
+constexpr int kWholeChunks = 8;  // a sequence of so many chunks is not cut into segments
 constexpr int kLds = 160 * 1024;  // bytes of LDS of a workgroup
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));

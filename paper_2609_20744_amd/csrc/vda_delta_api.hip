@@ -65,13 +65,19 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   // the rest is cut: 24 uneven sequences of 16411 tokens with 16 heads took
   // 233 us whole and 296 us cut into segments of 18 chunks.  Where they do not,
   // every unit gets a segment: the backward pass of 9 such sequences took 1.08 ms
-  // cut and 1.43 ms whole, one sequence of 1560 tokens with 24 heads takes 71 us
-  // cut and 97 whole.  A segment has at least four chunks and a sequence more than four
-  // segments, or the join outweighs what running side by side saves.
+  // cut and 1.43 ms whole, one sequence of 1560 tokens with 24 heads takes 64 us
+  // cut and 97 whole.  Shorter segments make the scans shorter (11 us a chunk
+  // for maps and outputs, 128 x 128, bf16) and the join longer (1.2 us a
+  // segment): the least time is at about the square root of an eighth of the
+  // sequence's chunks.  8 heads, segments of 4 chunks and so: 1088 tokens 55 and
+  // 44 us; 2 heads of 38400 tokens, segments of 5 chunks and so: 199 and 171 us.
+  // Of nine chunks (8 heads) the forward pass takes 38 us whole and cut, the
+  // backward pass 92 and 86; shorter sequences stay whole.
   const long long cus = vda::current_device_cus();
-  long long share = std::max(4LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
+  long long share = std::max(2LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
+  while (8 * share * share < longest) ++share;
   if (n * p->H_v >= cus) share = std::max(share, 4 * ((d.max_chunks + n - 1) / n));
-  d.split = longest > 4 * share;
+  d.split = longest > std::max<long long>(vda::kWholeChunks, 4 * share);
   d.seg_chunks = (int)(d.split ? share : std::max(longest, 1LL));
   d.max_segs =
       (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));

@@ -296,6 +296,7 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
   int4* seg_tab = chunk_tab + max_chunks;
   int* seg_id = reinterpret_cast<int*>(seg_tab + max_segs);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int whole = seg_chunks > kWholeChunks ? seg_chunks : kWholeChunks;  // the most chunks of one segment
   const bool small = n <= kPlanThreads;  // the prefixes are in LDS as well
   auto clamp = [&](int x) { return x < 0 ? 0 : x > T ? T : x; };
   auto add = [](int x, int y) { return x + y < kMost ? x + y : kMost; };
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
     if (i < n) {
       const int len = clamp(cu[i + 1]) - clamp(cu[i]);
       x[0] = len > 0 ? chunks_of(len) : 0;
-      x[1] = x[0] > seg_chunks ? (x[0] + seg_chunks - 1) / seg_chunks : 1;
+      x[1] = x[0] > whole ? (x[0] + seg_chunks - 1) / seg_chunks : 1;
     }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -361,13 +362,16 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
     const int at = s - prefix(1, seq), first = prefix(0, seq) + at * seg_chunks, from = at * seg_chunks * kChunk;
     const int b = clamp(cu[seq]);
     int len = clamp(cu[seq + 1]) - b - from;
-    if (len > seg_chunks * kChunk) len = seg_chunks * kChunk;
+    if (prefix(1, seq + 1) - prefix(1, seq) > 1 && len > seg_chunks * kChunk) len = seg_chunks * kChunk;
     const int room = nc > first ? nc - first : 0;  // offsets that decrease: the table of chunks ends
     if (len > room * kChunk) len = room * kChunk;
     const bool last = s + 1 >= prefix(1, seq + 1);
     return make_int4(first, b + from, len > 0 ? len : 0, seq << 2 | (at == 0 ? 1 : 0) | (last ? 2 : 0));
   };
-  auto cls = [&](int len) { return kClasses - 1 - chunks_of(len) * kClasses / (seg_chunks + 1); };
+  auto cls = [&](int len) {
+    const int c = chunks_of(len);
+    return kClasses - 1 - (c < whole ? c : whole) * kClasses / (whole + 1);
+  };
   int4 mine = make_int4(0, 0, 0, 0);
   if (tid < ns) mine = segment(tid);
   for (int s = tid; s < ns; s += kPlanThreads) atomicAdd(&at_class[cls(s == tid ? mine.z : segment(s).z)], 1);

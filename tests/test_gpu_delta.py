@@ -342,6 +342,16 @@ def test_one_long_sequence_among_many(V, dtype):
     c.check_backward(c.backward(V))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,uniform", [([64 * 8], False), ([64 * 8 + 1], False), ([64 * 9], True),
+                                          ([64 * 8, 64 * 9 + 5, 64 * 3, 1], False), ([64 * 9 - 1] * 3, True)],
+                         ids=["8", "8_and_a_token", "9", "ragged", "9_less_a_token"])
+def test_shortest_sequences_that_are_cut(V, lens, uniform, dtype):
+    c = Case(lens, Hk=2, dk=64, dv=64, dtype=dtype, uniform=uniform, rough=True)
+    c.check_forward(*c.forward(V))
+    c.check_backward(c.backward(V))
+
+
 @pytest.mark.parametrize("n", [1024, 1100, 2050])
 def test_more_sequences_than_the_planning_threads(V, n):
     lens = [int(x) for x in np.random.default_rng(n).integers(0, 4, n)]
