@@ -18,7 +18,6 @@
 namespace vda {
 
 constexpr int kChunk = 64;  // tokens of a chunk
-constexpr int kWholeChunks = 8;  // a sequence of so many chunks is not cut into segments
 constexpr int kLds = 160 * 1024;  // bytes of LDS of a workgroup
 
 typedef float floatx8 __attribute__((ext_vector_type(8)));
@@ -604,11 +603,12 @@ __device__ __forceinline__ double decay_prefix(float g, int lane) {
 struct DeltaPlan {
   bool split;        // sequences are cut into segments that run side by side
   int seg_chunks;    // chunks of a segment
+  int whole;         // a sequence of so many chunks is one segment
   int max_chunks, max_segs;
   size_t tabs, rec, segs, keep, total;  // workspace offsets
 };
-hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, int seg_chunks, int max_chunks,
-                             int max_segs, int* tabs, hipStream_t stream);
+hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, const DeltaPlan& plan, int* tabs,
+                             hipStream_t stream);
 hipError_t launch_delta_prepare(bool f32, int d_k, bool backward, const DeltaArgs& a, hipStream_t stream);
 // what: 0 the segments' maps, 1 the outputs, 2 the states and writes for the gradient kernel.
 hipError_t launch_delta_scan(bool f32, int d_k, int what, const DeltaArgs& a, hipStream_t stream);

@@ -71,14 +71,20 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   // segment): the least time is at about the square root of an eighth of the
   // sequence's chunks.  8 heads, segments of 4 chunks and so: 1088 tokens 55 and
   // 44 us; 2 heads of 38400 tokens, segments of 5 chunks and so: 199 and 171 us.
-  // Of nine chunks (8 heads) the forward pass takes 38 us whole and cut, the
-  // backward pass 92 and 86; shorter sequences stay whole.
+  // Shorter sequences stay whole: of 8 heads, in bf16, eight chunks take 35 us
+  // whole and 37 cut, and 84 and 83 backward (nine 38 and 38, 92 and 86); in
+  // fp32 with 64 channels, whose chunks take twice the time, six take 47 and 42,
+  // 94 and 91 in a graph, but more launches (eight 58 and 43, 114 and 93).
+  // Segments that the compute units make longer than two chunks pay from the
+  // fourth on.
   const long long cus = vda::current_device_cus();
   long long share = std::max(2LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
   while (8 * share * share < longest) ++share;
   if (n * p->H_v >= cus) share = std::max(share, 4 * ((d.max_chunks + n - 1) / n));
-  d.split = longest > std::max<long long>(vda::kWholeChunks, 4 * share);
+  const int whole = p->is_f32 ? 6 : 8;
+  d.split = longest > whole && (share == 2 || longest > 4 * share);
   d.seg_chunks = (int)(d.split ? share : std::max(longest, 1LL));
+  d.whole = std::max(d.seg_chunks, whole);
   d.max_segs =
       (int)(table ? d.max_chunks / d.seg_chunks + n : n * ((per + d.seg_chunks - 1) / d.seg_chunks));
   // Workspace.
@@ -163,8 +169,8 @@ Sizes sizes_of(const vda_delta_problem* p) {
 hipError_t plan_and_prepare(const vda_delta_problem* p, const vda::DeltaPlan& d, const vda::DeltaArgs& a,
                             bool backward, hipStream_t stream) {
   if (p->cu_seqlens) {
-    const hipError_t e = vda::launch_delta_plan(p->cu_seqlens, p->n_seqs, p->T, d.seg_chunks, d.max_chunks,
-                                                d.max_segs, const_cast<int*>(a.counts), stream);
+    const hipError_t e = vda::launch_delta_plan(p->cu_seqlens, p->n_seqs, p->T, d, const_cast<int*>(a.counts),
+                                                stream);
     if (e != hipSuccess) return e;
   }
   hipError_t e = vda::launch_delta_prepare(p->is_f32 != 0, p->d_k, backward, a, stream);

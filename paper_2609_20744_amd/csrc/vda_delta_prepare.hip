@@ -287,7 +287,8 @@ void delta_prepare_kernel(DeltaArgs a) {
 constexpr int kPlanThreads = 1024, kMost = 0x3fffffff, kClasses = 32;
 
 __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu, int n, int T, int seg_chunks,
-                                                                 int max_chunks, int max_segs, int* tabs) {
+                                                                 int whole, int max_chunks, int max_segs,
+                                                                 int* tabs) {
   __shared__ int pre[2][kPlanThreads], ends[2][kPlanThreads / 64], at_class[kClasses];
   int* counts = tabs;
   int* cpre = tabs + 4;
@@ -296,7 +297,6 @@ __global__ __launch_bounds__(kPlanThreads) void delta_plan_kernel(const int* cu,
   int4* seg_tab = chunk_tab + max_chunks;
   int* seg_id = reinterpret_cast<int*>(seg_tab + max_segs);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int whole = seg_chunks > kWholeChunks ? seg_chunks : kWholeChunks;  // the most chunks of one segment
   const bool small = n <= kPlanThreads;  // the prefixes are in LDS as well
   auto clamp = [&](int x) { return x < 0 ? 0 : x > T ? T : x; };
   auto add = [](int x, int y) { return x + y < kMost ? x + y : kMost; };
@@ -405,9 +405,10 @@ hipError_t run(bool backward, const DeltaArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, int seg_chunks, int max_chunks, int max_segs,
-                             int* tabs, hipStream_t stream) {
-  delta_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu, n_seqs, T, seg_chunks, max_chunks, max_segs, tabs);
+hipError_t launch_delta_plan(const int* cu, int n_seqs, int T, const DeltaPlan& plan, int* tabs,
+                             hipStream_t stream) {
+  delta_plan_kernel<<<1, kPlanThreads, 0, stream>>>(cu, n_seqs, T, plan.seg_chunks, plan.whole, plan.max_chunks,
+                                                    plan.max_segs, tabs);
   return hipGetLastError();
 }
 

@@ -344,8 +344,9 @@ def test_one_long_sequence_among_many(V, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens,uniform", [([64 * 8], False), ([64 * 8 + 1], False), ([64 * 9], True),
-                                          ([64 * 8, 64 * 9 + 5, 64 * 3, 1], False), ([64 * 9 - 1] * 3, True)],
-                         ids=["8", "8_and_a_token", "9", "ragged", "9_less_a_token"])
+                                          ([64 * 8, 64 * 9 + 5, 64 * 3, 1], False), ([64 * 9 - 1] * 3, True),
+                                          ([64 * 6], True), ([64 * 6 + 1], True), ([64 * 6, 64 * 7], False)],
+                         ids=["8", "8_and_a_token", "9", "ragged", "9_less_a_token", "6", "6_and_a_token", "6_and_7"])
 def test_shortest_sequences_that_are_cut(V, lens, uniform, dtype):
     c = Case(lens, Hk=2, dk=64, dv=64, dtype=dtype, uniform=uniform, rough=True)
     c.check_forward(*c.forward(V))
