@@ -544,9 +544,9 @@ typedef enum {
  *    H_k = B * heads, n_seqs = 1, T = L.
  *  - storage of q, k, v, out and their gradients: bf16 (is_f32 == 0) or fp32.
  *    g (log decay, <= 0; -inf resets the state; positive values are not
- *    checked, and grow it) and beta (write strength, any sign, below 2^-48 in
- *    magnitude taken as that; the rule is stable for beta |k|^2 in [0, 2]) are
- *    fp32.
+ *    checked, and grow it) and beta (write strength, any sign; the rule is
+ *    stable for beta |k|^2 in [0, 2]; a token of strength 0 writes nothing,
+ *    whatever its finite key and value) are fp32.
  * A NaN or infinity in a token's q, k, v, g or beta (but g = -inf) makes the
  * outputs of its group of 64 tokens (counted from the sequence's first) of its head undefined,
  * and those of all later ones; other sequences and heads are not touched.

@@ -4,13 +4,16 @@
 // Tokens are taken in chunks of 64.  With S the state entering a chunk
 // (d_v x d_k), G_i the sum of the chunk's log decays up to token i,
 // D_ij = e^(G_i - G_j), gam_i = e^(G_i), eta_i = e^(G_63 - G_i):
-//     L_ij = D_ij k_i.k_j (i > j),   T = (I + diag(beta) L)^-1,
+//     L_ij = D_ij k_i.k_j (i > j),   T = (I + L diag(beta))^-1,
 //     P_ij = scale D_ij q_i.k_j (i >= j),
-//     N = T diag(beta) (V - diag(gam) K S^T)   N_i = beta_i e_i, what token i writes
+//     E = T (V - diag(gam) K S^T),   N = diag(beta) E, what the tokens write
 //     O = scale diag(gam) Q S^T + P N
 //     S <- gam_63 S + N^T diag(eta) K
 // T and P do not depend on the state; the chunk-preparation kernel makes them
-// for all chunks at once, and the scans carry the state.
+// for all chunks at once, and the scans carry the state.  With the strengths on
+// the right of L, a token of strength 0 has a column of zeros in T and a row of
+// zeros in N, whatever its key and value are, and beta's gradient, E's with
+// respect to N, needs no division by a strength.
 #pragma once
 
 #include "vda_common.h"
@@ -415,10 +418,11 @@ __device__ __forceinline__ void store_tile_w(char* m, int tile, int lane, const 
   }
 }
 
-// What the preparation writes for a chunk of a value head: T (wide; beta stays
-// outside it, as a rounded beta would be an error of a whole row of N), gam,
-// eta and beta (fp32[64] each), and P (the forward pass: one part), or the wide
-// transposes of T and P and G in units of log2 (64 bits) (the backward pass).
+// What the preparation writes for a chunk of a value head: T (wide; the beta of
+// N = diag(beta) E stays outside it, as a rounded beta would be an error of a
+// whole row of N), gam, eta and beta (fp32[64] each), and P (the forward pass:
+// one part), or the wide transposes of T and P and G in units of log2 (64 bits)
+// (the backward pass).
 struct ChunkRecord {
   static constexpr int kT = 0, kVec = kWideTri, kP = kWideTri + 1024, kTt = kP, kPt = kP + kWideTri,
                        kPre = kPt + kWideTri;
@@ -429,7 +433,7 @@ struct ChunkRecord {
 };
 
 // What the scans keep for the gradient kernel (S and dS, value x key channels;
-// N and dv, value channels x tokens) lies as that kernel's row tiles, 32 value
+// E and dv, value channels x tokens) lies as that kernel's row tiles, 32 value
 // channels after 32, in bf16 hi and lo planes or one of fp32, so that it copies
 // contiguous memory.  Place r of tile t of 32 rows is row 8 (r / 4) + 4 t + r % 4
 // (paired order: the order that channels have, above, for rows that are
@@ -522,7 +526,7 @@ struct DeltaArgs {
   char* rec;          // [chunk][Hv] ChunkRecord
   float *segJ, *segdJ;  // [segment][Hv] states that maps add; the entering states replace them
   char* segM;           // [segment][Hv] map matrices, wide, by rows and by columns
-  char *keepS, *keepN, *keepdS, *keepdv;  // [chunk][Hv] what the gradient kernel reads
+  char *keepS, *keepE, *keepdS, *keepdv;  // [chunk][Hv] what the gradient kernel reads
 };
 
 __device__ __forceinline__ int chunks_of(int len) { return (len + kChunk - 1) / kChunk; }
@@ -561,15 +565,6 @@ __device__ __forceinline__ SegmentInfo segment_info(const DeltaArgs& a, int s) {
 // Log decays below this are taken as this: e^-200 is 0 in fp32, and sums of
 // them stay finite (a decay of exactly 0, log decay -inf, among them).
 constexpr float kMinLogDecay = -200.f;
-// Write strengths below this in magnitude are taken as this with their sign:
-// what such a token writes is below fp32's resolution of the state by 2^-24,
-// and the gradients can divide by the strength.
-constexpr float kMinBeta = 0x1p-48f;
-
-__device__ __forceinline__ float strength(float b) {
-  return fabsf(b) < kMinBeta ? copysignf(kMinBeta, b) : b;
-}
-
 // 2^x of the matrix of decays: one instruction, results below 2^-126 are 0.
 __device__ __forceinline__ float pow2(double x) { return __builtin_amdgcn_exp2f((float)x); }
 

@@ -139,8 +139,8 @@ vda::DeltaArgs args_of(const vda_delta_problem* p, const vda::DeltaPlan& d, bool
   if (backward) {
     a.keepS = w + d.keep;
     a.keepdS = a.keepS + chunks * mat * 4;
-    a.keepN = a.keepdS + chunks * mat * 4;
-    a.keepdv = a.keepN + chunks * p->d_v * vda::kChunk * 4;
+    a.keepE = a.keepdS + chunks * mat * 4;
+    a.keepdv = a.keepE + chunks * p->d_v * vda::kChunk * 4;
   }
   return a;
 }

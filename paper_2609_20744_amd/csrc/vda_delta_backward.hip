@@ -2,19 +2,23 @@
 // gradient over chunks, and the gradients of a chunk's inputs.
 //
 // With the forward pass's notation (vda_delta.h), dO the output's gradient,
-// dS the gradient of the state behind the chunk and dv = diag(beta) y:
-//     dN = P^T dO + diag(eta) K dS^T,      dv = diag(beta) T^T dN   (of V)
+// dS the gradient of the state behind the chunk:
+//     dN = P^T dO + diag(eta) K dS^T,      dv = T^T diag(beta) dN   (of V)
 //     dS <- gam_63 dS + scale dO^T diag(gam) Q - dv^T diag(gam) K
 //     W_ij = scale D_ij dO_i.N_j (i >= j), X_ij = -D_ij dv_i.N_j (i > j)
 //     dQ = scale diag(gam) dO S + W K
 //     dK = W^T Q + diag(eta) N dS - diag(gam) dv S + (X + X^T) K
-//     dbeta_i = (N_i / beta_i).(dv_i / beta_i)
+//     dbeta_j = E_j.(dN - L^T dv)_j
+//             = sum_{i >= j} P_ij dO_i.E_j - sum_{i > j} L_ij dv_i.E_j + eta_j k_j.(E dS)_j
 // The decay of token t scales what passes from before it to it or past it:
 // from a token j < t to one i >= t, from the entering state to those, from
 // those j to the state behind, and from state to state:
 //     dg_t = gam_63 <dS, S> + sum_{i >= t} a_i + sum_{j < t} b_j + sum_{i >= t > j} A_ij,
 //     A_ij = P_ij dO_i.N_j - D_ij (k_i.k_j) dv_i.N_j
 //     a_i  = gam_i (scale q_i.(dO S)_i - k_i.(dv S)_i),   b_j = eta_j k_j.(N dS)_j
+// The gradient kernel's products take E in N's place, and beta where their sums
+// end (N_j = beta_j E_j): dbeta_j is then what A and b of token j sum to before
+// beta_j, and its own output's share P_jj dO_j.E_j.
 // (the sum over all (q_i.dq_i - dv_i.v_i) behind t is the same in exact
 // arithmetic and needs no A, but its terms cancel to a fraction of their size:
 // with wide operands its error was 2e-5 of dg where this one's is 4e-6).
@@ -132,6 +136,9 @@ void delta_reverse_kernel(DeltaArgs a) {
       for (int t = 0; t < 4; ++t) dN[t] = O::mma(kr[s & 1][t], Sw, s == 0 ? zero : dN[t]);
     }
     W M0[2], Tt[4];
+    floatx4 bv[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) bv[t] = *reinterpret_cast<const floatx4*>(beta + 16 * t);
 #pragma unroll
     for (int t = 0; t < 2; ++t) M0[t] = tile_w<F32>(buf + kOffPt, tri_tile_t(t, 0), lane);
 #pragma unroll
@@ -145,15 +152,12 @@ void delta_reverse_kernel(DeltaArgs a) {
     fence<F32>();
     W dNw[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) dNw[s] = O::wide(dN[2 * s], dN[2 * s + 1]);
+    for (int s = 0; s < 2; ++s) dNw[s] = O::wide(bv[2 * s] * dN[2 * s], bv[2 * s + 1] * dN[2 * s + 1]);
 
-    // dv = beta T^T dN.
-    floatx4 y[4], gv[4], bv[4];
+    // dv = T^T (beta dN).
+    floatx4 y[4], gv[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      gv[t] = *reinterpret_cast<const floatx4*>(gam + 16 * t);
-      bv[t] = *reinterpret_cast<const floatx4*>(beta + 16 * t);
-    }
+    for (int t = 0; t < 4; ++t) gv[t] = *reinterpret_cast<const floatx4*>(gam + 16 * t);
     // Columns of Q, then of K, half u of the channels at a time.
     X ct[KS][2];
     auto columns = [&](const char* tiles, int u) {
@@ -200,8 +204,6 @@ void delta_reverse_kernel(DeltaArgs a) {
     update(1, dOw);
     columns(buf, 0);
     W yw[2];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) y[t] *= bv[t];
     if constexpr (!MAP) {
       char* kd = a.keepdv + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
 #pragma unroll
@@ -259,9 +261,9 @@ void delta_reverse_kernel(DeltaArgs a) {
 // w % 4, transposed (channels x tokens), of every other four channels; of the
 // scores between tokens it makes the rows of 32 tokens, and the other wave of
 // the tile the others, exchanged at a head's end.  The value channels come in
-// steps of 32 (S, dS, N, dv and dO of those channels), the next step's copied
+// steps of 32 (S, dS, E, dv and dO of those channels), the next step's copied
 // into LDS while this one's are used; all sums over value channels stay in
-// registers between steps, <dS, S> and N.dv too, as the diagonals of products.
+// registers between steps, <dS, S> too, as the diagonals of products.
 // Chunks start with different steps: their matrices lie a power of two apart,
 // and in step they would load the memory's channels one after another.  Tokens
 // and key channels are taken in twisted order, value channels in paired order
@@ -280,14 +282,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   constexpr int kTileK = kChunk * DK * ES, kTileS = 32 * DK * ES, kTileN = 32 * kChunk * ES;
   // Two steps in turn: a head's are then a whole number of turns.
   constexpr int steps = DV / 32, kBufs = F32 || steps == 1 ? 1 : 2;
-  constexpr int kOffdS = kPlanes * kTileS, kOffN = 2 * kPlanes * kTileS, kOffdv = kOffN + kPlanes * kTileN,
+  constexpr int kOffdS = kPlanes * kTileS, kOffE = 2 * kPlanes * kTileS, kOffdv = kOffE + kPlanes * kTileN,
                 kOffO = kOffdv + kPlanes * kTileN, kUsed = kOffO + kTileN;
   // (A head's end exchanges six operands of four tiles there.)
   constexpr int kSwap = 4 * 6 * 64 * (int)sizeof(X), kStage = kUsed > kSwap ? kUsed : kSwap;
   constexpr size_t mat = (size_t)DV * DK, nmat = (size_t)DV * kChunk;
   __shared__ __align__(16) char rowsKQ[2 * kTileK], buf0[kStage], buf1[kBufs == 2 ? kStage : 16];
   __shared__ double pre[kChunk];
-  __shared__ float suffix[2][kChunk], prefix[2][kChunk], passed[4][kChunk], states[8];
+  __shared__ __align__(16) float strengths[kChunk];
+  __shared__ float suffix[2][kChunk], prefix[2][kChunk], writes[2][kChunk], passed[4][kChunk], states[8];
 
   const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
   const int chunk = uniform(blockIdx.x / (unsigned)a.Hk);
@@ -324,7 +327,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const size_t at = first + n / steps;
     const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.keepS + at * mat * 4, kPlanes * kMat),
                                  dsr = make_rsrc(a.keepdS + at * mat * 4, kPlanes * kMat),
-                                 nr = make_rsrc(a.keepN + at * nmat * 4, kPlanes * kNmat),
+                                 er = make_rsrc(a.keepE + at * nmat * 4, kPlanes * kNmat),
                                  dvr = make_rsrc(a.keepdv + at * nmat * 4, kPlanes * kNmat);
 #pragma unroll
     for (int p = 0; p < kPlanes; ++p) {
@@ -332,11 +335,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       copy_flat<kTileS, 8>(sr, buf + p * kTileS, wave, lane, so);
       copy_flat<kTileS, 8>(dsr, buf + kOffdS + p * kTileS, wave, lane, so);
     }
-    // N and dv: the planes together are a piece for each wave.
+    // E and dv: the planes together are a piece for each wave.
     constexpr int kPieces = kTileN / 1024;
     static_assert(kPlanes * kPieces == 8, "a piece a wave");
     const uint32_t no = wave / kPieces * kNmat + s * kTileN + wave % kPieces * 1024;
-    copy_flat<1024, 1>(nr, buf + kOffN + wave * 1024, 0, lane, no);
+    copy_flat<1024, 1>(er, buf + kOffE + wave * 1024, 0, lane, no);
     copy_flat<1024, 1>(dvr, buf + kOffdv + wave * 1024, 0, lane, no);
     copy_tiles<F32, 1, 8, true>(
         make_rsrc((const char*)a.dout + vo + (n / steps) * a.v_head * ES, 64u * v_row), buf + kOffO, len, v_row, wave,
@@ -367,20 +370,20 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
   for (int s = 0; s < KS; ++s) dq[s] = zero, dk[s] = zero;
 
   // Sums over a head's value channels; the scores' rows are tiles 2 part, 2 part + 1.
-  floatx4 Wt[2], Wn[2], Xa[2], Xb[2], Q[KS], Ka[KS], Kb[KS], SS, ND;
-  // Of a head: this lane's token's, and (wave 0) token `lane`'s G and g.
+  floatx4 Wt[2], Wn[2], Xa[2], Xb[2], Q[KS], Ka[KS], Kb[KS], SS;
+  // Of a head: this lane's token's, and (wave 0) token `lane`'s G, beta and g.
   struct Gates {
-    float gam, eta, strength, ends, decay;
+    float gam, eta, beta, ends, strength, decay;
     double pre;
   };
   auto step = [&](int n, const char* buf) __attribute__((always_inline)) {
-    const char *tS = buf, *tdS = buf + kOffdS, *tN = buf + kOffN, *tdv = buf + kOffdv, *tO = buf + kOffO;
+    const char *tS = buf, *tdS = buf + kOffdS, *tE = buf + kOffE, *tdv = buf + kOffdv, *tO = buf + kOffO;
     const X Oj = rows(tO + w * kRow);
-    const W Nj = col_w(tN, kTileN, w >> 1, own), vj = col_w(tdv, kTileN, w >> 1, own);
+    const W Ej = col_w(tE, kTileN, w >> 1, own), vj = col_w(tdv, kTileN, w >> 1, own);
     // Products with the states, channels x tokens; operands one block ahead.
     W Sc[2], dSc[2];
     Sc[0] = col_w(tS, kTileS, 0, mine), dSc[0] = col_w(tdS, kTileS, 0, mine);
-    X Nt[2], Ot[2];
+    X Et[2], Ot[2];
     W vt[2];
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
@@ -389,26 +392,25 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       } else {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          Nt[u] = col_x(tN, part, tl.col[u]);
+          Et[u] = col_x(tE, part, tl.col[u]);
           vt[u] = col_w(tdv, kTileN, part, tl.col[u]);
           Ot[u] = rows(tO + (2 * part + u) * kRow);
         }
       }
       fence<F32>();
       Q[c] = O::mma(Sc[c & 1], Oj, Q[c]);
-      Ka[c] = O::mma(dSc[c & 1], Nj, Ka[c]);
+      Ka[c] = O::mma(dSc[c & 1], Ej, Ka[c]);
       Kb[c] = O::mma(Sc[c & 1], vj, Kb[c]);
       SS = O::mma(Sc[c & 1], dSc[c & 1], SS);
     }
-    ND = O::mma(Nj, vj, ND);
     // Scores between tokens, columns of this wave (those that the order of
     // tokens rules out are left out at the head's end).
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      Wt[u] = O::mma(Nt[u], Oj, Wt[u]);           // dO_j.N_i, for i <= j
-      Xb[u] = O::mma(Nt[u], O::head(vj), Xb[u]);  // dv_j.N_i
-      Wn[u] = O::mma(Ot[u], Nj, Wn[u]);           // dO_i.N_j, for i >= j
-      Xa[u] = O::mma(vt[u], Nj, Xa[u]);           // dv_i.N_j
+      Wt[u] = O::mma(Et[u], Oj, Wt[u]);           // dO_j.E_i, for i <= j
+      Xb[u] = O::mma(Et[u], O::head(vj), Xb[u]);  // dv_j.E_i
+      Wn[u] = O::mma(Ot[u], Ej, Wn[u]);           // dO_i.E_j, for i >= j
+      Xa[u] = O::mma(vt[u], Ej, Xa[u]);           // dv_i.E_j
     }
     // dv out: its rounding is its first part.  (Half of the waves store; the
     // others' stores are out of the buffer's range, as rows behind the end are.)
@@ -430,8 +432,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const char* rec = a.rec + ((size_t)chunk * a.Hv + h) * ChunkRecord::bytes(F32, true);
     const float* vec = reinterpret_cast<const float*>(rec + ChunkRecord::kVec);
     Gates g;
-    g.gam = vec[j], g.eta = vec[64 + j], g.ends = vec[63];
-    g.strength = j < len ? vec[128 + j] : 1.f;
+    g.gam = vec[j], g.eta = vec[64 + j], g.beta = vec[128 + j], g.ends = vec[63];
+    g.strength = vec[128 + lane];
     g.pre = reinterpret_cast<const double*>(rec + ChunkRecord::kPre)[lane];
     g.decay = wave == 0 && lane < len ? a.g[(size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head] : 0.f;
     return g;
@@ -441,22 +443,23 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int u = 0; u < 2; ++u) Wt[u] = Wn[u] = Xa[u] = Xb[u] = zero;
 #pragma unroll
     for (int c = 0; c < KS; ++c) Q[c] = Ka[c] = Kb[c] = zero;
-    SS = zero, ND = zero;
+    SS = zero;
   };
 
   // The end of a head; `swap` is LDS that nothing else uses now.
   auto finish = [&](int h, const Gates& g, char* swap) {
-    if (wave == 0) pre[lane] = g.pre;
+    if (wave == 0) pre[lane] = g.pre, strengths[lane] = g.strength;
     // (Opaque: the comparisons below, kept from head to head, would take 100
     // scalar registers, and the kernel 343 us instead of 309, of spilled ones.)
     int jj = j, ll = lane;
     asm volatile("" : "+v"(jj), "+v"(ll));
     lds_barrier();
     // Decays between tokens: columns j of this lane.  What passes from j to
-    // i > j (A): its sums over i, for token j, and over j, for tokens i.
+    // i > j (A): its sums over i, for token j (before beta_j), and over j, for
+    // tokens i; and what j's write gives its own output.
     const double gj = pre[jj];
     floatx4 Xs[2];
-    float below = 0.f;
+    float below = 0.f, self = 0.f;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int t = 2 * part + u;
@@ -468,17 +471,21 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         kk = O::mma(rows(tileK + (4 * s + t) * kRow), kj, kk);
       }
       floatx4 A = zero;
+      // (The four rows of a lane are consecutive tokens.)
+      const floatx4 bi = *reinterpret_cast<const floatx4*>(strengths + twisted_row(t, 4 * (ll >> 4)));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = twisted_row(t, 4 * (ll >> 4) + e);
         const double apart = pre[i] - gj;
         const float d = pow2(i >= jj ? apart : -apart);
-        Wt[u][e] = i <= jj ? a.scale * d * Wt[u][e] : 0.f;
-        Wn[u][e] = i >= jj && i < len ? a.scale * d * Wn[u][e] : 0.f;
-        Xs[u][e] = i > jj ? -d * Xa[u][e] : i < jj ? -d * Xb[u][e] : 0.f;
-        A[e] = i > jj && i < len ? Wn[u][e] * qk[e] + Xs[u][e] * kk[e] : 0.f;
-        below += A[e];
-        A[e] = group_sum<16>(A[e]);
+        const float wn = i >= jj && i < len ? a.scale * d * Wn[u][e] : 0.f, xa = -d * Xa[u][e];
+        const float past = i > jj && i < len ? wn * qk[e] + xa * kk[e] : 0.f;
+        below += past;
+        self += i == jj ? wn * qk[e] : 0.f;
+        A[e] = group_sum<16>(g.beta * past);
+        Wt[u][e] = i <= jj ? a.scale * d * bi[e] * Wt[u][e] : 0.f;
+        Wn[u][e] = g.beta * wn;
+        Xs[u][e] = i > jj ? g.beta * xa : i < jj ? -d * bi[e] * Xb[u][e] : 0.f;
       }
       if (li == 0)
 #pragma unroll
@@ -497,7 +504,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool second = part ^ (lg >> 1);  // this lane's half of eight channels
 #pragma unroll
     for (int c = 0; c < KS; ++c) {
-      floatx4 x = (a.scale * g.gam) * Q[c], y = g.eta * Ka[c] - g.gam * Kb[c];
+      floatx4 x = (a.scale * g.gam) * Q[c], y = (g.eta * g.beta) * Ka[c] - g.gam * Kb[c];
       // This lane's four channels of its token's q and k.
       const X qv = rows(tileQ + (4 * c + w) * kRow), kv = rows(tileK + (4 * c + w) * kRow);
 #pragma unroll
@@ -517,25 +524,21 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
       dq[c] += x;
       dk[c] += y;
     }
-    // Diagonals: this lane's token's N.dv, and its share of <dS, S>.
-    float db = 0.f, ss = 0.f;
+    // The diagonal: this lane's share of <dS, S>.
+    float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool diagonal = (ll & 15) == 4 * (ll >> 4) + e;
-      db += diagonal ? ND[e] : 0.f, ss += diagonal ? SS[e] : 0.f;
-    }
+    for (int e = 0; e < 4; ++e) ss += (ll & 15) == 4 * (ll >> 4) + e ? SS[e] : 0.f;
     // Sums over the lanes of a token (lg), over the channels' halves, then over the chunk.
     float past = below + g.eta * end;
     in += __shfl_xor(in, 16), in += __shfl_xor(in, 32);
     past += __shfl_xor(past, 16), past += __shfl_xor(past, 32);
-    db += __shfl_xor(db, 16), db += __shfl_xor(db, 32);
+    self += __shfl_xor(self, 16), self += __shfl_xor(self, 32);
     ss = group_sum<16>(ss);
     ss += __shfl_xor(ss, 16), ss += __shfl_xor(ss, 32);
     if (lg == 0) {
       suffix[part][j] = j < len ? in : 0.f;
-      prefix[part][j] = j < len ? past : 0.f;
-      if (part == 0 && j < len)
-        a.dbeta[(size_t)(ci.tok + j) * a.gate_tok + (size_t)h * a.gate_head] = db / g.strength / g.strength;
+      prefix[part][j] = j < len ? g.beta * past : 0.f;
+      writes[part][j] = past + self;
     }
     if (lane == 0) states[wave] = ss;
     lds_barrier();
@@ -555,6 +558,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
         // A decay of zero: nothing of the state before reaches the token.
         a.dg[at] = g.decay < kMinLogDecay ? 0.f : x;
+        a.dbeta[at] = writes[0][lane] + writes[1][lane];
       }
     }
   };

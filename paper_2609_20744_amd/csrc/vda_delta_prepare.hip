@@ -8,7 +8,7 @@
 // operands loaded straight from memory, 16 bytes of 16 rows at a time, the
 // kernel took 68 us where it now takes 48: 16411 tokens, 16 heads, 128 x 128;
 // backward, 16401 tokens, 102 and 54 us); wave w makes row block w.  The
-// decays multiply the fp32 results.  I + diag(beta) L is unit lower triangular
+// decays multiply the fp32 results.  I + L diag(beta) is unit lower triangular
 // and is inverted in fp32, in LDS: its four 16 x 16 diagonal blocks by
 // forward substitution (a lane per column; a series of powers would be all
 // products, but its terms grow with repeated keys before they cancel), then
@@ -141,7 +141,7 @@ void delta_prepare_kernel(DeltaArgs a) {
   float decay = 0.f, beta = 0.f;
   if (wave == 0 && lane < ci.len) {
     const size_t at = (size_t)(ci.tok + lane) * a.gate_tok + (size_t)h * a.gate_head;
-    decay = a.g[at], beta = strength(a.beta[at]);
+    decay = a.g[at], beta = a.beta[at];
   }
   // The rows.  Those behind the chunk's end repeat its last: of T they reach
   // nothing (such tokens have no strength), of P rows that only the backward
@@ -169,7 +169,6 @@ void delta_prepare_kernel(DeltaArgs a) {
 
   const int r0 = 16 * wave;
   const Prefix4 gi = prefix4(pre + r0 + 4 * lg);
-  const floatx4 bi = *reinterpret_cast<const floatx4*>(strengths + r0 + 4 * lg);
 
   // The operands of this wave's rows: of k, and in the forward pass of q.
   X kw[KS], qw[KS];
@@ -227,7 +226,7 @@ void delta_prepare_kernel(DeltaArgs a) {
   }
   lds_barrier();  // every wave is done with q
 
-  // M = diag(beta) L, rows of this wave.
+  // M = L diag(beta), rows of this wave.
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     if (t > wave) continue;
@@ -236,10 +235,11 @@ void delta_prepare_kernel(DeltaArgs a) {
     for (int s = 0; s < KS; ++s) acc = O::mma(kw[s], row(rowsK, t, s), acc);
     const int j = 16 * t + li;
     const double gj = pre[j];
+    const float bj = strengths[j];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = r0 + 4 * lg + e;
-      m[i * kLd + j] = keep_if(i > j, bi[e] * pow2(gi.x[e] - gj) * acc[e]);
+      m[i * kLd + j] = keep_if(i > j, bj * pow2(gi.x[e] - gj) * acc[e]);
     }
   }
   lds_barrier();

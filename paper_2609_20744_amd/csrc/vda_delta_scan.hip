@@ -6,7 +6,7 @@
 // the state (32 in the maps), transposed (key channels x value columns), in
 // registers, and nothing passes between waves: each product leaves its result
 // with the rows that the next one contracts,
-//     Z = K S^T -> X = beta (V - gam Z) -> N = T X -> S^T <- gam_63 S^T + K^T (eta N),
+//     Z = K S^T -> X = V - gam Z -> N = beta T X -> S^T <- gam_63 S^T + K^T (eta N),
 // so a step is three dependent products with no exchange through LDS.  The
 // matrices that all waves share (k, q and v rows, T, P) come through LDS, the
 // next chunk's copied by loads straight to LDS while this one's are used, one
@@ -226,7 +226,7 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
         }
     }
 
-    // X = beta (V - gam Z).
+    // X = V - gam Z.
     W Xw[2][NV];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -237,13 +237,13 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int t = 2 * half + u;
-          x[u] = bv[t] * (vv[t][n] - gv[t] * z[t][n]);
+          x[u] = vv[t][n] - gv[t] * z[t][n];
         }
         Xw[half][n] = O::wide(x[0], x[1]);
       }
     }
 
-    // N = T X.
+    // E = T X, which is kept, and N = beta E.
     floatx4 N[4][NV];
     if (NV == 2) inverse();
 #pragma unroll
@@ -256,6 +256,18 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
     for (int t = 2; t < 4; ++t)
 #pragma unroll
       for (int n = 0; n < NV; ++n) N[t][n] = O::mma(T[t], Xw[1][n], N[t][n]);
+    if constexpr (MODE == kKeep) {
+      char* ke = a.keepE + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+          keep_tokens<F32>(ke, keep_tile(vb, n0 + n, t >> 1, 2), t & 1, li, lg, (size_t)DV * kChunk, N[t][n]);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int n = 0; n < NV; ++n) N[t][n] *= bv[t];
 
     // Columns of K for the update, half u of the channels at a time.
     X kt[KS][2];
@@ -266,15 +278,6 @@ __attribute__((amdgpu_waves_per_eu(1, 2))) void delta_scan_kernel(DeltaArgs a) {
         for (int t = 0; t < 2; ++t)
           kt[s][t] = tile_cols<F32>(buf + RowsK::tile(s, 2 * t), buf + RowsK::tile(s, 2 * t + 1), u, RowsK::odd(s), tl);
     };
-
-    if constexpr (MODE == kKeep) {
-      char* kn = a.keepN + ((size_t)chunk * a.Hv + h) * DV * kChunk * 4;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int n = 0; n < NV; ++n)
-          keep_tokens<F32>(kn, keep_tile(vb, n0 + n, t >> 1, 2), t & 1, li, lg, (size_t)DV * kChunk, N[t][n]);
-    }
 
     if constexpr (MODE == kOutput) {
       X Nx[2][NV], P[kTriTiles];
