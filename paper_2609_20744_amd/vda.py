@@ -779,8 +779,8 @@ def delta_step(q, k, v, g, beta, state, slots=None, scale=None, out=None, stream
 
 def _token_rows(t, name, H):
     """Row stride of a [B, L, H * d] tensor whose token rows are equally far apart."""
-    if t.dim() != 3 or t.shape[2] % H:
-        raise ValueError(f"{name} must be [B, L, H * d]")
+    if H < 1 or t.dim() != 3 or t.shape[2] % H:
+        raise ValueError(f"{name} must be [B, L, H * d], H at least 1")
     B, L, C = t.shape
     row = t.stride(1) if L > 1 else t.stride(0) if B > 1 else C
     if t.stride(2) != 1 or row < C or (B > 1 and t.stride(0) != L * row):
@@ -841,12 +841,12 @@ def rope_backward(dout, inv_freq, axes, H, x=None, positions=None, grid=None, fr
     Returns dx [B, L, H * d] (`out` may be a slice of a fused gradient)."""
     dt, dev = _storage(dout, "dout")
     if layout == "heads":
-        if dout.dim() != 3 or dout.shape[0] % H:
-            raise ValueError("dout must be [B * H, L, d]")
+        if H < 1 or dout.dim() != 3 or dout.shape[0] % H:
+            raise ValueError("dout must be [B * H, L, d], H at least 1")
         B, L, d = dout.shape[0] // H, dout.shape[1], dout.shape[2]
     else:
-        if dout.dim() != 3 or dout.shape[2] % H:
-            raise ValueError("dout must be [B, L, H * d]")
+        if H < 1 or dout.dim() != 3 or dout.shape[2] % H:
+            raise ValueError("dout must be [B, L, H * d], H at least 1")
         B, L, d = dout.shape[0], dout.shape[1], dout.shape[2] // H
     _require(dout, "dout", dt, dev)
     o = _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interleaved, l2,
