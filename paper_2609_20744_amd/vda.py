@@ -777,6 +777,14 @@ def delta_step(q, k, v, g, beta, state, slots=None, scale=None, out=None, stream
     return out
 
 
+def _int32(name, x):
+    """x as an int that a C int holds; ctypes would take it modulo 2^32."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} {x} does not fit 32 bits")
+    return x
+
+
 def _token_rows(t, name, H):
     """Row stride of a [B, L, H * d] tensor whose token rows are equally far apart."""
     if H < 1 or t.dim() != 3 or t.shape[2] % H:
@@ -785,14 +793,16 @@ def _token_rows(t, name, H):
     row = t.stride(1) if L > 1 else t.stride(0) if B > 1 else C
     if t.stride(2) != 1 or row < C or (B > 1 and t.stride(0) != L * row):
         raise ValueError(f"{name} must have contiguous rows at one stride over the batch and tokens")
-    return row
+    return _int32(f"the row stride of {name}", row)
 
 
 def _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interleaved, l2, layout,
                dev):
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {sorted(LAYOUTS)}")
-    pt, ph, pw = (int(a) for a in axes)
+    pt, ph, pw = (_int32("axes", a) for a in axes)
+    for n, x in (("H", H), ("B", B), ("L", L)):
+        _int32(n, x)
     _expect(inv_freq, "inv_freq", (pt + ph + pw,), torch.float32, dev)
     if positions is not None:
         if grid is not None:
@@ -802,9 +812,9 @@ def _rope_args(inv_freq, axes, H, B, L, d, positions, grid, frame_offset, interl
     elif grid is None:
         raise ValueError("positions or a grid (height, width) is needed")
     else:
-        gh, gw = (int(x) for x in grid)
+        gh, gw = (_int32("grid", x) for x in grid)
     return VdaRopeOptions(pt, ph, pw, int(bool(interleaved)), int(bool(l2)), LAYOUTS[layout], gh, gw,
-                          int(frame_offset), 0, 0)
+                          _int32("frame_offset", frame_offset), 0, 0)
 
 
 def rope(x, inv_freq, axes, H, positions=None, grid=None, frame_offset=0, interleaved=True,
