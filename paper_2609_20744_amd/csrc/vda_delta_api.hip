@@ -282,8 +282,10 @@ namespace {
 
 int rope_impl(bool backward, const void* x, const void* dout, const float* inv_freq, const int* positions, int B,
               int L, int H, int d, const vda_rope_options* o, int is_f32, void* out, hipStream_t stream) {
-  if (!o || !inv_freq || !out || (backward ? !dout : !x)) return VDA_ERR_NULL;
-  if (backward && o->l2 && !x) return VDA_ERR_NULL;
+  if (!o || !inv_freq || !out || (backward && !dout)) return VDA_ERR_NULL;
+  const bool reads_x = !backward || o->l2;  // otherwise x may be anything
+  if (!reads_x) x = nullptr;
+  if (reads_x && !x) return VDA_ERR_NULL;
   if (B < 1 || L < 1 || H < 1) return VDA_ERR_SIZE;
   if (d != 16 && !supported_dim(d)) return VDA_ERR_UNSUPPORTED;
   if (o->pairs_t < 0 || o->pairs_h < 0 || o->pairs_w < 0) return VDA_ERR_SIZE;
@@ -296,7 +298,7 @@ int rope_impl(bool backward, const void* x, const void* dout, const float* inv_f
     return VDA_ERR_SIZE;
   const long long row = (long long)H * d;
   const size_t es = is_f32 ? 4 : 2;
-  const long long xs = o->x_row_stride ? o->x_row_stride : row;
+  const long long xs = reads_x && o->x_row_stride ? o->x_row_stride : row;
   const long long ds = backward && o->dx_row_stride ? o->dx_row_stride : row;
   // One workgroup of 256 threads per four tokens; a workgroup's items are 32-bit.
   if (row > 0x7fffffffLL / 64 || xs < row || ds < row || (long long)B * L > (kMaxThreads / 256) * 4 ||
@@ -308,9 +310,8 @@ int rope_impl(bool backward, const void* x, const void* dout, const float* inv_f
     return VDA_ERR_ALIGN;
   const size_t rows = (size_t)B * L;
   auto bytes = [&](long long stride) { return ((rows - 1) * stride + row) * es; };
-  const bool reads_x = !backward || o->l2;
   if (any_overlap({range_of(out, bytes(ds))},
-                  {opt_range(reads_x ? x : nullptr, bytes(xs)), opt_range(dout, bytes(row)),
+                  {opt_range(x, bytes(xs)), opt_range(dout, bytes(row)),
                    range_of(inv_freq, (size_t)pairs * 4), opt_range(positions, rows * 12)}))
     return VDA_ERR_OVERLAP;
   vda::RopeArgs a = {};

@@ -847,7 +847,7 @@ def rope(x, inv_freq, axes, H, positions=None, grid=None, frame_offset=0, interl
 def rope_backward(dout, inv_freq, axes, H, x=None, positions=None, grid=None, frame_offset=0,
                   interleaved=True, l2=False, layout="heads", out=None, stream=None):
     """The gradient of rope (vda_rope_backward): dout in the output's layout,
-    x the forward input (needed with l2 only); the other arguments as there.
+    x the forward input (needed and read with l2 only); the other arguments as there.
     Returns dx [B, L, H * d] (`out` may be a slice of a fused gradient)."""
     dt, dev = _storage(dout, "dout")
     if layout == "heads":
@@ -863,6 +863,8 @@ def rope_backward(dout, inv_freq, axes, H, x=None, positions=None, grid=None, fr
                    layout, dev)
     if l2 and x is None:
         raise ValueError("x is needed with l2")
+    if not l2:
+        x = None  # not read
     for t, n in ((x, "x"), (out, "out")):
         if t is None:
             continue

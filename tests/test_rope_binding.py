@@ -47,3 +47,32 @@ def test_head_counts_below_one_through_the_calls(H, layout):
         vda.rope(x, f, (8, 0, 0), H, grid=(2, 2), layout=layout)
     with pytest.raises(ValueError):
         vda.rope_backward(x, f, (8, 0, 0), H, grid=(2, 2), layout=layout)
+
+
+def test_input_that_is_not_read_is_not_checked():
+    """Without l2 the gradient does not read x.  (Every call below is refused for its output's place, after the checks
+    of alignment and strides, so nothing is launched on the made-up addresses.)"""
+    import ctypes
+    big = 1 << 36
+
+    def call(x, stride, l2):
+        o = vda.VdaRopeOptions(8, 8, 16, 1, l2, 0, 1, 1, 0, stride, 0)
+        return vda.lib.vda_rope_backward(2 * big, x, 3 * big, 4 * big, 2, 10, 3, 64, ctypes.byref(o), 0, 2 * big, None)
+
+    overlap, align, size = 5, 4, 2
+    assert call(None, 0, 0) == overlap
+    assert call(big + 8, 0, 0) == overlap and call(big + 8, 0, 1) == align
+    assert call(big, 100, 0) == overlap and call(big, 100, 1) == size
+    assert call(big, 196, 0) == overlap and call(big, 196, 1) == align
+
+
+@pytest.mark.gpu
+def test_input_that_is_not_read_may_have_any_form():
+    f = torch.rand(16, device="cuda")
+    dy = torch.randn(2, 6, 2 * 32, device="cuda")
+    kw = dict(grid=(2, 3), layout="tokens")
+    want = vda.rope_backward(dy, f, (4, 6, 6), 2, **kw)
+    x = torch.zeros(2, 12, 2 * 32 + 1, device="cuda")[:, ::2, 1:]
+    assert torch.equal(vda.rope_backward(dy, f, (4, 6, 6), 2, x=x, **kw), want)
+    with pytest.raises(ValueError):
+        vda.rope_backward(dy, f, (4, 6, 6), 2, x=x, l2=True, **kw)
