@@ -32,8 +32,8 @@ namespace {
 // owns 16 value columns of dS, transposed, in registers.  MAP: only what a
 // segment adds to the gradient that enters it (its map's matrix is the
 // forward one's transpose).  Bound by memory where its workgroups fill the
-// device: 135 us for 16401 tokens of 16 heads, 128 x 128, 5.4 TB/s; the map
-// 87 us.
+// device: 134 us for 16401 tokens of 16 heads, 128 x 128, 5.4 TB/s; the map
+// 83 us.
 template <bool F32, int DK, int DV, bool MAP>
 __global__ __launch_bounds__(4 * DV) __attribute__((amdgpu_waves_per_eu(1, 2)))
 void delta_reverse_kernel(DeltaArgs a) {
@@ -269,7 +269,7 @@ void delta_reverse_kernel(DeltaArgs a) {
 // and key channels are taken in twisted order, value channels in paired order
 // (vda_delta.h).
 //
-// 309 us for 16401 tokens of 16 heads, 128 x 128, bf16: the copies alone take
+// 310 us for 16401 tokens of 16 heads, 128 x 128, bf16: the copies alone take
 // 267 us (3.6 TB/s: with 142 KB of LDS one workgroup runs on a compute unit, one
 // step's 52 KB on the way); the heads' ends, short chains of reads, sums over
 // lanes and barriers, hide least of theirs.
@@ -650,7 +650,6 @@ hipError_t launch_delta_reverse(bool f32, int d_k, bool map, const DeltaArgs& a,
 }
 
 hipError_t launch_delta_grad(bool f32, int d_k, const DeltaArgs& a, hipStream_t stream) {
-  if (a.max_chunks == 0) return hipSuccess;
   switch (d_k) {
     case 32: return f32 ? grad<true, 32>(a, stream) : grad<false, 32>(a, stream);
     case 64: return f32 ? grad<true, 64>(a, stream) : grad<false, 64>(a, stream);
