@@ -527,7 +527,7 @@ typedef enum {
  * fp32); its tokens, in order, give
  *     Sbar = exp(g_t) S,   e_t = v_t - Sbar k_t,
  *     S = Sbar + beta_t e_t k_t^T,   o_t = scale * S q_t.
- *  - T tokens in n_seqs sequences: with cu_seqlens NULL, n_seqs sequences of
+ *  - T >= 1 tokens in n_seqs >= 1 sequences: with cu_seqlens NULL, n_seqs sequences of
  *    T / n_seqs consecutive tokens each (VDA_ERR_SIZE if that is no whole
  *    number); otherwise cu_seqlens is a DEVICE pointer to n_seqs + 1 int32
  *    offsets, not decreasing, sequence i being tokens cu_seqlens[i] ..
@@ -549,7 +549,9 @@ typedef enum {
  *    whatever its finite key and value) are fp32.
  * A NaN or infinity in a token's q, k, v, g or beta (but g = -inf) makes the
  * outputs of its group of 64 tokens (counted from the sequence's first) of its head undefined,
- * and those of all later ones; other sequences and heads are not touched.
+ * and those of all later ones; other sequences and heads are not touched.  In the
+ * backward pass it, or one in dout, makes all gradients of its sequence and head
+ * undefined, dq and dk of the key head among them.
  * bf16 storage: products run on bf16 matrix cores with fp32 accumulation;
  * the state, what is written to it and the triangular inverses are carried as
  * two bf16 parts (about 16 mantissa bits) where they enter a product, once
@@ -577,8 +579,10 @@ typedef struct vda_delta_problem {
  *    kept.  Calls that may run at the same time (other streams, graphs
  *    replayed side by side) need buffers of their own.
  * Long sequences of few heads are cut into segments whose maps are scanned
- * side by side and joined (fp32), so results depend on the sizes, but not on
- * timing: equal calls on equal devices give equal bits.
+ * side by side and joined (fp32), so results depend on the sizes.  No sum's
+ * order depends on timing: equal calls on equal devices are to give equal bits.
+ * (One pair of equal calls has been seen to differ while this was developed, for
+ * a reason that was not found, and none since.)
  * q, k, v, out, states and work 16-byte aligned, g, beta and cu_seqlens 4-byte
  * aligned; no output or work buffer may overlap an input or another output
  * (S_out is not S_in).  Nothing is allocated or copied: the call can be
@@ -602,10 +606,10 @@ size_t vda_delta_forward_workspace(const vda_delta_problem* p);
  *    them), dg, dbeta as g, beta, fp32; dS_in [n_seqs][H_v][d_v][d_k] fp32 or
  *    NULL.  dg is the gradient of the log decay; where g < -200 (a decay of
  *    zero in fp32) it is 0.
- *  - work: vda_delta_backward_workspace(p) bytes, as above: mostly the states
- *    at every 64th token, what the tokens write, and the gradients of both,
- *    8 d_v (d_k + 64) bytes per 64 tokens of a head.
- * Deterministic; otherwise as vda_delta_forward.
+ *  - work: vda_delta_backward_workspace(p) bytes, as above: for each 64 tokens
+ *    of a value head, the states there, the tokens' errors e_t and the gradients
+ *    of both, 8 d_v (d_k + 64) bytes, and a record of 38 KB.
+ * No sum's order depends on timing; otherwise as vda_delta_forward.
  */
 int vda_delta_backward(const vda_delta_problem* p, const void* dout, const void* q, const void* k,
                        const void* v, const float* g, const float* beta, const float* S_in,

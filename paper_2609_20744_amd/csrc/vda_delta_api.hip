@@ -60,23 +60,36 @@ vda::DeltaPlan plan_of(const vda_delta_problem* p, bool backward) {
   const long long longest = table ? (T + vda::kChunk - 1) / vda::kChunk : per;
   d.max_chunks = (int)(table ? (T + (vda::kChunk - 1) * n) / vda::kChunk : per * n);
   // Segments.  A sequence that is cut costs each of its chunks a second scan
-  // (the segment's map) and a step of the join per segment.  Where sequences
-  // and heads alone fill the compute units, only one that is far longer than
-  // the rest is cut: 24 uneven sequences of 16411 tokens with 16 heads took
-  // 233 us whole and 296 us cut into segments of 18 chunks.  Where they do not,
-  // every unit gets a segment: the backward pass of 9 such sequences took 1.08 ms
-  // cut and 1.43 ms whole, one sequence of 1560 tokens with 24 heads takes 64 us
-  // cut and 97 whole.  Shorter segments make the scans shorter (11 us a chunk
-  // for maps and outputs, 128 x 128, bf16) and the join longer (1.2 us a
-  // segment): the least time is at about the square root of an eighth of the
-  // sequence's chunks.  8 heads, segments of 4 chunks and so: 1088 tokens 55 and
-  // 44 us; 2 heads of 38400 tokens, segments of 5 chunks and so: 199 and 171 us.
-  // Shorter sequences stay whole: of 8 heads, in bf16, eight chunks take 35 us
-  // whole and 37 cut, and 84 and 83 backward (nine 38 and 38, 92 and 86); in
-  // fp32 with 64 channels, whose chunks take twice the time, six take 47 and 42,
-  // 94 and 91 in a graph, but more launches (eight 58 and 43, 114 and 93).
-  // Segments that the compute units make longer than two chunks pay from the
-  // fourth on.
+  // (5.9 us beside an output's 3.4, 128 x 128, bf16) and a step of the join per
+  // segment (1.1 us).  Figures: us of a forward and a backward call, bf16,
+  // 128 x 128 where not said.
+  //  - Where sequences and heads alone fill the compute units, only one that is
+  //    far longer than the rest is cut, into segments of four times the mean.  24
+  //    uneven sequences of 16411 tokens, 16 heads: 158 and 722 whole (166 and 738
+  //    as here, with maps and a join that find nothing to do), 184 and 755 in
+  //    segments of 16 chunks.  40 sequences of 4 chunks in the mean, 8 heads, one of
+  //    them 12 times as long: 198 and 522 as here, 184 and 559 whole, 139 and 410
+  //    in segments of twice the mean; one 6 times as long: 161 and 434, 109 and
+  //    383, 116 and 393.  So four is right for what it leaves whole, and too long
+  //    for what it cuts.
+  //  - Where they do not, every unit gets a segment: 9 uneven sequences of 16401
+  //    tokens, 16 heads, 218 and 786 cut, 389 and 1308 whole; 1560 tokens of 24
+  //    heads 64 and 173 cut, 95 and 250 whole.
+  //  - Shorter segments make the scans shorter and the join longer: the least time
+  //    is at about the square root of an eighth of the sequence's chunks.  8 heads
+  //    of 1088 tokens in segments of 2, 3 and 4 chunks 45, 48 and 55 (100, 108 and
+  //    120); 2 heads of 38400 tokens of 5, 7, 9 and 12 chunks 205, 179, 172 and 175
+  //    (569, 495, 473 and 473).
+  //  - Short sequences stay whole.  8 heads of eight chunks: 36 and 84 whole, 38 and
+  //    83 in segments of two chunks (nine: 39 and 92, 39 and 87; 24 heads of nine: 39
+  //    and 99, 43 and 97; 64 channels, nine: 25 and 51, 24 and 50).  fp32, six chunks:
+  //    64 channels 47 and 94 whole, 43 and 91 cut, in two more launches and four
+  //    (seven: 52 and 104, 43 and 92); 128 channels 115 and 225, 97 and 212 (five: 98
+  //    and 196, 97 and 211).
+  //  - Segments that the compute units make longer than two chunks pay from the
+  //    fourth on, or later: of three chunks, 32 heads of 24 chunks 67 and 202 cut, 93
+  //    and 261 whole, but 64 heads of 12 chunks 65 and 194 cut, 55 and 175 whole; of
+  //    six chunks, 64 heads of 24 chunks 99 and 357 cut, 102 and 374 whole.
   const long long cus = vda::current_device_cus();
   long long share = std::max(2LL, (d.max_chunks * (long long)p->H_v + cus - 1) / cus);
   while (8 * share * share < longest) ++share;

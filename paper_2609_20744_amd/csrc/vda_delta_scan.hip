@@ -18,8 +18,8 @@
 // is waited for with, 40320 tokens of 7 heads went from 455 to 362 us).  What
 // bounds it, bf16, 128 x 128: where a workgroup runs alone the chain of a chunk,
 // 3.4 us (matrix cores, LDS and vector ALUs are busy a third of it each); with
-// one on every compute unit memory, 83 KB a chunk: 86 us for the outputs of
-// those 40320 tokens, 4.3 TB/s, and 108 us for what the gradient kernel reads
+// one on every compute unit memory, 83 KB a chunk: 90 us for the outputs of
+// those 40320 tokens, 4.1 TB/s, and 106 us for what the gradient kernel reads
 // (16401 tokens, 16 heads), 5.7 TB/s.  The maps' 5.9 us a chunk are products and
 // vector operations, twice those of a scan.  Outputs that went through LDS to
 // be stored in whole lines were 2% slower than eight bytes a lane.

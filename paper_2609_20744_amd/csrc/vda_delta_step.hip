@@ -4,13 +4,14 @@
 // The call reads and writes each state once, 8 d_v d_k bytes, beside which
 // everything else is small, so it is bound by HBM for a full batch and by latency
 // for one sequence.  The rows of a state are independent but for k and q: a
-// group of d_k / 8 lanes (at most 16) holds a row, a wave ROWS rows, all
+// group of d_k / 4 lanes (at most 16) holds a row, a wave ROWS rows, all
 // loaded before the first is used, and the rows stay in registers over the
 // call's tokens.  Both products with the state take it before the update,
 //     u = S k, w = S q:  e = v - a u,  S <- a S + beta e k,  o = scale (a w + beta e (k.q)),
 // so their sums over a row's lanes (DPP adds within 16 lanes) run together.
-// fp32 throughout.  192 sequences of 32 heads, 128 x 128: 154 us, 5.26 TB/s (a
-// large copy: 4.96); one sequence of 16 heads: 4.5 us.
+// fp32 throughout.  192 sequences of 32 heads, 128 x 128: 163 us, 4.98 TB/s (a
+// large copy: 4.96; rows of padding cost nothing: 180 of 192, 153 us); one
+// sequence of 16 heads: 4.5 us.
 #include "vda_delta.h"
 #include "vda_delta_step.h"
 

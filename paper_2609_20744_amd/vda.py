@@ -672,7 +672,8 @@ def delta_forward(q, k, v, g, beta, cu_seqlens=None, layout="heads", scale=None,
     return_state.  work: a device buffer of delta_workspace(...) bytes
     (allocated if None); calls that may run at the same time need their own.
     Packed rows outside every sequence are left as they are in `out` (a new
-    output holds anything there)."""
+    output holds anything there).  Nothing is recorded for autograd: the
+    gradients come from delta_backward."""
     p, states, dt, dev = _delta_problem(q, k, v, g, beta, cu_seqlens, layout, scale)
     if state is not None:
         _expect(state, "state", states, torch.float32, dev)
@@ -825,7 +826,8 @@ def rope(x, inv_freq, axes, H, positions=None, grid=None, frame_offset=0, interl
     axes].  The tokens' positions: `positions` int32 [B, L, 3], or grid =
     (height, width) with the first frame at frame_offset.  l2 divides each
     token of each head by its length first.  Returns [B * H, L, d] (layout
-    'heads', as prep) or [B, L, H * d] ('tokens')."""
+    'heads', as prep) or [B, L, H * d] ('tokens').  Nothing is recorded for
+    autograd: the gradient comes from rope_backward."""
     dt, dev = _storage(x, "x")
     row = _token_rows(x, "x", H)
     B, L, C = x.shape
