@@ -546,7 +546,8 @@ typedef enum {
  *    g (log decay, <= 0; -inf resets the state; positive values are not
  *    checked, and grow it) and beta (write strength, any sign; the rule is
  *    stable for beta |k|^2 in [0, 2]; a token of strength 0 writes nothing,
- *    whatever its finite key and value) are fp32.
+ *    whatever its key and value are, if their products with each other, the
+ *    queries and the state are finite in fp32) are fp32.
  * A NaN or infinity in a token's q, k, v, g or beta (but g = -inf) makes the
  * outputs of its group of 64 tokens (counted from the sequence's first) of its head undefined,
  * and those of all later ones; other sequences and heads are not touched.  In the

@@ -11,9 +11,9 @@
 //     S <- gam_63 S + N^T diag(eta) K
 // T and P do not depend on the state; the chunk-preparation kernel makes them
 // for all chunks at once, and the scans carry the state.  With the strengths on
-// the right of L, a token of strength 0 has a column of zeros in T and a row of
-// zeros in N, whatever its key and value are, and beta's gradient, E's with
-// respect to N, needs no division by a strength.
+// the right of L, a token of strength 0 has zeros in its column of T (but the
+// diagonal) and its row of N, whatever its key and value are, and beta's gradient,
+// E times that of N, needs no division by a strength.
 #pragma once
 
 #include "vda_common.h"

@@ -24,16 +24,17 @@ SHAPES = [dict(lens=[100], Hk=1, dk=32, dv=32), dict(lens=[70, 0, 130], Hk=2, gr
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shape", SHAPES, ids=["32", "packed", "cut"])
 def test_tokens_of_no_strength_hold_anything_finite(V, shape, dtype):
-    """Padding inside a sequence: strength 0 and values of 1e20 there.  Nothing of them reaches a state, another
-    token's output or another token's gradient."""
-    print(f"strength 0, values of 1e20: {shape} {dtype}", flush=True)
+    """Padding inside a sequence: strength 0, keys of 1e10 and values of 1e20 there.  Nothing of them reaches a state,
+    another token's output or another token's gradient."""
+    print(f"strength 0, keys of 1e10, values of 1e20: {shape} {dtype}", flush=True)
     c = Case(dtype=dtype, **shape)
     T = c.host["beta"].shape[1]
     pad = np.random.default_rng(11).random(T) < 0.2
     pad[-1] = True
     c.host["beta"][:, pad] = 0.0
     c.host["v"][:, pad] *= 1e20
-    for x in ("beta", "v"):
+    c.host["k"][:, pad] *= 1e10
+    for x in ("beta", "v", "k"):
         c.dev[x] = c.to_layout(c.host[x])
     c.check_forward(*c.forward(V))
     got, want = c.backward(V), c.oracle_backward()
