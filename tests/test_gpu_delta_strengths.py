@@ -75,3 +75,26 @@ def test_no_strength_at_all(V):
     assert all((t == 0).all() for t in (dq, dk, dv, dg))
     want = c.oracle_backward()[4]
     assert np.linalg.norm(want) > 0 and _err(c.back(dbeta), want) <= TOL_F32_OUT["bf16"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shape", SHAPES, ids=["32", "packed", "cut"])
+def test_strengths_up_to_two_and_below_zero(V, shape, dtype):
+    """The whole range that is stable for keys of length 1, and some tokens that are unlearned.  Writes are up to twice
+    the errors that the tolerances count roundings of, so twice those."""
+    import torch
+    print(f"strengths in [-0.25, 2]: {shape} {dtype}", flush=True)
+    c = Case(dtype=dtype, **shape)
+    rng = np.random.default_rng(12)
+    b = c.host["beta"]
+    b.uniform_(0, 2, generator=torch.Generator().manual_seed(5))
+    b[:, rng.random(b.shape[1]) < 0.1] = -0.25
+    c.dev["beta"] = c.to_layout(b)
+    out, S = c.forward(V)
+    ref, last = c.oracle()
+    assert _err(c.back(out), ref) <= 2 * TOL_OUT[dtype]
+    assert _err(S.double().cpu().numpy(), last) <= 2 * TOL_F32_OUT[dtype]
+    for name, g, w in zip(("dq", "dk", "dv", "dg", "dbeta"), c.backward(V), c.oracle_backward()):
+        e, tol = _err(c.back(g), w), 2 * (TOL_OUT[dtype] if name in ("dq", "dk", "dv") else TOL_F32_OUT[dtype])
+        print(name, f"{e:.1e}", flush=True)
+        assert e <= tol, (name, e, tol)
