@@ -172,7 +172,7 @@ def prepare(case, seed):
         if op == "recur_step":
             s["state"] = randn(case["slots"], C)
             slots = torch.randperm(case["slots"], generator=g, device="cuda")[:n].to(torch.int32)
-            slots[rand(n) < 0.06] = -1
+            slots[1:][rand(n - 1) < 0.06] = -1
             s["slots"], s["out"] = slots, torch.zeros_like(s["x"])
             return s
         s["cu"] = _cuts(case["T"], n, g) if case["ragged"] else None
@@ -193,7 +193,7 @@ def prepare(case, seed):
         s["k_lens"] = _filled(m, S, g) if case["uneven"] else None
         # Streams of one prompt share its slot; a few rows are padding.
         slots = torch.randint(0, m, (n,), generator=g, device="cuda", dtype=torch.int32)
-        slots[rand(n) < 0.06] = -1
+        slots[1:][rand(n - 1) < 0.06] = -1
         s["slots"], s["out"] = slots, torch.zeros_like(s["q"])
         return s
 
