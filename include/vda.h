@@ -702,6 +702,214 @@ int vda_rope_backward(const void* dout, const void* x, const float* inv_freq, co
                       int B, int L, int H, int d, const vda_rope_options* opts, int is_f32, void* dx,
                       hipStream_t stream);
 
+/* ------------------------------------------------------------------------- */
+/* Cross attention to an encoder's states                                     */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * One problem of softmax attention from a sequence's queries to the states of
+ * an encoder (a prompt, audio), of another length: the attention that stays
+ * Softmax beside the linear branch (Sec. 2.1).  Per sequence and query head h,
+ * with key head h / G, G = H_q / H_k, over the states j that are seen,
+ *     s_j = scale * q . k_j,   lse = log sum_j exp(s_j),
+ *     out = sum_j exp(s_j - lse) v_j.
+ * A query that sees no state has out = 0 and lse = -inf, and leaves no gradient.
+ *  - T >= 1 query tokens and S >= 1 states in n_seqs >= 1 sequences.  cu_q
+ *    NULL: T / n_seqs tokens each (VDA_ERR_SIZE if that is no whole number);
+ *    otherwise a DEVICE pointer to n_seqs + 1 int32 offsets, as cu_seqlens of
+ *    vda_delta_problem.  cu_k likewise for the states.  Sequences may be empty.
+ *    Rows of outputs before the first and behind the last sequence are left as
+ *    they are.
+ *  - k_lens: NULL, or a DEVICE pointer to n_seqs int32: of sequence i's states the
+ *    first k_lens[i] are seen (values outside [0, its states] are taken as the
+ *    nearest bound).
+ *  - k_mask: NULL, or a DEVICE pointer to S bytes, one per state in the order of
+ *    the sequences: a state whose byte is 0 is not seen.  Whatever k and v hold
+ *    where a state is not seen (infinities and NaN too) changes nothing; such
+ *    states have gradients of 0.
+ *  - H_q a multiple of H_k, at most 1024 times it; d in {32, 64, 128}.
+ *  - layout (of q and dq), out_layout (of out and dout), kv_layout (of k, v and
+ *    their gradients), each a vda_layout: tokens [T][H][d]; heads [H][T][d]
+ *    where the tensor's sequences are packed (its offsets given), and
+ *    [n_seqs][H][T / n_seqs][d] where they are of equal length.
+ *  - q_row_stride, k_row_stride, v_row_stride, dq_row_stride, dk_row_stride,
+ *    dv_row_stride: elements from one token's row to the next in the tokens
+ *    layout, 0 for H * d; larger where the tensor is a slice of a fused
+ *    projection.  A multiple of 16 bytes, below 2^24 bytes.  In the heads layout
+ *    VDA_ERR_UNSUPPORTED unless 0.
+ *  - storage of q, k, v, out and their gradients: bf16 (is_f32 == 0) or fp32.
+ *    lse is fp32, the natural logarithm: [H_q][T] with cu_q, else
+ *    [n_seqs][H_q][T / n_seqs].
+ * A NaN or infinity in q, or in a state that is seen, makes the rows that meet it
+ * undefined, in the backward pass the gradients of its sequence and key head.
+ * bf16 storage: products run on bf16 matrix cores with fp32 accumulation, the
+ * softmax and its sums are fp32, and its weights (and the scores' gradients) are
+ * rounded to bf16 once, where they enter a product.  fp32 storage: fp32
+ * throughout.
+ */
+typedef struct vda_cross_problem {
+  int T, S;
+  int n_seqs;
+  const int* cu_q;
+  const int* cu_k;
+  const int* k_lens;
+  const unsigned char* k_mask;
+  int H_q, H_k;
+  int d;
+  int layout, kv_layout, out_layout;
+  int q_row_stride, k_row_stride, v_row_stride;
+  int dq_row_stride, dk_row_stride, dv_row_stride;
+  int is_f32;
+  float scale;
+} vda_cross_problem;
+
+/*
+ * vda_cross_forward -- the attention over whole sequences.
+ *  - lse: [..] fp32 as above, written for the backward pass, or NULL.
+ *  - work: a caller-owned DEVICE buffer of vda_cross_forward_workspace(p)
+ *    bytes, queried with the call's device current (may be NULL where that is 0);
+ *    its contents need not be kept.  Calls that may run at the same time (other
+ *    streams, graphs replayed side by side) need buffers of their own.
+ * Where the queries are too few to fill the device, ranges of the states are
+ * taken side by side and joined (fp32), so results depend on the sizes.  No
+ * sum's order depends on timing.
+ * Tensors and work 16-byte, lse, offsets and lengths 4-byte aligned; no output or
+ * work buffer may overlap an input or another output.  Nothing is allocated or
+ * copied: the call can be captured into a graph.  Errors: VDA_ERR_NULL,
+ * VDA_ERR_SIZE, VDA_ERR_UNSUPPORTED (d, layouts), VDA_ERR_ALIGN,
+ * VDA_ERR_OVERLAP, VDA_ERR_HIP.
+ */
+int vda_cross_forward(const vda_cross_problem* p, const void* q, const void* k, const void* v,
+                      void* out, float* lse, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_cross_forward on the current device (0 also
+ * for an invalid problem). */
+size_t vda_cross_forward_workspace(const vda_cross_problem* p);
+
+/*
+ * vda_cross_backward -- the gradients of vda_cross_forward: given dout (of
+ * out), the forward pass's inputs and its out and lse, those of q, k and v.
+ * dk and dv are summed over the query heads that share a key head, and 0 for
+ * states that are not seen.  dk and dv may be slices of one fused gradient
+ * (equal row strides).  Otherwise as vda_cross_forward.
+ */
+int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void* q, const void* k,
+                       const void* v, const void* out, const float* lse, void* dq, void* dk,
+                       void* dv, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_cross_backward on the current device (0 for
+ * an invalid problem). */
+size_t vda_cross_backward_workspace(const vda_cross_problem* p);
+
+/*
+ * vda_cross_step -- a few tokens of each of n_seqs sequences against a pool of
+ * cached states: p->T = n_seqs * tokens of each, p->S = n_slots * states of a
+ * slot (equal lengths: cu_q and cu_k NULL).
+ *  - slots: DEVICE pointer to n_seqs int32, the slot that sequence i reads (the
+ *    same one may be given more than once), or NULL (slot i; then n_seqs <=
+ *    n_slots).  A slot outside [0, n_slots) marks padding: nothing of that row is
+ *    read, and its part of out is left as it is.
+ *  - k, v [n_slots][states][H_k][d] (tokens) or [n_slots][H_k][states][d]
+ *    (heads); k_lens [n_slots] and k_mask [n_slots][states] belong to the slots.
+ *  - work: vda_cross_step_workspace(p, n_slots) bytes, as above.
+ * Bound by reading the states.  Otherwise as vda_cross_forward.
+ */
+int vda_cross_step(const vda_cross_problem* p, const void* q, const void* k, const void* v,
+                   const int* slots, int n_slots, void* out, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_cross_step on the current device (0 also for
+ * an invalid problem). */
+size_t vda_cross_step_workspace(const vda_cross_problem* p, int n_slots);
+
+/* ------------------------------------------------------------------------- */
+/* The channel-wise gated recurrence                                          */
+/* ------------------------------------------------------------------------- */
+
+/* How a token's gate g gives its decay a and what it adds, u. */
+typedef enum {
+  VDA_GATE_LOG = 0,   /* a = exp(g), u = x: g fp32, <= 0 (-inf resets the state)   */
+  VDA_GATE_LOGIT = 1, /* a = sigmoid(g), u = (1 - a) x: g in the storage type     */
+  VDA_GATE_NORM = 2   /* a = sigmoid(g), u = sqrt(1 - a^2) x: likewise            */
+} vda_gate;
+
+/*
+ * One problem of the channel-wise recurrence, the rule of vda_delta_problem with
+ * a diagonal in place of the keys: for each channel of each sequence, from a state
+ * h_0, the tokens in order give
+ *     h_t = a_t h_{t-1} + u_t,   out_t = h_t.
+ *  - T, n_seqs, cu_seqlens: as in vda_delta_problem.
+ *  - C >= 1 channels, a multiple of 8 (VDA_ERR_UNSUPPORTED).
+ *  - gate: a vda_gate.
+ *  - reverse: the tokens are taken from the last to the first (the states are then
+ *    those behind the first token).
+ *  - x, g, out and their gradients are [T][C], rows of x, g, dx and dg
+ *    x_row_stride, g_row_stride, dx_row_stride, dg_row_stride elements apart
+ *    (0 for C; larger where they are slices of a fused projection; a multiple of
+ *    16 bytes).  Storage of x, out, dout and dx: bf16 (is_f32 == 0) or fp32;
+ *    of g and dg: fp32 with VDA_GATE_LOG, else the same.
+ * A NaN or infinity in a token's x or g (but g = -inf) makes the outputs of its
+ * channel and sequence from its group of 128 tokens on undefined, and in the
+ * backward pass, as one in dout, all gradients of its channel and sequence;
+ * nothing else.  A positive log decay is not checked, and grows the state.
+ * States and sums are fp32, and outputs are rounded once.
+ */
+typedef struct vda_recur_problem {
+  int T;
+  int n_seqs;
+  const int* cu_seqlens;
+  int C;
+  int gate;
+  int reverse;
+  int x_row_stride, g_row_stride, dx_row_stride, dg_row_stride;
+  int is_f32;
+} vda_recur_problem;
+
+/*
+ * vda_recur_forward -- the recurrence over whole sequences.
+ *  - S_in: the states the sequences start from, [n_seqs][C] fp32, or NULL
+ *    (zero).  S_out: the states that they end with, likewise, or NULL.  An empty
+ *    sequence's state passes through.
+ *  - work: a caller-owned DEVICE buffer of vda_recur_forward_workspace(p) bytes
+ *    (may be NULL where that is 0); its contents need not be kept.  Calls that may
+ *    run at the same time need buffers of their own.
+ * No sum's order depends on timing.  x, g, out, states and work 16-byte aligned,
+ * cu_seqlens 4-byte; no output or work buffer may overlap an input or another
+ * output.  Nothing is allocated or copied: the call can be captured into a
+ * graph.  Errors: VDA_ERR_NULL, VDA_ERR_SIZE, VDA_ERR_UNSUPPORTED (C, gate),
+ * VDA_ERR_ALIGN, VDA_ERR_OVERLAP, VDA_ERR_HIP.
+ */
+int vda_recur_forward(const vda_recur_problem* p, const void* x, const void* g, const float* S_in,
+                      void* out, float* S_out, void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_recur_forward (0 also for an invalid problem). */
+size_t vda_recur_forward_workspace(const vda_recur_problem* p);
+
+/*
+ * vda_recur_backward -- the gradients of vda_recur_forward: given dout (of
+ * out) and dS_out (of S_out, or NULL: zero), those of x, g and S_in.  Nothing is
+ * kept from the forward call: states are computed again.  dS_in [n_seqs][C]
+ * fp32 or NULL; dx and dg may be slices of one fused gradient (equal row strides
+ * and types).  Otherwise as vda_recur_forward.
+ */
+int vda_recur_backward(const vda_recur_problem* p, const void* dout, const void* x, const void* g,
+                       const float* S_in, const float* dS_out, void* dx, void* dg, float* dS_in,
+                       void* work, hipStream_t stream);
+
+/* Bytes of the work buffer of vda_recur_backward (0 also for an invalid problem). */
+size_t vda_recur_backward_workspace(const vda_recur_problem* p);
+
+/*
+ * vda_recur_step -- the recurrent form: `tokens` further tokens of each of n
+ * sequences, whose states live in a pool and are updated in place.
+ *  - x, g, out [n][tokens][C] (types as above); state [n_slots][C] fp32.
+ *  - slots: as in vda_delta_step (distinct; one outside the pool marks padding, or
+ *    NULL: slot i).
+ * Needs no workspace.  Alignment, overlap (of out and of the whole pool) and
+ * errors as vda_recur_forward.
+ */
+int vda_recur_step(const void* x, const void* g, int n, int tokens, int C, int gate, int is_f32,
+                   const int* slots, int n_slots, float* state, void* out, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,328 @@
+// Internal definitions of the cross attention to an encoder's states (vda.h,
+// vda_cross_*), shared by its kernels and its host code.
+//
+// The query heads that share a key head are taken together: a sequence of lq
+// tokens has lq * group rows per key head, row r being token r / group of query
+// head key_head * group + r % group.  So states are read once for all of them, and
+// the gradients of a shared key head are one sum over rows.
+//
+// Every product runs on 32 x 32 results of which a lane holds one column: column
+// li = lane % 32, rows 8 (i / 4) + 4 lh + i % 4 (lh = lane / 32).  Scores are taken
+// transposed (states x queries) where a softmax runs along the states, so its
+// maximum and sum are a lane's own; and the 16 rows of a result that a lane half
+// holds are what the next product contracts, in the order of col_frag.
+#pragma once
+
+#include "vda_common.h"
+
+namespace vda {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+typedef short shortx8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+typedef __attribute__((address_space(1))) const void global_void;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kCrossTile = 64;   // states (or rows) of a tile in LDS
+constexpr int kCrossRows = 128;  // rows (or states) of a workgroup, 32 a wave
+constexpr int kFewRows = 32;     // rows of a workgroup whose waves share them
+
+// Where a tensor's tokens are: element strides.
+struct CrossStrides {
+  size_t tok, head, seq;  // seq: equal lengths only; a packed sequence starts tok * its first token in
+};
+
+struct CrossArgs {
+  const void *q, *k, *v, *o, *dout;
+  void *out, *dq, *dk, *dv;
+  const float* lse_in;
+  float* lse;
+  CrossStrides sq, sk, sv, so, sdq, sdk, sdv;  // so: out, its gradient and what the backward pass reads of it
+  const int *cu_q, *cu_k, *k_lens, *slots;
+  const uint8_t* k_mask;
+  int n, n_slots, T, S, Lq, Lk;
+  int Hq, Hk, group;
+  uint32_t group_magic;  // x / group = x * group_magic >> 24 for x < group + 64
+  float scale, c;        // c = |scale| log2 e
+  int flip;              // scale < 0: the sign of one factor of each score is changed
+  int tiles, splits;     // tiles of rows (of states in the gradient of k and v) of a head
+  float *part, *part2;  // workspace: what splits leave
+  float2* stats;        // [T * Hq] backward: lse in powers of two, and D = sum of dout o
+};
+
+// One sequence's queries and states.
+struct CrossSeq {
+  int i, kv;        // its index, and that of its states (the slot)
+  int q0, lq;       // packed: first token; tokens
+  int k0, lk, seen; // packed: first state; states; of which the length leaves `seen`
+};
+
+__device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// Offsets outside [0, total] are taken as the nearest bound, and a length below 0 as 0.
+__device__ __forceinline__ void packed_range(const int* cu, int i, int total, int& first, int& len) {
+  first = uniform(clamp_to(cu[i], 0, total));
+  const int end = uniform(clamp_to(cu[i + 1], 0, total));
+  len = end > first ? end - first : 0;
+}
+
+__device__ __forceinline__ CrossSeq cross_seq(const CrossArgs& a, int i) {
+  CrossSeq s;
+  s.i = s.kv = i;
+  s.q0 = s.k0 = 0;
+  s.lq = a.Lq, s.lk = a.Lk;
+  if (a.cu_q != nullptr) packed_range(a.cu_q, i, a.T, s.q0, s.lq);
+  if (a.cu_k != nullptr) packed_range(a.cu_k, i, a.S, s.k0, s.lk);
+  if (a.slots != nullptr) {
+    s.kv = uniform(a.slots[i]);
+    if (s.kv < 0 || s.kv >= a.n_slots) s.lq = s.lk = s.kv = 0;  // a row of padding
+  }
+  s.seen = s.lk;
+  if (a.k_lens != nullptr) s.seen = uniform(clamp_to(a.k_lens[s.kv], 0, s.lk));
+  return s;
+}
+
+__device__ __forceinline__ size_t seq_base(const CrossStrides& s, const int* cu, int first, int i) {
+  return cu != nullptr ? (size_t)first * s.tok : (size_t)i * s.seq;
+}
+
+// The sequence that tile `t` of a head belongs to, and which of its tiles it is;
+// sequence -1: none.  A packed sequence i has the tiles from first_i / per + i on,
+// first_i being its first row: as many places as it needs or one more, so no
+// table is made and every place is found from the offsets alone.
+__device__ __forceinline__ int2 seq_of_tile(const int* cu, int n, int total, int L, int group, int per, int t) {
+  if (cu == nullptr) {
+    const int each = (L * group + per - 1) / per;
+    const int i = uniform(t / each);
+    return make_int2(i < n ? i : -1, t - i * each);
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int b = 0; b < n; b += 64) {
+    const int i = b + lane;
+    const bool is = i < n && clamp_to(cu[i < n ? i : 0], 0, total) * group / per + i <= t;
+    before += __popcll(__ballot(is));
+  }
+  const int i = uniform(before) - 1;
+  if (i < 0) return make_int2(-1, 0);
+  const int from = uniform(clamp_to(cu[i], 0, total) * group / per + i);
+  return make_int2(from <= t ? i : -1, t - from);  // -1 for offsets that are out of order only
+}
+
+// ---------------------------------------------------------------------------
+// Operands: eight elements a lane.
+// ---------------------------------------------------------------------------
+template <bool F32>
+struct Frag;
+
+template <>
+struct Frag<false> {
+  typedef bf16x8 X;
+  static __device__ __forceinline__ floatx16 mma(X a, X b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  // Elements 8 t .. of a result, rounded: the first factor of a product that has two roundings at most.
+  static __device__ __forceinline__ X of(const floatx16& s, int t) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(s[8 * t + 2 * e], s[8 * t + 2 * e + 1]);
+    return __builtin_bit_cast(X, w);
+  }
+  static __device__ __forceinline__ X load(const void* p, size_t at) {
+    return *reinterpret_cast<const bf16x8*>((const uint16_t*)p + at);
+  }
+  static __device__ __forceinline__ X flip(X x) { return __builtin_bit_cast(X, __builtin_bit_cast(u32x4, x) ^ 0x80008000u); }
+  static __device__ __forceinline__ X zero() { return __builtin_bit_cast(X, u32x4{0u, 0u, 0u, 0u}); }
+  static __device__ __forceinline__ float value(X x, int e) { return (float)x[e]; }
+};
+
+template <>
+struct Frag<true> {
+  typedef floatx8 X;
+  static __device__ __forceinline__ floatx16 mma(X a, X b, floatx16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ X of(const floatx16& s, int t) {
+    X x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = s[8 * t + e];
+    return x;
+  }
+  static __device__ __forceinline__ X load(const void* p, size_t at) {
+    const floatx4* f = reinterpret_cast<const floatx4*>((const float*)p + at);
+    const floatx4 a = f[0], b = f[1];
+    return X{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+  static __device__ __forceinline__ X flip(X x) { return -x; }
+  static __device__ __forceinline__ X zero() { return X{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+  static __device__ __forceinline__ float value(X x, int e) { return x[e]; }
+};
+
+// ---------------------------------------------------------------------------
+// Tiles in LDS: rows of D channels, as they are in memory but for the order of a
+// row's 16-byte pieces: piece c of row r stands at place c ^ swizzle(r).  With it
+// the 16 lanes whose 16 bytes of one column LDS serves together (rows that differ
+// modulo 16) meet all banks, and so do the four rows by 64 bytes that a transposing
+// read takes.  A copy of 1 KB fills consecutive places, and reads whole rows.
+// ---------------------------------------------------------------------------
+template <bool F32, int D>
+struct CrossTile {
+  typedef typename Frag<F32>::X X;
+  static constexpr int kEs = F32 ? 4 : 2, kRow = D * kEs, kPieces = kRow / 16;
+  static __device__ __forceinline__ int swizzle(int r) {
+    if constexpr (kPieces >= 16) return (r & 3) << 2 | (r >> 2 & 3);
+    if constexpr (kPieces == 8) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+    return r >> 2 & 3;
+  }
+  // Channels 16 s + 8 lh .. + 7 of row li of the rows at byte `at` (a multiple of 16 rows in).
+  // The address is one addition to the tile's array: of a longer chain the
+  // compiler does not see which array it is in, and waits for copies into the others.
+  static __device__ __forceinline__ X row_frag(const char* tile, int at, int s, int lane) {
+    const int li = lane & 31, lh = lane >> 5;
+    const int row = at + li * kRow;
+    if constexpr (F32) {
+      const floatx4 a = *reinterpret_cast<const floatx4*>(tile + (row + ((4 * s + 2 * lh) ^ swizzle(li)) * 16));
+      const floatx4 b = *reinterpret_cast<const floatx4*>(tile + (row + ((4 * s + 2 * lh + 1) ^ swizzle(li)) * 16));
+      return X{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    } else {
+      return *reinterpret_cast<const bf16x8*>(tile + (row + ((2 * s + lh) ^ swizzle(li)) * 16));
+    }
+  }
+  // Channel 32 b + li of the rows 4 lh + e and 8 + 4 lh + e, e < 4, behind byte `at`.
+  static __device__ __forceinline__ X col_frag(const char* tile, int at, int b, int lane) {
+    if constexpr (F32) {
+      const int li = lane & 31, lh = lane >> 5;
+      X x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int r = (e >> 2) * 8 + 4 * lh + (e & 3);
+        x[e] = *reinterpret_cast<const float*>(
+            tile + (at + r * kRow + ((8 * b + (li >> 2)) ^ swizzle(r)) * 16 + (li & 3) * 4));
+      }
+      return x;
+    } else {
+      // ds_read_b64_tr_b16: lane i of 16 receives element i % 4 of the 8 bytes that lanes i / 4 + 4 e address.
+      shortx4 v[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int r = 8 * w + 4 * (lane >> 5) + (lane >> 2 & 3);
+        const int piece = 4 * b + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_shortx4*)(tile + (at + r * kRow + (piece ^ swizzle(r)) * 16 + (lane & 1) * 8)));
+      }
+      return __builtin_bit_cast(bf16x8, shortx8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]});
+    }
+  }
+  // Writes zeros over the rows whose bit is not set.
+  template <int ROWS, int THREADS>
+  static __device__ __forceinline__ void clear_rows(char* tile, int at, uint64_t bits, int tid) {
+    for (int p = tid; p < ROWS * kPieces; p += THREADS)
+      if (!(bits >> (p / kPieces) & 1)) *reinterpret_cast<uint4*>(tile + (at + p * 16)) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  static constexpr int kCopies = kCrossTile * kRow / 1024;  // of a tile of 64 rows
+};
+
+// Copies ROWS rows of consecutive tokens into a tile; rows behind `last` repeat
+// it.  base: the tile's first row.
+template <bool F32, int D, int ROWS, int WAVES>
+__device__ __forceinline__ void copy_states(const void* base, size_t row_elems, int last, char* tile, int wave, int lane) {
+  typedef CrossTile<F32, D> Tile;
+  const __amdgpu_buffer_rsrc_t src = make_rsrc(base, 0xfffffff0u);
+  const uint32_t row_bytes = (uint32_t)row_elems * Tile::kEs;
+#pragma unroll
+  for (int i = 0; i < ROWS * Tile::kRow / 1024 / WAVES; ++i) {
+    const int p = wave + i * WAVES, at = p * 64 + lane;
+    const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
+                                             (uint32_t)(r < last ? r : last) * row_bytes + piece * 16u, 0, 0, 0);
+  }
+}
+
+// Copies 64 rows of queries (token x head) into a tile; rows behind `last` repeat it.
+// base: the sequence's first token of the key head's first query head.
+template <bool F32, int D, int WAVES>
+__device__ __forceinline__ void copy_rows(const CrossArgs& a, const void* base, const CrossStrides& s, int r0, int last,
+                                          char* tile, int wave, int lane) {
+  typedef CrossTile<F32, D> Tile;
+  const int t0 = r0 / a.group, g0 = r0 - t0 * a.group;
+  const char* from = (const char*)base + (size_t)t0 * s.tok * Tile::kEs;
+#pragma unroll
+  for (int i = 0; i < Tile::kCopies / WAVES; ++i) {
+    const int p = wave + i * WAVES, at = p * 64 + lane;
+    const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
+    const uint32_t x = g0 + (r < last ? r : last);
+    const uint32_t t = x * a.group_magic >> 24, g = x - t * a.group;
+    __builtin_amdgcn_global_load_lds((global_void*)(from + (t * s.tok + g * s.head) * Tile::kEs + piece * 16),
+                                     (lds_void*)(tile + p * 1024), 16, 0, 0);
+  }
+}
+
+// Barrier behind which the copies into LDS that any wave issued before it are there.
+__device__ __forceinline__ void cross_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+  __syncthreads();
+}
+
+// A lane's row: where its query, output and lse are.
+struct Row {
+  bool real;
+  size_t q, out, dq, lse, part;
+};
+__device__ __forceinline__ Row row_of(const CrossArgs& a, const CrossSeq& s, int hk, int r) {
+  Row w;
+  const int rows = s.lq * a.group;
+  w.real = r < rows;
+  if (!w.real) r = rows - 1;
+  const int t = r / a.group, h = hk * a.group + r - t * a.group;
+  w.q = seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)t * a.sq.tok + (size_t)h * a.sq.head;
+  w.out = seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)t * a.so.tok + (size_t)h * a.so.head;
+  w.dq = seq_base(a.sdq, a.cu_q, s.q0, s.i) + (size_t)t * a.sdq.tok + (size_t)h * a.sdq.head;
+  w.lse = a.cu_q != nullptr ? (size_t)h * a.T + s.q0 + t : ((size_t)s.i * a.Hq + h) * a.Lq + t;
+  w.part = ((a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) + t) * a.Hq + h;
+  return w;
+}
+
+// Which of states at .. at + 63 (or 31) are seen.
+template <int TILE>
+__device__ __forceinline__ uint64_t seen_bits(int left, bool masked, uint8_t byte, int lane) {
+  uint64_t bits = left >= 64 ? ~0ull : (1ull << left) - 1;
+  if (TILE < 64) bits &= (1ull << (TILE & 63)) - 1;
+  if (masked) bits &= __ballot(byte != 0 && lane < left);
+  return bits;
+}
+
+// The other lane half's value.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// Four channels to memory.
+template <bool F32>
+__device__ __forceinline__ void store4(void* p, size_t at, floatx4 x) {
+  if constexpr (F32)
+    *reinterpret_cast<floatx4*>((float*)p + at) = x;
+  else
+    *reinterpret_cast<uint2*>((uint16_t*)p + at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+}
+
+// Host-side launchers (arguments validated).
+hipError_t launch_cross_forward(bool f32, int d, bool few, const CrossArgs& a, hipStream_t stream);
+hipError_t launch_cross_join(bool f32, int d, const CrossArgs& a, hipStream_t stream);
+hipError_t launch_cross_dq(bool f32, int d, const CrossArgs& a, hipStream_t stream);
+hipError_t launch_cross_dkv(bool f32, int d, const CrossArgs& a, hipStream_t stream);
+// part sums [splits][rows][d] to rows of a tensor of H heads.
+struct CrossSum {
+  const float* part;
+  void* out;
+  CrossStrides s;
+  const int* cu;
+  int n, L, H, splits;
+  long long rows;  // tokens * H
+};
+hipError_t launch_cross_sum(bool f32, int d, const CrossSum& a, hipStream_t stream);
+
+}  // namespace vda

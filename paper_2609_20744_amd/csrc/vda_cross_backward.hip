@@ -1,0 +1,325 @@
+// Cross attention to an encoder's states: the gradients (vda.h,
+// vda_cross_backward).  With p_j = 2^(c s_j - lse) made again from q, k and the
+// kept lse, and D = sum dout o over a row's channels,
+//     dP_j = dout . v_j,  dS_j = p_j (dP_j - D),
+//     dq = scale sum_j dS_j k_j,  dk_j = scale sum_r dS_j q_r,  dv_j = sum_r p_j dout_r.
+//
+// Two kernels, each with its own sums in registers and no atomics: one goes along
+// the states for 128 rows (dq, and D and lse of each row for the other), one along
+// the rows for 128 states (dk and dv).  Scores and dP are made in both, seven
+// products where one kernel would need five, and a sum over the other side's
+// workgroups.  The rows of all query heads of a key head are one sequence of rows
+// (vda_cross.h), so the gradients of shared heads are ordinary sums.  Where a
+// side's tiles are too few to fill the device, the other side is cut into ranges,
+// whose fp32 sums are added in their order.
+#include "vda_cross.h"
+
+namespace vda {
+namespace {
+
+template <bool F32, int D>
+__global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossArgs a) {
+  typedef Frag<F32> Fr;
+  typedef CrossTile<F32, D> Tile;
+  constexpr int kTileBytes = kCrossTile * Tile::kRow;
+  __shared__ __align__(16) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
+  const int hk = uniform(id / (unsigned)a.tiles);
+  if (hk >= a.Hk) return;
+  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kCrossRows, id - hk * a.tiles);
+  if (at.x < 0) return;
+  const CrossSeq s = cross_seq(a, at.x);
+  const int r0 = at.y * kCrossRows;
+  if (r0 >= s.lq * a.group) return;
+  const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
+
+  const int tiles = (s.seen + kCrossTile - 1) / kCrossTile, per = (tiles + a.splits - 1) / a.splits;
+  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+  const char* kb = (const char*)a.k + (seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head) * Tile::kEs;
+  const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
+  const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
+
+  typename Fr::X q[D / 16], g[D / 16];
+  float dot = 0.f;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) {
+    q[e] = Fr::load(a.q, row.q + 16 * e + 8 * (lane >> 5));
+    if (a.flip) q[e] = Fr::flip(q[e]);
+    g[e] = Fr::load(a.dout, row.out + 16 * e + 8 * (lane >> 5));
+    const typename Fr::X o = Fr::load(a.o, row.out + 16 * e + 8 * (lane >> 5));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dot = fmaf(Fr::value(g[e], i), Fr::value(o, i), dot);
+  }
+  dot += other_half(dot);
+  // A row that sees no state has an lse of -inf: as +inf it leaves no p.
+  float lse = a.lse_in[row.lse] * kLog2e;
+  lse = lse == -INFINITY ? INFINITY : lse;
+  if (blockIdx.y == 0 && row.real && lane < 32) a.stats[row.part] = make_float2(lse, dot);
+  floatx16 dq[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) dq[e] = floatx16{};
+  uint8_t byte = 1;
+
+  auto copy = [&](int t, char* kt, char* vt) {
+    const int first = t * kCrossTile, last = s.seen - 1 - first;
+    copy_states<F32, D, kCrossTile, 4>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
+    copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
+    if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
+  };
+  auto step = [&](int t, uint8_t byte_t, char* kt, char* vt) {
+    const uint64_t bits = seen_bits<64>(s.seen - t * kCrossTile, mask != nullptr, byte_t, lane);
+    if (bits == 0) return;
+    const bool all = ~bits == 0;
+    if (mask != nullptr && !all) {
+      Tile::template clear_rows<kCrossTile, kThreads>(kt, 0, bits, tid);
+      Tile::template clear_rows<kCrossTile, kThreads>(vt, 0, bits, tid);
+      lds_barrier();
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      floatx16 p = {}, dp = {};
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) p = Fr::mma(Tile::row_frag(kt, 32 * b * Tile::kRow, e, lane), q[e], p);
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) dp = Fr::mma(Tile::row_frag(vt, 32 * b * Tile::kRow, e, lane), g[e], dp);
+      const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - dot);
+        if (!all) x = w >> (8 * (i >> 2) + (i & 3)) & 1 ? x : 0.f;
+        p[i] = x;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const typename Fr::X x = Fr::of(p, h);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+          dq[e] = Fr::mma(Tile::col_frag(kt, (32 * b + 16 * h) * Tile::kRow, e, lane), x, dq[e]);
+      }
+    }
+  };
+  if (from < to) {
+    copy(from, k0, v0);
+    for (int t = from;;) {
+      cross_barrier();
+      uint8_t b = byte;
+      if (t + 1 < to) copy(t + 1, k1, v1);
+      step(t, b, k0, v0);
+      if (++t >= to) break;
+      cross_barrier();
+      b = byte;
+      if (t + 1 < to) copy(t + 1, k0, v0);
+      step(t, b, k1, v1);
+      if (++t >= to) break;
+    }
+  }
+  if (!row.real) return;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 x = floatx4{dq[e][4 * i], dq[e][4 * i + 1], dq[e][4 * i + 2], dq[e][4 * i + 3]} * a.scale;
+      const int chan = 32 * e + 8 * i + 4 * (lane >> 5);
+      if (a.splits > 1)
+        *reinterpret_cast<floatx4*>(a.part + ((size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part) * D + chan) = x;
+      else
+        store4<F32>(a.dq, row.dq + chan, x);
+    }
+}
+
+template <bool F32, int D>
+__global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs a) {
+  typedef Frag<F32> Fr;
+  typedef CrossTile<F32, D> Tile;
+  constexpr int kTileBytes = kCrossTile * Tile::kRow;
+  __shared__ __align__(16) char q0[kTileBytes], g0[kTileBytes], q1[kTileBytes], g1[kTileBytes];
+  __shared__ __align__(16) float lse0[kCrossTile], dot0[kCrossTile], lse1[kCrossTile], dot1[kCrossTile];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
+  const int hk = uniform(id / (unsigned)a.tiles);
+  if (hk >= a.Hk) return;
+  const int2 at = seq_of_tile(a.cu_k, a.n, a.S, a.Lk, 1, kCrossRows, id - hk * a.tiles);
+  if (at.x < 0) return;
+  const CrossSeq s = cross_seq(a, at.x);
+  const int j0 = at.y * kCrossRows;
+  if (j0 >= s.lk) return;
+
+  // The lane's state.
+  const int j = j0 + wave * 32 + (lane & 31), jc = j < s.lk ? j : s.lk - 1;
+  bool seen = j < s.seen;
+  if (seen && a.k_mask != nullptr)
+    seen = a.k_mask[(a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + jc] != 0;
+  typename Fr::X k[D / 16], v[D / 16];
+  const size_t kat = seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head + (size_t)jc * a.sk.tok;
+  const size_t vat = seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head + (size_t)jc * a.sv.tok;
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) {
+    k[e] = Fr::load(a.k, kat + 16 * e + 8 * (lane >> 5));
+    v[e] = Fr::load(a.v, vat + 16 * e + 8 * (lane >> 5));
+    if (a.flip) k[e] = Fr::flip(k[e]);
+    // What stands in a masked place may be anything.
+    if (!seen) k[e] = Fr::zero(), v[e] = Fr::zero();
+  }
+  floatx16 dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) dk[e] = floatx16{}, dv[e] = floatx16{};
+
+  // The range of rows of this split, in tiles; none where no state of the tile is seen.
+  const int rows = s.lq * a.group;
+  const int tiles = j0 < s.seen ? (rows + kCrossTile - 1) / kCrossTile : 0, per = (tiles + a.splits - 1) / a.splits;
+  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+  const char* qb = (const char*)a.q +
+                   (seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.sq.head) * Tile::kEs;
+  const char* gb = (const char*)a.dout +
+                   (seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.so.head) * Tile::kEs;
+  const float2* stats = a.stats + (a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) * a.Hq + hk * a.group;
+  float2 mine = make_float2(0.f, 0.f);
+
+  auto copy = [&](int t, char* qt, char* gt) {
+    const int first = t * kCrossTile, last = rows - 1 - first;
+    copy_rows<F32, D, 4>(a, qb, a.sq, first, last, qt, wave, lane);
+    copy_rows<F32, D, 4>(a, gb, a.so, first, last, gt, wave, lane);
+    if (wave == 0) {
+      const int r = first + (lane < last ? lane : last), tok = r / a.group;
+      mine = stats[(size_t)tok * a.Hq + r - tok * a.group];
+      if (lane > last) mine.x = INFINITY;  // a row behind the last leaves no p
+    }
+  };
+  auto keep = [&](float* lse, float* dot) {
+    if (wave == 0) lse[lane] = mine.x, dot[lane] = mine.y;
+  };
+  auto step = [&](const char* qt, const char* gt, const float* lse, const float* dot) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      floatx16 p = {}, dp = {};
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) p = Fr::mma(Tile::row_frag(qt, 32 * b * Tile::kRow, e, lane), k[e], p);
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) dp = Fr::mma(Tile::row_frag(gt, 32 * b * Tile::kRow, e, lane), v[e], dp);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const floatx4 z = *reinterpret_cast<const floatx4*>(lse + 32 * b + 8 * i + 4 * (lane >> 5));
+        const floatx4 y = *reinterpret_cast<const floatx4*>(dot + 32 * b + 8 * i + 4 * (lane >> 5));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = seen ? __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e])) : 0.f;
+          p[4 * i + e] = x;
+          dp[4 * i + e] = x * (dp[4 * i + e] - y[e]);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const typename Fr::X x = Fr::of(p, h), y = Fr::of(dp, h);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          dv[e] = Fr::mma(Tile::col_frag(gt, (32 * b + 16 * h) * Tile::kRow, e, lane), x, dv[e]);
+          dk[e] = Fr::mma(Tile::col_frag(qt, (32 * b + 16 * h) * Tile::kRow, e, lane), y, dk[e]);
+        }
+      }
+    }
+  };
+  if (from < to) {
+    copy(from, q0, g0);
+    for (int t = from;;) {
+      keep(lse0, dot0);
+      cross_barrier();
+      if (t + 1 < to) copy(t + 1, q1, g1);
+      step(q0, g0, lse0, dot0);
+      if (++t >= to) break;
+      keep(lse1, dot1);
+      cross_barrier();
+      if (t + 1 < to) copy(t + 1, q0, g0);
+      step(q1, g1, lse1, dot1);
+      if (++t >= to) break;
+    }
+  }
+  if (j >= s.lk) return;
+  const size_t dkat = seq_base(a.sdk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdk.head + (size_t)jc * a.sdk.tok;
+  const size_t dvat = seq_base(a.sdv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdv.head + (size_t)jc * a.sdv.tok;
+  const size_t part = (size_t)blockIdx.y * ((size_t)a.S * a.Hk) +
+                      ((a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + jc) * a.Hk + hk;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 x = floatx4{dk[e][4 * i], dk[e][4 * i + 1], dk[e][4 * i + 2], dk[e][4 * i + 3]} * a.scale;
+      const floatx4 y = floatx4{dv[e][4 * i], dv[e][4 * i + 1], dv[e][4 * i + 2], dv[e][4 * i + 3]};
+      const int chan = 32 * e + 8 * i + 4 * (lane >> 5);
+      if (a.splits > 1) {
+        *reinterpret_cast<floatx4*>(a.part + part * D + chan) = x;
+        *reinterpret_cast<floatx4*>(a.part2 + part * D + chan) = y;
+      } else {
+        store4<F32>(a.dk, dkat + chan, x);
+        store4<F32>(a.dv, dvat + chan, y);
+      }
+    }
+}
+
+// Adds the parts of the splits, in their order: D / 4 lanes a row (token x head).
+template <bool F32, int D>
+__global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossSum a) {
+  constexpr int LANES = D / 4, ROWS = kThreads / LANES;
+  const size_t R = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (R >= (size_t)a.rows) return;
+  const int tok = (int)(R / (unsigned)a.H), h = (int)(R - (size_t)tok * a.H), chan = threadIdx.x % LANES * 4;
+  size_t out;
+  if (a.cu != nullptr) {
+    const int total = (int)(a.rows / a.H);
+    if (tok < clamp_to(a.cu[0], 0, total) || tok >= clamp_to(a.cu[a.n], 0, total)) return;
+    out = (size_t)tok * a.s.tok + (size_t)h * a.s.head;
+  } else {
+    const int i = tok / a.L, t = tok - i * a.L;
+    out = (size_t)i * a.s.seq + (size_t)t * a.s.tok + (size_t)h * a.s.head;
+  }
+  floatx4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.splits; ++p) x += *reinterpret_cast<const floatx4*>(a.part + (p * (size_t)a.rows + R) * D + chan);
+  store4<F32>(a.out, out + chan, x);
+}
+
+template <bool F32, int D>
+hipError_t dq(const CrossArgs& a, hipStream_t stream) {
+  const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
+  cross_dq_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+template <bool F32, int D>
+hipError_t dkv(const CrossArgs& a, hipStream_t stream) {
+  const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
+  cross_dkv_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+template <bool F32, int D>
+hipError_t sum(const CrossSum& a, hipStream_t stream) {
+  constexpr int ROWS = kThreads / (D / 4);
+  cross_sum_kernel<F32, D><<<(unsigned)(((size_t)a.rows + ROWS - 1) / ROWS), kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cross_dq(bool f32, int d, const CrossArgs& a, hipStream_t stream) {
+  switch (d) {
+    case 32: return f32 ? dq<true, 32>(a, stream) : dq<false, 32>(a, stream);
+    case 64: return f32 ? dq<true, 64>(a, stream) : dq<false, 64>(a, stream);
+    default: return f32 ? dq<true, 128>(a, stream) : dq<false, 128>(a, stream);
+  }
+}
+
+hipError_t launch_cross_dkv(bool f32, int d, const CrossArgs& a, hipStream_t stream) {
+  switch (d) {
+    case 32: return f32 ? dkv<true, 32>(a, stream) : dkv<false, 32>(a, stream);
+    case 64: return f32 ? dkv<true, 64>(a, stream) : dkv<false, 64>(a, stream);
+    default: return f32 ? dkv<true, 128>(a, stream) : dkv<false, 128>(a, stream);
+  }
+}
+
+hipError_t launch_cross_sum(bool f32, int d, const CrossSum& a, hipStream_t stream) {
+  switch (d) {
+    case 32: return f32 ? sum<true, 32>(a, stream) : sum<false, 32>(a, stream);
+    case 64: return f32 ? sum<true, 64>(a, stream) : sum<false, 64>(a, stream);
+    default: return f32 ? sum<true, 128>(a, stream) : sum<false, 128>(a, stream);
+  }
+}
+
+}  // namespace vda

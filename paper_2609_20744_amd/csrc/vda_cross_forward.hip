@@ -1,0 +1,368 @@
+// Cross attention to an encoder's states: the forward pass, for whole sequences
+// and for a few tokens of each (vda.h, vda_cross_forward, vda_cross_step), and
+// the join of states that several workgroups shared.
+//
+// One pass over the states with the running maximum and sum of the softmax
+// (vda_cross.h has the operands).  Per 64 states and 32 rows a wave makes
+//     S^T = K Q^T -> p = 2^(c s - m) -> O^T += V^T P^T,
+// all in registers: a lane has one row's column of S^T and of O^T, so the
+// maximum, the sum and the scaling of O are its own, and the rounded p are the
+// next product's operand as they stand.  The maximum is taken up where it grew by
+// more than 2^8 only: p stays below 2^8 then, where a rounding to bf16 is as good.
+//
+// Many rows: a wave has 32 rows, the four waves of a workgroup share the states'
+// tiles.  Few rows (a step, learned queries): the waves share 32 rows, take 32 states
+// of each tile each, and join at the end.
+// Where workgroups would not fill the device, each takes a range of the states
+// and the join kernel adds their parts.
+#include "vda_cross.h"
+
+namespace vda {
+namespace {
+
+constexpr float kGrow = 8.f;  // in powers of two
+
+// The softmax's part of a tile of 32 NB states, and its product with V.
+template <bool F32, int D, int NB>
+__device__ __forceinline__ void attend(const char* kt, const char* vt, int at, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
+                                       bool all, float c, floatx16 (&o)[D / 32], float& m, float& l, int lane) {
+  typedef Frag<F32> Fr;
+  typedef CrossTile<F32, D> Tile;
+  floatx16 s[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    s[b] = floatx16{};
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) s[b] = Fr::mma(Tile::row_frag(kt, at + 32 * b * Tile::kRow, e, lane), q[e], s[b]);
+  }
+  if (!all) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = w >> (8 * (i >> 2) + (i & 3)) & 1 ? s[b][i] : -INFINITY;
+    }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+  top = fmaxf(top, other_half(top));
+  top = top == -INFINITY ? top : top * c;
+  if (__any(top > m + kGrow)) {
+    const float to = top > m + kGrow ? top : m;
+    const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    l *= f;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) o[b] *= f;
+  }
+  const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float p = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
+      if (!all) p = s[b][i] == -INFINITY ? 0.f : p;
+      s[b][i] = p;
+      l += p;
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const typename Fr::X p = Fr::of(s[b], t);
+#pragma unroll
+      for (int e = 0; e < D / 32; ++e) o[e] = Fr::mma(Tile::col_frag(vt, at + (32 * b + 16 * t) * Tile::kRow, e, lane), p, o[e]);
+    }
+}
+
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+template <bool F32, int D>
+__global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(CrossArgs a) {
+  typedef Frag<F32> Fr;
+  typedef CrossTile<F32, D> Tile;
+  constexpr int kTileBytes = kCrossTile * Tile::kRow;
+  __shared__ __align__(16) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
+  const int hk = uniform(id / (unsigned)a.tiles);
+  if (hk >= a.Hk) return;
+  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kCrossRows, id - hk * a.tiles);
+  if (at.x < 0) return;
+  const CrossSeq s = cross_seq(a, at.x);
+  const int r0 = at.y * kCrossRows;
+  if (r0 >= s.lq * a.group) return;
+  const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
+
+  // The range of states of this split, in tiles.
+  const int tiles = (s.seen + kCrossTile - 1) / kCrossTile, per = (tiles + a.splits - 1) / a.splits;
+  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+  const char* kb = (const char*)a.k + (seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head) * Tile::kEs;
+  const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
+  const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
+
+  typename Fr::X q[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) {
+    q[e] = Fr::load(a.q, row.q + 16 * e + 8 * (lane >> 5));
+    if (a.flip) q[e] = Fr::flip(q[e]);
+  }
+  floatx16 o[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
+  float m = -INFINITY, l = 0.f;
+  uint8_t byte = 1;
+
+  auto copy = [&](int t, char* kt, char* vt) {
+    const int first = t * kCrossTile, last = s.seen - 1 - first;
+    copy_states<F32, D, kCrossTile, 4>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
+    copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
+    if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
+  };
+  auto step = [&](int t, uint8_t b, char* kt, char* vt) {
+    const uint64_t bits = seen_bits<64>(s.seen - t * kCrossTile, mask != nullptr, b, lane);
+    if (bits == 0) return;
+    if (mask != nullptr && ~bits != 0) {
+      // What stands in a masked place may be anything: 0 times it has to be 0.
+      Tile::template clear_rows<kCrossTile, kThreads>(kt, 0, bits, tid);
+      Tile::template clear_rows<kCrossTile, kThreads>(vt, 0, bits, tid);
+      lds_barrier();
+    }
+    attend<F32, D, 2>(kt, vt, 0, q, bits, ~bits == 0, a.c, o, m, l, lane);
+  };
+  if (from < to) {
+    copy(from, k0, v0);
+    for (int t = from;;) {
+      cross_barrier();
+      uint8_t b = byte;
+      if (t + 1 < to) copy(t + 1, k1, v1);
+      step(t, b, k0, v0);
+      if (++t >= to) break;
+      cross_barrier();
+      b = byte;
+      if (t + 1 < to) copy(t + 1, k0, v0);
+      step(t, b, k1, v1);
+      if (++t >= to) break;
+    }
+  }
+  l += other_half(l);
+  if (!row.real) return;
+  if (a.splits > 1) {
+    const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<floatx4*>(a.part + part * D + 32 * e + 8 * i + 4 * (lane >> 5)) =
+            floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+    if (lane < 32) *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(m, l);
+    return;
+  }
+  const float r = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      store4<F32>(a.out, row.out + 32 * e + 8 * i + 4 * (lane >> 5),
+                  floatx4{o[e][4 * i] * r, o[e][4 * i + 1] * r, o[e][4 * i + 2] * r, o[e][4 * i + 3] * r});
+  if (a.lse != nullptr && lane < 32) a.lse[row.lse] = lse_of(m, l);
+}
+
+// Few rows: 32 of them, shared by the waves, each of which takes 32 states of every tile.
+template <bool F32, int D>
+struct FewShape {
+  static constexpr int kWaves = F32 && D == 128 ? 2 : 4;
+  static constexpr int kStates = 32 * kWaves;  // of a tile
+};
+
+template <bool F32, int D>
+__global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_kernel(CrossArgs a) {
+  typedef Frag<F32> Fr;
+  typedef CrossTile<F32, D> Tile;
+  constexpr int W = FewShape<F32, D>::kWaves, kStates = FewShape<F32, D>::kStates, kBytes = 32 * Tile::kRow;
+  __shared__ __align__(16) char k0[W * kBytes], v0[W * kBytes], k1[W * kBytes], v1[W * kBytes];
+  __shared__ float2 ml[W][32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int mine = wave * kBytes;  // the wave's states of each tile
+  const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
+  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kFewRows, blockIdx.x / (unsigned)a.Hk);
+  if (at.x < 0) return;
+  const CrossSeq s = cross_seq(a, at.x);
+  const int r0 = at.y * kFewRows;
+  if (r0 >= s.lq * a.group) return;
+  const Row row = row_of(a, s, hk, r0 + (lane & 31));
+
+  const int tiles = (s.seen + kStates - 1) / kStates, per = (tiles + a.splits - 1) / a.splits;
+  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+  const char* kb = (const char*)a.k + (seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head) * Tile::kEs;
+  const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
+  const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
+
+  typename Fr::X q[D / 16];
+#pragma unroll
+  for (int e = 0; e < D / 16; ++e) {
+    q[e] = Fr::load(a.q, row.q + 16 * e + 8 * (lane >> 5));
+    if (a.flip) q[e] = Fr::flip(q[e]);
+  }
+  floatx16 o[D / 32];
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
+  float m = -INFINITY, l = 0.f;
+  uint8_t byte = 1;
+
+  auto copy = [&](int t, char* kt, char* vt) {
+    const int first = t * kStates, last = s.seen - 1 - first;
+    copy_states<F32, D, kStates, W>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
+    copy_states<F32, D, kStates, W>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
+    const int place = wave * 32 + lane;
+    if (mask != nullptr) byte = mask[first + (place < last ? place : last)];
+  };
+  auto step = [&](int t, uint8_t b, char* kt, char* vt) {
+    const int left = s.seen - t * kStates - wave * 32;
+    if (left <= 0) return;
+    const uint64_t bits = seen_bits<32>(left, mask != nullptr, b, lane);
+    if (bits == 0) return;
+    const bool all = bits == 0xffffffffull;
+    if (mask != nullptr && !all) {
+      Tile::template clear_rows<32, 64>(kt, mine, bits, lane);
+      Tile::template clear_rows<32, 64>(vt, mine, bits, lane);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // the wave's own
+      __builtin_amdgcn_wave_barrier();
+    }
+    attend<F32, D, 1>(kt, vt, mine, q, bits, all, a.c, o, m, l, lane);
+  };
+  if (from < to) {
+    copy(from, k0, v0);
+    for (int t = from;;) {
+      cross_barrier();
+      uint8_t b = byte;
+      if (t + 1 < to) copy(t + 1, k1, v1);
+      step(t, b, k0, v0);
+      if (++t >= to) break;
+      cross_barrier();
+      b = byte;
+      if (t + 1 < to) copy(t + 1, k0, v0);
+      step(t, b, k1, v1);
+      if (++t >= to) break;
+    }
+  }
+  l += other_half(l);
+  // The waves' parts: piece p is channels 8 p + 4 lh .. of every row.
+  constexpr int kPieces = D / 8;
+  lds_barrier();
+#pragma unroll
+  for (int p = 0; p < kPieces; ++p) {
+    char* to_lds = (p < kPieces / 2 ? k0 + p * 1024 : v0 + (p - kPieces / 2) * 1024) + mine;
+    const int e = p / 4, i = p % 4;
+    *reinterpret_cast<floatx4*>(to_lds + lane * 16) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+  }
+  if (lane < 32) ml[wave][lane] = make_float2(m, l);
+  lds_barrier();
+  if (!row.real) return;
+  float f[W], top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w][lane & 31].x);
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float2 x = ml[w][lane & 31];
+    f[w] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - top);
+    sum += x.x == -INFINITY ? x.y : f[w] * x.y;
+  }
+  const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
+  const float r = a.splits > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  for (int p = wave; p < kPieces; p += W) {
+    floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const char* from_lds = (p < kPieces / 2 ? k0 + p * 1024 : v0 + (p - kPieces / 2) * 1024) + w * kBytes;
+      x += f[w] * *reinterpret_cast<const floatx4*>(from_lds + lane * 16);
+    }
+    const int chan = 8 * p + 4 * (lane >> 5);
+    if (a.splits > 1)
+      *reinterpret_cast<floatx4*>(a.part + part * D + chan) = x;
+    else
+      store4<F32>(a.out, row.out + chan, x * r);
+  }
+  if (wave == 0 && lane < 32) {
+    if (a.splits > 1)
+      *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(top, sum);
+    else if (a.lse != nullptr)
+      a.lse[row.lse] = lse_of(top, sum);
+  }
+}
+
+// Adds the parts of a row's splits, in their order: D / 4 lanes a row.
+template <bool F32, int D>
+__global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
+  constexpr int LANES = D / 4, ROWS = kThreads / LANES;
+  const size_t rows = (size_t)a.T * a.Hq, R = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  if (R >= rows) return;
+  const int tok = (int)(R / (unsigned)a.Hq), h = (int)(R - (size_t)tok * a.Hq), chan = threadIdx.x % LANES * 4;
+  size_t out, lse;
+  if (a.cu_q != nullptr) {
+    if (tok < clamp_to(a.cu_q[0], 0, a.T) || tok >= clamp_to(a.cu_q[a.n], 0, a.T)) return;
+    out = (size_t)tok * a.so.tok + (size_t)h * a.so.head;
+    lse = (size_t)h * a.T + tok;
+  } else {
+    const int i = tok / a.Lq, t = tok - i * a.Lq;
+    if (a.slots != nullptr && (a.slots[i] < 0 || a.slots[i] >= a.n_slots)) return;
+    out = (size_t)i * a.so.seq + (size_t)t * a.so.tok + (size_t)h * a.so.head;
+    lse = ((size_t)i * a.Hq + h) * a.Lq + t;
+  }
+  const float2* ml = reinterpret_cast<const float2*>(a.part2);
+  float top = -INFINITY, sum = 0.f;
+  for (int p = 0; p < a.splits; ++p) top = fmaxf(top, ml[p * rows + R].x);
+  floatx4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.splits; ++p) {
+    const float2 y = ml[p * rows + R];
+    const floatx4 z = *reinterpret_cast<const floatx4*>(a.part + (p * rows + R) * D + chan);
+    const float f = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - top);
+    sum += y.x == -INFINITY ? y.y : f * y.y;
+    x += f * z;
+  }
+  store4<F32>(a.out, out + chan, x * (sum == 0.f ? 0.f : 1.f / sum));
+  if (a.lse != nullptr && chan == 0) a.lse[lse] = lse_of(top, sum);
+}
+
+template <bool F32, int D>
+hipError_t forward(bool few, const CrossArgs& a, hipStream_t stream) {
+  if (few) {
+    cross_few_kernel<F32, D>
+        <<<dim3((unsigned)a.tiles * a.Hk, a.splits), 64 * FewShape<F32, D>::kWaves, 0, stream>>>(a);
+  } else {
+    const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
+    cross_forward_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <bool F32, int D>
+hipError_t join(const CrossArgs& a, hipStream_t stream) {
+  constexpr int ROWS = kThreads / (D / 4);
+  cross_join_kernel<F32, D><<<(unsigned)(((size_t)a.T * a.Hq + ROWS - 1) / ROWS), kThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cross_forward(bool f32, int d, bool few, const CrossArgs& a, hipStream_t stream) {
+  switch (d) {
+    case 32: return f32 ? forward<true, 32>(few, a, stream) : forward<false, 32>(few, a, stream);
+    case 64: return f32 ? forward<true, 64>(few, a, stream) : forward<false, 64>(few, a, stream);
+    default: return f32 ? forward<true, 128>(few, a, stream) : forward<false, 128>(few, a, stream);
+  }
+}
+
+hipError_t launch_cross_join(bool f32, int d, const CrossArgs& a, hipStream_t stream) {
+  switch (d) {
+    case 32: return f32 ? join<true, 32>(a, stream) : join<false, 32>(a, stream);
+    case 64: return f32 ? join<true, 64>(a, stream) : join<false, 64>(a, stream);
+    default: return f32 ? join<true, 128>(a, stream) : join<false, 128>(a, stream);
+  }
+}
+
+}  // namespace vda

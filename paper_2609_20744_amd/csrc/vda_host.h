@@ -27,6 +27,15 @@ inline Range range_of(const void* p, size_t bytes) {
 
 inline bool overlaps(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
 
+// Whether two tensors of rows of `row` bytes, at the same row stride (elements of
+// es bytes), are slices of one: their ranges meet, their rows do not.
+inline bool slices_apart(const void* a, long long a_stride, const void* b, long long b_stride, size_t row, size_t es) {
+  if (a_stride != b_stride || a_stride <= 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const size_t apart = x < y ? y - x : x - y, stride = (size_t)a_stride * es;
+  return apart >= row && apart + row <= stride;
+}
+
 inline int hip_status(hipError_t e) { return e == hipSuccess ? VDA_OK : VDA_ERR_HIP; }
 
 inline int current_device_cus() {

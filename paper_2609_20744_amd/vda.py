@@ -60,7 +60,25 @@ class VdaRopeOptions(ctypes.Structure):
         "frame_offset", "x_row_stride", "dx_row_stride")]
 
 
+class VdaCrossProblem(ctypes.Structure):
+    """struct vda_cross_problem (include/vda.h)."""
+    _fields_ = [("T", ctypes.c_int), ("S", ctypes.c_int), ("n_seqs", ctypes.c_int),
+                ("cu_q", ctypes.c_void_p), ("cu_k", ctypes.c_void_p), ("k_lens", ctypes.c_void_p),
+                ("k_mask", ctypes.c_void_p)] + [(n, ctypes.c_int) for n in (
+                    "H_q", "H_k", "d", "layout", "kv_layout", "out_layout", "q_row_stride",
+                    "k_row_stride", "v_row_stride", "dq_row_stride", "dk_row_stride",
+                    "dv_row_stride", "is_f32")] + [("scale", ctypes.c_float)]
+
+
+class VdaRecurProblem(ctypes.Structure):
+    """struct vda_recur_problem (include/vda.h)."""
+    _fields_ = [("T", ctypes.c_int), ("n_seqs", ctypes.c_int), ("cu_seqlens", ctypes.c_void_p)] + [
+        (n, ctypes.c_int) for n in ("C", "gate", "reverse", "x_row_stride", "g_row_stride",
+                                    "dx_row_stride", "dg_row_stride", "is_f32")]
+
+
 RULES = {"joint": 0, "frozen": 1}
+GATES = {"log": 0, "logit": 1, "norm": 2}
 LAYOUTS = {"heads": 0, "tokens": 1}
 
 _SIGNATURES = {
@@ -88,6 +106,17 @@ _SIGNATURES = {
     "vda_delta_step": (_I, [_P] * 5 + [_I] * 7 + [ctypes.c_float, _P, _I, _P, _P, _P]),
     "vda_rope": (_I, [_P, _P, _P, _I, _I, _I, _I, _P, _I, _P, _P]),
     "vda_rope_backward": (_I, [_P, _P, _P, _P, _I, _I, _I, _I, _P, _I, _P, _P]),
+    "vda_cross_forward": (_I, [_P] * 8),
+    "vda_cross_forward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_cross_backward": (_I, [_P] * 12),
+    "vda_cross_backward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_cross_step": (_I, [_P] * 5 + [_I, _P, _P, _P]),
+    "vda_cross_step_workspace": (ctypes.c_size_t, [_P, _I]),
+    "vda_recur_forward": (_I, [_P] * 8),
+    "vda_recur_forward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_recur_backward": (_I, [_P] * 11),
+    "vda_recur_backward_workspace": (ctypes.c_size_t, [_P]),
+    "vda_recur_step": (_I, [_P, _P] + [_I] * 5 + [_P, _I, _P, _P, _P]),
     "vda_release_workspace": (_I, [_I, _P]),
     "vda_workspace_bytes": (_I, [_I, _P]),
 }
@@ -884,4 +913,364 @@ def rope_backward(dout, inv_freq, axes, H, x=None, positions=None, grid=None, fr
                _ptr(positions), B, L, H, d, ctypes.byref(o), int(dt == torch.float32),
                out.data_ptr(), _stream_ptr(dev, stream))
     _check(st, "vda_rope_backward")
+    return out
+
+
+# ----------------------------------------------------------------------------
+# Cross attention to an encoder's states, and the channel-wise gated recurrence
+# ----------------------------------------------------------------------------
+
+def _like(t, name, shape, dtype, dev):
+    """A tensor of this shape, contiguous but for its rows' stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} shape {tuple(t.shape)} must be {tuple(shape)}")
+
+
+def _row_stride(t, name, inner):
+    """Elements between the token rows of a [..., L, `inner` dimensions] tensor, 0 where it is
+    contiguous; the rows may be slices, the same stride apart over the batch and tokens."""
+    if t.is_contiguous():
+        return 0
+    row = 1
+    for size, stride in zip(reversed(t.shape[-inner:]), reversed(t.stride()[-inner:])):
+        if size > 1 and stride != row:
+            raise ValueError(f"{name} must have contiguous rows")
+        row *= size
+    step = rows = None
+    for size, stride in zip(reversed(t.shape[:-inner]), reversed(t.stride()[:-inner])):
+        if size == 1:
+            continue
+        if step is None:
+            step, rows = stride, 1
+        if stride != step * rows:
+            raise ValueError(f"{name} must have rows at one stride over the batch and tokens")
+        rows *= size
+    step = row if step is None else step
+    if step < row:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    return _int32(f"the row stride of {name}", step)
+
+
+def _cross_side(t, name, layout, cu, dt, dev):
+    """(sequences' leading shape, H, L, d, row stride) of q, or of k or v."""
+    if layout not in LAYOUTS:
+        raise ValueError(f"layouts must be of {sorted(LAYOUTS)}")
+    _like(t, name, None, dt, dev)
+    if t.dim() < 3:
+        raise ValueError(f"{name} must be [..., H, L, d] (heads) or [..., L, H, d] (tokens)")
+    lead, d = tuple(t.shape[:-3]), t.shape[-1]
+    if cu is not None:
+        if lead:
+            raise ValueError(f"with offsets, {name} has three dimensions (one packed batch)")
+        _require(cu, "cu_q, cu_k", torch.int32, dev)
+        if cu.dim() != 1 or cu.numel() < 2:
+            raise ValueError("offsets must hold one more than there are sequences")
+    if layout == "heads":
+        _require(t, name, dt, dev)
+        return lead, t.shape[-3], t.shape[-2], d, 0
+    return lead, t.shape[-2], t.shape[-3], d, _row_stride(t, name, 2)
+
+
+def _cross_problem(q, k, v, cu_q, cu_k, k_lens, k_mask, layout, kv_layout, out_layout, scale):
+    """The problem, and the shapes of the output and of lse."""
+    dt, dev = _storage(q, "q")
+    kv_layout = layout if kv_layout is None else kv_layout
+    out_layout = layout if out_layout is None else out_layout
+    if out_layout not in LAYOUTS:
+        raise ValueError(f"layouts must be of {sorted(LAYOUTS)}")
+    lead_q, H_q, L, d, q_stride = _cross_side(q, "q", layout, cu_q, dt, dev)
+    lead_k, H_k, S, d_k, k_stride = _cross_side(k, "k", kv_layout, cu_k, dt, dev)
+    v_stride = _cross_side(v, "v", kv_layout, cu_k, dt, dev)[4]
+    if v.shape != k.shape or d_k != d:
+        raise ValueError("k and v must have one shape, and q's head dimension")
+    if H_k < 1 or H_q < 1 or H_q % H_k:
+        raise ValueError(f"{H_q} query heads must be a multiple of {H_k} key heads")
+    n = cu_q.numel() - 1 if cu_q is not None else math.prod(lead_q)
+    n_k = cu_k.numel() - 1 if cu_k is not None else math.prod(lead_k)
+    if n != n_k or (cu_q is None and cu_k is None and lead_q != lead_k):
+        raise ValueError(f"queries of {n} sequences and states of {n_k}")
+    if k_lens is not None:
+        _require(k_lens, "k_lens", torch.int32, dev)
+        if k_lens.numel() != n:
+            raise ValueError(f"k_lens must have a length for each of the {n} sequences")
+    if k_mask is not None:
+        _expect(k_mask, "k_mask", lead_k + (S,), torch.bool, dev)
+    T, total = (L if cu_q is not None else n * L), (S if cu_k is not None else n * S)
+    for name, x in (("tokens", T), ("states", total)):
+        _int32(name, x)
+    shape = lead_q + ((H_q, L, d) if out_layout == "heads" else (L, H_q, d))
+    lse = (H_q, T) if cu_q is not None else lead_q + (H_q, L)
+    p = VdaCrossProblem(T, total, n, _ptr(cu_q), _ptr(cu_k), _ptr(k_lens), _ptr(k_mask), H_q, H_k, d,
+                        LAYOUTS[layout], LAYOUTS[kv_layout], LAYOUTS[out_layout], q_stride, k_stride,
+                        v_stride, 0, 0, 0, int(dt == torch.float32),
+                        d ** -0.5 if scale is None else float(scale))
+    return p, shape, lse, dt, dev
+
+
+def _work_for(work, dev, stream, fn, *args):
+    """The given work buffer, or a new one of the bytes that fn says."""
+    need = int(_call(fn, dev, *args))
+    if work is None:
+        return _new((need,), torch.uint8, dev, stream) if need else None
+    _require(work, "work", torch.uint8, dev)
+    if work.numel() < need:
+        raise ValueError(f"work holds {work.numel()} bytes, {need} are needed")
+    return work
+
+
+def cross_forward(q, k, v, cu_q=None, cu_k=None, k_lens=None, k_mask=None, layout="heads",
+                  kv_layout=None, out_layout=None, scale=None, return_lse=False, out=None, lse=None,
+                  work=None, stream=None):
+    """Softmax attention of q to an encoder's states k, v of another length (vda_cross_forward).
+
+    layout 'heads': q [..., H_q, L, d]; 'tokens': q [..., L, H_q, d]; kv_layout (default: layout):
+    k, v [..., H_k, S, d] or [..., S, H_k, d]; out_layout (default: layout) that of the output.
+    bfloat16 or float32, H_q a multiple of H_k, d 32, 64 or 128.  Each leading index is a sequence;
+    with cu_q (int32 [n + 1]) q has none and its L tokens are n packed sequences, and likewise the
+    states with cu_k.  In the tokens layout tensors may be slices of a fused projection.  k_lens
+    (int32, one per sequence): only the first states of each are seen; k_mask (bool [..., S], or [S]
+    with cu_k): only states that are True.  scale defaults to d ** -0.5.  A query that sees no state
+    gives 0.  Returns the output, or (output, lse) with return_lse, lse float32 [..., H_q, L] ([H_q, L]
+    with cu_q).  work: a device buffer of cross_workspace(...) bytes (allocated if None); calls
+    that may run at the same time need their own.  Packed rows outside every sequence are left as
+    they are.  Nothing is recorded for autograd: the gradients come from cross_backward."""
+    p, shape, lse_shape, dt, dev = _cross_problem(q, k, v, cu_q, cu_k, k_lens, k_mask, layout,
+                                                  kv_layout, out_layout, scale)
+    if out is None:
+        out = _new(shape, dt, dev, stream)
+    else:
+        _expect(out, "out", shape, dt, dev)
+    if lse is not None:
+        _expect(lse, "lse", lse_shape, torch.float32, dev)
+    elif return_lse:
+        lse = _new(lse_shape, torch.float32, dev, stream)
+    work = _work_for(work, dev, stream, lib.vda_cross_forward_workspace, ctypes.byref(p))
+    st = _call(lib.vda_cross_forward, dev, ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+               out.data_ptr(), _ptr(lse), _ptr(work), _stream_ptr(dev, stream))
+    _check(st, "vda_cross_forward")
+    return (out, lse) if return_lse else out
+
+
+def cross_workspace(q, k, v, cu_q=None, cu_k=None, layout="heads", kv_layout=None, backward=False):
+    """Bytes of the work buffer of cross_forward (or cross_backward) for these arguments."""
+    p, _, _, _, dev = _cross_problem(q, k, v, cu_q, cu_k, None, None, layout, kv_layout, None, None)
+    fn = lib.vda_cross_backward_workspace if backward else lib.vda_cross_forward_workspace
+    return int(_call(fn, dev, ctypes.byref(p)))
+
+
+def cross_backward(dout, q, k, v, out, lse, cu_q=None, cu_k=None, k_lens=None, k_mask=None,
+                   layout="heads", kv_layout=None, out_layout=None, scale=None, outs=None, work=None,
+                   stream=None):
+    """The gradients of cross_forward (vda_cross_backward): dout of the output, out and lse the
+    forward pass's; the other arguments as there.  Returns (dq, dk, dv); `outs`, such a tuple, is
+    filled instead of new tensors (in the tokens layout they may be slices of fused gradients)."""
+    p, shape, lse_shape, dt, dev = _cross_problem(q, k, v, cu_q, cu_k, k_lens, k_mask, layout,
+                                                  kv_layout, out_layout, scale)
+    _expect(dout, "dout", shape, dt, dev)
+    _expect(out, "out", shape, dt, dev)
+    _expect(lse, "lse", lse_shape, torch.float32, dev)
+    if outs is None:
+        outs = tuple(_new(t.shape, dt, dev, stream) for t in (q, k, v))
+    else:
+        if len(outs) != 3:
+            raise ValueError("outs must be (dq, dk, dv)")
+        sides = (layout, layout if kv_layout is None else kv_layout)
+        strides = []
+        for t, like, name, lay in zip(outs, (q, k, v), ("dq", "dk", "dv"), (sides[0], sides[1], sides[1])):
+            _like(t, name, like.shape, dt, dev)
+            if lay == "heads":
+                _require(t, name, dt, dev)
+            strides.append(0 if lay == "heads" else _row_stride(t, name, 2))
+        p.dq_row_stride, p.dk_row_stride, p.dv_row_stride = strides
+    work = _work_for(work, dev, stream, lib.vda_cross_backward_workspace, ctypes.byref(p))
+    st = _call(lib.vda_cross_backward, dev, ctypes.byref(p), dout.data_ptr(), q.data_ptr(),
+               k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+               *(t.data_ptr() for t in outs), _ptr(work), _stream_ptr(dev, stream))
+    _check(st, "vda_cross_backward")
+    return tuple(outs)
+
+
+def _cross_step_problem(q, k, v, k_lens, k_mask, slots, kv_layout, scale):
+    dt, dev = _storage(q, "q")
+    if q.dim() != 4 or not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("q must be [n, t, H_q, d] and k, v [n_slots, S, H_k, d] or [n_slots, H_k, S, d]")
+    _require(q, "q", dt, dev)
+    (m,), H_k, S, d, k_stride = _cross_side(k, "k", kv_layout, None, dt, dev)
+    v_stride = _cross_side(v, "v", kv_layout, None, dt, dev)[4]
+    n, t, H_q, d_q = q.shape
+    if v.shape != k.shape or d_q != d:
+        raise ValueError("k and v must have one shape, and q's head dimension")
+    if H_k < 1 or H_q < 1 or H_q % H_k:
+        raise ValueError(f"{H_q} query heads must be a multiple of {H_k} key heads")
+    if k_lens is not None:
+        _expect(k_lens, "k_lens", (m,), torch.int32, dev)
+    if k_mask is not None:
+        _expect(k_mask, "k_mask", (m, S), torch.bool, dev)
+    if slots is not None:
+        _expect(slots, "slots", (n,), torch.int32, dev)
+    p = VdaCrossProblem(_int32("tokens", n * t), _int32("states", m * S), n, None, None, _ptr(k_lens),
+                        _ptr(k_mask), H_q, H_k, d, LAYOUTS["tokens"], LAYOUTS[kv_layout],
+                        LAYOUTS["tokens"], 0, k_stride, v_stride, 0, 0, 0, int(dt == torch.float32),
+                        d ** -0.5 if scale is None else float(scale))
+    return p, m, dt, dev
+
+
+def cross_step(q, k, v, k_lens=None, k_mask=None, slots=None, kv_layout="tokens", scale=None,
+               out=None, work=None, stream=None):
+    """A few tokens of each of n sequences against a pool of cached states (vda_cross_step): q [n,
+    t, H_q, d]; k, v [n_slots, S, H_k, d] (kv_layout 'tokens'; slices of a fused cache are fine) or
+    [n_slots, H_k, S, d] ('heads'); k_lens int32 [n_slots] and k_mask bool [n_slots, S] say which
+    of a slot's states are seen.  slots: int32 [n], the slot that each sequence reads (the same one
+    may be given to several; one outside the pool marks a row of padding, whose output is left as
+    it is), or None (slot i for sequence i).  Returns the output [n, t, H_q, d].  work: a device
+    buffer of cross_step_workspace(...) bytes (allocated if None)."""
+    p, m, dt, dev = _cross_step_problem(q, k, v, k_lens, k_mask, slots, kv_layout, scale)
+    if out is None:
+        out = _new(q.shape, dt, dev, stream)
+    else:
+        _expect(out, "out", q.shape, dt, dev)
+    work = _work_for(work, dev, stream, lib.vda_cross_step_workspace, ctypes.byref(p), m)
+    st = _call(lib.vda_cross_step, dev, ctypes.byref(p), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+               _ptr(slots), m, out.data_ptr(), _ptr(work), _stream_ptr(dev, stream))
+    _check(st, "vda_cross_step")
+    return out
+
+
+def cross_step_workspace(q, k, v, kv_layout="tokens"):
+    """Bytes of the work buffer of cross_step for these arguments."""
+    p, m, _, dev = _cross_step_problem(q, k, v, None, None, None, kv_layout, None)
+    return int(_call(lib.vda_cross_step_workspace, dev, ctypes.byref(p), m))
+
+
+def _gate_type(gate, dt):
+    if gate not in GATES:
+        raise ValueError(f"gate must be one of {sorted(GATES)}")
+    return torch.float32 if gate == "log" else dt
+
+
+def _recur_problem(x, g, gate, cu_seqlens, reverse):
+    """The problem, and the shape of its states."""
+    dt, dev = _storage(x, "x")
+    gt = _gate_type(gate, dt)
+    if x.dim() < 2:
+        raise ValueError("x must be [..., L, C]")
+    _like(g, "g", x.shape, gt, dev)
+    lead, (L, C) = tuple(x.shape[:-2]), x.shape[-2:]
+    if cu_seqlens is not None:
+        if lead:
+            raise ValueError("with cu_seqlens, x and g have two dimensions (one packed batch)")
+        _require(cu_seqlens, "cu_seqlens", torch.int32, dev)
+        if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+            raise ValueError("cu_seqlens must hold one more offset than there are sequences")
+        n, T, states = cu_seqlens.numel() - 1, L, (cu_seqlens.numel() - 1, C)
+    else:
+        n, states = math.prod(lead), lead + (C,)
+        T = n * L
+    p = VdaRecurProblem(_int32("tokens", T), n, _ptr(cu_seqlens), _int32("channels", C), GATES[gate],
+                        int(bool(reverse)), _row_stride(x, "x", 1), _row_stride(g, "g", 1), 0, 0,
+                        int(dt == torch.float32))
+    return p, states, dt, gt, dev
+
+
+def recur_forward(x, g, gate="log", cu_seqlens=None, reverse=False, state=None, return_state=False,
+                  out=None, state_out=None, work=None, stream=None):
+    """The channel-wise gated recurrence h_t = a_t h_{t-1} + u_t over whole sequences
+    (vda_recur_forward).
+
+    x, g [..., L, C] (slices of a fused projection are fine), x bfloat16 or float32, C a multiple of
+    8.  gate 'log': a = exp(g), u = x, g float32; 'logit': a = sigmoid(g), u = (1 - a) x; 'norm':
+    a = sigmoid(g), u = sqrt(1 - a^2) x; g of x's type in both.  Each leading index is a sequence;
+    with cu_seqlens (int32 [n + 1]) there is none, and the L tokens are n packed sequences.
+    reverse: from the last token to the first.  state: the states to start from, [..., C] float32
+    ([n, C] with cu_seqlens), or None (zero).  Returns the output (x's shape), or (output, last
+    states) with return_state.  work: a device buffer of recur_workspace(...) bytes (allocated
+    if None); calls that may run at the same time need their own.  Packed rows outside every
+    sequence are left as they are.  Nothing is recorded for autograd: the gradients come from
+    recur_backward."""
+    p, states, dt, _, dev = _recur_problem(x, g, gate, cu_seqlens, reverse)
+    if state is not None:
+        _expect(state, "state", states, torch.float32, dev)
+    if out is None:
+        out = _new(x.shape, dt, dev, stream)
+    else:
+        _expect(out, "out", x.shape, dt, dev)
+    if state_out is not None:
+        _expect(state_out, "state_out", states, torch.float32, dev)
+    elif return_state:
+        state_out = _new(states, torch.float32, dev, stream)
+    work = _work_for(work, dev, stream, lib.vda_recur_forward_workspace, ctypes.byref(p))
+    st = _call(lib.vda_recur_forward, dev, ctypes.byref(p), x.data_ptr(), g.data_ptr(), _ptr(state),
+               out.data_ptr(), _ptr(state_out), _ptr(work), _stream_ptr(dev, stream))
+    _check(st, "vda_recur_forward")
+    return (out, state_out) if return_state else out
+
+
+def recur_workspace(x, g, gate="log", cu_seqlens=None, backward=False):
+    """Bytes of the work buffer of recur_forward (or recur_backward) for these arguments."""
+    p, _, _, _, dev = _recur_problem(x, g, gate, cu_seqlens, False)
+    fn = lib.vda_recur_backward_workspace if backward else lib.vda_recur_forward_workspace
+    return int(_call(fn, dev, ctypes.byref(p)))
+
+
+def recur_backward(dout, x, g, gate="log", cu_seqlens=None, reverse=False, state=None, dstate=None,
+                   outs=None, work=None, stream=None):
+    """The gradients of recur_forward (vda_recur_backward): dout of the output, dstate of the last
+    states (or None: zero); the other arguments as there.  Returns (dx, dg, dstate_in), dstate_in
+    None where state is None; `outs`, such a tuple, is filled instead of new tensors (dx and dg
+    may be slices of a fused gradient)."""
+    p, states, dt, gt, dev = _recur_problem(x, g, gate, cu_seqlens, reverse)
+    _expect(dout, "dout", x.shape, dt, dev)
+    for t, n in ((state, "state"), (dstate, "dstate")):
+        if t is not None:
+            _expect(t, n, states, torch.float32, dev)
+    if outs is None:
+        outs = (_new(x.shape, dt, dev, stream), _new(x.shape, gt, dev, stream),
+                _new(states, torch.float32, dev, stream) if state is not None else None)
+    else:
+        if len(outs) != 3:
+            raise ValueError("outs must be (dx, dg, dstate_in)")
+        _like(outs[0], "dx", x.shape, dt, dev)
+        _like(outs[1], "dg", x.shape, gt, dev)
+        if outs[2] is not None:
+            _expect(outs[2], "dstate_in", states, torch.float32, dev)
+        p.dx_row_stride, p.dg_row_stride = _row_stride(outs[0], "dx", 1), _row_stride(outs[1], "dg", 1)
+    work = _work_for(work, dev, stream, lib.vda_recur_backward_workspace, ctypes.byref(p))
+    st = _call(lib.vda_recur_backward, dev, ctypes.byref(p), dout.data_ptr(), x.data_ptr(),
+               g.data_ptr(), _ptr(state), _ptr(dstate), *(_ptr(t) for t in outs), _ptr(work),
+               _stream_ptr(dev, stream))
+    _check(st, "vda_recur_backward")
+    return tuple(outs)
+
+
+def recur_step(x, g, state, gate="log", slots=None, out=None, stream=None):
+    """A few tokens of each of n sequences (vda_recur_step): x, g [n, t, C] (types as in
+    recur_forward), state [n_slots, C] float32, updated in place.  slots: int32 [n], the sequences'
+    slots (distinct; one outside the pool marks a row of padding, whose output is left as it is),
+    or None (slot i for sequence i).  Returns the output [n, t, C]."""
+    dt, dev = _storage(x, "x")
+    gt = _gate_type(gate, dt)
+    if x.dim() != 3:
+        raise ValueError("x must be [n, t, C]")
+    n, t, C = x.shape
+    _require(x, "x", dt, dev)
+    _expect(g, "g", x.shape, gt, dev)
+    _require(state, "state", torch.float32, dev)
+    if state.dim() != 2 or state.shape[1] != C:
+        raise ValueError(f"state shape {tuple(state.shape)} must be [n_slots, {C}]")
+    if slots is not None:
+        _expect(slots, "slots", (n,), torch.int32, dev)
+    if out is None:
+        out = _new(x.shape, dt, dev, stream)
+    else:
+        _expect(out, "out", x.shape, dt, dev)
+    st = _call(lib.vda_recur_step, dev, x.data_ptr(), g.data_ptr(), n, t, C, GATES[gate],
+               int(dt == torch.float32), _ptr(slots), state.shape[0], state.data_ptr(), out.data_ptr(),
+               _stream_ptr(dev, stream))
+    _check(st, "vda_recur_step")
     return out
