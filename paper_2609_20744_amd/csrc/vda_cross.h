@@ -49,7 +49,9 @@ struct CrossArgs {
   float scale, c;        // c = |scale| log2 e
   int flip;              // scale < 0: the sign of one factor of each score is changed
   int tiles, splits;     // tiles of rows (of states in the gradient of k and v) of a head
+  int range;             // gradient of k and v: rows that a workgroup takes, about; at most `splits` ranges
   float *part, *part2;  // workspace: what splits leave
+  int* counts;          // [S] ranges of a state's sequence
   float2* stats;        // [T * Hq] backward: lse in powers of two, and D = sum of dout o
 };
 
@@ -62,54 +64,72 @@ struct CrossSeq {
 
 __device__ __forceinline__ int clamp_to(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// Offsets outside [0, total] are taken as the nearest bound, and a length below 0 as 0.
-__device__ __forceinline__ void packed_range(const int* cu, int i, int total, int& first, int& len) {
-  first = uniform(clamp_to(cu[i], 0, total));
-  const int end = uniform(clamp_to(cu[i + 1], 0, total));
+// Offsets of sequence i of a packed tensor, from those of a wave's lanes (b + lane) where
+// it has both.  Offsets outside [0, total] are taken as the nearest bound, and a length
+// below 0 as 0.
+__device__ __forceinline__ void packed_range(const int* cu, int lanes, int b, int i, int total, int& first, int& len) {
+  const int at = i - b;
+  const int c = at < 64 ? __builtin_amdgcn_readlane(lanes, at) : cu[i];
+  const int d = at < 63 ? __builtin_amdgcn_readlane(lanes, at + 1) : cu[i + 1];
+  first = uniform(clamp_to(c, 0, total));
+  const int end = uniform(clamp_to(d, 0, total));
   len = end > first ? end - first : 0;
-}
-
-__device__ __forceinline__ CrossSeq cross_seq(const CrossArgs& a, int i) {
-  CrossSeq s;
-  s.i = s.kv = i;
-  s.q0 = s.k0 = 0;
-  s.lq = a.Lq, s.lk = a.Lk;
-  if (a.cu_q != nullptr) packed_range(a.cu_q, i, a.T, s.q0, s.lq);
-  if (a.cu_k != nullptr) packed_range(a.cu_k, i, a.S, s.k0, s.lk);
-  if (a.slots != nullptr) {
-    s.kv = uniform(a.slots[i]);
-    if (s.kv < 0 || s.kv >= a.n_slots) s.lq = s.lk = s.kv = 0;  // a row of padding
-  }
-  s.seen = s.lk;
-  if (a.k_lens != nullptr) s.seen = uniform(clamp_to(a.k_lens[s.kv], 0, s.lk));
-  return s;
 }
 
 __device__ __forceinline__ size_t seq_base(const CrossStrides& s, const int* cu, int first, int i) {
   return cu != nullptr ? (size_t)first * s.tok : (size_t)i * s.seq;
 }
 
-// The sequence that tile `t` of a head belongs to, and which of its tiles it is;
-// sequence -1: none.  A packed sequence i has the tiles from first_i / per + i on,
-// first_i being its first row: as many places as it needs or one more, so no
-// table is made and every place is found from the offsets alone.
-__device__ __forceinline__ int2 seq_of_tile(const int* cu, int n, int total, int L, int group, int per, int t) {
+// The sequence that tile `t` of a head belongs to, and which of its tiles it is; false: none.
+// Tiles of `per` rows of the queries' side, or (KEYS) of the states'.  A packed
+// sequence i has the tiles from first_i / per + i on, first_i being its first row: as many
+// places as it needs or one more, so no table is made and every place is found from the
+// offsets alone.  Both lists are loaded before either is waited for.
+template <bool KEYS>
+__device__ __forceinline__ bool seq_of_tile(const CrossArgs& a, int per, int t, CrossSeq& s, int& tile) {
+  const int* cu = KEYS ? a.cu_k : a.cu_q;
+  const int total = KEYS ? a.S : a.T, group = KEYS ? 1 : a.group, lane = threadIdx.x & 63;
+  s.q0 = s.k0 = 0;
+  s.lq = a.Lq, s.lk = a.Lk;
+  int lanes_q = 0, lanes_k = 0, base = 0;
   if (cu == nullptr) {
-    const int each = (L * group + per - 1) / per;
-    const int i = uniform(t / each);
-    return make_int2(i < n ? i : -1, t - i * each);
+    const int each = ((KEYS ? a.Lk : a.Lq) * group + per - 1) / per;
+    s.i = uniform(t / each);
+    if (s.i >= a.n) return false;
+    tile = t - s.i * each;
+    base = s.i;  // one lane's worth
+    const int at = s.i + lane < a.n + 1 ? s.i + lane : a.n;
+    if (a.cu_q != nullptr) lanes_q = a.cu_q[at];
+    if (a.cu_k != nullptr) lanes_k = a.cu_k[at];
+  } else {
+    int before = 0;
+    for (int b = 0; b < a.n; b += 64) {
+      const int at = b + lane < a.n + 1 ? b + lane : a.n;
+      int x = 0, y = 0;
+      if (a.cu_q != nullptr) x = a.cu_q[at];
+      if (a.cu_k != nullptr) y = a.cu_k[at];
+      const uint64_t is = __ballot(b + lane < a.n && clamp_to(KEYS ? y : x, 0, total) * group / per + b + lane <= t);
+      if (is == 0) break;  // in order, so that no later one starts before t
+      before += __popcll(is);
+      lanes_q = x, lanes_k = y, base = b;
+    }
+    s.i = uniform(before) - 1;
+    if (s.i < base) return false;  // none; or offsets out of order
   }
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b = 0; b < n; b += 64) {
-    const int i = b + lane;
-    const bool is = i < n && clamp_to(cu[i < n ? i : 0], 0, total) * group / per + i <= t;
-    before += __popcll(__ballot(is));
+  if (a.cu_q != nullptr) packed_range(a.cu_q, lanes_q, base, s.i, a.T, s.q0, s.lq);
+  if (a.cu_k != nullptr) packed_range(a.cu_k, lanes_k, base, s.i, a.S, s.k0, s.lk);
+  if (cu != nullptr) {
+    tile = t - (uniform((KEYS ? s.k0 : s.q0) * group / per) + s.i);
+    if (tile < 0) return false;  // out of order
   }
-  const int i = uniform(before) - 1;
-  if (i < 0) return make_int2(-1, 0);
-  const int from = uniform(clamp_to(cu[i], 0, total) * group / per + i);
-  return make_int2(from <= t ? i : -1, t - from);  // -1 for offsets that are out of order only
+  s.kv = s.i;
+  if (a.slots != nullptr) {
+    s.kv = uniform(a.slots[s.i]);
+    if (s.kv < 0 || s.kv >= a.n_slots) return false;  // a row of padding
+  }
+  s.seen = s.lk;
+  if (a.k_lens != nullptr) s.seen = uniform(clamp_to(a.k_lens[s.kv], 0, s.lk));
+  return true;
 }
 
 // ---------------------------------------------------------------------------
@@ -179,52 +199,64 @@ struct CrossTile {
     if constexpr (kPieces == 8) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
     return r >> 2 & 3;
   }
-  // Channels 16 s + 8 lh .. + 7 of row li of the rows at byte `at` (a multiple of 16 rows in).
-  // The address is one addition to the tile's array: of a longer chain the
-  // compiler does not see which array it is in, and waits for copies into the others.
-  static __device__ __forceinline__ X row_frag(const char* tile, int at, int s, int lane) {
+  // A lane's offsets in a tile `from` bytes behind an array's begin, opaque: the
+  // others are these with constant bits changed, so that an address is one instruction
+  // and one register, not one of its own for each of a tile's reads.
+  static constexpr int kColOffs = F32 ? 8 : 2;
+  struct Lane {
+    int row, col[kColOffs];
+  };
+  static __device__ __forceinline__ Lane lane_of(int lane, int from = 0) {
+    Lane l;
     const int li = lane & 31, lh = lane >> 5;
-    const int row = at + li * kRow;
+    l.row = from + li * kRow + ((F32 ? 2 * lh : lh) ^ swizzle(li)) * 16;
+#pragma unroll
+    for (int s = 0; s < kColOffs; ++s) {
+      if constexpr (F32) {
+        const int r = (s >> 2) * 8 + 4 * lh + (s & 3);
+        l.col[s] = from + r * kRow + ((li >> 2) ^ swizzle(r)) * 16 + (li & 3) * 4;
+      } else {
+        // ds_read_b64_tr_b16: lane i of 16 receives element i % 4 of the 8 bytes that lanes i / 4 + 4 e address.
+        const int r = 8 * s + 4 * lh + (lane >> 2 & 3);
+        const int piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+        l.col[s] = from + r * kRow + (piece ^ swizzle(r)) * 16 + (lane & 1) * 8;
+      }
+    }
+    return again(l);
+  }
+  // Offsets that the compiler takes for new: used in a loop's body, they keep the
+  // others from being computed before the loop and held through it.
+  static __device__ __forceinline__ Lane again(Lane l) {
+    asm volatile("" : "+v"(l.row));
+#pragma unroll
+    for (int s = 0; s < kColOffs; ++s) asm volatile("" : "+v"(l.col[s]));
+    return l;
+  }
+  // Channels 16 s + 8 lh .. + 7 of row li of the rows behind `tile` (a multiple of 16 rows in).
+  // An address is one addition to a named array: of a longer chain the compiler
+  // does not see which array it is in, and waits for copies into the others.
+  static __device__ __forceinline__ X row_frag(const char* tile, int s, const Lane& l) {
     if constexpr (F32) {
-      const floatx4 a = *reinterpret_cast<const floatx4*>(tile + (row + ((4 * s + 2 * lh) ^ swizzle(li)) * 16));
-      const floatx4 b = *reinterpret_cast<const floatx4*>(tile + (row + ((4 * s + 2 * lh + 1) ^ swizzle(li)) * 16));
+      const floatx4 a = *reinterpret_cast<const floatx4*>(tile + (l.row ^ 64 * s));
+      const floatx4 b = *reinterpret_cast<const floatx4*>(tile + (l.row ^ (64 * s + 16)));
       return X{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     } else {
-      return *reinterpret_cast<const bf16x8*>(tile + (row + ((2 * s + lh) ^ swizzle(li)) * 16));
+      return *reinterpret_cast<const bf16x8*>(tile + (l.row ^ 32 * s));
     }
   }
-  // Channel 32 b + li of the rows 4 lh + e and 8 + 4 lh + e, e < 4, behind byte `at`.
-  static __device__ __forceinline__ X col_frag(const char* tile, int at, int b, int lane) {
+  // Channel 32 b + li of the rows 4 lh + e and 8 + 4 lh + e, e < 4, behind `tile`.
+  static __device__ __forceinline__ X col_frag(const char* tile, int b, const Lane& l) {
     if constexpr (F32) {
-      const int li = lane & 31, lh = lane >> 5;
       X x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = (e >> 2) * 8 + 4 * lh + (e & 3);
-        x[e] = *reinterpret_cast<const float*>(
-            tile + (at + r * kRow + ((8 * b + (li >> 2)) ^ swizzle(r)) * 16 + (li & 3) * 4));
-      }
+      for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const float*>(tile + (l.col[e] ^ 128 * b));
       return x;
     } else {
-      // ds_read_b64_tr_b16: lane i of 16 receives element i % 4 of the 8 bytes that lanes i / 4 + 4 e address.
-      shortx4 v[2];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const int r = 8 * w + 4 * (lane >> 5) + (lane >> 2 & 3);
-        const int piece = 4 * b + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-        v[w] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_shortx4*)(tile + (at + r * kRow + (piece ^ swizzle(r)) * 16 + (lane & 1) * 8)));
-      }
-      return __builtin_bit_cast(bf16x8, shortx8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]});
+      const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + (l.col[0] ^ 64 * b)));
+      const shortx4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + (l.col[1] ^ 64 * b)));
+      return __builtin_bit_cast(bf16x8, shortx8{v[0], v[1], v[2], v[3], w[0], w[1], w[2], w[3]});
     }
   }
-  // Writes zeros over the rows whose bit is not set.
-  template <int ROWS, int THREADS>
-  static __device__ __forceinline__ void clear_rows(char* tile, int at, uint64_t bits, int tid) {
-    for (int p = tid; p < ROWS * kPieces; p += THREADS)
-      if (!(bits >> (p / kPieces) & 1)) *reinterpret_cast<uint4*>(tile + (at + p * 16)) = make_uint4(0u, 0u, 0u, 0u);
-  }
-  static constexpr int kCopies = kCrossTile * kRow / 1024;  // of a tile of 64 rows
 };
 
 // Copies ROWS rows of consecutive tokens into a tile; rows behind `last` repeat
@@ -232,34 +264,61 @@ struct CrossTile {
 template <bool F32, int D, int ROWS, int WAVES>
 __device__ __forceinline__ void copy_states(const void* base, size_t row_elems, int last, char* tile, int wave, int lane) {
   typedef CrossTile<F32, D> Tile;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024;
   const __amdgpu_buffer_rsrc_t src = make_rsrc(base, 0xfffffff0u);
   const uint32_t row_bytes = (uint32_t)row_elems * Tile::kEs;
 #pragma unroll
-  for (int i = 0; i < ROWS * Tile::kRow / 1024 / WAVES; ++i) {
+  for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
     const int p = wave + i * WAVES, at = p * 64 + lane;
+    if (kPieces % WAVES != 0 && p >= kPieces) break;
     const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
                                              (uint32_t)(r < last ? r : last) * row_bytes + piece * 16u, 0, 0, 0);
   }
 }
 
-// Copies 64 rows of queries (token x head) into a tile; rows behind `last` repeat it.
+// Writes zeros over the rows whose bit is not set, each wave over what it copied
+// itself, once that is there.  bits: 64 rows each.
+template <bool F32, int D, int ROWS, int WAVES>
+__device__ __forceinline__ void clear_copied(char* tile, const uint64_t (&bits)[(ROWS + 63) / 64], int wave, int lane) {
+  typedef CrossTile<F32, D> Tile;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024;
+#pragma unroll
+  for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
+    const int p = wave + i * WAVES, at = p * 64 + lane;
+    if (kPieces % WAVES != 0 && p >= kPieces) break;
+    const int r = at / Tile::kPieces;
+    const uint64_t w = ROWS > 64 && r >= 64 ? bits[ROWS > 64 ? 1 : 0] : bits[0];
+    if (!(w >> (r & 63) & 1)) *reinterpret_cast<uint4*>(tile + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// Copies ROWS rows of queries (token x head) into a tile; rows behind `last` repeat it.
 // base: the sequence's first token of the key head's first query head.
-template <bool F32, int D, int WAVES>
+template <bool F32, int D, int ROWS, int WAVES>
 __device__ __forceinline__ void copy_rows(const CrossArgs& a, const void* base, const CrossStrides& s, int r0, int last,
                                           char* tile, int wave, int lane) {
   typedef CrossTile<F32, D> Tile;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024;
   const int t0 = r0 / a.group, g0 = r0 - t0 * a.group;
   const char* from = (const char*)base + (size_t)t0 * s.tok * Tile::kEs;
 #pragma unroll
-  for (int i = 0; i < Tile::kCopies / WAVES; ++i) {
+  for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
     const int p = wave + i * WAVES, at = p * 64 + lane;
+    if (kPieces % WAVES != 0 && p >= kPieces) break;
     const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
     const uint32_t x = g0 + (r < last ? r : last);
     const uint32_t t = x * a.group_magic >> 24, g = x - t * a.group;
     __builtin_amdgcn_global_load_lds((global_void*)(from + (t * s.tok + g * s.head) * Tile::kEs + piece * 16),
                                      (lds_void*)(tile + p * 1024), 16, 0, 0);
   }
+}
+
+// The wave's copies into LDS are there.
+__device__ __forceinline__ void copies_landed() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt 0
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Barrier behind which the copies into LDS that any wave issued before it are there.
@@ -288,11 +347,10 @@ __device__ __forceinline__ Row row_of(const CrossArgs& a, const CrossSeq& s, int
   return w;
 }
 
-// Which of states at .. at + 63 (or 31) are seen.
-template <int TILE>
+// Which of the 64 states from one on are seen: `left` of them are the sequence's,
+// byte is the mask's of the lane's.
 __device__ __forceinline__ uint64_t seen_bits(int left, bool masked, uint8_t byte, int lane) {
-  uint64_t bits = left >= 64 ? ~0ull : (1ull << left) - 1;
-  if (TILE < 64) bits &= (1ull << (TILE & 63)) - 1;
+  uint64_t bits = left >= 64 ? ~0ull : left <= 0 ? 0 : (1ull << left) - 1;
   if (masked) bits &= __ballot(byte != 0 && lane < left);
   return bits;
 }
@@ -314,9 +372,10 @@ hipError_t launch_cross_forward(bool f32, int d, bool few, const CrossArgs& a, h
 hipError_t launch_cross_join(bool f32, int d, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_dq(bool f32, int d, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_dkv(bool f32, int d, const CrossArgs& a, hipStream_t stream);
-// part sums [splits][rows][d] to rows of a tensor of H heads.
+// Sums of part [splits][rows][d] to the rows of a tensor of H heads; counts: of how many each token's are, or null (all).
 struct CrossSum {
   const float* part;
+  const int* counts;
   void* out;
   CrossStrides s;
   const int* cu;

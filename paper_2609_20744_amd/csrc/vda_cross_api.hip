@@ -72,8 +72,8 @@ CrossStrides strides_of(int layout, bool packed, int total, int n, int H, int d,
 struct CrossPlan {
   bool few;             // the waves of a workgroup share its rows
   int tiles, splits;    // of the rows; ranges of the states
-  int tiles_k, splits_k;  // backward: of the states; ranges of the rows
-  size_t part, part2, stats, total;  // workspace offsets
+  int tiles_k, splits_k, range;  // backward: of the states; ranges of the rows at most, and their rows
+  size_t part, part2, stats, counts, total;  // workspace offsets
 };
 
 long long tiles_of(bool packed, long long total, int n, long long per_token, int tile) {
@@ -107,8 +107,13 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     }
   } else {
     c.tiles_k = (int)tiles_of(p->cu_k != nullptr, p->S, p->n_seqs, 1, vda::kCrossRows);
-    c.splits_k = (int)ranges((long long)c.tiles_k * p->H_k, (rows + vda::kCrossTile - 1) / vda::kCrossTile);
+    const long long most = p->cu_q ? (long long)p->T * group : rows;
+    const long long groups = (long long)c.tiles_k * p->H_k;
+    const long long share = rows * groups / (3 * cus);
+    c.range = (int)std::max(groups < cus ? 64LL : 512LL, (share + 63) / 64 * 64);
+    c.splits_k = (int)std::min(8LL, (most + c.range - 1) / c.range);
     c.stats = take(q_rows * 8);
+    c.counts = take((size_t)p->S * 4);
     const size_t a = c.splits > 1 ? c.splits * q_rows * p->d * 4 : 0;
     const size_t b = c.splits_k > 1 ? round_up(c.splits_k * k_rows * p->d * 4, 256) : 0;
     c.part = take(std::max(a, 2 * b));
@@ -141,6 +146,8 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.part = reinterpret_cast<float*>(w + c.part);
   a.part2 = reinterpret_cast<float*>(w + c.part2);
   a.stats = reinterpret_cast<float2*>(w + c.stats);
+  a.counts = reinterpret_cast<int*>(w + c.counts);
+  a.range = c.range;
   return a;
 }
 
@@ -259,12 +266,12 @@ int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void*
   const bool f32 = p->is_f32 != 0;
   hipError_t e = vda::launch_cross_dq(f32, p->d, a, stream);
   if (e == hipSuccess && c.splits > 1)
-    e = vda::launch_cross_sum(f32, p->d, vda::CrossSum{a.part, dq, a.sdq, a.cu_q, a.n, a.Lq, a.Hq, a.splits, (long long)a.T * a.Hq},
+    e = vda::launch_cross_sum(f32, p->d, vda::CrossSum{a.part, nullptr, dq, a.sdq, a.cu_q, a.n, a.Lq, a.Hq, a.splits, (long long)a.T * a.Hq},
                               stream);
   a.tiles = c.tiles_k, a.splits = c.splits_k;
   if (e == hipSuccess) e = vda::launch_cross_dkv(f32, p->d, a, stream);
   if (e == hipSuccess && c.splits_k > 1) {
-    vda::CrossSum s = {a.part, dk, a.sdk, a.cu_k, a.n, a.Lk, a.Hk, a.splits, (long long)a.S * a.Hk};
+    vda::CrossSum s = {a.part, a.counts, dk, a.sdk, a.cu_k, a.n, a.Lk, a.Hk, a.splits, (long long)a.S * a.Hk};
     e = vda::launch_cross_sum(f32, p->d, s, stream);
     s.part = a.part2, s.out = dv, s.s = a.sdv;
     if (e == hipSuccess) e = vda::launch_cross_sum(f32, p->d, s, stream);

@@ -27,10 +27,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
   const int hk = uniform(id / (unsigned)a.tiles);
   if (hk >= a.Hk) return;
-  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kCrossRows, id - hk * a.tiles);
-  if (at.x < 0) return;
-  const CrossSeq s = cross_seq(a, at.x);
-  const int r0 = at.y * kCrossRows;
+  CrossSeq s;
+  int tile;
+  if (!seq_of_tile<false>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
 
@@ -60,6 +60,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dq[e] = floatx16{};
   uint8_t byte = 1;
+  const typename Tile::Lane offs = Tile::lane_of(lane);
 
   auto copy = [&](int t, char* kt, char* vt) {
     const int first = t * kCrossTile, last = s.seen - 1 - first;
@@ -67,22 +68,25 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
     copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
     if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
   };
-  auto step = [&](int t, uint8_t byte_t, char* kt, char* vt) {
-    const uint64_t bits = seen_bits<64>(s.seen - t * kCrossTile, mask != nullptr, byte_t, lane);
-    if (bits == 0) return;
+  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
+    copies_landed();
+    const uint64_t seen[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
+    const uint64_t bits = seen[0];
     const bool all = ~bits == 0;
-    if (mask != nullptr && !all) {
-      Tile::template clear_rows<kCrossTile, kThreads>(kt, 0, bits, tid);
-      Tile::template clear_rows<kCrossTile, kThreads>(vt, 0, bits, tid);
-      lds_barrier();
-    }
+    // What stands in a masked place may be anything: 0 times it has to be 0.
+    if (mask != nullptr && !all) clear_copied<F32, D, kCrossTile, 4>(kt, seen, wave, lane);
+    lds_barrier();
+    if (t + 1 < to) copy(t + 1, next_k, next_v);
+    if (bits == 0) return;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      const typename Tile::Lane here = Tile::again(offs);
       floatx16 p = {}, dp = {};
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) p = Fr::mma(Tile::row_frag(kt, 32 * b * Tile::kRow, e, lane), q[e], p);
-#pragma unroll
-      for (int e = 0; e < D / 16; ++e) dp = Fr::mma(Tile::row_frag(vt, 32 * b * Tile::kRow, e, lane), g[e], dp);
+      for (int e = 0; e < D / 16; ++e) {
+        p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, e, here), q[e], p);
+        dp = Fr::mma(Tile::row_frag(vt + 32 * b * Tile::kRow, e, here), g[e], dp);
+      }
       const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -95,23 +99,15 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
         const typename Fr::X x = Fr::of(p, h);
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
-          dq[e] = Fr::mma(Tile::col_frag(kt, (32 * b + 16 * h) * Tile::kRow, e, lane), x, dq[e]);
+          dq[e] = Fr::mma(Tile::col_frag(kt + (32 * b + 16 * h) * Tile::kRow, e, here), x, dq[e]);
       }
     }
   };
   if (from < to) {
     copy(from, k0, v0);
-    for (int t = from;;) {
-      cross_barrier();
-      uint8_t b = byte;
-      if (t + 1 < to) copy(t + 1, k1, v1);
-      step(t, b, k0, v0);
-      if (++t >= to) break;
-      cross_barrier();
-      b = byte;
-      if (t + 1 < to) copy(t + 1, k0, v0);
-      step(t, b, k1, v1);
-      if (++t >= to) break;
+    for (int t = from; t < to; t += 2) {
+      step(t, k0, v0, k1, v1);
+      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
     }
   }
   if (!row.real) return;
@@ -128,117 +124,169 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
     }
 }
 
+// Shape of the kernel of dk and dv: 128 states a workgroup, 32 a wave.  In bf16
+// two waves have the same states and every other 32 rows, so that each SIMD has two
+// waves whose products and exponentials overlap; to leave them 256 registers, v
+// comes from LDS and k alone is held.
+template <bool F32>
+struct DkvShape {
+  static constexpr int kHalves = F32 ? 1 : 2, kWaves = 4 * kHalves, kRows = 32 * kHalves;  // rows of a tile
+};
+
 template <bool F32, int D>
-__global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs a) {
+__global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void cross_dkv_kernel(CrossArgs a) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
-  constexpr int kTileBytes = kCrossTile * Tile::kRow;
-  __shared__ __align__(16) char q0[kTileBytes], g0[kTileBytes], q1[kTileBytes], g1[kTileBytes];
-  __shared__ __align__(16) float lse0[kCrossTile], dot0[kCrossTile], lse1[kCrossTile], dot1[kCrossTile];
+  typedef DkvShape<F32> Shape;
+  constexpr int kRows = Shape::kRows, kTileBytes = kRows * Tile::kRow;
+  __shared__ __align__(16) char q0[kTileBytes], g0[kTileBytes], q1[kTileBytes], g1[kTileBytes], vt[kCrossRows * Tile::kRow];
+  __shared__ __align__(16) float lse0[kRows], dot0[kRows], lse1[kRows], dot1[kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int part_of = wave & 3, half = wave >> 2;  // which 32 states, which rows
   const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
   const int hk = uniform(id / (unsigned)a.tiles);
   if (hk >= a.Hk) return;
-  const int2 at = seq_of_tile(a.cu_k, a.n, a.S, a.Lk, 1, kCrossRows, id - hk * a.tiles);
-  if (at.x < 0) return;
-  const CrossSeq s = cross_seq(a, at.x);
-  const int j0 = at.y * kCrossRows;
+  CrossSeq s;
+  int tile;
+  if (!seq_of_tile<true>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  const int j0 = tile * kCrossRows;
   if (j0 >= s.lk) return;
 
+  // The sequence's rows in ranges of about a.range, this workgroup's in tiles; none where no state is seen.
+  const int rows = s.lq * a.group;
+  int ranges = (rows + a.range - 1) / a.range;
+  ranges = ranges < 1 ? 1 : ranges > a.splits ? a.splits : ranges;
+  if ((int)blockIdx.y >= ranges) return;
+  const int tiles = j0 < s.seen ? (rows + kRows - 1) / kRows : 0, per = (tiles + ranges - 1) / ranges;
+  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+
   // The lane's state.
-  const int j = j0 + wave * 32 + (lane & 31), jc = j < s.lk ? j : s.lk - 1;
+  const int j = j0 + part_of * 32 + (lane & 31), jc = j < s.lk ? j : s.lk - 1;
   bool seen = j < s.seen;
   if (seen && a.k_mask != nullptr)
     seen = a.k_mask[(a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + jc] != 0;
-  typename Fr::X k[D / 16], v[D / 16];
-  const size_t kat = seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head + (size_t)jc * a.sk.tok;
-  const size_t vat = seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head + (size_t)jc * a.sv.tok;
+  const size_t token = (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + jc;
+  if (blockIdx.y == 0 && hk == 0 && half == 0 && lane < 32 && j < s.lk) a.counts[token] = ranges;
+  typename Fr::X k[D / 16];
+  const size_t kat = seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head;
+  const size_t vat = seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head + (size_t)j0 * a.sv.tok;
+  copy_states<F32, D, kCrossRows, Shape::kWaves>((const char*)a.v + vat * Tile::kEs, a.sv.tok, s.lk - 1 - j0, vt, wave, lane);
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) {
-    k[e] = Fr::load(a.k, kat + 16 * e + 8 * (lane >> 5));
-    v[e] = Fr::load(a.v, vat + 16 * e + 8 * (lane >> 5));
+    k[e] = Fr::load(a.k, kat + (size_t)jc * a.sk.tok + 16 * e + 8 * (lane >> 5));
     if (a.flip) k[e] = Fr::flip(k[e]);
     // What stands in a masked place may be anything.
-    if (!seen) k[e] = Fr::zero(), v[e] = Fr::zero();
+    if (!seen) k[e] = Fr::zero();
+  }
+  cross_barrier();
+  if (!seen && half == 0) {
+    constexpr int kEach = Tile::kPieces / 2;
+    for (int e = 0; e < kEach; ++e)
+      *reinterpret_cast<uint4*>(vt + ((part_of * 32 + (lane & 31)) * Tile::kRow + ((lane >> 5) * kEach + e) * 16)) =
+          make_uint4(0u, 0u, 0u, 0u);
   }
   floatx16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dk[e] = floatx16{}, dv[e] = floatx16{};
 
-  // The range of rows of this split, in tiles; none where no state of the tile is seen.
-  const int rows = s.lq * a.group;
-  const int tiles = j0 < s.seen ? (rows + kCrossTile - 1) / kCrossTile : 0, per = (tiles + a.splits - 1) / a.splits;
-  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
   const char* qb = (const char*)a.q +
                    (seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.sq.head) * Tile::kEs;
   const char* gb = (const char*)a.dout +
                    (seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.so.head) * Tile::kEs;
   const float2* stats = a.stats + (a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) * a.Hq + hk * a.group;
   float2 mine = make_float2(0.f, 0.f);
+  const typename Tile::Lane offs = Tile::lane_of(lane);
+  const char* vmine = vt + part_of * 32 * Tile::kRow;
 
   auto copy = [&](int t, char* qt, char* gt) {
-    const int first = t * kCrossTile, last = rows - 1 - first;
-    copy_rows<F32, D, 4>(a, qb, a.sq, first, last, qt, wave, lane);
-    copy_rows<F32, D, 4>(a, gb, a.so, first, last, gt, wave, lane);
+    const int first = t * kRows, last = rows - 1 - first;
+    copy_rows<F32, D, kRows, Shape::kWaves>(a, qb, a.sq, first, last, qt, wave, lane);
+    copy_rows<F32, D, kRows, Shape::kWaves>(a, gb, a.so, first, last, gt, wave, lane);
     if (wave == 0) {
       const int r = first + (lane < last ? lane : last), tok = r / a.group;
       mine = stats[(size_t)tok * a.Hq + r - tok * a.group];
-      if (lane > last) mine.x = INFINITY;  // a row behind the last leaves no p
     }
   };
-  auto keep = [&](float* lse, float* dot) {
-    if (wave == 0) lse[lane] = mine.x, dot[lane] = mine.y;
+  auto keep = [&](int t, float* lse, float* dot) {
+    // A row behind the last leaves no p.
+    if (wave == 0 && lane < kRows) lse[lane] = t * kRows + lane < rows ? mine.x : INFINITY, dot[lane] = mine.y;
   };
   auto step = [&](const char* qt, const char* gt, const float* lse, const float* dot) {
+    const typename Tile::Lane here = Tile::again(offs);
+    const int h32 = half * 32 * Tile::kRow;
+    floatx16 p = {}, dp = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      floatx16 p = {}, dp = {};
+    for (int e = 0; e < D / 16; ++e) {
+      p = Fr::mma(Tile::row_frag(qt + h32, e, here), k[e], p);
+      dp = Fr::mma(Tile::row_frag(gt + h32, e, here), Tile::row_frag(vmine, e, here), dp);
+    }
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) p = Fr::mma(Tile::row_frag(qt, 32 * b * Tile::kRow, e, lane), k[e], p);
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 z = *reinterpret_cast<const floatx4*>(lse + 32 * half + 8 * i + 4 * (lane >> 5));
+      const floatx4 y = *reinterpret_cast<const floatx4*>(dot + 32 * half + 8 * i + 4 * (lane >> 5));
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) dp = Fr::mma(Tile::row_frag(gt, 32 * b * Tile::kRow, e, lane), v[e], dp);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const floatx4 z = *reinterpret_cast<const floatx4*>(lse + 32 * b + 8 * i + 4 * (lane >> 5));
-        const floatx4 y = *reinterpret_cast<const floatx4*>(dot + 32 * b + 8 * i + 4 * (lane >> 5));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = seen ? __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e])) : 0.f;
-          p[4 * i + e] = x;
-          dp[4 * i + e] = x * (dp[4 * i + e] - y[e]);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float x = seen ? __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e])) : 0.f;
+        p[4 * i + e] = x;
+        dp[4 * i + e] = x * (dp[4 * i + e] - y[e]);
       }
+    }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const typename Fr::X x = Fr::of(p, h), y = Fr::of(dp, h);
+    for (int h = 0; h < 2; ++h) {
+      const typename Fr::X x = Fr::of(p, h), y = Fr::of(dp, h);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) {
-          dv[e] = Fr::mma(Tile::col_frag(gt, (32 * b + 16 * h) * Tile::kRow, e, lane), x, dv[e]);
-          dk[e] = Fr::mma(Tile::col_frag(qt, (32 * b + 16 * h) * Tile::kRow, e, lane), y, dk[e]);
-        }
+      for (int e = 0; e < D / 32; ++e) {
+        dv[e] = Fr::mma(Tile::col_frag(gt + h32 + 16 * h * Tile::kRow, e, here), x, dv[e]);
+        dk[e] = Fr::mma(Tile::col_frag(qt + h32 + 16 * h * Tile::kRow, e, here), y, dk[e]);
       }
     }
   };
   if (from < to) {
     copy(from, q0, g0);
     for (int t = from;;) {
-      keep(lse0, dot0);
+      keep(t, lse0, dot0);
       cross_barrier();
       if (t + 1 < to) copy(t + 1, q1, g1);
       step(q0, g0, lse0, dot0);
       if (++t >= to) break;
-      keep(lse1, dot1);
+      keep(t, lse1, dot1);
       cross_barrier();
       if (t + 1 < to) copy(t + 1, q0, g0);
       step(q1, g1, lse1, dot1);
       if (++t >= to) break;
     }
   }
+  if constexpr (Shape::kHalves == 2) {
+    // The second half's sums, through the four tiles.
+    char* room = part_of == 0 ? q0 : part_of == 1 ? g0 : part_of == 2 ? q1 : g1;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      floatx16(&x)[D / 32] = w == 0 ? dk : dv;
+      lds_barrier();
+      if (half == 1)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<floatx4*>(room + (4 * e + i) * 1024 + lane * 16) =
+                floatx4{x[e][4 * i], x[e][4 * i + 1], x[e][4 * i + 2], x[e][4 * i + 3]};
+      lds_barrier();
+      if (half == 0)
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const floatx4 y = *reinterpret_cast<const floatx4*>(room + (4 * e + i) * 1024 + lane * 16);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[e][4 * i + u] += y[u];
+          }
+    }
+    if (half == 1) return;
+  }
   if (j >= s.lk) return;
   const size_t dkat = seq_base(a.sdk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdk.head + (size_t)jc * a.sdk.tok;
   const size_t dvat = seq_base(a.sdv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdv.head + (size_t)jc * a.sdv.tok;
-  const size_t part = (size_t)blockIdx.y * ((size_t)a.S * a.Hk) +
-                      ((a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + jc) * a.Hk + hk;
+  const size_t part = (size_t)blockIdx.y * ((size_t)a.S * a.Hk) + token * a.Hk + hk;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
@@ -246,7 +294,7 @@ __global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs a) {
       const floatx4 x = floatx4{dk[e][4 * i], dk[e][4 * i + 1], dk[e][4 * i + 2], dk[e][4 * i + 3]} * a.scale;
       const floatx4 y = floatx4{dv[e][4 * i], dv[e][4 * i + 1], dv[e][4 * i + 2], dv[e][4 * i + 3]};
       const int chan = 32 * e + 8 * i + 4 * (lane >> 5);
-      if (a.splits > 1) {
+      if (ranges > 1) {
         *reinterpret_cast<floatx4*>(a.part + part * D + chan) = x;
         *reinterpret_cast<floatx4*>(a.part2 + part * D + chan) = y;
       } else {
@@ -256,7 +304,7 @@ __global__ __launch_bounds__(kThreads, 1) void cross_dkv_kernel(CrossArgs a) {
     }
 }
 
-// Adds the parts of the splits, in their order: D / 4 lanes a row (token x head).
+// Adds the parts of a row's (token x head) ranges, in their order: D / 4 lanes a row.
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossSum a) {
   constexpr int LANES = D / 4, ROWS = kThreads / LANES;
@@ -272,8 +320,10 @@ __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossSum a) {
     const int i = tok / a.L, t = tok - i * a.L;
     out = (size_t)i * a.s.seq + (size_t)t * a.s.tok + (size_t)h * a.s.head;
   }
+  const int count = a.counts != nullptr ? clamp_to(a.counts[tok], 1, a.splits) : a.splits;
+  if (count == 1) return;  // there already
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < a.splits; ++p) x += *reinterpret_cast<const floatx4*>(a.part + (p * (size_t)a.rows + R) * D + chan);
+  for (int p = 0; p < count; ++p) x += *reinterpret_cast<const floatx4*>(a.part + (p * (size_t)a.rows + R) * D + chan);
   store4<F32>(a.out, out + chan, x);
 }
 
@@ -286,7 +336,7 @@ hipError_t dq(const CrossArgs& a, hipStream_t stream) {
 template <bool F32, int D>
 hipError_t dkv(const CrossArgs& a, hipStream_t stream) {
   const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
-  cross_dkv_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
+  cross_dkv_kernel<F32, D><<<dim3(grid, a.splits), 64 * DkvShape<F32>::kWaves, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <bool F32, int D>

@@ -24,17 +24,18 @@ constexpr float kGrow = 8.f;  // in powers of two
 
 // The softmax's part of a tile of 32 NB states, and its product with V.
 template <bool F32, int D, int NB>
-__device__ __forceinline__ void attend(const char* kt, const char* vt, int at, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
-                                       bool all, float c, floatx16 (&o)[D / 32], float& m, float& l, int lane) {
+__device__ __forceinline__ void attend(const char* kt, const char* vt, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
+                                       bool all, float c, floatx16 (&o)[D / 32], float& m, float& l,
+                                       const typename CrossTile<F32, D>::Lane& at, int lane) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
   floatx16 s[NB];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    s[b] = floatx16{};
+  for (int b = 0; b < NB; ++b) s[b] = floatx16{};
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) s[b] = Fr::mma(Tile::row_frag(kt, at + 32 * b * Tile::kRow, e, lane), q[e], s[b]);
-  }
+  for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, e, at), q[e], s[b]);
   if (!all) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -75,7 +76,7 @@ __device__ __forceinline__ void attend(const char* kt, const char* vt, int at, c
     for (int t = 0; t < 2; ++t) {
       const typename Fr::X p = Fr::of(s[b], t);
 #pragma unroll
-      for (int e = 0; e < D / 32; ++e) o[e] = Fr::mma(Tile::col_frag(vt, at + (32 * b + 16 * t) * Tile::kRow, e, lane), p, o[e]);
+      for (int e = 0; e < D / 32; ++e) o[e] = Fr::mma(Tile::col_frag(vt + (32 * b + 16 * t) * Tile::kRow, e, at), p, o[e]);
     }
 }
 
@@ -91,10 +92,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
   const int hk = uniform(id / (unsigned)a.tiles);
   if (hk >= a.Hk) return;
-  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kCrossRows, id - hk * a.tiles);
-  if (at.x < 0) return;
-  const CrossSeq s = cross_seq(a, at.x);
-  const int r0 = at.y * kCrossRows;
+  CrossSeq s;
+  int tile;
+  if (!seq_of_tile<false>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
 
@@ -116,6 +117,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
   float m = -INFINITY, l = 0.f;
   uint8_t byte = 1;
+  const typename Tile::Lane offs = Tile::lane_of(lane);
 
   auto copy = [&](int t, char* kt, char* vt) {
     const int first = t * kCrossTile, last = s.seen - 1 - first;
@@ -123,30 +125,21 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
     copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
     if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
   };
-  auto step = [&](int t, uint8_t b, char* kt, char* vt) {
-    const uint64_t bits = seen_bits<64>(s.seen - t * kCrossTile, mask != nullptr, b, lane);
-    if (bits == 0) return;
-    if (mask != nullptr && ~bits != 0) {
-      // What stands in a masked place may be anything: 0 times it has to be 0.
-      Tile::template clear_rows<kCrossTile, kThreads>(kt, 0, bits, tid);
-      Tile::template clear_rows<kCrossTile, kThreads>(vt, 0, bits, tid);
-      lds_barrier();
-    }
-    attend<F32, D, 2>(kt, vt, 0, q, bits, ~bits == 0, a.c, o, m, l, lane);
+  // Tile t, whose copies are there when it begins; the next one's begin behind the barrier.
+  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
+    copies_landed();
+    const uint64_t bits[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
+    // What stands in a masked place may be anything: 0 times it has to be 0.
+    if (mask != nullptr && ~bits[0] != 0) clear_copied<F32, D, kCrossTile, 4>(vt, bits, wave, lane);
+    lds_barrier();
+    if (t + 1 < to) copy(t + 1, next_k, next_v);
+    if (bits[0] != 0) attend<F32, D, 2>(kt, vt, q, bits[0], ~bits[0] == 0, a.c, o, m, l, offs, lane);
   };
   if (from < to) {
     copy(from, k0, v0);
-    for (int t = from;;) {
-      cross_barrier();
-      uint8_t b = byte;
-      if (t + 1 < to) copy(t + 1, k1, v1);
-      step(t, b, k0, v0);
-      if (++t >= to) break;
-      cross_barrier();
-      b = byte;
-      if (t + 1 < to) copy(t + 1, k0, v0);
-      step(t, b, k1, v1);
-      if (++t >= to) break;
+    for (int t = from; t < to; t += 2) {
+      step(t, k0, v0, k1, v1);
+      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
     }
   }
   l += other_half(l);
@@ -189,10 +182,10 @@ __global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int mine = wave * kBytes;  // the wave's states of each tile
   const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
-  const int2 at = seq_of_tile(a.cu_q, a.n, a.T, a.Lq, a.group, kFewRows, blockIdx.x / (unsigned)a.Hk);
-  if (at.x < 0) return;
-  const CrossSeq s = cross_seq(a, at.x);
-  const int r0 = at.y * kFewRows;
+  CrossSeq s;
+  int tile;
+  if (!seq_of_tile<false>(a, kFewRows, blockIdx.x / (unsigned)a.Hk, s, tile)) return;
+  const int r0 = tile * kFewRows;
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + (lane & 31));
 
@@ -212,42 +205,40 @@ __global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
   float m = -INFINITY, l = 0.f;
-  uint8_t byte = 1;
+  constexpr int kWords = kStates / 64;
+  uint8_t byte[kWords] = {};
+  const typename Tile::Lane offs = Tile::lane_of(lane, mine);
 
   auto copy = [&](int t, char* kt, char* vt) {
     const int first = t * kStates, last = s.seen - 1 - first;
     copy_states<F32, D, kStates, W>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
     copy_states<F32, D, kStates, W>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
-    const int place = wave * 32 + lane;
-    if (mask != nullptr) byte = mask[first + (place < last ? place : last)];
-  };
-  auto step = [&](int t, uint8_t b, char* kt, char* vt) {
-    const int left = s.seen - t * kStates - wave * 32;
-    if (left <= 0) return;
-    const uint64_t bits = seen_bits<32>(left, mask != nullptr, b, lane);
-    if (bits == 0) return;
-    const bool all = bits == 0xffffffffull;
-    if (mask != nullptr && !all) {
-      Tile::template clear_rows<32, 64>(kt, mine, bits, lane);
-      Tile::template clear_rows<32, 64>(vt, mine, bits, lane);
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // the wave's own
-      __builtin_amdgcn_wave_barrier();
+    if (mask != nullptr) {
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) byte[w] = mask[first + (64 * w + lane < last ? 64 * w + lane : last)];
     }
-    attend<F32, D, 1>(kt, vt, mine, q, bits, all, a.c, o, m, l, lane);
+  };
+  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
+    copies_landed();
+    const int left = s.seen - t * kStates;
+    uint64_t bits[kWords], all = ~0ull;
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+      bits[w] = seen_bits(left - 64 * w, mask != nullptr, byte[w], lane);
+      all &= bits[w];
+    }
+    // What stands in a masked place may be anything: 0 times it has to be 0.
+    if (mask != nullptr && ~all != 0) clear_copied<F32, D, kStates, W>(vt, bits, wave, lane);
+    lds_barrier();
+    if (t + 1 < to) copy(t + 1, next_k, next_v);
+    const uint32_t own = (uint32_t)(bits[wave >> 1] >> 32 * (wave & 1));
+    if (own != 0) attend<F32, D, 1>(kt, vt, q, own, ~own == 0, a.c, o, m, l, offs, lane);
   };
   if (from < to) {
     copy(from, k0, v0);
-    for (int t = from;;) {
-      cross_barrier();
-      uint8_t b = byte;
-      if (t + 1 < to) copy(t + 1, k1, v1);
-      step(t, b, k0, v0);
-      if (++t >= to) break;
-      cross_barrier();
-      b = byte;
-      if (t + 1 < to) copy(t + 1, k0, v0);
-      step(t, b, k1, v1);
-      if (++t >= to) break;
+    for (int t = from; t < to; t += 2) {
+      step(t, k0, v0, k1, v1);
+      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
     }
   }
   l += other_half(l);
