@@ -24,12 +24,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   constexpr int kTileBytes = kCrossTile * Tile::kRow;
   __shared__ __align__(16) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
-  const int hk = uniform(id / (unsigned)a.tiles);
-  if (hk >= a.Hk) return;
   CrossSeq s;
-  int tile;
-  if (!seq_of_tile<false>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  int hk, place, tile;
+  if (!place_of(a, hk, place)) return;
+  if (!seq_of_tile<false>(a, kCrossRows, place, s, tile)) return;
   const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
@@ -143,12 +141,10 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
   __shared__ __align__(16) float lse0[kRows], dot0[kRows], lse1[kRows], dot1[kRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int part_of = wave & 3, half = wave >> 2;  // which 32 states, which rows
-  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
-  const int hk = uniform(id / (unsigned)a.tiles);
-  if (hk >= a.Hk) return;
   CrossSeq s;
-  int tile;
-  if (!seq_of_tile<true>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  int hk, place, tile;
+  if (!place_of(a, hk, place)) return;
+  if (!seq_of_tile<true>(a, kCrossRows, place, s, tile)) return;
   const int j0 = tile * kCrossRows;
   if (j0 >= s.lk) return;
 

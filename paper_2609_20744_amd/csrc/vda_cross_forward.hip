@@ -89,12 +89,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   constexpr int kTileBytes = kCrossTile * Tile::kRow;
   __shared__ __align__(16) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const unsigned id = xcd_grouped_id(blockIdx.x, gridDim.x);
-  const int hk = uniform(id / (unsigned)a.tiles);
-  if (hk >= a.Hk) return;
   CrossSeq s;
-  int tile;
-  if (!seq_of_tile<false>(a, kCrossRows, id - hk * a.tiles, s, tile)) return;
+  int hk, place, tile;
+  if (!place_of(a, hk, place)) return;
+  if (!seq_of_tile<false>(a, kCrossRows, place, s, tile)) return;
   const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
@@ -168,7 +166,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
 // Few rows: 32 of them, shared by the waves, each of which takes 32 states of every tile.
 template <bool F32, int D>
 struct FewShape {
-  static constexpr int kWaves = F32 && D == 128 ? 2 : 4;
+  static constexpr int kWaves = 2;
   static constexpr int kStates = 32 * kWaves;  // of a tile
 };
 
@@ -286,37 +284,50 @@ __global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_
   }
 }
 
-// Adds the parts of a row's splits, in their order: D / 4 lanes a row.
+// Adds the parts of a row's splits: a wave per row, whose lanes have a split's maximum
+// and sum each, and then four channels of every 256 / D-th split; the order is fixed.
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
-  constexpr int LANES = D / 4, ROWS = kThreads / LANES;
-  const size_t rows = (size_t)a.T * a.Hq, R = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  constexpr int LANES = D / 4, SIDE = 64 / LANES;  // splits side by side
+  const int lane = threadIdx.x & 63;
+  const size_t rows = (size_t)a.T * a.Hq, R = (size_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
   if (R >= rows) return;
-  const int tok = (int)(R / (unsigned)a.Hq), h = (int)(R - (size_t)tok * a.Hq), chan = threadIdx.x % LANES * 4;
+  const int tok = uniform((int)(R / (unsigned)a.Hq)), h = uniform((int)(R - (size_t)tok * a.Hq));
   size_t out, lse;
   if (a.cu_q != nullptr) {
     if (tok < clamp_to(a.cu_q[0], 0, a.T) || tok >= clamp_to(a.cu_q[a.n], 0, a.T)) return;
     out = (size_t)tok * a.so.tok + (size_t)h * a.so.head;
     lse = (size_t)h * a.T + tok;
   } else {
-    const int i = tok / a.Lq, t = tok - i * a.Lq;
+    const int i = uniform(tok / a.Lq), t = tok - i * a.Lq;
     if (a.slots != nullptr && (a.slots[i] < 0 || a.slots[i] >= a.n_slots)) return;
     out = (size_t)i * a.so.seq + (size_t)t * a.so.tok + (size_t)h * a.so.head;
     lse = ((size_t)i * a.Hq + h) * a.Lq + t;
   }
   const float2* ml = reinterpret_cast<const float2*>(a.part2);
-  float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < a.splits; ++p) top = fmaxf(top, ml[p * rows + R].x);
+  const float2 mine = lane < a.splits ? ml[lane * rows + R] : make_float2(-INFINITY, 0.f);
+  float top = mine.x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float f = mine.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine.x - top);
+  float sum = mine.x == -INFINITY ? mine.y : f * mine.y;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  const int chan = lane % LANES * 4, side = lane / LANES;
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < a.splits; ++p) {
-    const float2 y = ml[p * rows + R];
+#pragma unroll 4
+  for (int b = 0; b < a.splits; b += SIDE) {
+    const int p = b + side < a.splits ? b + side : a.splits - 1;
     const floatx4 z = *reinterpret_cast<const floatx4*>(a.part + (p * rows + R) * D + chan);
-    const float f = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - top);
-    sum += y.x == -INFINITY ? y.y : f * y.y;
-    x += f * z;
+    const float w = __shfl(f, p);
+    x += (b + side < a.splits ? w : 0.f) * z;
   }
-  store4<F32>(a.out, out + chan, x * (sum == 0.f ? 0.f : 1.f / sum));
-  if (a.lse != nullptr && chan == 0) a.lse[lse] = lse_of(top, sum);
+#pragma unroll
+  for (int d = LANES; d < 64; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], d);
+  if (side == 0) store4<F32>(a.out, out + chan, x * (sum == 0.f ? 0.f : 1.f / sum));
+  if (a.lse != nullptr && lane == 0) a.lse[lse] = lse_of(top, sum);
 }
 
 template <bool F32, int D>
@@ -333,8 +344,7 @@ hipError_t forward(bool few, const CrossArgs& a, hipStream_t stream) {
 
 template <bool F32, int D>
 hipError_t join(const CrossArgs& a, hipStream_t stream) {
-  constexpr int ROWS = kThreads / (D / 4);
-  cross_join_kernel<F32, D><<<(unsigned)(((size_t)a.T * a.Hq + ROWS - 1) / ROWS), kThreads, 0, stream>>>(a);
+  cross_join_kernel<F32, D><<<(unsigned)(((size_t)a.T * a.Hq + 3) / 4), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
