@@ -315,12 +315,18 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   const int chan = lane % LANES * 4, side = lane / LANES;
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int b = 0; b < a.splits; b += SIDE) {
-    const int p = b + side < a.splits ? b + side : a.splits - 1;
-    const floatx4 z = *reinterpret_cast<const floatx4*>(a.part + (p * rows + R) * D + chan);
-    const float w = __shfl(f, p);
-    x += (b + side < a.splits ? w : 0.f) * z;
+  for (int b = side; b - side < a.splits; b += 4 * SIDE) {
+    floatx4 z[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int p = b + u * SIDE < a.splits ? b + u * SIDE : a.splits - 1;
+      z[u] = *reinterpret_cast<const floatx4*>(a.part + (p * rows + R) * D + chan);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float w = __shfl(f, b + u * SIDE & 63);
+      x += (b + u * SIDE < a.splits ? w : 0.f) * z[u];
+    }
   }
 #pragma unroll
   for (int d = LANES; d < 64; d <<= 1)

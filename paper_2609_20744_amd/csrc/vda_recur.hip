@@ -1,18 +1,25 @@
 // The channel-wise gated recurrence, its gradients and its recurrent form (vda.h,
 // vda_recur_*): h_t = a_t h_{t-1} + u_t for each channel of each sequence.
 //
-// Sequences are taken in tiles of 128 tokens by 128 channels.  A workgroup has 16
-// runs of eight consecutive tokens, a lane eight channels of one run: it makes the
-// run's decay A = prod a and what the run adds from zero, H, and the 16 runs are
-// joined through LDS.  A tile acts on the state that enters it as h -> A h + H, so
-// sequences longer than a tile take three kernels: what every tile does (reduce),
-// the states that enter them (carry), the outputs (apply).  The gradient runs the
-// other way: with E_t = a_t D_t, D_t = dout_t + E_{t+1}, a tile takes the E that
-// enters at its end to A E + G, with the same A and G = sum_t (a_1 .. a_t) dout_t, so one
-// reduction makes all three; h is made again from x and the gates, nothing is kept.
+// A stretch of tokens acts on the state that enters it as h -> A h + H, A = prod a.  A
+// workgroup has 128 channels, eight to a lane, and 16 runs of consecutive tokens side by
+// side: each run makes its A and H from zero in registers, and the 16 are joined
+// through LDS.
+//
+// Forward: sequences are cut into segments, as many as fill the device.  One kernel
+// makes the segments' A and H, the other composes those before its own segment,
+// and goes through it in tiles, the next tile's loads on the way.  A
+// sequence of one segment takes the second kernel alone.
+//
+// The gradient runs the other way: with E_t = a_t D_t, D_t = dout_t + E_{t+1}, a tile takes the
+// E that enters at its end to A E + G, with the same A and G = sum_t (a_1 .. a_t) dout_t, so
+// one reduction makes all three; h is made again from x and the gates, nothing is kept.
+// Three kernels: what every tile does, what enters it from both sides, the gradients.
 // A place behind a sequence's end has a = 1, u = 0 and dout = 0.
 //
 // Bytes bound it: each pass streams its inputs once.
+#include <type_traits>
+
 #include "vda_recur.h"
 #include "../../include/vda.h"
 
@@ -45,46 +52,39 @@ __device__ __forceinline__ void store8(void* p, size_t at, const float (&x)[8]) 
   }
 }
 
-// A token's gate.  a near 1 is 1 less an exact rest, so that it has its own
-// rounding only: a long memory's length is 1 / (1 - a).  b = 1 - a.
+// A token's decay a, and b = 1 - a with its own rounding only (log: not made).
 template <int GATE>
 __device__ __forceinline__ void gate_of(float g, float& a, float& b) {
   if constexpr (GATE == VDA_GATE_LOG) {
-    const float e = __builtin_amdgcn_exp2f(g * 1.4426950408889634f);
-    const float near = fmaf(g * g, fmaf(g, fmaf(g, fmaf(g, 1.f / 120.f, 1.f / 24.f), 1.f / 6.f), 0.5f), g);
-    a = fabsf(g) < 0.0625f ? 1.f + near : e;
-    b = 0.f;  // not used
+    a = __builtin_amdgcn_exp2f(g * 1.4426950408889634f), b = 0.f;
   } else {
-    const float z = __builtin_amdgcn_fmed3f(g, -80.f, 80.f);
-    const float e = __builtin_amdgcn_exp2f(z * -1.4426950408889634f);
-    const float r = __builtin_amdgcn_rcpf(1.f + e);
-    b = e * r;
-    a = e < 1.f ? 1.f - b : r;
-    // fmed3 gives -80 for a NaN.
-    if (g != g) a = b = g;
+    // Below -80 a is 0 beside any state; e stays finite there.
+    const float e = __builtin_amdgcn_exp2f(fmaxf(g, -80.f) * -1.4426950408889634f);
+    a = __builtin_amdgcn_rcpf(1.f + e), b = e * a;
   }
 }
+// What x is multiplied by.
 template <int GATE>
 __device__ __forceinline__ float weight_of(float a, float b) {
   return GATE == VDA_GATE_LOG ? 1.f : GATE == VDA_GATE_LOGIT ? b : __builtin_amdgcn_sqrtf(b * (1.f + a));
 }
 
-// A sequence and a tile of it.
+// A sequence and a part of it, of `per` tokens (a tile, a segment).
 struct RecurTile {
-  int seq, first, len, tile, last;  // first token and tokens of the sequence; the tile's index and that of its last
+  int seq, first, len, tile, last;  // first token and tokens of the sequence; the part's index and that of its last
 };
-__device__ __forceinline__ bool tile_of(const RecurArgs& a, int t, RecurTile& r) {
+__device__ __forceinline__ bool tile_of(const RecurArgs& a, int t, int per, RecurTile& r) {
   if (a.cu == nullptr) {
-    const int each = (a.L + kRecurTile - 1) / kRecurTile;
+    const int each = (a.L + per - 1) / per;
     r.seq = uniform(t / each), r.tile = t - r.seq * each;
     r.first = r.seq * a.L, r.len = a.L;
   } else {
-    // Sequence i has the places from first_i / tile + i on.
+    // Sequence i has the places from first_i / per + i on.
     const int lane = threadIdx.x & 63;
     int before = 0;
     for (int b = 0; b < a.n; b += 64) {
       const int i = b + lane, c = a.cu[i < a.n ? i : 0];
-      before += __popcll(__ballot(i < a.n && (c < 0 ? 0 : c > a.T ? a.T : c) / kRecurTile + i <= t));
+      before += __popcll(__ballot(i < a.n && (c < 0 ? 0 : c > a.T ? a.T : c) / per + i <= t));
     }
     r.seq = uniform(before) - 1;
     if (r.seq < 0) return false;
@@ -92,123 +92,290 @@ __device__ __forceinline__ bool tile_of(const RecurArgs& a, int t, RecurTile& r)
     r.first = c < 0 ? 0 : c > a.T ? a.T : c;
     const int end = d < 0 ? 0 : d > a.T ? a.T : d;
     r.len = end > r.first ? end - r.first : 0;
-    r.tile = t - (r.first / kRecurTile + r.seq);
+    r.tile = t - (r.first / per + r.seq);
     if (r.tile < 0) return false;
   }
-  r.last = r.len > 0 ? (r.len - 1) / kRecurTile : 0;
+  r.last = r.len > 0 ? (r.len - 1) / per : 0;
   return r.tile <= r.last;
 }
 
-// A lane's run: its channels and where its tokens are.
-struct Run {
-  bool real;     // the lane has channels
-  int chan, run, left;  // tokens of the run that there are
-  size_t tok;    // the first one's row
+// A workgroup's part and channels: all channels of a part after each other, so that
+// workgroups that run together read and write whole rows.
+__device__ __forceinline__ void place_of(const RecurArgs& a, int& place, int& slab) {
+  const unsigned slabs = (unsigned)(a.C + kRecurChans - 1) / kRecurChans;
+  place = uniform(blockIdx.x / slabs), slab = uniform(blockIdx.x - place * slabs);
+}
+
+// A lane's channels and run.
+struct Lane {
+  bool real;  // there are such channels
+  int chan, run;
 };
-__device__ __forceinline__ Run run_of(const RecurArgs& a, const RecurTile& r) {
-  Run w;
-  w.chan = (blockIdx.y * 16 + (threadIdx.x & 15)) * 8;
+__device__ __forceinline__ Lane lane_of(const RecurArgs& a, int slab) {
+  Lane w;
+  w.chan = (slab * 16 + (threadIdx.x & 15)) * 8;
   w.real = w.chan < a.C;
   if (!w.real) w.chan = 0;
   w.run = threadIdx.x >> 4;
-  const int p = r.tile * kRecurTile + w.run * kRecurRun;
-  w.left = r.len - p;
-  w.tok = a.reverse ? (size_t)r.first + (r.len - 1 - p) : (size_t)r.first + p;  // read only where left > 0
   return w;
 }
-// Row of the run's i-th token (of its last one behind its end).
-__device__ __forceinline__ size_t row_of(const RecurArgs& a, const Run& w, int i) {
-  const int at = i < w.left ? i : w.left - 1;
-  return a.reverse ? w.tok - at : w.tok + at;
+
+// The row of place p of a sequence, in the order of the recurrence; the last one's behind its end.
+__device__ __forceinline__ size_t row_at(const RecurArgs& a, const RecurTile& r, int p) {
+  p = p < r.len ? p : r.len - 1;
+  return (size_t)(a.reverse ? r.first + r.len - 1 - p : r.first + p);
 }
 
-__device__ __forceinline__ void clear(float (&x)[kRecurRun][8]) {
+// Eight channels of N tokens as they are in memory.
+template <bool F32, int N>
+struct Raw {
+  static constexpr int kWords = F32 ? 8 : 4;
+  uint32_t w[N][kWords];
+  __device__ __forceinline__ void load(const void* p, size_t at, int i) {
+    const uint4* from = reinterpret_cast<const uint4*>((const char*)p + at * (F32 ? 4 : 2));
 #pragma unroll
-  for (int i = 0; i < kRecurRun; ++i)
+    for (int j = 0; j < kWords / 4; ++j) {
+      const uint4 v = from[j];
+      w[i][4 * j] = v.x, w[i][4 * j + 1] = v.y, w[i][4 * j + 2] = v.z, w[i][4 * j + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ float value(int i, int e) const {
+    if constexpr (F32)
+      return __uint_as_float(w[i][e]);
+    else
+      return e & 1 ? bf16_hi(w[i][e / 2]) : bf16_lo(w[i][e / 2]);
+  }
+};
+
+// A run of N tokens from place p of the sequence (none read where it is empty).
+template <bool F32, int GATE, int N>
+struct Tokens {
+  static constexpr bool kGate32 = F32 || GATE == VDA_GATE_LOG;
+  Raw<F32, N> x;
+  Raw<kGate32, N> g;
+  __device__ __forceinline__ void load(const RecurArgs& a, const RecurTile& r, const Lane& w, int p) {
+    if (r.len == 0) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
+    for (int i = 0; i < N; ++i) {
+      const size_t row = row_at(a, r, p + i);
+      x.load(a.x, row * a.xs + w.chan, i);
+      g.load(a.g, row * a.gs + w.chan, i);
+    }
+  }
+  // a and u of token i, channel e; `is`: whether there is such a token.
+  __device__ __forceinline__ void step(int i, int e, bool is, float& al, float& u) const {
+    float b;
+    gate_of<GATE>(g.value(i, e), al, b);
+    u = weight_of<GATE>(al, b) * x.value(i, e);
+    if (!is) al = 1.f, u = 0.f;
+  }
+};
+
+// What the runs of a tile do, through LDS: [run][A or H][channel].
+typedef float RunTable[kRecurRuns][2][kRecurChans];
+__device__ __forceinline__ void put_run(RunTable& t, int run, const float (&A)[8], const float (&H)[8]) {
+  const int c = (threadIdx.x & 15) * 8;
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) {
+    *reinterpret_cast<floatx4*>(&t[run][0][c + e]) = floatx4{A[e], A[e + 1], A[e + 2], A[e + 3]};
+    *reinterpret_cast<floatx4*>(&t[run][1][c + e]) = floatx4{H[e], H[e + 1], H[e + 2], H[e + 3]};
+  }
+}
+// What enters each run, given what enters the first: the state (h -> A h + H), a thread a
+// channel, which keeps it from tile to tile.
+typedef float RunStates[kRecurRuns][kRecurChans];
+__device__ __forceinline__ float scan_runs(const RunTable& t, RunStates& to, float h, int c) {
+  float A[kRecurRuns], H[kRecurRuns];
+#pragma unroll
+  for (int i = 0; i < kRecurRuns; ++i) A[i] = t[i][0][c], H[i] = t[i][1][c];
+#pragma unroll
+  for (int i = 0; i < kRecurRuns; ++i) {
+    to[i][c] = h;
+    h = fmaf(A[i], h, H[i]);
+  }
+  return h;
+}
+__device__ __forceinline__ void get_states(const RunStates& t, int run, float (&h)[8]) {
+  const int c = (threadIdx.x & 15) * 8;
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) {
+    const floatx4 x = *reinterpret_cast<const floatx4*>(&t[run][c + e]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) h[e + u] = x[u];
+  }
 }
 
-template <bool F32>
-__device__ __forceinline__ void load_dout(const RecurArgs& a, const Run& w, float (&y)[kRecurRun][8]) {
-  if (w.left <= 0) return clear(y);
+// What a segment does: a run has an equal share of its tokens, kBatch at a time.
+template <bool F32, int GATE>
+__global__ __launch_bounds__(kThreads) void recur_segment_kernel(RecurArgs a) {
+  constexpr int N = F32 || GATE == VDA_GATE_LOG ? 4 : 8;
+  __shared__ __align__(16) RunTable table;
+  RecurTile r;
+  int place, slab;
+  place_of(a, place, slab);
+  if (!tile_of(a, place, a.seg, r)) return;
+  if (r.tile == r.last) return;  // nothing comes behind it
+  const Lane w = lane_of(a, slab);
+  const int share = a.seg / kRecurRuns, p0 = r.tile * a.seg + w.run * share;
+  float A[8], H[8];
 #pragma unroll
-  for (int i = 0; i < kRecurRun; ++i) load8<F32>(a.dout, row_of(a, w, i) * a.C + w.chan, y[i]);
+  for (int e = 0; e < 8; ++e) A[e] = 1.f, H[e] = 0.f;
+  Tokens<F32, GATE, N> now, next;
+  now.load(a, r, w, p0);
+  for (int i0 = 0; i0 < share; i0 += N) {
+    if (i0 + N < share) next.load(a, r, w, p0 + i0 + N);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float al, u;
+        now.step(i, e, true, al, u);  // only the last segment has an end
+        H[e] = fmaf(al, H[e], u);
+        A[e] *= al;
+      }
+    now = next;
+  }
+  put_run(table, w.run, A, H);
+  __syncthreads();
+  const int at = threadIdx.x, chan = slab * kRecurChans + at;
+  if (at >= kRecurChans || chan >= a.C) return;
+  float X = 1.f, Y = 0.f;
+#pragma unroll
+  for (int i = 0; i < kRecurRuns; ++i) {
+    Y = fmaf(table[i][0][at], Y, table[i][1][at]);
+    X *= table[i][0][at];
+  }
+  const size_t to = (size_t)place * a.C + chan;
+  a.A[to] = X, a.H[to] = Y;
 }
 
 template <bool F32, int GATE>
-__device__ __forceinline__ void load_run(const RecurArgs& a, const Run& w, float (&x)[kRecurRun][8], float (&g)[kRecurRun][8]) {
-  if (w.left <= 0) {
-    clear(x), clear(g);
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < kRecurRun; ++i) {
-    const size_t row = row_of(a, w, i);
-    load8<F32>(a.x, row * a.xs + w.chan, x[i]);
-    load8<F32 || GATE == VDA_GATE_LOG>(a.g, row * a.gs + w.chan, g[i]);
-  }
-}
-
-// The gates of a run in place: x becomes u, g becomes a.
-template <int GATE>
-__device__ __forceinline__ void make_run(const Run& w, float (&x)[kRecurRun][8], float (&g)[kRecurRun][8]) {
-#pragma unroll
-  for (int i = 0; i < kRecurRun; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float al, b;
-      gate_of<GATE>(g[i][e], al, b);
-      const bool is = i < w.left;
-      x[i][e] = is ? weight_of<GATE>(al, b) * x[i][e] : 0.f;
-      g[i][e] = is ? al : 1.f;
-    }
-}
-
-template <bool F32, int GATE, bool BACKWARD>
-__global__ __launch_bounds__(kThreads) void recur_reduce_kernel(RecurArgs a) {
-  __shared__ __align__(16) float sA[kRecurRuns][kRecurChans], sH[kRecurRuns][kRecurChans];
-  __shared__ __align__(16) float sG[BACKWARD ? kRecurRuns : 1][kRecurChans];
+__global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
+  constexpr int N = 4, kTile = kRecurRuns * N;
+  __shared__ __align__(16) RunTable table;
+  __shared__ __align__(16) RunStates states;
   RecurTile r;
-  if (!tile_of(a, blockIdx.x, r)) return;
+  int place, slab;
+  place_of(a, place, slab);
+  if (!tile_of(a, place, a.seg, r)) return;
+  const Lane w = lane_of(a, slab);
+  const int begin = r.tile * a.seg, end = r.tile == r.last ? r.len : begin + a.seg;
+  Tokens<F32, GATE, N> now, next;
+  now.load(a, r, w, begin + w.run * N);
+  // The thread's channel, whose state it carries.
+  const int c = threadIdx.x, chan = slab * kRecurChans + c;
+  const bool carries = c < kRecurChans, real = carries && chan < a.C;
+  float h = 0.f;
+  if (real && a.S_in != nullptr) h = a.S_in[(size_t)r.seq * a.C + chan];
+  if (r.tile > 0) {
+    // The segments before this one, an equal share of them by each run.
+    const int share = (r.tile + kRecurRuns - 1) / kRecurRuns;
+    const int from = w.run * share, to = from + share < r.tile ? from + share : r.tile;
+    const size_t base = ((size_t)place - r.tile) * a.C + w.chan;
+    float A[8], H[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) A[e] = 1.f, H[e] = 0.f;
+#pragma unroll 4
+    for (int j = from; j < to; ++j) {
+      float x[8], y[8];
+      load8<true>(a.A, base + (size_t)j * a.C, x);
+      load8<true>(a.H, base + (size_t)j * a.C, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) H[e] = fmaf(x[e], H[e], y[e]), A[e] *= x[e];
+    }
+    put_run(table, w.run, A, H);
+    __syncthreads();
+    if (carries) h = scan_runs(table, states, h, c);
+    __syncthreads();
+  }
+  auto tile = [&](int p0, auto full) {
+    const int p = p0 + w.run * N;
+    float al[N][8], u[N][8], A[8], H[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) A[e] = 1.f, H[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        now.step(i, e, full || p + i < end, al[i][e], u[i][e]);
+        H[e] = fmaf(al[i][e], H[e], u[i][e]);
+        A[e] *= al[i][e];
+      }
+    put_run(table, w.run, A, H);
+    __syncthreads();
+    if (carries) h = scan_runs(table, states, h, c);
+    __syncthreads();
+    get_states(states, w.run, H);
+    if (w.real) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) H[e] = fmaf(al[i][e], H[e], u[i][e]);
+        if (full || p + i < end) store8<F32>(a.out, row_at(a, r, p + i) * a.C + w.chan, H);
+      }
+    }
+  };
+  int p0 = begin;
+  for (; p0 + kTile < end; p0 += kTile) {
+    next.load(a, r, w, p0 + kTile + w.run * N);
+    tile(p0, std::true_type());
+    now = next;
+  }
+  tile(p0, std::false_type());
+  if (a.S_out != nullptr && r.tile == r.last && real) a.S_out[(size_t)r.seq * a.C + chan] = h;
+}
+
+// What every tile of 64 tokens does, in both directions.
+template <bool F32, int GATE>
+__global__ __launch_bounds__(kThreads) void recur_reduce_kernel(RecurArgs a) {
+  __shared__ __align__(16) RunTable table;
+  __shared__ __align__(16) float sG[kRecurRuns][kRecurChans];
+  RecurTile r;
+  int place, slab;
+  place_of(a, place, slab);
+  if (!tile_of(a, place, kRecurTile, r)) return;
   if (r.len <= kRecurTile) return;  // nothing enters its one tile from another
-  const Run w = run_of(a, r);
-  float x[kRecurRun][8], g[kRecurRun][8], y[kRecurRun][8];
-  load_run<F32, GATE>(a, w, x, g);
-  if constexpr (BACKWARD) load_dout<F32>(a, w, y);
-  make_run<GATE>(w, x, g);
-  const int c = (threadIdx.x & 15) * 8;
+  const Lane w = lane_of(a, slab);
+  const int p = r.tile * kRecurTile + w.run * kRecurRun;
+  Tokens<F32, GATE, kRecurRun> t;
+  Raw<F32, kRecurRun> y;
+  t.load(a, r, w, p);
+#pragma unroll
+  for (int i = 0; i < kRecurRun; ++i) y.load(a.dout, row_at(a, r, p + i) * a.C + w.chan, i);
+  float A[8], H[8], G[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float A = 1.f, H = 0.f, G = 0.f;
+    A[e] = 1.f, H[e] = 0.f, G[e] = 0.f;
 #pragma unroll
     for (int i = 0; i < kRecurRun; ++i) {
-      H = fmaf(g[i][e], H, x[i][e]);
-      A *= g[i][e];
-      if constexpr (BACKWARD) G = i < w.left ? fmaf(A, y[i][e], G) : G;
+      float al, u;
+      t.step(i, e, p + i < r.len, al, u);
+      H[e] = fmaf(al, H[e], u);
+      A[e] *= al;
+      G[e] = p + i < r.len ? fmaf(A[e], y.value(i, e), G[e]) : G[e];
     }
-    sA[w.run][c + e] = A, sH[w.run][c + e] = H;
-    if constexpr (BACKWARD) sG[w.run][c + e] = G;
   }
+  put_run(table, w.run, A, H);
+  const int c = (threadIdx.x & 15) * 8;
+#pragma unroll
+  for (int e = 0; e < 8; e += 4) *reinterpret_cast<floatx4*>(&sG[w.run][c + e]) = floatx4{G[e], G[e + 1], G[e + 2], G[e + 3]};
   __syncthreads();
-  const int at = threadIdx.x, chan = blockIdx.y * kRecurChans + at;
+  const int at = threadIdx.x, chan = slab * kRecurChans + at;
   if (at >= kRecurChans || chan >= a.C) return;
-  float A = 1.f, H = 0.f, G = 0.f;
+  float X = 1.f, Y = 0.f, Z = 0.f;
 #pragma unroll
   for (int i = 0; i < kRecurRuns; ++i) {
-    if constexpr (BACKWARD) G = fmaf(A, sG[i][at], G);
-    H = fmaf(sA[i][at], H, sH[i][at]);
-    A *= sA[i][at];
+    Z = fmaf(X, sG[i][at], Z);
+    Y = fmaf(table[i][0][at], Y, table[i][1][at]);
+    X *= table[i][0][at];
   }
-  const size_t to = (size_t)blockIdx.x * a.C + chan;
-  a.A[to] = A, a.H[to] = H;
-  if constexpr (BACKWARD) a.G[to] = G;
+  const size_t to = (size_t)place * a.C + chan;
+  a.A[to] = X, a.H[to] = Y, a.G[to] = Z;
 }
 
 // What enters each tile of a sequence: a lane has a channel, a wave a range of the
 // tiles.  H becomes the state that enters a tile, G the E that enters at its end.
 constexpr int kCarryWaves = 16;
-template <bool BACKWARD>
 __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs a) {
   __shared__ float sA[kCarryWaves][64], sH[kCarryWaves][64], sG[kCarryWaves][64];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -236,7 +403,7 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
   for (int t = from; t < to; ++t) {
     const size_t at = base + (size_t)t * a.C;
     const float ta = a.A[at], th = a.H[at];
-    if constexpr (BACKWARD) G = fmaf(A, a.G[at], G);
+    G = fmaf(A, a.G[at], G);
     H = fmaf(ta, H, th);
     A *= ta;
   }
@@ -245,11 +412,8 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
   const size_t st = (size_t)seq * a.C + chan;
   float h = real && a.S_in != nullptr ? a.S_in[st] : 0.f;
   for (int w = 0; w < wave; ++w) h = fmaf(sA[w][lane], h, sH[w][lane]);
-  float e = 0.f;
-  if constexpr (BACKWARD) {
-    e = real && a.dS_out != nullptr ? a.dS_out[st] : 0.f;
-    for (int w = kCarryWaves - 1; w > wave; --w) e = fmaf(sA[w][lane], e, sG[w][lane]);
-  }
+  float e = real && a.dS_out != nullptr ? a.dS_out[st] : 0.f;
+  for (int w = kCarryWaves - 1; w > wave; --w) e = fmaf(sA[w][lane], e, sG[w][lane]);
   if (!real) return;
 #pragma unroll 8
   for (int t = from; t < to; ++t) {
@@ -258,133 +422,107 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
     a.H[at] = h;
     h = next;
   }
-  if constexpr (BACKWARD) {
 #pragma unroll 8
-    for (int t = to - 1; t >= from; --t) {
-      const size_t at = base + (size_t)t * a.C;
-      const float next = fmaf(a.A[at], e, a.G[at]);
-      a.G[at] = e;
-      e = next;
-    }
+  for (int t = to - 1; t >= from; --t) {
+    const size_t at = base + (size_t)t * a.C;
+    const float next = fmaf(a.A[at], e, a.G[at]);
+    a.G[at] = e;
+    e = next;
   }
-}
-
-// Eight values of a [.., C] fp32 array, or zeros.
-__device__ __forceinline__ void entering(const float* p, size_t at, bool is, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = 0.f;
-  if (is && p != nullptr) load8<true>(p, at, x);
-}
-
-template <bool F32, int GATE>
-__global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
-  __shared__ __align__(16) float sA[kRecurRuns][kRecurChans], sH[kRecurRuns][kRecurChans];
-  RecurTile r;
-  if (!tile_of(a, blockIdx.x, r)) return;
-  const Run w = run_of(a, r);
-  const bool carried = a.carried && r.len > kRecurTile;
-  float x[kRecurRun][8], g[kRecurRun][8], h[8];
-  load_run<F32, GATE>(a, w, x, g);
-  entering(carried ? a.H : a.S_in, (carried ? (size_t)blockIdx.x : (size_t)r.seq) * a.C + w.chan, w.real, h);
-  make_run<GATE>(w, x, g);
-  const int c = (threadIdx.x & 15) * 8;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float A = 1.f, H = 0.f;
-#pragma unroll
-    for (int i = 0; i < kRecurRun; ++i) H = fmaf(g[i][e], H, x[i][e]), A *= g[i][e];
-    sA[w.run][c + e] = A, sH[w.run][c + e] = H;
-  }
-  __syncthreads();
-  for (int i = 0; i < w.run; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = fmaf(sA[i][c + e], h[e], sH[i][c + e]);
-  if (!w.real) return;
-#pragma unroll
-  for (int i = 0; i < kRecurRun; ++i) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = fmaf(g[i][e], h[e], x[i][e]);
-    if (i < w.left) store8<F32>(a.out, row_of(a, w, i) * a.C + w.chan, h);
-  }
-  if (a.S_out != nullptr && r.tile == r.last && w.run == kRecurRuns - 1) store8<true>(a.S_out, (size_t)r.seq * a.C + w.chan, h);
 }
 
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
-  __shared__ __align__(16) float sA[kRecurRuns][kRecurChans], sH[kRecurRuns][kRecurChans], sG[kRecurRuns][kRecurChans];
+  constexpr int N = kRecurRun;
+  constexpr bool kGate32 = F32 || GATE == VDA_GATE_LOG;
+  __shared__ __align__(16) RunTable table;
+  __shared__ __align__(16) RunStates sG, states, grads;
   RecurTile r;
-  if (!tile_of(a, blockIdx.x, r)) return;
-  const Run w = run_of(a, r);
+  int place, slab;
+  place_of(a, place, slab);
+  if (!tile_of(a, place, kRecurTile, r)) return;
+  const Lane w = lane_of(a, slab);
+  const int p = r.tile * kRecurTile + w.run * N;
+  Tokens<F32, GATE, N> t;
+  Raw<F32, N> y;
+  t.load(a, r, w, p);
+  if (r.len > 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) y.load(a.dout, row_at(a, r, p + i) * a.C + w.chan, i);
+  // A thread has the state of a channel, or the gradient that comes to it from behind.
+  const int c = threadIdx.x % kRecurChans, chan = slab * kRecurChans + c;
+  const bool back = threadIdx.x >= kRecurChans, real = chan < a.C;
   const bool carried = a.carried && r.len > kRecurTile;
-  const size_t at = (carried ? (size_t)blockIdx.x : (size_t)r.seq) * a.C + w.chan;
-  float x[kRecurRun][8], g[kRecurRun][8], y[kRecurRun][8], h[8], D[8];
-  load_run<F32, GATE>(a, w, x, g);
-  load_dout<F32>(a, w, y);
-  entering(carried ? a.H : a.S_in, at, w.real, h);
-  entering(carried ? a.G : a.dS_out, at, w.real, D);
-  const int c = (threadIdx.x & 15) * 8;
-  // x stays the input; a and the weight are made again where they are used.
+  const float* from = carried ? (back ? a.G : a.H) : back ? a.dS_out : a.S_in;
+  float z = 0.f;
+  if (real && from != nullptr) z = from[(carried ? (size_t)place : (size_t)r.seq) * a.C + chan];
+
+  float al[N][8], b[N][8], A[8], H[8], G[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float A = 1.f, H = 0.f, G = 0.f;
+    A[e] = 1.f, H[e] = 0.f, G[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kRecurRun; ++i) {
-      if (i >= w.left) {
-        x[i][e] = 0.f, g[i][e] = GATE == VDA_GATE_LOG ? 0.f : INFINITY, y[i][e] = 0.f;
-      }
-      float al, b;
-      gate_of<GATE>(g[i][e], al, b);
-      if (i >= w.left) al = 1.f;
-      H = fmaf(al, H, weight_of<GATE>(al, b) * x[i][e]);
-      A *= al;
-      G = fmaf(A, y[i][e], G);
+    for (int i = 0; i < N; ++i) {
+      gate_of<GATE>(t.g.value(i, e), al[i][e], b[i][e]);
+      float u = weight_of<GATE>(al[i][e], b[i][e]) * t.x.value(i, e), d = y.value(i, e);
+      if (p + i >= r.len) al[i][e] = 1.f, u = d = 0.f;
+      H[e] = fmaf(al[i][e], H[e], u);
+      A[e] *= al[i][e];
+      G[e] = fmaf(A[e], d, G[e]);
     }
-    sA[w.run][c + e] = A, sH[w.run][c + e] = H, sG[w.run][c + e] = G;
+  }
+  put_run(table, w.run, A, H);
+#pragma unroll
+  for (int e = 0; e < 8; e += 4)
+    *reinterpret_cast<floatx4*>(&sG[w.run][(threadIdx.x & 15) * 8 + e]) = floatx4{G[e], G[e + 1], G[e + 2], G[e + 3]};
+  __syncthreads();
+  if (!back) {
+    scan_runs(table, states, z, c);
+  } else {
+#pragma unroll
+    for (int i = kRecurRuns - 1; i >= 0; --i) {
+      grads[i][c] = z;
+      z = fmaf(table[i][0][c], z, sG[i][c]);
+    }
+    if (a.dS_in != nullptr && r.tile == 0 && real) a.dS_in[(size_t)r.seq * a.C + chan] = z;
   }
   __syncthreads();
-  for (int i = 0; i < w.run; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = fmaf(sA[i][c + e], h[e], sH[i][c + e]);
-  for (int i = kRecurRuns - 1; i > w.run; --i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) D[e] = fmaf(sA[i][c + e], D[e], sG[i][c + e]);
   if (!w.real) return;
-  // Forward over the states, then back: y becomes dx, and x the gate's gradient.
+  get_states(states, w.run, H);
+  get_states(grads, w.run, G);
+  // Over the states, then back.
+  float dx[N][8], dg[N][8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float before[kRecurRun], s = h[e], E = D[e];
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int i = 0; i < kRecurRun; ++i) {
-      float al, b;
-      gate_of<GATE>(g[i][e], al, b);
-      before[i] = s;
-      s = fmaf(al, s, weight_of<GATE>(al, b) * x[i][e]);
+    for (int e = 0; e < 8; ++e) {
+      dg[i][e] = H[e];  // the state before the token
+      dx[i][e] = weight_of<GATE>(al[i][e], b[i][e]);
+      H[e] = fmaf(al[i][e], H[e], dx[i][e] * t.x.value(i, e));
     }
 #pragma unroll
-    for (int i = kRecurRun - 1; i >= 0; --i) {
-      float al, b;
-      gate_of<GATE>(g[i][e], al, b);
-      if (i >= w.left) al = 1.f;
-      const float wt = weight_of<GATE>(al, b), d = y[i][e] + E;
+  for (int i = N - 1; i >= 0; --i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool is = p + i < r.len;
+      const float x = t.x.value(i, e), d = (is ? y.value(i, e) : 0.f) + G[e], ai = al[i][e];
       if constexpr (GATE == VDA_GATE_LOG)
-        x[i][e] = d * al * before[i];
+        dg[i][e] *= d * ai;
       else if constexpr (GATE == VDA_GATE_LOGIT)
-        x[i][e] = d * al * b * (before[i] - x[i][e]);
+        dg[i][e] = d * ai * b[i][e] * (dg[i][e] - x);
       else
-        x[i][e] = d * (al * b * before[i] - al * al * __builtin_amdgcn_sqrtf(b * __builtin_amdgcn_rcpf(1.f + al)) * x[i][e]);
-      y[i][e] = d * wt;
-      E = al * d;
+        dg[i][e] = d * (ai * b[i][e] * dg[i][e] -
+                        ai * ai * __builtin_amdgcn_sqrtf(b[i][e] * __builtin_amdgcn_rcpf(1.f + ai)) * x);
+      dx[i][e] *= d;
+      G[e] = ai * d;
     }
-    D[e] = E;
-  }
 #pragma unroll
-  for (int i = 0; i < kRecurRun; ++i)
-    if (i < w.left) {
-      const size_t row = row_of(a, w, i);
-      store8<F32>(a.dx, row * a.dxs + w.chan, y[i]);
-      store8<F32 || GATE == VDA_GATE_LOG>(a.dg, row * a.dgs + w.chan, x[i]);
+  for (int i = 0; i < N; ++i)
+    if (p + i < r.len) {
+      const size_t row = row_at(a, r, p + i);
+      store8<F32>(a.dx, row * a.dxs + w.chan, dx[i]);
+      store8<kGate32>(a.dg, row * a.dgs + w.chan, dg[i]);
     }
-  if (a.dS_in != nullptr && r.tile == 0 && w.run == 0) store8<true>(a.dS_in, (size_t)r.seq * a.C + w.chan, D);
 }
 
 __device__ __forceinline__ floatx4 load4(const float* p) { return *reinterpret_cast<const floatx4*>(p); }
@@ -430,18 +568,21 @@ __global__ __launch_bounds__(kThreads) void recur_step_kernel(RecurStepArgs a) {
   *reinterpret_cast<floatx4*>(S) = h;
 }
 
-dim3 grid_of(const RecurArgs& a) { return dim3(a.tiles, (a.C + kRecurChans - 1) / kRecurChans); }
+unsigned grid_of(const RecurArgs& a) { return (unsigned)a.tiles * (unsigned)((a.C + kRecurChans - 1) / kRecurChans); }
 
 template <bool F32, int GATE>
-hipError_t reduce(bool backward, const RecurArgs& a, hipStream_t stream) {
-  backward ? recur_reduce_kernel<F32, GATE, true><<<grid_of(a), kThreads, 0, stream>>>(a)
-           : recur_reduce_kernel<F32, GATE, false><<<grid_of(a), kThreads, 0, stream>>>(a);
+hipError_t forward(const RecurArgs& a, hipStream_t stream) {
+  if (a.carried) recur_segment_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a);
+  recur_apply_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <bool F32, int GATE>
-hipError_t apply(bool backward, const RecurArgs& a, hipStream_t stream) {
-  backward ? recur_grad_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a)
-           : recur_apply_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a);
+hipError_t backward(const RecurArgs& a, hipStream_t stream) {
+  if (a.carried) {
+    recur_reduce_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a);
+    recur_carry_kernel<<<dim3(a.n, (a.C + 63) / 64), 64 * kCarryWaves, 0, stream>>>(a);
+  }
+  recur_grad_kernel<F32, GATE><<<grid_of(a), kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 template <bool F32, int GATE>
@@ -453,29 +594,18 @@ hipError_t step(const RecurStepArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_recur_reduce(bool f32, bool backward, const RecurArgs& a, hipStream_t stream) {
+hipError_t launch_recur(bool f32, bool back, const RecurArgs& a, hipStream_t stream) {
   switch (a.gate) {
-    case VDA_GATE_LOG: return f32 ? reduce<true, VDA_GATE_LOG>(backward, a, stream) : reduce<false, VDA_GATE_LOG>(backward, a, stream);
+    case VDA_GATE_LOG:
+      return f32 ? (back ? backward<true, VDA_GATE_LOG>(a, stream) : forward<true, VDA_GATE_LOG>(a, stream))
+                 : (back ? backward<false, VDA_GATE_LOG>(a, stream) : forward<false, VDA_GATE_LOG>(a, stream));
     case VDA_GATE_LOGIT:
-      return f32 ? reduce<true, VDA_GATE_LOGIT>(backward, a, stream) : reduce<false, VDA_GATE_LOGIT>(backward, a, stream);
-    default: return f32 ? reduce<true, VDA_GATE_NORM>(backward, a, stream) : reduce<false, VDA_GATE_NORM>(backward, a, stream);
+      return f32 ? (back ? backward<true, VDA_GATE_LOGIT>(a, stream) : forward<true, VDA_GATE_LOGIT>(a, stream))
+                 : (back ? backward<false, VDA_GATE_LOGIT>(a, stream) : forward<false, VDA_GATE_LOGIT>(a, stream));
+    default:
+      return f32 ? (back ? backward<true, VDA_GATE_NORM>(a, stream) : forward<true, VDA_GATE_NORM>(a, stream))
+                 : (back ? backward<false, VDA_GATE_NORM>(a, stream) : forward<false, VDA_GATE_NORM>(a, stream));
   }
-}
-
-hipError_t launch_recur_apply(bool f32, bool backward, const RecurArgs& a, hipStream_t stream) {
-  switch (a.gate) {
-    case VDA_GATE_LOG: return f32 ? apply<true, VDA_GATE_LOG>(backward, a, stream) : apply<false, VDA_GATE_LOG>(backward, a, stream);
-    case VDA_GATE_LOGIT:
-      return f32 ? apply<true, VDA_GATE_LOGIT>(backward, a, stream) : apply<false, VDA_GATE_LOGIT>(backward, a, stream);
-    default: return f32 ? apply<true, VDA_GATE_NORM>(backward, a, stream) : apply<false, VDA_GATE_NORM>(backward, a, stream);
-  }
-}
-
-hipError_t launch_recur_carry(bool backward, const RecurArgs& a, hipStream_t stream) {
-  const dim3 grid(a.n, (a.C + 63) / 64);
-  backward ? recur_carry_kernel<true><<<grid, 64 * kCarryWaves, 0, stream>>>(a)
-           : recur_carry_kernel<false><<<grid, 64 * kCarryWaves, 0, stream>>>(a);
-  return hipGetLastError();
 }
 
 hipError_t launch_recur_step(bool f32, const RecurStepArgs& a, hipStream_t stream) {

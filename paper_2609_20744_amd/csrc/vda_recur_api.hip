@@ -27,9 +27,18 @@ int check_channels(int C, int gate) {
   return C > 128 * 65535 ? VDA_ERR_SIZE : VDA_OK;
 }
 
-long long tiles_of(const vda_recur_problem* p) {
+// Tokens of a part of a sequence: a tile backward; forward a segment, so long that about
+// three workgroups of 128 channels are there for each compute unit.
+int part_of(const vda_recur_problem* p, bool backward) {
+  if (backward) return vda::kRecurTile;
+  const long long slabs = (p->C + vda::kRecurChans - 1) / vda::kRecurChans;
+  const long long share = (long long)p->T * slabs / (3LL * vda::current_device_cus());
+  return (int)std::min(2048LL, std::max(1LL, (share + vda::kRecurUnit - 1) / vda::kRecurUnit) * vda::kRecurUnit);
+}
+
+long long parts_of(const vda_recur_problem* p, int part) {
   const long long n = p->n_seqs, T = p->T;
-  return p->cu_seqlens ? T / vda::kRecurTile + n : n * ((T / n + vda::kRecurTile - 1) / vda::kRecurTile);
+  return p->cu_seqlens ? T / part + n : n * ((T / n + part - 1) / part);
 }
 
 int check_stride(int stride, int C, size_t es) {
@@ -51,28 +60,29 @@ int check_problem(const vda_recur_problem* p, bool backward) {
     return st;
   if (!aligned(p->cu_seqlens, 4)) return VDA_ERR_ALIGN;
   // A workgroup of 256 threads per tile, one of 1024 per sequence; tokens are counted in 32 bits.
-  if (tiles_of(p) * 256 > kMaxThreads || (long long)p->n_seqs * 1024 > kMaxThreads ||
+  const long long slabs = (p->C + vda::kRecurChans - 1) / vda::kRecurChans;
+  if (parts_of(p, vda::kRecurTile) * slabs > kMaxThreads / 256 || (long long)p->n_seqs * 1024 > kMaxThreads ||
       (long long)p->T + vda::kRecurTile > 0x7fffffffLL)
     return VDA_ERR_SIZE;
   return VDA_OK;
 }
 
-bool carried(const vda_recur_problem* p) {
-  return (p->cu_seqlens ? p->T : p->T / p->n_seqs) > vda::kRecurTile;
-}
+bool carried(const vda_recur_problem* p, int part) { return (p->cu_seqlens ? p->T : p->T / p->n_seqs) > part; }
 
 size_t workspace(const vda_recur_problem* p, bool backward) {
-  if (!carried(p)) return 0;
-  return (backward ? 3 : 2) * round_up((size_t)tiles_of(p) * p->C * 4, 256);
+  const int part = part_of(p, backward);
+  if (!carried(p, part)) return 0;
+  return (backward ? 3 : 2) * round_up((size_t)parts_of(p, part) * p->C * 4, 256);
 }
 
-RecurArgs args_of(const vda_recur_problem* p, void* work) {
+RecurArgs args_of(const vda_recur_problem* p, bool backward, void* work) {
   RecurArgs a = {};
   a.cu = p->cu_seqlens, a.n = p->n_seqs, a.T = p->T, a.L = p->T / p->n_seqs, a.C = p->C;
   a.xs = p->x_row_stride ? p->x_row_stride : p->C, a.gs = p->g_row_stride ? p->g_row_stride : p->C;
   a.dxs = p->dx_row_stride ? p->dx_row_stride : p->C, a.dgs = p->dg_row_stride ? p->dg_row_stride : p->C;
   a.gate = p->gate, a.reverse = p->reverse != 0;
-  a.tiles = (int)tiles_of(p), a.carried = carried(p);
+  a.seg = part_of(p, backward);
+  a.tiles = (int)parts_of(p, a.seg), a.carried = carried(p, a.seg);
   const size_t each = round_up((size_t)a.tiles * p->C * 4, 256) / 4;
   a.A = static_cast<float*>(work), a.H = a.A + each, a.G = a.H + each;
   return a;
@@ -121,16 +131,9 @@ int vda_recur_forward(const vda_recur_problem* p, const void* x, const void* g, 
                   {rows_range(x, p, p->x_row_stride, es), rows_range(g, p, p->g_row_stride, ge), opt_range(S_in, state),
                    opt_range(p->cu_seqlens, (size_t)(p->n_seqs + 1) * 4)}))
     return VDA_ERR_OVERLAP;
-  RecurArgs a = args_of(p, work);
+  RecurArgs a = args_of(p, false, work);
   a.x = x, a.g = g, a.S_in = S_in, a.out = out, a.S_out = S_out;
-  const bool f32 = p->is_f32 != 0;
-  hipError_t e = hipSuccess;
-  if (a.carried) {
-    e = vda::launch_recur_reduce(f32, false, a, stream);
-    if (e == hipSuccess) e = vda::launch_recur_carry(false, a, stream);
-  }
-  if (e == hipSuccess) e = vda::launch_recur_apply(f32, false, a, stream);
-  return hip_status(e);
+  return hip_status(vda::launch_recur(p->is_f32 != 0, false, a, stream));
 }
 
 int vda_recur_backward(const vda_recur_problem* p, const void* dout, const void* x, const void* g, const float* S_in,
@@ -155,16 +158,9 @@ int vda_recur_backward(const vda_recur_problem* p, const void* dout, const void*
                                             opt_range(dS_out, state), opt_range(p->cu_seqlens, (size_t)(p->n_seqs + 1) * 4)};
   const Range rs = opt_range(dS_in, state), rw = opt_range(work, need);
   if (meet ? any_overlap({both, rs, rw}, ins) : any_overlap({rdx, rdg, rs, rw}, ins)) return VDA_ERR_OVERLAP;
-  RecurArgs a = args_of(p, work);
+  RecurArgs a = args_of(p, true, work);
   a.x = x, a.g = g, a.dout = dout, a.S_in = S_in, a.dS_out = dS_out, a.dx = dx, a.dg = dg, a.dS_in = dS_in;
-  const bool f32 = p->is_f32 != 0;
-  hipError_t e = hipSuccess;
-  if (a.carried) {
-    e = vda::launch_recur_reduce(f32, true, a, stream);
-    if (e == hipSuccess) e = vda::launch_recur_carry(true, a, stream);
-  }
-  if (e == hipSuccess) e = vda::launch_recur_apply(f32, true, a, stream);
-  return hip_status(e);
+  return hip_status(vda::launch_recur(p->is_f32 != 0, true, a, stream));
 }
 
 int vda_recur_step(const void* x, const void* g, int n, int tokens, int C, int gate, int is_f32, const int* slots, int n_slots,
