@@ -22,6 +22,9 @@ typedef float floatx8 __attribute__((ext_vector_type(8)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 typedef short shortx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) char lds_char;  // tiles: never through a generic pointer
+template <typename T>
+using Lds = __attribute__((address_space(3))) T;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 typedef __attribute__((address_space(1))) const void global_void;
 
@@ -46,7 +49,8 @@ struct CrossArgs {
   int n, n_slots, T, S, Lq, Lk;
   int Hq, Hk, group;
   uint32_t group_magic;  // x / group = x * group_magic >> 24 for x < group + 64
-  float scale, c;        // c = |scale| log2 e
+  float scale, c;        // c = |scale| log2 e, above 0
+  int near;              // a tile's rows are within 2^31 bytes of its first, whichever their heads
   int flip;              // scale < 0: the sign of one factor of each score is changed
   int tiles, splits;     // tiles of rows (of states in the gradient of k and v) of a head
   int range;             // gradient of k and v: rows that a workgroup takes, about; at most `splits` ranges
@@ -245,21 +249,21 @@ struct CrossTile {
   // Channels 16 s + 8 lh .. + 7 of row li of the rows behind `tile` (a multiple of 16 rows in).
   // An address is one addition to a named array: of a longer chain the compiler
   // does not see which array it is in, and waits for copies into the others.
-  static __device__ __forceinline__ X row_frag(const char* tile, int s, const Lane& l) {
+  static __device__ __forceinline__ X row_frag(const lds_char* tile, int s, const Lane& l) {
     if constexpr (F32) {
-      const floatx4 a = *reinterpret_cast<const floatx4*>(tile + (l.row ^ 64 * s));
-      const floatx4 b = *reinterpret_cast<const floatx4*>(tile + (l.row ^ (64 * s + 16)));
+      const floatx4 a = *(const Lds<floatx4>*)(tile + (l.row ^ 64 * s));
+      const floatx4 b = *(const Lds<floatx4>*)(tile + (l.row ^ (64 * s + 16)));
       return X{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     } else {
-      return *reinterpret_cast<const bf16x8*>(tile + (l.row ^ 32 * s));
+      return *(const Lds<bf16x8>*)(tile + (l.row ^ 32 * s));
     }
   }
   // Channel 32 b + li of the rows 4 lh + e and 8 + 4 lh + e, e < 4, behind `tile`.
-  static __device__ __forceinline__ X col_frag(const char* tile, int b, const Lane& l) {
+  static __device__ __forceinline__ X col_frag(const lds_char* tile, int b, const Lane& l) {
     if constexpr (F32) {
       X x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = *reinterpret_cast<const float*>(tile + (l.col[e] ^ 128 * b));
+      for (int e = 0; e < 8; ++e) x[e] = *(const Lds<float>*)(tile + (l.col[e] ^ 128 * b));
       return x;
     } else {
       const shortx4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(tile + (l.col[0] ^ 64 * b)));
@@ -270,27 +274,31 @@ struct CrossTile {
 };
 
 // Copies ROWS rows of consecutive tokens into a tile; rows behind `last` repeat
-// it.  base: the tile's first row.
+// it.  base: the tile's first row.  One way for whole tiles and others: of copies that only
+// one way to a read has, the compiler does not see where they go, and waits for all.
 template <bool F32, int D, int ROWS, int WAVES>
-__device__ __forceinline__ void copy_states(const void* base, size_t row_elems, int last, char* tile, int wave, int lane) {
+__device__ __forceinline__ void copy_states(const void* base, size_t row_elems, int last, lds_char* tile, int wave, int lane) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the compiler's host pass refuses the builtin in some kernels
   typedef CrossTile<F32, D> Tile;
-  constexpr int kPieces = ROWS * Tile::kRow / 1024;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024, kStep = 64 * WAVES / Tile::kPieces;
   const __amdgpu_buffer_rsrc_t src = make_rsrc(base, 0xfffffff0u);
-  const uint32_t row_bytes = (uint32_t)row_elems * Tile::kEs;
+  const uint32_t row_bytes = (uint32_t)row_elems * Tile::kEs;  // below 2^24
+  const int r0 = (wave * 64 + lane) / Tile::kPieces, piece0 = lane % Tile::kPieces ^ Tile::swizzle(r0);
 #pragma unroll
   for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
-    const int p = wave + i * WAVES, at = p * 64 + lane;
+    const int p = wave + i * WAVES, r = r0 + i * kStep;
     if (kPieces % WAVES != 0 && p >= kPieces) break;
-    const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
-                                             (uint32_t)(r < last ? r : last) * row_bytes + piece * 16u, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        src, (lds_void*)(tile + p * 1024), 16,
+        __umul24(min(r, last), row_bytes) + (piece0 ^ Tile::swizzle(i * kStep)) * 16u, 0, 0, 0);
   }
+#endif
 }
 
 // Writes zeros over the rows whose bit is not set, each wave over what it copied
 // itself, once that is there.  bits: 64 rows each.
 template <bool F32, int D, int ROWS, int WAVES>
-__device__ __forceinline__ void clear_copied(char* tile, const uint64_t (&bits)[(ROWS + 63) / 64], int wave, int lane) {
+__device__ __forceinline__ void clear_copied(lds_char* tile, const uint64_t (&bits)[(ROWS + 63) / 64], int wave, int lane) {
   typedef CrossTile<F32, D> Tile;
   constexpr int kPieces = ROWS * Tile::kRow / 1024;
 #pragma unroll
@@ -299,29 +307,52 @@ __device__ __forceinline__ void clear_copied(char* tile, const uint64_t (&bits)[
     if (kPieces % WAVES != 0 && p >= kPieces) break;
     const int r = at / Tile::kPieces;
     const uint64_t w = ROWS > 64 && r >= 64 ? bits[ROWS > 64 ? 1 : 0] : bits[0];
-    if (!(w >> (r & 63) & 1)) *reinterpret_cast<uint4*>(tile + at * 16) = make_uint4(0u, 0u, 0u, 0u);
+    if (!(w >> (r & 63) & 1)) *(Lds<u32x4>*)(tile + at * 16) = u32x4{0u, 0u, 0u, 0u};
   }
 }
 
 // Copies ROWS rows of queries (token x head) into a tile; rows behind `last` repeat it.
-// base: the sequence's first token of the key head's first query head.
+// base: the sequence's first token of the key head's first query head.  Where the
+// query heads of a key head divide what a wave's copies step by, one offset again.
 template <bool F32, int D, int ROWS, int WAVES>
 __device__ __forceinline__ void copy_rows(const CrossArgs& a, const void* base, const CrossStrides& s, int r0, int last,
-                                          char* tile, int wave, int lane) {
+                                          lds_char* tile, int wave, int lane) {
   typedef CrossTile<F32, D> Tile;
-  constexpr int kPieces = ROWS * Tile::kRow / 1024;
-  const int t0 = r0 / a.group, g0 = r0 - t0 * a.group;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024, kStep = 64 * WAVES / Tile::kPieces;
+  const int t0 = uniform(r0 / a.group), g0 = r0 - t0 * a.group;
   const char* from = (const char*)base + (size_t)t0 * s.tok * Tile::kEs;
+  const int first = (wave * 64 + lane) / Tile::kPieces, piece0 = lane % Tile::kPieces ^ Tile::swizzle(first);
+  if (a.near && g0 == 0 && kStep % a.group == 0 && last >= ROWS - 1) {
+    const __amdgpu_buffer_rsrc_t src = make_rsrc(from, 0xfffffff0u);
+    const uint32_t t = first * a.group_magic >> 24, g = first - t * a.group;
+    const uint32_t at = (t * (uint32_t)s.tok + g * (uint32_t)s.head) * Tile::kEs;
+    const uint32_t step = kStep / a.group * (uint32_t)s.tok * Tile::kEs;
+#pragma unroll
+    for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
+      const int p = wave + i * WAVES;
+      if (kPieces % WAVES != 0 && p >= kPieces) break;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + p * 1024), 16,
+                                               at + (piece0 ^ Tile::swizzle(i * kStep)) * 16u, i * step, 0, 0);
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
-    const int p = wave + i * WAVES, at = p * 64 + lane;
+    const int p = wave + i * WAVES, r = first + i * kStep;
     if (kPieces % WAVES != 0 && p >= kPieces) break;
-    const int r = at / Tile::kPieces, piece = (at % Tile::kPieces) ^ Tile::swizzle(r);
     const uint32_t x = g0 + (r < last ? r : last);
     const uint32_t t = x * a.group_magic >> 24, g = x - t * a.group;
-    __builtin_amdgcn_global_load_lds((global_void*)(from + (t * s.tok + g * s.head) * Tile::kEs + piece * 16),
-                                     (lds_void*)(tile + p * 1024), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(
+        (global_void*)(from + (t * s.tok + g * s.head) * Tile::kEs + (piece0 ^ Tile::swizzle(i * kStep)) * 16),
+        (lds_void*)(tile + p * 1024), 16, 0, 0);
   }
+}
+
+// Whether bit 8 (i / 4) + 4 lh + i % 4 of w (the same in all lanes) is set: that of a result's row i.
+__device__ __forceinline__ bool row_bit(uint32_t w, int i) {
+  const int b = 8 * (i >> 2) + (i & 3);
+  const uint32_t lo = 0u - (w >> b & 1u), hi = 0u - (w >> (b + 4) & 1u);
+  return __builtin_amdgcn_inverse_ballot_w64((uint64_t)hi << 32 | lo);
 }
 
 // The wave's copies into LDS are there.

@@ -92,7 +92,14 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     if (groups >= cus) return 1LL;
     return std::max(1LL, std::min({(2 * cus + groups - 1) / groups, (units + 1) / 2, 64LL}));
   };
-  c.splits = (int)ranges((long long)c.tiles * p->H_k, (states + vda::kCrossTile - 1) / vda::kCrossTile);
+  const long long groups_q = (long long)c.tiles * p->H_k;
+  if (c.few) {
+    // Two waves a CU, of 128 states at least: three a CU unsplit measured 75 us where six and
+    // a join took 78 us and twelve 81 us (96 sequences of 8 key heads, 1500 states, D = 128);
+    // of one sequence ranges of 64, 128 and 256 states are alike within the launches' noise.
+    c.splits = (int)std::max(1LL, std::min({(2 * cus + groups_q - 1) / groups_q, (states + 127) / 128, 64LL}));
+  } else
+    c.splits = (int)ranges(groups_q, (states + vda::kCrossTile - 1) / vda::kCrossTile);
   const size_t q_rows = (size_t)p->T * p->H_q, k_rows = (size_t)p->S * p->H_k;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -140,7 +147,10 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.Hq = p->H_q, a.Hk = p->H_k, a.group = p->H_q / p->H_k;
   a.group_magic = (uint32_t)(((1u << 24) + a.group - 1) / a.group);
   a.scale = p->scale, a.flip = p->scale < 0.f;
-  a.c = (a.flip ? -p->scale : p->scale) * vda::kLog2e;
+  // Above 0, so that a score of -inf has no weight; a scale of 0 is 1e-37, below what fp32 tells from it.
+  a.c = std::max((a.flip ? -p->scale : p->scale) * vda::kLog2e, 1e-37f);
+  auto near = [&](const CrossStrides& s) { return (64 * s.tok + a.group * s.head) * (p->is_f32 ? 4 : 2) < (size_t)1 << 31; };
+  a.near = near(a.sq) && near(a.so);
   a.tiles = c.tiles, a.splits = c.splits;
   char* w = static_cast<char*>(work);
   a.part = reinterpret_cast<float*>(w + c.part);

@@ -60,13 +60,13 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   uint8_t byte = 1;
   const typename Tile::Lane offs = Tile::lane_of(lane);
 
-  auto copy = [&](int t, char* kt, char* vt) {
+  auto copy = [&](int t, lds_char* kt, lds_char* vt) {
     const int first = t * kCrossTile, last = s.seen - 1 - first;
     copy_states<F32, D, kCrossTile, 4>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
     copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
     if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
   };
-  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
+  auto step = [&](int t, lds_char* kt, lds_char* vt, lds_char* next_k, lds_char* next_v) {
     copies_landed();
     const uint64_t seen[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
     const uint64_t bits = seen[0];
@@ -85,13 +85,11 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
         p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, e, here), q[e], p);
         dp = Fr::mma(Tile::row_frag(vt + 32 * b * Tile::kRow, e, here), g[e], dp);
       }
-      const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float x = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - dot);
-        if (!all) x = w >> (8 * (i >> 2) + (i & 3)) & 1 ? x : 0.f;
-        p[i] = x;
-      }
+      for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - dot);
+      if (!all)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = row_bit((uint32_t)(bits >> 32 * b), i) ? p[i] : 0.f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const typename Fr::X x = Fr::of(p, h);
@@ -102,10 +100,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
     }
   };
   if (from < to) {
-    copy(from, k0, v0);
+    copy(from, (lds_char*)k0, (lds_char*)v0);
     for (int t = from; t < to; t += 2) {
-      step(t, k0, v0, k1, v1);
-      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
+      step(t, (lds_char*)k0, (lds_char*)v0, (lds_char*)k1, (lds_char*)v1);
+      if (t + 1 < to) step(t + 1, (lds_char*)k1, (lds_char*)v1, (lds_char*)k0, (lds_char*)v0);
     }
   }
   if (!row.real) return;
@@ -166,7 +164,7 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
   typename Fr::X k[D / 16];
   const size_t kat = seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head;
   const size_t vat = seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head + (size_t)j0 * a.sv.tok;
-  copy_states<F32, D, kCrossRows, Shape::kWaves>((const char*)a.v + vat * Tile::kEs, a.sv.tok, s.lk - 1 - j0, vt, wave, lane);
+  copy_states<F32, D, kCrossRows, Shape::kWaves>((const char*)a.v + vat * Tile::kEs, a.sv.tok, s.lk - 1 - j0, (lds_char*)vt, wave, lane);
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) {
     k[e] = Fr::load(a.k, kat + (size_t)jc * a.sk.tok + 16 * e + 8 * (lane >> 5));
@@ -192,9 +190,10 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
   const float2* stats = a.stats + (a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) * a.Hq + hk * a.group;
   float2 mine = make_float2(0.f, 0.f);
   const typename Tile::Lane offs = Tile::lane_of(lane);
-  const char* vmine = vt + part_of * 32 * Tile::kRow;
+  const bool all = __all(seen);
+  const lds_char* vmine = (const lds_char*)vt + part_of * 32 * Tile::kRow;
 
-  auto copy = [&](int t, char* qt, char* gt) {
+  auto copy = [&](int t, lds_char* qt, lds_char* gt) {
     const int first = t * kRows, last = rows - 1 - first;
     copy_rows<F32, D, kRows, Shape::kWaves>(a, qb, a.sq, first, last, qt, wave, lane);
     copy_rows<F32, D, kRows, Shape::kWaves>(a, gb, a.so, first, last, gt, wave, lane);
@@ -207,7 +206,7 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
     // A row behind the last leaves no p.
     if (wave == 0 && lane < kRows) lse[lane] = t * kRows + lane < rows ? mine.x : INFINITY, dot[lane] = mine.y;
   };
-  auto step = [&](const char* qt, const char* gt, const float* lse, const float* dot) {
+  auto step = [&](const lds_char* qt, const lds_char* gt, const float* lse, const float* dot) {
     const typename Tile::Lane here = Tile::again(offs);
     const int h32 = half * 32 * Tile::kRow;
     floatx16 p = {}, dp = {};
@@ -216,13 +215,16 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
       p = Fr::mma(Tile::row_frag(qt + h32, e, here), k[e], p);
       dp = Fr::mma(Tile::row_frag(gt + h32, e, here), Tile::row_frag(vmine, e, here), dp);
     }
+    if (!all)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = seen ? p[i] : -INFINITY;  // a.c > 0: no weight
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const floatx4 z = *reinterpret_cast<const floatx4*>(lse + 32 * half + 8 * i + 4 * (lane >> 5));
       const floatx4 y = *reinterpret_cast<const floatx4*>(dot + 32 * half + 8 * i + 4 * (lane >> 5));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = seen ? __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e])) : 0.f;
+        const float x = __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e]));
         p[4 * i + e] = x;
         dp[4 * i + e] = x * (dp[4 * i + e] - y[e]);
       }
@@ -238,17 +240,17 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
     }
   };
   if (from < to) {
-    copy(from, q0, g0);
+    copy(from, (lds_char*)q0, (lds_char*)g0);
     for (int t = from;;) {
       keep(t, lse0, dot0);
       cross_barrier();
-      if (t + 1 < to) copy(t + 1, q1, g1);
-      step(q0, g0, lse0, dot0);
+      if (t + 1 < to) copy(t + 1, (lds_char*)q1, (lds_char*)g1);
+      step((lds_char*)q0, (lds_char*)g0, lse0, dot0);
       if (++t >= to) break;
       keep(t, lse1, dot1);
       cross_barrier();
-      if (t + 1 < to) copy(t + 1, q0, g0);
-      step(q1, g1, lse1, dot1);
+      if (t + 1 < to) copy(t + 1, (lds_char*)q0, (lds_char*)g0);
+      step((lds_char*)q1, (lds_char*)g1, lse1, dot1);
       if (++t >= to) break;
     }
   }

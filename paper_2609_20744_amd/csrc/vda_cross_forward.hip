@@ -11,8 +11,8 @@
 // more than 2^8 only: p stays below 2^8 then, where a rounding to bf16 is as good.
 //
 // Many rows: a wave has 32 rows, the four waves of a workgroup share the states'
-// tiles.  Few rows (a step, learned queries): the waves share 32 rows, take 32 states
-// of each tile each, and join at the end.
+// tiles.  Few rows (a step, learned queries): a wave by itself, bound by the copies that it
+// has on the way.
 // Where workgroups would not fill the device, each takes a range of the states
 // and the join kernel adds their parts.
 #include "vda_cross.h"
@@ -24,9 +24,9 @@ constexpr float kGrow = 8.f;  // in powers of two
 
 // The softmax's part of a tile of 32 NB states, and its product with V.
 template <bool F32, int D, int NB>
-__device__ __forceinline__ void attend(const char* kt, const char* vt, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
+__device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
                                        bool all, float c, floatx16 (&o)[D / 32], float& m, float& l,
-                                       const typename CrossTile<F32, D>::Lane& at, int lane) {
+                                       const typename CrossTile<F32, D>::Lane& at) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
   floatx16 s[NB];
@@ -39,9 +39,8 @@ __device__ __forceinline__ void attend(const char* kt, const char* vt, const typ
   if (!all) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = w >> (8 * (i >> 2) + (i & 3)) & 1 ? s[b][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[b][i] = row_bit((uint32_t)(bits >> 32 * b), i) ? s[b][i] : -INFINITY;
     }
   }
   float top = s[0][0];
@@ -50,7 +49,7 @@ __device__ __forceinline__ void attend(const char* kt, const char* vt, const typ
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
   top = fmaxf(top, other_half(top));
-  top = top == -INFINITY ? top : top * c;
+  top *= c;
   if (__any(top > m + kGrow)) {
     const float to = top > m + kGrow ? top : m;
     const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
@@ -64,10 +63,8 @@ __device__ __forceinline__ void attend(const char* kt, const char* vt, const typ
   for (int b = 0; b < NB; ++b) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float p = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
-      if (!all) p = s[b][i] == -INFINITY ? 0.f : p;
-      s[b][i] = p;
-      l += p;
+      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));  // c > 0: 0 where s is -inf
+      l += s[b][i];
     }
   }
 #pragma unroll
@@ -81,6 +78,31 @@ __device__ __forceinline__ void attend(const char* kt, const char* vt, const typ
 }
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+
+// A lane's row: the output, or its split's part of it (not divided by the sum).
+template <bool F32, int D>
+__device__ __forceinline__ void put_rows(const CrossArgs& a, const Row& row, const floatx16 (&o)[D / 32], float m, float l,
+                                         int lane) {
+  if (a.splits > 1) {
+    const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<floatx4*>(a.part + part * D + 32 * e + 8 * i + 4 * (lane >> 5)) =
+            floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+    if (lane < 32) *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(m, l);
+    return;
+  }
+  const float r = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      store4<F32>(a.out, row.out + 32 * e + 8 * i + 4 * (lane >> 5),
+                  floatx4{o[e][4 * i] * r, o[e][4 * i + 1] * r, o[e][4 * i + 2] * r, o[e][4 * i + 3] * r});
+  if (a.lse != nullptr && lane < 32) a.lse[row.lse] = lse_of(m, l);
+}
 
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(CrossArgs a) {
@@ -117,68 +139,44 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   uint8_t byte = 1;
   const typename Tile::Lane offs = Tile::lane_of(lane);
 
-  auto copy = [&](int t, char* kt, char* vt) {
+  auto copy = [&](int t, lds_char* kt, lds_char* vt) {
     const int first = t * kCrossTile, last = s.seen - 1 - first;
     copy_states<F32, D, kCrossTile, 4>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
     copy_states<F32, D, kCrossTile, 4>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
     if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
   };
   // Tile t, whose copies are there when it begins; the next one's begin behind the barrier.
-  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
+  auto step = [&](int t, lds_char* kt, lds_char* vt, lds_char* next_k, lds_char* next_v) {
     copies_landed();
     const uint64_t bits[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
     // What stands in a masked place may be anything: 0 times it has to be 0.
     if (mask != nullptr && ~bits[0] != 0) clear_copied<F32, D, kCrossTile, 4>(vt, bits, wave, lane);
     lds_barrier();
     if (t + 1 < to) copy(t + 1, next_k, next_v);
-    if (bits[0] != 0) attend<F32, D, 2>(kt, vt, q, bits[0], ~bits[0] == 0, a.c, o, m, l, offs, lane);
+    if (bits[0] != 0) attend<F32, D, 2>(kt, vt, q, bits[0], ~bits[0] == 0, a.c, o, m, l, offs);
   };
   if (from < to) {
-    copy(from, k0, v0);
+    copy(from, (lds_char*)k0, (lds_char*)v0);
     for (int t = from; t < to; t += 2) {
-      step(t, k0, v0, k1, v1);
-      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
+      step(t, (lds_char*)k0, (lds_char*)v0, (lds_char*)k1, (lds_char*)v1);
+      if (t + 1 < to) step(t + 1, (lds_char*)k1, (lds_char*)v1, (lds_char*)k0, (lds_char*)v0);
     }
   }
   l += other_half(l);
-  if (!row.real) return;
-  if (a.splits > 1) {
-    const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<floatx4*>(a.part + part * D + 32 * e + 8 * i + 4 * (lane >> 5)) =
-            floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
-    if (lane < 32) *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(m, l);
-    return;
-  }
-  const float r = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      store4<F32>(a.out, row.out + 32 * e + 8 * i + 4 * (lane >> 5),
-                  floatx4{o[e][4 * i] * r, o[e][4 * i + 1] * r, o[e][4 * i + 2] * r, o[e][4 * i + 3] * r});
-  if (a.lse != nullptr && lane < 32) a.lse[row.lse] = lse_of(m, l);
+  if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
 }
 
-// Few rows: 32 of them, shared by the waves, each of which takes 32 states of every tile.
-template <bool F32, int D>
-struct FewShape {
-  static constexpr int kWaves = 2;
-  static constexpr int kStates = 32 * kWaves;  // of a tile
-};
+// Few rows: a workgroup is one wave with 32 rows, which takes tiles of 32 states through
+// two places in LDS, one on the way while the other is used, with no barrier.
+constexpr int kFewStates = 32;
 
-template <bool F32, int D>
-__global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_kernel(CrossArgs a) {
+template <bool F32, int D, bool MASKED>
+__global__ __launch_bounds__(64, 1) void cross_few_kernel(CrossArgs a) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
-  constexpr int W = FewShape<F32, D>::kWaves, kStates = FewShape<F32, D>::kStates, kBytes = 32 * Tile::kRow;
-  __shared__ __align__(16) char k0[W * kBytes], v0[W * kBytes], k1[W * kBytes], v1[W * kBytes];
-  __shared__ float2 ml[W][32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int mine = wave * kBytes;  // the wave's states of each tile
+  constexpr int kBytes = kFewStates * Tile::kRow, kCopies = 2 * kBytes / 1024;
+  __shared__ __align__(16) char k0[kBytes], v0[kBytes], k1[kBytes], v1[kBytes];
+  const int lane = threadIdx.x;
   const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
   CrossSeq s;
   int tile;
@@ -187,11 +185,11 @@ __global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_
   if (r0 >= s.lq * a.group) return;
   const Row row = row_of(a, s, hk, r0 + (lane & 31));
 
-  const int tiles = (s.seen + kStates - 1) / kStates, per = (tiles + a.splits - 1) / a.splits;
+  const int tiles = (s.seen + kFewStates - 1) / kFewStates, per = (tiles + a.splits - 1) / a.splits;
   const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
   const char* kb = (const char*)a.k + (seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head) * Tile::kEs;
   const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
-  const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
+  const uint8_t* mask = !MASKED ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
 
   typename Fr::X q[D / 16];
 #pragma unroll
@@ -203,85 +201,46 @@ __global__ __launch_bounds__((64 * FewShape<F32, D>::kWaves), 1) void cross_few_
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
   float m = -INFINITY, l = 0.f;
-  constexpr int kWords = kStates / 64;
-  uint8_t byte[kWords] = {};
-  const typename Tile::Lane offs = Tile::lane_of(lane, mine);
+  uint8_t b0 = 0, b1 = 0;  // the mask's bytes of the tiles
+  const typename Tile::Lane offs = Tile::lane_of(lane);
 
-  auto copy = [&](int t, char* kt, char* vt) {
-    const int first = t * kStates, last = s.seen - 1 - first;
-    copy_states<F32, D, kStates, W>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, wave, lane);
-    copy_states<F32, D, kStates, W>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, wave, lane);
-    if (mask != nullptr) {
-#pragma unroll
-      for (int w = 0; w < kWords; ++w) byte[w] = mask[first + (64 * w + lane < last ? 64 * w + lane : last)];
-    }
+  auto copy = [&](int t, lds_char* kt, lds_char* vt, uint8_t& byte) {
+    const int first = (t < to ? t : to - 1) * kFewStates, last = s.seen - 1 - first;
+    if (MASKED) byte = mask[first + (lane < last ? lane : last)];
+    copy_states<F32, D, kFewStates, 1>(kb + (size_t)first * a.sk.tok * Tile::kEs, a.sk.tok, last, kt, 0, lane);
+    copy_states<F32, D, kFewStates, 1>(vb + (size_t)first * a.sv.tok * Tile::kEs, a.sv.tok, last, vt, 0, lane);
   };
-  auto step = [&](int t, char* kt, char* vt, char* next_k, char* next_v) {
-    copies_landed();
-    const int left = s.seen - t * kStates;
-    uint64_t bits[kWords], all = ~0ull;
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) {
-      bits[w] = seen_bits(left - 64 * w, mask != nullptr, byte[w], lane);
-      all &= bits[w];
-    }
+  auto step = [&](int t, lds_char* kt, lds_char* vt, uint8_t byte) {
+    __builtin_amdgcn_sched_barrier(0);
+    // All copies but those of the next tile, the newest ones, have landed.
+    __builtin_amdgcn_s_waitcnt((kCopies & 15) | 0x0f70 | (kCopies >> 4 << 14));
+    __builtin_amdgcn_sched_barrier(0);
+    const uint64_t bits[1] = {seen_bits(s.seen - t * kFewStates, MASKED, byte, lane) & 0xffffffffull};
     // What stands in a masked place may be anything: 0 times it has to be 0.
-    if (mask != nullptr && ~all != 0) clear_copied<F32, D, kStates, W>(vt, bits, wave, lane);
-    lds_barrier();
-    if (t + 1 < to) copy(t + 1, next_k, next_v);
-    const uint32_t own = (uint32_t)(bits[wave >> 1] >> 32 * (wave & 1));
-    if (own != 0) attend<F32, D, 1>(kt, vt, q, own, ~own == 0, a.c, o, m, l, offs, lane);
+    const bool all = bits[0] == 0xffffffffull;
+    if (bits[0] != 0) {
+      if (MASKED && !all) clear_copied<F32, D, kFewStates, 1>(vt, bits, 0, lane);
+      attend<F32, D, 1>(kt, vt, q, bits[0], all, a.c, o, m, l, offs);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   };
   if (from < to) {
-    copy(from, k0, v0);
-    for (int t = from; t < to; t += 2) {
-      step(t, k0, v0, k1, v1);
-      if (t + 1 < to) step(t + 1, k1, v1, k0, v0);
+    // Each step has the copies of one more tile on the way, behind the last one that one's
+    // again: where not every way through had them, the compiler could not count them and
+    // would wait for all before each read.
+    copy(from, (lds_char*)k0, (lds_char*)v0, b0);
+    for (int t = from;; t += 2) {
+      copy(t + 1, (lds_char*)k1, (lds_char*)v1, b1);
+      step(t, (lds_char*)k0, (lds_char*)v0, b0);
+      if (t + 1 >= to) break;
+      copy(t + 2, (lds_char*)k0, (lds_char*)v0, b0);
+      step(t + 1, (lds_char*)k1, (lds_char*)v1, b1);
+      if (t + 2 >= to) break;
     }
+    copies_landed();
   }
   l += other_half(l);
-  // The waves' parts: piece p is channels 8 p + 4 lh .. of every row.
-  constexpr int kPieces = D / 8;
-  lds_barrier();
-#pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-    char* to_lds = (p < kPieces / 2 ? k0 + p * 1024 : v0 + (p - kPieces / 2) * 1024) + mine;
-    const int e = p / 4, i = p % 4;
-    *reinterpret_cast<floatx4*>(to_lds + lane * 16) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
-  }
-  if (lane < 32) ml[wave][lane] = make_float2(m, l);
-  lds_barrier();
-  if (!row.real) return;
-  float f[W], top = -INFINITY, sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w][lane & 31].x);
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const float2 x = ml[w][lane & 31];
-    f[w] = x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.x - top);
-    sum += x.x == -INFINITY ? x.y : f[w] * x.y;
-  }
-  const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
-  const float r = a.splits > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-  for (int p = wave; p < kPieces; p += W) {
-    floatx4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const char* from_lds = (p < kPieces / 2 ? k0 + p * 1024 : v0 + (p - kPieces / 2) * 1024) + w * kBytes;
-      x += f[w] * *reinterpret_cast<const floatx4*>(from_lds + lane * 16);
-    }
-    const int chan = 8 * p + 4 * (lane >> 5);
-    if (a.splits > 1)
-      *reinterpret_cast<floatx4*>(a.part + part * D + chan) = x;
-    else
-      store4<F32>(a.out, row.out + chan, x * r);
-  }
-  if (wave == 0 && lane < 32) {
-    if (a.splits > 1)
-      *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(top, sum);
-    else if (a.lse != nullptr)
-      a.lse[row.lse] = lse_of(top, sum);
-  }
+  if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
 }
 
 // Adds the parts of a row's splits: a wave per row, whose lanes have a split's maximum
@@ -339,8 +298,11 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
 template <bool F32, int D>
 hipError_t forward(bool few, const CrossArgs& a, hipStream_t stream) {
   if (few) {
-    cross_few_kernel<F32, D>
-        <<<dim3((unsigned)a.tiles * a.Hk, a.splits), 64 * FewShape<F32, D>::kWaves, 0, stream>>>(a);
+    const dim3 grid((unsigned)a.tiles * a.Hk, a.splits);
+    if (a.k_mask != nullptr)
+      cross_few_kernel<F32, D, true><<<grid, 64, 0, stream>>>(a);
+    else
+      cross_few_kernel<F32, D, false><<<grid, 64, 0, stream>>>(a);
   } else {
     const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
     cross_forward_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
