@@ -348,11 +348,11 @@ __device__ __forceinline__ void copy_rows(const CrossArgs& a, const void* base, 
   }
 }
 
-// Whether bit 8 (i / 4) + 4 lh + i % 4 of w (the same in all lanes) is set: that of a result's row i.
-__device__ __forceinline__ bool row_bit(uint32_t w, int i) {
-  const int b = 8 * (i >> 2) + (i & 3);
-  const uint32_t lo = 0u - (w >> b & 1u), hi = 0u - (w >> (b + 4) & 1u);
-  return __builtin_amdgcn_inverse_ballot_w64((uint64_t)hi << 32 | lo);
+// x where the lane's bit of a result's row i is set, else `otherwise` (a constant), whatever
+// x is; two operations.  w: the bits of the 32 rows, from the lane's first row on.
+__device__ __forceinline__ float row_or(float x, uint32_t w, int i, float otherwise) {
+  const int m = __builtin_amdgcn_sbfe((int)w, 8 * (i >> 2) + (i & 3), 1);
+  return __int_as_float((m & __float_as_int(x)) | (~m & __float_as_int(otherwise)));
 }
 
 // The wave's copies into LDS are there.

@@ -87,9 +87,11 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - dot);
-      if (!all)
+      if (!all) {
+        const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = row_bit((uint32_t)(bits >> 32 * b), i) ? p[i] : 0.f;
+        for (int i = 0; i < 16; ++i) p[i] = row_or(p[i], w, i, 0.f);
+      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const typename Fr::X x = Fr::of(p, h);

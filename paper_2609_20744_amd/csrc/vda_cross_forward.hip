@@ -39,8 +39,9 @@ __device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, c
   if (!all) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
+      const uint32_t w = (uint32_t)(bits >> 32 * b) >> (threadIdx.x & 32) / 8;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[b][i] = row_bit((uint32_t)(bits >> 32 * b), i) ? s[b][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[b][i] = row_or(s[b][i], w, i, -INFINITY);
     }
   }
   float top = s[0][0];
