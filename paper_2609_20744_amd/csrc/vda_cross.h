@@ -409,16 +409,20 @@ __device__ __forceinline__ void store4(void* p, size_t at, floatx4 x) {
 }
 
 // Host-side launchers (arguments validated).
-hipError_t launch_cross_forward(bool f32, int d, bool few, const CrossArgs& a, hipStream_t stream);
+// Waves of a workgroup of few rows that share its range of the states; their tiles have to fit LDS.
+constexpr int few_waves(bool f32, int d) { return f32 && d == 128 ? 2 : 4; }
+
+// few: waves of a workgroup of few rows, 1 or few_waves(); 0: many rows
+hipError_t launch_cross_forward(bool f32, int d, int few, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_join(bool f32, int d, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_dq(bool f32, int d, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_dkv(bool f32, int d, const CrossArgs& a, hipStream_t stream);
 // Sums of part [splits][rows][d] to the rows of a tensor of H heads; counts: of how many each token's are, or null (all).
 struct CrossSum {
-  const float* part;
+  const float* part[2];  // of one gradient, or of two at once
   const int* counts;
-  void* out;
-  CrossStrides s;
+  void* out[2];
+  CrossStrides s[2];
   const int* cu;
   int n, L, H, splits;
   long long rows;  // tokens * H

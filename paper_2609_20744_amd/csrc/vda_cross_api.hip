@@ -70,7 +70,7 @@ CrossStrides strides_of(int layout, bool packed, int total, int n, int H, int d,
 }
 
 struct CrossPlan {
-  bool few;             // the waves of a workgroup share its rows
+  int few;              // waves of a workgroup of few rows, which share them; 0: many rows
   int tiles, splits;    // of the rows; ranges of the states
   int tiles_k, splits_k, range;  // backward: of the states; ranges of the rows at most, and their rows
   size_t part, part2, stats, counts, total;  // workspace offsets
@@ -93,13 +93,20 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     return std::max(1LL, std::min({(2 * cus + groups - 1) / groups, (units + 1) / 2, 64LL}));
   };
   const long long groups_q = (long long)c.tiles * p->H_k;
-  if (c.few) {
+  const int waves = vda::few_waves(p->is_f32 != 0, p->d);
+  if (c.few && groups_q <= cus && states <= 128 * waves) {
+    // A workgroup a CU, 128 states a wave: no join to launch.  One sequence of 16 heads and 512
+    // states, D = 128: 11.6 us where ranges of single waves and a join took 15.5 us (captured,
+    // 9.6 and 9.8 us); of 2048 states 16 to 20 us against 10 us captured.
+    c.few = waves;
+    c.splits = 1;
+  } else if (c.few) {
     // Two waves a CU, of 128 states at least: three a CU unsplit measured 75 us where six and
-    // a join took 78 us and twelve 81 us (96 sequences of 8 key heads, 1500 states, D = 128);
-    // of one sequence ranges of 64, 128 and 256 states are alike within the launches' noise.
+    // a join took 78 us and twelve 81 us (96 sequences of 8 key heads, 1500 states, D = 128).
     c.splits = (int)std::max(1LL, std::min({(2 * cus + groups_q - 1) / groups_q, (states + 127) / 128, 64LL}));
-  } else
+  } else {
     c.splits = (int)ranges(groups_q, (states + vda::kCrossTile - 1) / vda::kCrossTile);
+  }
   const size_t q_rows = (size_t)p->T * p->H_q, k_rows = (size_t)p->S * p->H_k;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -276,16 +283,13 @@ int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void*
   const bool f32 = p->is_f32 != 0;
   hipError_t e = vda::launch_cross_dq(f32, p->d, a, stream);
   if (e == hipSuccess && c.splits > 1)
-    e = vda::launch_cross_sum(f32, p->d, vda::CrossSum{a.part, nullptr, dq, a.sdq, a.cu_q, a.n, a.Lq, a.Hq, a.splits, (long long)a.T * a.Hq},
-                              stream);
+    e = vda::launch_cross_sum(
+        f32, p->d, vda::CrossSum{{a.part}, nullptr, {dq}, {a.sdq}, a.cu_q, a.n, a.Lq, a.Hq, a.splits, (long long)a.T * a.Hq}, stream);
   a.tiles = c.tiles_k, a.splits = c.splits_k;
   if (e == hipSuccess) e = vda::launch_cross_dkv(f32, p->d, a, stream);
-  if (e == hipSuccess && c.splits_k > 1) {
-    vda::CrossSum s = {a.part, a.counts, dk, a.sdk, a.cu_k, a.n, a.Lk, a.Hk, a.splits, (long long)a.S * a.Hk};
-    e = vda::launch_cross_sum(f32, p->d, s, stream);
-    s.part = a.part2, s.out = dv, s.s = a.sdv;
-    if (e == hipSuccess) e = vda::launch_cross_sum(f32, p->d, s, stream);
-  }
+  if (e == hipSuccess && c.splits_k > 1)
+    e = vda::launch_cross_sum(f32, p->d, vda::CrossSum{{a.part, a.part2}, a.counts, {dk, dv}, {a.sdk, a.sdv}, a.cu_k, a.n, a.Lk, a.Hk,
+                                                       a.splits, (long long)a.S * a.Hk}, stream);
   return hip_status(e);
 }
 

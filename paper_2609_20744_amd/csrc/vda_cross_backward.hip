@@ -309,22 +309,24 @@ template <bool F32, int D>
 __global__ __launch_bounds__(kThreads) void cross_sum_kernel(CrossSum a) {
   constexpr int LANES = D / 4, ROWS = kThreads / LANES;
   const size_t R = (size_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+  const bool second = blockIdx.y != 0;
+  const CrossStrides& s = a.s[second];
   if (R >= (size_t)a.rows) return;
   const int tok = (int)(R / (unsigned)a.H), h = (int)(R - (size_t)tok * a.H), chan = threadIdx.x % LANES * 4;
   size_t out;
   if (a.cu != nullptr) {
     const int total = (int)(a.rows / a.H);
     if (tok < clamp_to(a.cu[0], 0, total) || tok >= clamp_to(a.cu[a.n], 0, total)) return;
-    out = (size_t)tok * a.s.tok + (size_t)h * a.s.head;
+    out = (size_t)tok * s.tok + (size_t)h * s.head;
   } else {
     const int i = tok / a.L, t = tok - i * a.L;
-    out = (size_t)i * a.s.seq + (size_t)t * a.s.tok + (size_t)h * a.s.head;
+    out = (size_t)i * s.seq + (size_t)t * s.tok + (size_t)h * s.head;
   }
   const int count = a.counts != nullptr ? clamp_to(a.counts[tok], 1, a.splits) : a.splits;
   if (count == 1) return;  // there already
   floatx4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int p = 0; p < count; ++p) x += *reinterpret_cast<const floatx4*>(a.part + (p * (size_t)a.rows + R) * D + chan);
-  store4<F32>(a.out, out + chan, x);
+  for (int p = 0; p < count; ++p) x += *reinterpret_cast<const floatx4*>(a.part[second] + (p * (size_t)a.rows + R) * D + chan);
+  store4<F32>(a.out[second], out + chan, x);
 }
 
 template <bool F32, int D>
@@ -342,7 +344,8 @@ hipError_t dkv(const CrossArgs& a, hipStream_t stream) {
 template <bool F32, int D>
 hipError_t sum(const CrossSum& a, hipStream_t stream) {
   constexpr int ROWS = kThreads / (D / 4);
-  cross_sum_kernel<F32, D><<<(unsigned)(((size_t)a.rows + ROWS - 1) / ROWS), kThreads, 0, stream>>>(a);
+  const dim3 grid((unsigned)(((size_t)a.rows + ROWS - 1) / ROWS), a.out[1] != nullptr ? 2 : 1);
+  cross_sum_kernel<F32, D><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -80,29 +80,39 @@ __device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, c
 
 __device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
 
-// A lane's row: the output, or its split's part of it (not divided by the sum).
+// Where a lane's row goes: to the output, or (not divided by the sum) to its split's part.
+template <bool F32, int D>
+struct Put {
+  const CrossArgs& a;
+  const Row& row;
+  float m, l, r;
+  size_t part;
+  __device__ __forceinline__ Put(const CrossArgs& a, const Row& row, float m, float l)
+      : a(a), row(row), m(m), l(l), r(l == 0.f ? 0.f : 1.f / l), part((size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part) {}
+  __device__ __forceinline__ void channels(int first, floatx4 x) const {
+    if (a.splits > 1)
+      *reinterpret_cast<floatx4*>(a.part + part * D + first) = x;
+    else
+      store4<F32>(a.out, row.out + first, x * r);
+  }
+  __device__ __forceinline__ void stats() const {
+    if (a.splits > 1)
+      *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(m, l);
+    else if (a.lse != nullptr)
+      a.lse[row.lse] = lse_of(m, l);
+  }
+};
+
 template <bool F32, int D>
 __device__ __forceinline__ void put_rows(const CrossArgs& a, const Row& row, const floatx16 (&o)[D / 32], float m, float l,
                                          int lane) {
-  if (a.splits > 1) {
-    const size_t part = (size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part;
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<floatx4*>(a.part + part * D + 32 * e + 8 * i + 4 * (lane >> 5)) =
-            floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
-    if (lane < 32) *reinterpret_cast<float2*>(a.part2 + part * 2) = make_float2(m, l);
-    return;
-  }
-  const float r = l == 0.f ? 0.f : 1.f / l;
+  const Put<F32, D> put(a, row, m, l);
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      store4<F32>(a.out, row.out + 32 * e + 8 * i + 4 * (lane >> 5),
-                  floatx4{o[e][4 * i] * r, o[e][4 * i + 1] * r, o[e][4 * i + 2] * r, o[e][4 * i + 3] * r});
-  if (a.lse != nullptr && lane < 32) a.lse[row.lse] = lse_of(m, l);
+      put.channels(32 * e + 8 * i + 4 * (lane >> 5), floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]});
+  if (lane < 32) put.stats();
 }
 
 template <bool F32, int D>
@@ -167,17 +177,22 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
 }
 
-// Few rows: a workgroup is one wave with 32 rows, which takes tiles of 32 states through
-// two places in LDS, one on the way while the other is used, with no barrier.
+// Few rows: a wave with 32 rows takes tiles of 32 states through two places in LDS, one on
+// the way while the other is used, with no barrier.  WAVES of them share a workgroup's
+// rows, take a part of its range each and add their parts behind a barrier.
 constexpr int kFewStates = 32;
 
-template <bool F32, int D, bool MASKED>
-__global__ __launch_bounds__(64, 1) void cross_few_kernel(CrossArgs a) {
+template <bool F32, int D, bool MASKED, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 1) void cross_few_kernel(CrossArgs a) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
   constexpr int kBytes = kFewStates * Tile::kRow, kCopies = 2 * kBytes / 1024;
-  __shared__ __align__(16) char k0[kBytes], v0[kBytes], k1[kBytes], v1[kBytes];
-  const int lane = threadIdx.x;
+  __shared__ __align__(16) char ks0[WAVES * kBytes], vs0[WAVES * kBytes], ks1[WAVES * kBytes], vs1[WAVES * kBytes];
+  const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : uniform(threadIdx.x >> 6);
+  lds_char* const k0 = (lds_char*)ks0 + wave * kBytes;
+  lds_char* const v0 = (lds_char*)vs0 + wave * kBytes;
+  lds_char* const k1 = (lds_char*)ks1 + wave * kBytes;
+  lds_char* const v1 = (lds_char*)vs1 + wave * kBytes;
   const int hk = uniform(blockIdx.x % (unsigned)a.Hk);
   CrossSeq s;
   int tile;
@@ -187,7 +202,9 @@ __global__ __launch_bounds__(64, 1) void cross_few_kernel(CrossArgs a) {
   const Row row = row_of(a, s, hk, r0 + (lane & 31));
 
   const int tiles = (s.seen + kFewStates - 1) / kFewStates, per = (tiles + a.splits - 1) / a.splits;
-  const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
+  const int first = per * (int)blockIdx.y, behind = first + per < tiles ? first + per : tiles;
+  const int each = (behind - first + WAVES - 1) / WAVES, from = first + wave * each;
+  const int to = WAVES == 1 || from + each > behind ? behind : from + each;
   const char* kb = (const char*)a.k + (seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head) * Tile::kEs;
   const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
   const uint8_t* mask = !MASKED ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
@@ -229,19 +246,55 @@ __global__ __launch_bounds__(64, 1) void cross_few_kernel(CrossArgs a) {
     // Each step has the copies of one more tile on the way, behind the last one that one's
     // again: where not every way through had them, the compiler could not count them and
     // would wait for all before each read.
-    copy(from, (lds_char*)k0, (lds_char*)v0, b0);
+    copy(from, k0, v0, b0);
     for (int t = from;; t += 2) {
-      copy(t + 1, (lds_char*)k1, (lds_char*)v1, b1);
-      step(t, (lds_char*)k0, (lds_char*)v0, b0);
+      copy(t + 1, k1, v1, b1);
+      step(t, k0, v0, b0);
       if (t + 1 >= to) break;
-      copy(t + 2, (lds_char*)k0, (lds_char*)v0, b0);
-      step(t + 1, (lds_char*)k1, (lds_char*)v1, b1);
+      copy(t + 2, k0, v0, b0);
+      step(t + 1, k1, v1, b1);
       if (t + 2 >= to) break;
     }
     copies_landed();
   }
   l += other_half(l);
-  if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
+  if constexpr (WAVES == 1) {
+    if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
+  } else {
+    // o goes to the wave's own places, 16 bytes a lane in the lanes' order; then each wave
+    // adds a share of the channels up, in the waves' order.
+    __shared__ float2 stats[WAVES][32];
+    auto place = [&](int w, int block) -> Lds<floatx4>* {  // 4 channels of 32 rows
+      const int byte = block * 512;
+      return (Lds<floatx4>*)((byte < kBytes ? (lds_char*)ks0 + w * kBytes + byte : (lds_char*)vs0 + w * kBytes + byte - kBytes) +
+                             (lane & 31) * 16);
+    };
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *place(wave, 8 * e + 2 * i + (lane >> 5)) = floatx4{o[e][4 * i], o[e][4 * i + 1], o[e][4 * i + 2], o[e][4 * i + 3]};
+    if (lane < 32) stats[wave][lane] = make_float2(m, l);
+    lds_barrier();
+    float2 each_of[WAVES];
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) each_of[w] = stats[w][lane & 31], top = fmaxf(top, each_of[w].x);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      each_of[w].x = each_of[w].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(each_of[w].x - top);
+      sum += each_of[w].x * each_of[w].y;
+    }
+    if (!row.real) return;
+    const Put<F32, D> put(a, row, top, sum);
+    for (int b = 2 * wave + (lane >> 5); b < D / 4; b += 2 * WAVES) {
+      floatx4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) x += each_of[w].x * *place(w, b);
+      put.channels(4 * b, x);
+    }
+    if (wave == 0 && lane < 32) put.stats();
+  }
 }
 
 // Adds the parts of a row's splits: a wave per row, whose lanes have a split's maximum
@@ -296,14 +349,21 @@ __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   if (a.lse != nullptr && lane == 0) a.lse[lse] = lse_of(top, sum);
 }
 
+template <bool F32, int D, int WAVES>
+void few_rows(const CrossArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)a.tiles * a.Hk, a.splits);
+  if (a.k_mask != nullptr)
+    cross_few_kernel<F32, D, true, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a);
+  else
+    cross_few_kernel<F32, D, false, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a);
+}
+
 template <bool F32, int D>
-hipError_t forward(bool few, const CrossArgs& a, hipStream_t stream) {
-  if (few) {
-    const dim3 grid((unsigned)a.tiles * a.Hk, a.splits);
-    if (a.k_mask != nullptr)
-      cross_few_kernel<F32, D, true><<<grid, 64, 0, stream>>>(a);
-    else
-      cross_few_kernel<F32, D, false><<<grid, 64, 0, stream>>>(a);
+hipError_t forward(int few, const CrossArgs& a, hipStream_t stream) {
+  if (few == 1) {
+    few_rows<F32, D, 1>(a, stream);
+  } else if (few != 0) {
+    few_rows<F32, D, few_waves(F32, D)>(a, stream);
   } else {
     const unsigned grid = ((unsigned)a.tiles * a.Hk + 7) / 8 * 8;
     cross_forward_kernel<F32, D><<<dim3(grid, a.splits), kThreads, 0, stream>>>(a);
@@ -319,7 +379,7 @@ hipError_t join(const CrossArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_cross_forward(bool f32, int d, bool few, const CrossArgs& a, hipStream_t stream) {
+hipError_t launch_cross_forward(bool f32, int d, int few, const CrossArgs& a, hipStream_t stream) {
   switch (d) {
     case 32: return f32 ? forward<true, 32>(few, a, stream) : forward<false, 32>(few, a, stream);
     case 64: return f32 ? forward<true, 64>(few, a, stream) : forward<false, 64>(few, a, stream);
