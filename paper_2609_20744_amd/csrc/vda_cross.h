@@ -408,6 +408,38 @@ __device__ __forceinline__ void store4(void* p, size_t at, floatx4 x) {
     *reinterpret_cast<uint2*>((uint16_t*)p + at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
+// A wave's 32 rows (token x head) from r0 on of `rows`, D channels each as a product leaves
+// them, times `by`, to memory: through its own part of LDS (32 rows of a tile), so that
+// 16 bytes a lane are next to one another.  base: as for copy_rows.
+template <bool F32, int D>
+__device__ __forceinline__ void store_rows(const CrossArgs& a, void* base, const CrossStrides& s, int r0, int rows,
+                                           const floatx16 (&x)[D / 32], float by, lds_char* tile, int lane) {
+  typedef CrossTile<F32, D> Tile;
+  const int li = lane & 31, lh = lane >> 5;
+  const int at = li * Tile::kRow + (F32 ? lh ^ Tile::swizzle(li) : Tile::swizzle(li)) * 16 + (F32 ? 0 : lh * 8);
+#pragma unroll
+  for (int e = 0; e < D / 32; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const floatx4 z = floatx4{x[e][4 * i], x[e][4 * i + 1], x[e][4 * i + 2], x[e][4 * i + 3]} * by;
+      if constexpr (F32)
+        *(Lds<floatx4>*)(tile + (at ^ (8 * e + 2 * i) * 16)) = z;
+      else
+        *(Lds<u32x2>*)(tile + (at ^ (4 * e + i) * 16)) = u32x2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
+    }
+  const int t0 = uniform(r0 / a.group), g0 = r0 - t0 * a.group;
+  char* to = (char*)base + (size_t)t0 * s.tok * Tile::kEs;
+  const int first = lane / Tile::kPieces, piece = lane % Tile::kPieces;
+  constexpr int kStep = 64 / Tile::kPieces;
+#pragma unroll
+  for (int i = 0; i < 32 / kStep; ++i) {
+    const int r = first + i * kStep;
+    const u32x4 z = *(const Lds<u32x4>*)(tile + r * Tile::kRow + (piece ^ Tile::swizzle(r)) * 16);
+    const uint32_t y = g0 + r, t = y * a.group_magic >> 24, g = y - t * a.group;
+    if (r0 + r < rows) *reinterpret_cast<u32x4*>(to + (t * s.tok + g * s.head) * Tile::kEs + piece * 16) = z;
+  }
+}
+
 // Host-side launchers (arguments validated).
 // Waves of a workgroup of few rows that share its range of the states; their tiles have to fit LDS.
 constexpr int few_waves(bool f32, int d) { return f32 && d == 128 ? 2 : 4; }

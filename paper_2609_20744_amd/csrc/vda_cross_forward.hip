@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   if (!seq_of_tile<false>(a, kCrossRows, place, s, tile)) return;
   const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
-  const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
+  const int rows = s.lq * a.group, w0 = r0 + wave * 32;
 
   // The range of states of this split, in tiles.
   const int tiles = (s.seen + kCrossTile - 1) / kCrossTile, per = (tiles + a.splits - 1) / a.splits;
@@ -138,11 +138,6 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
 
   typename Fr::X q[D / 16];
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) {
-    q[e] = Fr::load(a.q, row.q + 16 * e + 8 * (lane >> 5));
-    if (a.flip) q[e] = Fr::flip(q[e]);
-  }
   floatx16 o[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) o[e] = floatx16{};
@@ -166,15 +161,37 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
     if (t + 1 < to) copy(t + 1, next_k, next_v);
     if (bits[0] != 0) attend<F32, D, 2>(kt, vt, q, bits[0], ~bits[0] == 0, a.c, o, m, l, offs);
   };
+  // A wave's part of two tiles' places: its q comes and its output goes through it.
+  auto part = [&](lds_char* kt, lds_char* vt) { return (wave < 2 ? kt : vt) + (wave & 1) * 32 * Tile::kRow; };
   if (from < to) {
+    lds_char* mine = part((lds_char*)k1, (lds_char*)v1);
+    const int r = w0 < rows ? w0 : rows - 1;
+    const size_t qb = seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.sq.head;
+    copy_rows<F32, D, 32, 1>(a, (const char*)a.q + qb * Tile::kEs, a.sq, r, rows - 1 - r, mine, 0, lane);
     copy(from, (lds_char*)k0, (lds_char*)v0);
+    copies_landed();
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      q[e] = Tile::row_frag(mine, e, offs);
+      if (a.flip) q[e] = Fr::flip(q[e]);
+    }
     for (int t = from; t < to; t += 2) {
       step(t, (lds_char*)k0, (lds_char*)v0, (lds_char*)k1, (lds_char*)v1);
       if (t + 1 < to) step(t + 1, (lds_char*)k1, (lds_char*)v1, (lds_char*)k0, (lds_char*)v0);
     }
   }
   l += other_half(l);
-  if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
+  if (w0 >= rows) return;
+  const Row row = row_of(a, s, hk, w0 + (lane & 31));
+  if (a.splits > 1) {
+    if (row.real) put_rows<F32, D>(a, row, o, m, l, lane);
+    return;
+  }
+  const bool odd = (to - from) & 1;  // the last tile's places were k0 and v0
+  lds_char* mine = from < to && !odd ? part((lds_char*)k0, (lds_char*)v0) : part((lds_char*)k1, (lds_char*)v1);
+  const size_t ob = seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.so.head;
+  store_rows<F32, D>(a, (uint16_t*)a.out + ob * (Tile::kEs / 2), a.so, w0, rows, o, l == 0.f ? 0.f : 1.f / l, mine, lane);
+  if (a.lse != nullptr && row.real && lane < 32) a.lse[row.lse] = lse_of(m, l);
 }
 
 // Few rows: a wave with 32 rows takes tiles of 32 states through two places in LDS, one on
