@@ -408,6 +408,22 @@ __device__ __forceinline__ void store4(void* p, size_t at, floatx4 x) {
     *reinterpret_cast<uint2*>((uint16_t*)p + at) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
 }
 
+// What copy_rows would copy of 32 rows with one wave, in registers.
+template <bool F32, int D>
+__device__ __forceinline__ void load_rows(const CrossArgs& a, const void* base, const CrossStrides& s, int r0, int last,
+                                          u32x4 (&x)[CrossTile<F32, D>::kPieces / 2], int lane) {
+  typedef CrossTile<F32, D> Tile;
+  const int t0 = uniform(r0 / a.group), g0 = r0 - t0 * a.group;
+  const char* from = (const char*)base + (size_t)t0 * s.tok * Tile::kEs;
+#pragma unroll
+  for (int i = 0; i < Tile::kPieces / 2; ++i) {
+    const int r = lane / Tile::kPieces + i * (64 / Tile::kPieces);
+    const uint32_t y = g0 + (r < last ? r : last), t = y * a.group_magic >> 24, g = y - t * a.group;
+    x[i] = *reinterpret_cast<const u32x4*>(from + (t * s.tok + g * s.head) * Tile::kEs +
+                                           (lane % Tile::kPieces ^ Tile::swizzle(r)) * 16);
+  }
+}
+
 // A wave's 32 rows (token x head) from r0 on of `rows`, D channels each as a product leaves
 // them, times `by`, to memory: through its own part of LDS (32 rows of a tile), so that
 // 16 bytes a lane are next to one another.  base: as for copy_rows.

@@ -30,7 +30,8 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   if (!seq_of_tile<false>(a, kCrossRows, place, s, tile)) return;
   const int r0 = tile * kCrossRows;
   if (r0 >= s.lq * a.group) return;
-  const Row row = row_of(a, s, hk, r0 + wave * 32 + (lane & 31));
+  const int rows = s.lq * a.group, w0 = r0 + wave * 32;
+  const Row row = row_of(a, s, hk, w0 + (lane & 31));
 
   const int tiles = (s.seen + kCrossTile - 1) / kCrossTile, per = (tiles + a.splits - 1) / a.splits;
   const int from = per * (int)blockIdx.y, to = from + per < tiles ? from + per : tiles;
@@ -38,27 +39,47 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   const char* vb = (const char*)a.v + (seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head) * Tile::kEs;
   const uint8_t* mask = a.k_mask == nullptr ? nullptr : a.k_mask + (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk);
 
+  // q, dout and the output come through a wave's part of the tiles' places, memory's rows
+  // whole; the output in registers until q's place is free.
+  auto part = [&](lds_char* kt, lds_char* vt) { return (wave < 2 ? kt : vt) + (wave & 1) * 32 * Tile::kRow; };
+  const typename Tile::Lane offs = Tile::lane_of(lane);
   typename Fr::X q[D / 16], g[D / 16];
-  float dot = 0.f;
+  float dot = 0.f, lse = a.lse_in[row.lse] * kLog2e;
+  {
+    lds_char* const q_part = part((lds_char*)k1, (lds_char*)v1);
+    lds_char* const g_part = part((lds_char*)k0, (lds_char*)v0);
+    const int r = w0 < rows ? w0 : rows - 1;
+    const size_t qb = seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.sq.head;
+    const size_t ob = seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.so.head;
+    copy_rows<F32, D, 32, 1>(a, (const char*)a.q + qb * Tile::kEs, a.sq, r, rows - 1 - r, q_part, 0, lane);
+    copy_rows<F32, D, 32, 1>(a, (const char*)a.dout + ob * Tile::kEs, a.so, r, rows - 1 - r, g_part, 0, lane);
+    u32x4 o[32 * Tile::kPieces / 64];
+    load_rows<F32, D>(a, (const char*)a.o + ob * Tile::kEs, a.so, r, rows - 1 - r, o, lane);
+    copies_landed();
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) {
-    q[e] = Fr::load(a.q, row.q + 16 * e + 8 * (lane >> 5));
-    if (a.flip) q[e] = Fr::flip(q[e]);
-    g[e] = Fr::load(a.dout, row.out + 16 * e + 8 * (lane >> 5));
-    const typename Fr::X o = Fr::load(a.o, row.out + 16 * e + 8 * (lane >> 5));
+    for (int e = 0; e < D / 16; ++e) {
+      q[e] = Tile::row_frag(q_part, e, offs);
+      if (a.flip) q[e] = Fr::flip(q[e]);
+      g[e] = Tile::row_frag(g_part, e, offs);
+    }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dot = fmaf(Fr::value(g[e], i), Fr::value(o, i), dot);
+    for (int i = 0; i < 32 * Tile::kPieces / 64; ++i) *(Lds<u32x4>*)(q_part + (64 * i + lane) * 16) = o[i];
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) {
+      const typename Fr::X x = Tile::row_frag(q_part, e, offs);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot = fmaf(Fr::value(g[e], i), Fr::value(x, i), dot);
+    }
+    lds_barrier();  // the first tile is copied over all of them
   }
   dot += other_half(dot);
   // A row that sees no state has an lse of -inf: as +inf it leaves no p.
-  float lse = a.lse_in[row.lse] * kLog2e;
   lse = lse == -INFINITY ? INFINITY : lse;
   if (blockIdx.y == 0 && row.real && lane < 32) a.stats[row.part] = make_float2(lse, dot);
   floatx16 dq[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dq[e] = floatx16{};
   uint8_t byte = 1;
-  const typename Tile::Lane offs = Tile::lane_of(lane);
 
   auto copy = [&](int t, lds_char* kt, lds_char* vt) {
     const int first = t * kCrossTile, last = s.seen - 1 - first;
@@ -108,18 +129,22 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
       if (t + 1 < to) step(t + 1, (lds_char*)k1, (lds_char*)v1, (lds_char*)k0, (lds_char*)v0);
     }
   }
+  if (w0 >= rows) return;
+  if (a.splits == 1) {
+    const bool odd = (to - from) & 1;  // the last tile's places were k0 and v0
+    lds_char* mine = from < to && !odd ? part((lds_char*)k0, (lds_char*)v0) : part((lds_char*)k1, (lds_char*)v1);
+    const size_t at = seq_base(a.sdq, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.sdq.head;
+    store_rows<F32, D>(a, (uint16_t*)a.dq + at * (Tile::kEs / 2), a.sdq, w0, rows, dq, a.scale, mine, lane);
+    return;
+  }
   if (!row.real) return;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 x = floatx4{dq[e][4 * i], dq[e][4 * i + 1], dq[e][4 * i + 2], dq[e][4 * i + 3]} * a.scale;
-      const int chan = 32 * e + 8 * i + 4 * (lane >> 5);
-      if (a.splits > 1)
-        *reinterpret_cast<floatx4*>(a.part + ((size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part) * D + chan) = x;
-      else
-        store4<F32>(a.dq, row.dq + chan, x);
-    }
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<floatx4*>(a.part + ((size_t)blockIdx.y * ((size_t)a.T * a.Hq) + row.part) * D + 32 * e + 8 * i +
+                                  4 * (lane >> 5)) =
+          floatx4{dq[e][4 * i], dq[e][4 * i + 1], dq[e][4 * i + 2], dq[e][4 * i + 3]} * a.scale;
 }
 
 // Shape of the kernel of dk and dv: 128 states a workgroup, 32 a wave.  In bf16
