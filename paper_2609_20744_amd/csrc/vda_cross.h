@@ -424,12 +424,11 @@ __device__ __forceinline__ void load_rows(const CrossArgs& a, const void* base, 
   }
 }
 
-// A wave's 32 rows (token x head) from r0 on of `rows`, D channels each as a product leaves
-// them, times `by`, to memory: through its own part of LDS (32 rows of a tile), so that
-// 16 bytes a lane are next to one another.  base: as for copy_rows.
-template <bool F32, int D>
-__device__ __forceinline__ void store_rows(const CrossArgs& a, void* base, const CrossStrides& s, int r0, int rows,
-                                           const floatx16 (&x)[D / 32], float by, lds_char* tile, int lane) {
+// A wave's 32 rows of D channels, as a product leaves them, times `by`, through its own part
+// of LDS (32 rows of a tile): put(r, piece, 16 bytes) then has rows' bytes next to one another
+// in the lanes.
+template <bool F32, int D, typename Put>
+__device__ __forceinline__ void rows_through(const floatx16 (&x)[D / 32], float by, lds_char* tile, int lane, Put put) {
   typedef CrossTile<F32, D> Tile;
   const int li = lane & 31, lh = lane >> 5;
   const int at = li * Tile::kRow + (F32 ? lh ^ Tile::swizzle(li) : Tile::swizzle(li)) * 16 + (F32 ? 0 : lh * 8);
@@ -443,17 +442,33 @@ __device__ __forceinline__ void store_rows(const CrossArgs& a, void* base, const
       else
         *(Lds<u32x2>*)(tile + (at ^ (4 * e + i) * 16)) = u32x2{pack_bf16x2(z[0], z[1]), pack_bf16x2(z[2], z[3])};
     }
-  const int t0 = uniform(r0 / a.group), g0 = r0 - t0 * a.group;
-  char* to = (char*)base + (size_t)t0 * s.tok * Tile::kEs;
-  const int first = lane / Tile::kPieces, piece = lane % Tile::kPieces;
-  constexpr int kStep = 64 / Tile::kPieces;
+  const int piece = lane % Tile::kPieces;
 #pragma unroll
-  for (int i = 0; i < 32 / kStep; ++i) {
-    const int r = first + i * kStep;
-    const u32x4 z = *(const Lds<u32x4>*)(tile + r * Tile::kRow + (piece ^ Tile::swizzle(r)) * 16);
-    const uint32_t y = g0 + r, t = y * a.group_magic >> 24, g = y - t * a.group;
-    if (r0 + r < rows) *reinterpret_cast<u32x4*>(to + (t * s.tok + g * s.head) * Tile::kEs + piece * 16) = z;
+  for (int i = 0; i < Tile::kPieces / 2; ++i) {
+    const int r = lane / Tile::kPieces + i * (64 / Tile::kPieces);
+    put(r, piece, *(const Lds<u32x4>*)(tile + r * Tile::kRow + (piece ^ Tile::swizzle(r)) * 16));
   }
+}
+
+// The rows (token x head) from r0 on of `rows` to memory.  base: as for copy_rows.
+template <bool F32, int D>
+__device__ __forceinline__ void store_rows(const CrossArgs& a, void* base, const CrossStrides& s, int r0, int rows,
+                                           const floatx16 (&x)[D / 32], float by, lds_char* tile, int lane) {
+  const int t0 = uniform(r0 / a.group), g0 = r0 - t0 * a.group;
+  char* to = (char*)base + (size_t)t0 * s.tok * CrossTile<F32, D>::kEs;
+  rows_through<F32, D>(x, by, tile, lane, [&](int r, int piece, u32x4 z) {
+    const uint32_t y = g0 + r, t = y * a.group_magic >> 24, g = y - t * a.group;
+    if (r0 + r < rows) *reinterpret_cast<u32x4*>(to + (t * s.tok + g * s.head) * CrossTile<F32, D>::kEs + piece * 16) = z;
+  });
+}
+
+// `rows` rows (at most 32) that are row_bytes apart to memory, in the type of F32.
+template <bool F32, int D>
+__device__ __forceinline__ void store_states(void* to, size_t row_bytes, int rows, const floatx16 (&x)[D / 32], float by,
+                                             lds_char* tile, int lane) {
+  rows_through<F32, D>(x, by, tile, lane, [&](int r, int piece, u32x4 z) {
+    if (r < rows) *reinterpret_cast<u32x4*>((char*)to + r * row_bytes + piece * 16) = z;
+  });
 }
 
 // Host-side launchers (arguments validated).

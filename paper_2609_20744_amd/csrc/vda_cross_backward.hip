@@ -157,7 +157,7 @@ struct DkvShape {
 };
 
 template <bool F32, int D>
-__global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void cross_dkv_kernel(CrossArgs a) {
+__global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 4 : 2)) void cross_dkv_kernel(CrossArgs a) {
   typedef Frag<F32> Fr;
   typedef CrossTile<F32, D> Tile;
   typedef DkvShape<F32> Shape;
@@ -192,20 +192,27 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
   const size_t kat = seq_base(a.sk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sk.head;
   const size_t vat = seq_base(a.sv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sv.head + (size_t)j0 * a.sv.tok;
   copy_states<F32, D, kCrossRows, Shape::kWaves>((const char*)a.v + vat * Tile::kEs, a.sv.tok, s.lk - 1 - j0, (lds_char*)vt, wave, lane);
+  // k comes through the tiles' places, a place 32 states, memory's rows whole.
+  lds_char* const room = (lds_char*)(part_of == 0 ? q0 : part_of == 1 ? g0 : part_of == 2 ? q1 : g1);
+  const int w0 = j0 + part_of * 32, k0 = w0 < s.lk ? w0 : s.lk - 1;
+  copy_states<F32, D, 32, Shape::kHalves>((const char*)a.k + (kat + (size_t)k0 * a.sk.tok) * Tile::kEs, a.sk.tok, s.lk - 1 - k0, room,
+                                          half, lane);
+  const typename Tile::Lane offs = Tile::lane_of(lane);
+  cross_barrier();
 #pragma unroll
   for (int e = 0; e < D / 16; ++e) {
-    k[e] = Fr::load(a.k, kat + (size_t)jc * a.sk.tok + 16 * e + 8 * (lane >> 5));
+    k[e] = Tile::row_frag(room, e, offs);
     if (a.flip) k[e] = Fr::flip(k[e]);
     // What stands in a masked place may be anything.
     if (!seen) k[e] = Fr::zero();
   }
-  cross_barrier();
   if (!seen && half == 0) {
     constexpr int kEach = Tile::kPieces / 2;
     for (int e = 0; e < kEach; ++e)
       *reinterpret_cast<uint4*>(vt + ((part_of * 32 + (lane & 31)) * Tile::kRow + ((lane >> 5) * kEach + e) * 16)) =
           make_uint4(0u, 0u, 0u, 0u);
   }
+  lds_barrier();  // the first tile is copied over k
   floatx16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dk[e] = floatx16{}, dv[e] = floatx16{};
@@ -216,7 +223,6 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
                    (seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)hk * a.group * a.so.head) * Tile::kEs;
   const float2* stats = a.stats + (a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) * a.Hq + hk * a.group;
   float2 mine = make_float2(0.f, 0.f);
-  const typename Tile::Lane offs = Tile::lane_of(lane);
   const bool all = __all(seen);
   const lds_char* vmine = (const lds_char*)vt + part_of * 32 * Tile::kRow;
 
@@ -283,7 +289,6 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
   }
   if constexpr (Shape::kHalves == 2) {
     // The second half's sums, through the four tiles.
-    char* room = part_of == 0 ? q0 : part_of == 1 ? g0 : part_of == 2 ? q1 : g1;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       floatx16(&x)[D / 32] = w == 0 ? dk : dv;
@@ -293,7 +298,7 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<floatx4*>(room + (4 * e + i) * 1024 + lane * 16) =
+            *(Lds<floatx4>*)(room + (4 * e + i) * 1024 + lane * 16) =
                 floatx4{x[e][4 * i], x[e][4 * i + 1], x[e][4 * i + 2], x[e][4 * i + 3]};
       lds_barrier();
       if (half == 0)
@@ -301,32 +306,28 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : 2)) void c
         for (int e = 0; e < D / 32; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const floatx4 y = *reinterpret_cast<const floatx4*>(room + (4 * e + i) * 1024 + lane * 16);
+            const floatx4 y = *(const Lds<floatx4>*)(room + (4 * e + i) * 1024 + lane * 16);
 #pragma unroll
             for (int u = 0; u < 4; ++u) x[e][4 * i + u] += y[u];
           }
     }
     if (half == 1) return;
+  } else {
+    lds_barrier();
   }
-  if (j >= s.lk) return;
-  const size_t dkat = seq_base(a.sdk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdk.head + (size_t)jc * a.sdk.tok;
-  const size_t dvat = seq_base(a.sdv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdv.head + (size_t)jc * a.sdv.tok;
-  const size_t part = (size_t)blockIdx.y * ((size_t)a.S * a.Hk) + token * a.Hk + hk;
-#pragma unroll
-  for (int e = 0; e < D / 32; ++e)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 x = floatx4{dk[e][4 * i], dk[e][4 * i + 1], dk[e][4 * i + 2], dk[e][4 * i + 3]} * a.scale;
-      const floatx4 y = floatx4{dv[e][4 * i], dv[e][4 * i + 1], dv[e][4 * i + 2], dv[e][4 * i + 3]};
-      const int chan = 32 * e + 8 * i + 4 * (lane >> 5);
-      if (ranges > 1) {
-        *reinterpret_cast<floatx4*>(a.part + part * D + chan) = x;
-        *reinterpret_cast<floatx4*>(a.part2 + part * D + chan) = y;
-      } else {
-        store4<F32>(a.dk, dkat + chan, x);
-        store4<F32>(a.dv, dvat + chan, y);
-      }
-    }
+  const int count = s.lk - w0;  // the wave's states
+  if (count <= 0) return;
+  if (ranges > 1) {
+    const size_t first = (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + w0;
+    const size_t part = ((size_t)blockIdx.y * ((size_t)a.S * a.Hk) + first * a.Hk + hk) * D;
+    store_states<true, D>(a.part + part, (size_t)a.Hk * D * 4, count, dk, a.scale, room, lane);
+    store_states<true, D>(a.part2 + part, (size_t)a.Hk * D * 4, count, dv, 1.f, room, lane);
+  } else {
+    const size_t dkat = seq_base(a.sdk, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdk.head + (size_t)w0 * a.sdk.tok;
+    const size_t dvat = seq_base(a.sdv, a.cu_k, s.k0, s.kv) + (size_t)hk * a.sdv.head + (size_t)w0 * a.sdv.tok;
+    store_states<F32, D>((uint16_t*)a.dk + dkat * (Tile::kEs / 2), a.sdk.tok * Tile::kEs, count, dk, a.scale, room, lane);
+    store_states<F32, D>((uint16_t*)a.dv + dvat * (Tile::kEs / 2), a.sdv.tok * Tile::kEs, count, dv, 1.f, room, lane);
+  }
 }
 
 // Adds the parts of a row's (token x head) ranges, in their order: D / 4 lanes a row.
