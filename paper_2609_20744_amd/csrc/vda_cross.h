@@ -295,19 +295,20 @@ __device__ __forceinline__ void copy_states(const void* base, size_t row_elems, 
 #endif
 }
 
-// Writes zeros over the rows whose bit is not set, each wave over what it copied
-// itself, once that is there.  bits: 64 rows each.
-template <bool F32, int D, int ROWS, int WAVES>
-__device__ __forceinline__ void clear_copied(lds_char* tile, const uint64_t (&bits)[(ROWS + 63) / 64], int wave, int lane) {
+// Writes zeros over the rows of tiles whose bit is not set, each wave over what it copied
+// itself, once that is there: what stands in a masked place may be anything, and 0 times it
+// has to be 0.  A copy's 1024 bytes whose rows are all seen cost no more than a scalar look.
+template <bool F32, int D, int ROWS, int WAVES, typename... Tiles>
+__device__ __forceinline__ void clear_copied(uint64_t bits, int wave, int lane, Tiles... tiles) {
   typedef CrossTile<F32, D> Tile;
-  constexpr int kPieces = ROWS * Tile::kRow / 1024;
+  constexpr int kPieces = ROWS * Tile::kRow / 1024, kRows = 64 / Tile::kPieces;
 #pragma unroll
   for (int i = 0; i < (kPieces + WAVES - 1) / WAVES; ++i) {
-    const int p = wave + i * WAVES, at = p * 64 + lane;
+    const int p = wave + i * WAVES;
     if (kPieces % WAVES != 0 && p >= kPieces) break;
-    const int r = at / Tile::kPieces;
-    const uint64_t w = ROWS > 64 && r >= 64 ? bits[ROWS > 64 ? 1 : 0] : bits[0];
-    if (!(w >> (r & 63) & 1)) *(Lds<u32x4>*)(tile + at * 16) = u32x4{0u, 0u, 0u, 0u};
+    const uint32_t w = (uint32_t)(bits >> p * kRows) & ((1u << kRows) - 1);
+    if (w != (1u << kRows) - 1 && !(w >> lane / Tile::kPieces & 1))
+      ((*(Lds<u32x4>*)(tiles + (p * 64 + lane) * 16) = u32x4{0u, 0u, 0u, 0u}), ...);
   }
 }
 
@@ -353,6 +354,23 @@ __device__ __forceinline__ void copy_rows(const CrossArgs& a, const void* base, 
 __device__ __forceinline__ float row_or(float x, uint32_t w, int i, float otherwise) {
   const int m = __builtin_amdgcn_sbfe((int)w, 8 * (i >> 2) + (i & 3), 1);
   return __int_as_float((m & __float_as_int(x)) | (~m & __float_as_int(otherwise)));
+}
+
+// What the scores of a tile's states start from where not all are seen, a wave's own in LDS:
+// -inf stays in the sum of finite products (the rows that are not seen are zeros, or the
+// last one again), so that no score has to be looked at by itself.
+__device__ __forceinline__ void put_start(Lds<float>* start, uint64_t bits, int lane) {
+  start[lane] = __builtin_amdgcn_inverse_ballot_w64(bits) ? 0.f : -INFINITY;
+}
+__device__ __forceinline__ floatx16 start_of(const Lds<float>* start, int lane) {
+  floatx16 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const floatx4 y = *(const Lds<floatx4>*)(start + 8 * i + 4 * (lane >> 5));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[4 * i + e] = y[e];
+  }
+  return x;
 }
 
 // The wave's copies into LDS are there.

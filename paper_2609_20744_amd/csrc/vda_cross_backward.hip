@@ -23,7 +23,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   typedef CrossTile<F32, D> Tile;
   constexpr int kTileBytes = kCrossTile * Tile::kRow;
   __shared__ __align__(16) char k0[kTileBytes], v0[kTileBytes], k1[kTileBytes], v1[kTileBytes];
+  __shared__ __align__(16) float starts[4][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  Lds<float>* const start = (Lds<float>*)starts[wave];
   CrossSeq s;
   int hk, place, tile;
   if (!place_of(a, hk, place)) return;
@@ -89,30 +91,30 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   };
   auto step = [&](int t, lds_char* kt, lds_char* vt, lds_char* next_k, lds_char* next_v) {
     copies_landed();
-    const uint64_t seen[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
-    const uint64_t bits = seen[0];
+    const uint64_t bits = seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane);
     const bool all = ~bits == 0;
-    // What stands in a masked place may be anything: 0 times it has to be 0.
-    if (mask != nullptr && !all) clear_copied<F32, D, kCrossTile, 4>(kt, seen, wave, lane);
+    if (!all) {
+      if (mask != nullptr) clear_copied<F32, D, kCrossTile, 4>(bits, wave, lane, kt, vt);
+      put_start(start, bits, lane);
+    }
     lds_barrier();
     if (t + 1 < to) copy(t + 1, next_k, next_v);
     if (bits == 0) return;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const typename Tile::Lane here = Tile::again(offs);
-      floatx16 p = {}, dp = {};
+      floatx16 p, dp = {};
+      if (all)
+        p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, 0, here), q[0], floatx16{});
+      else  // a score of -inf leaves no p
+        p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, 0, here), q[0], start_of(start + 32 * b, lane));
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) {
-        p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, e, here), q[e], p);
+        if (e > 0) p = Fr::mma(Tile::row_frag(kt + 32 * b * Tile::kRow, e, here), q[e], p);
         dp = Fr::mma(Tile::row_frag(vt + 32 * b * Tile::kRow, e, here), g[e], dp);
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * (dp[i] - dot);
-      if (!all) {
-        const uint32_t w = (uint32_t)(bits >> 32 * b) >> (lane >> 5) * 4;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = row_or(p[i], w, i, 0.f);
-      }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const typename Fr::X x = Fr::of(p, h);

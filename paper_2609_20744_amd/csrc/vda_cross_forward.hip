@@ -154,12 +154,11 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
   // Tile t, whose copies are there when it begins; the next one's begin behind the barrier.
   auto step = [&](int t, lds_char* kt, lds_char* vt, lds_char* next_k, lds_char* next_v) {
     copies_landed();
-    const uint64_t bits[1] = {seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane)};
-    // What stands in a masked place may be anything: 0 times it has to be 0.
-    if (mask != nullptr && ~bits[0] != 0) clear_copied<F32, D, kCrossTile, 4>(vt, bits, wave, lane);
+    const uint64_t bits = seen_bits(s.seen - t * kCrossTile, mask != nullptr, byte, lane);
+    if (mask != nullptr && ~bits != 0) clear_copied<F32, D, kCrossTile, 4>(bits, wave, lane, vt);
     lds_barrier();
     if (t + 1 < to) copy(t + 1, next_k, next_v);
-    if (bits[0] != 0) attend<F32, D, 2>(kt, vt, q, bits[0], ~bits[0] == 0, a.c, o, m, l, offs);
+    if (bits != 0) attend<F32, D, 2>(kt, vt, q, bits, ~bits == 0, a.c, o, m, l, offs);
   };
   // A wave's part of two tiles' places: its q comes and its output goes through it.
   auto part = [&](lds_char* kt, lds_char* vt) { return (wave < 2 ? kt : vt) + (wave & 1) * 32 * Tile::kRow; };
@@ -250,12 +249,11 @@ __global__ __launch_bounds__(64 * WAVES, 1) void cross_few_kernel(CrossArgs a) {
     // All copies but those of the next tile, the newest ones, have landed.
     __builtin_amdgcn_s_waitcnt((kCopies & 15) | 0x0f70 | (kCopies >> 4 << 14));
     __builtin_amdgcn_sched_barrier(0);
-    const uint64_t bits[1] = {seen_bits(s.seen - t * kFewStates, MASKED, byte, lane) & 0xffffffffull};
-    // What stands in a masked place may be anything: 0 times it has to be 0.
-    const bool all = bits[0] == 0xffffffffull;
-    if (bits[0] != 0) {
-      if (MASKED && !all) clear_copied<F32, D, kFewStates, 1>(vt, bits, 0, lane);
-      attend<F32, D, 1>(kt, vt, q, bits[0], all, a.c, o, m, l, offs);
+    const uint64_t bits = seen_bits(s.seen - t * kFewStates, MASKED, byte, lane) & 0xffffffffull;
+    const bool all = bits == 0xffffffffull;
+    if (bits != 0) {
+      if (MASKED && !all) clear_copied<F32, D, kFewStates, 1>(bits, 0, lane, vt);
+      attend<F32, D, 1>(kt, vt, q, bits, all, a.c, o, m, l, offs);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
