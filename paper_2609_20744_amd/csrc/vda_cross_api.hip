@@ -158,6 +158,7 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.c = std::max((a.flip ? -p->scale : p->scale) * vda::kLog2e, 1e-37f);
   auto near = [&](const CrossStrides& s) { return (64 * s.tok + a.group * s.head) * (p->is_f32 ? 4 : 2) < (size_t)1 << 31; };
   a.near = near(a.sq) && near(a.so);
+  a.sorted = pq && pk && p->n_seqs < 64 && !c.few;
   a.tiles = c.tiles, a.splits = c.splits;
   char* w = static_cast<char*>(work);
   a.part = reinterpret_cast<float*>(w + c.part);
