@@ -150,6 +150,13 @@ CASES = {
     "packed": dict(lq=[70, 0, 1, 200, 33], lk=[130, 5, 64, 1, 90], Hq=4, Hk=2, d=128, lead=3, tail=5),
     "packed_heads": dict(lq=[5, 260, 0, 40], lk=[300, 0, 7, 129], Hq=4, Hk=4, layout="heads", lead=1, tail=2),
     "packed_many": dict(lq=[(7 * i) % 23 for i in range(70)], lk=[(5 * i) % 31 for i in range(70)], d=32),
+    # Many rows each: up to 63 sequences are taken longest first, more in their own order.
+    "packed_63": dict(lq=[(37 * i) % 101 for i in range(63)], lk=[(29 * i) % 83 for i in range(63)], Hq=3, Hk=1, d=32, lead=2, tail=2),
+    "packed_64": dict(lq=[(37 * i) % 101 for i in range(64)], lk=[(29 * i) % 83 for i in range(64)], Hq=3, Hk=1, d=32, lead=2, tail=2),
+    "packed_alike": dict(lq=[130] * 5, lk=[65] * 5, Hq=2, Hk=1, d=64, packed=True, mask="holes"),
+    "packed_rows_of_one": dict(lq=[400, 1, 0, 900], lk=[1, 700, 300, 64], Hq=5, Hk=5, d=128, lens=[1, 650, 300, 64]),
+    "few_short": dict(lq=[2, 2], lk=[250, 250], Hq=4, Hk=2, d=128, mask="holes", lens=[250, 100]),
+    "few_of_many": dict(lq=[3] * 140, lk=[70] * 140, Hq=2, Hk=2, d=32, mask="left"),
     "few_long": dict(lq=[9, 9], lk=[2500, 2500], Hq=2, Hk=1, d=64),
     "some_long": dict(lq=[100], lk=[3001], Hq=1, Hk=1, d=128, layout="heads"),
     "lens": dict(lq=[40, 40, 40, 40], lk=[100, 100, 100, 100], lens=[0, 1, 64, 1000], d=128),
@@ -273,6 +280,9 @@ STEPS = {
     "mask_lens": dict(n=4, t=1, m=6, S=1030, Hq=4, Hk=1, d=64, kv_layout="heads", mask=True, lens=[5, 1030, 600, 2000, 0, 31],
                       slots=[0, 1, 3, 2]),
     "fused": dict(n=3, t=1, m=3, S=90, Hq=6, Hk=3, d=32, kv_layout="tokens", fused=True),
+    "short": dict(n=2, t=3, m=2, S=256, Hq=8, Hk=2, d=128, kv_layout="heads", mask=True, lens=[256, 97]),
+    "short_64": dict(n=2, t=1, m=2, S=512, Hq=8, Hk=2, d=64, kv_layout="tokens", mask=True, lens=[1, 512]),
+    "unsplit": dict(n=40, t=1, m=40, S=300, Hq=16, Hk=8, d=64, kv_layout="tokens", mask=True),
     "many": dict(n=300, t=1, m=300, S=33, Hq=2, Hk=1, d=32, kv_layout="tokens"),
 }
 
