@@ -449,6 +449,12 @@ __device__ __forceinline__ uint64_t seen_bits(int left, bool masked, uint8_t byt
   return bits;
 }
 
+// A value that the compiler takes for new: what is made of it is not held through a loop.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // The other lane half's value.
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 

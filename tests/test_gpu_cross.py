@@ -186,6 +186,54 @@ def test_forward_and_gradients(V, name, dtype):
     c.check(out, lse, grads)
 
 
+ALONE = {
+    "one_state": dict(lq=[70, 5], lk=[1, 1], Hq=4, Hk=2, d=128),
+    "lens": dict(lq=[40, 40], lk=[120, 120], lens=[1, 1], d=64, layout="heads"),
+    "masked": dict(lq=[200, 3, 40], lk=[128, 70, 65], Hq=3, Hk=1, d=32),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", ALONE)
+def test_a_state_seen_alone_has_no_gradient_of_scores(V, name, dtype):
+    """A softmax over one state is constant: dq and dk are zeros, not what roundings leave."""
+    import torch
+    c = Case(dtype=dtype, **ALONE[name])
+    if name == "masked":  # one state of each sequence: the first, the last of the first tile, the last
+        at = [0, c.ck[1] + 63, c.ck[3] - 1]
+        c.seen[:] = False
+        c.seen[at] = True
+        c.mask = torch.from_numpy(c.seen.copy())
+        hidden = torch.from_numpy(~c.seen).cuda()
+        c.dev["k"][hidden], c.dev["v"][hidden] = float("nan"), float("inf")
+    d, o = c.dev, c.options()
+    out, lse = V.cross_forward(d["q"], d["k"], d["v"], return_lse=True, **o)
+    dq, dk, dv = V.cross_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, **o)
+    c.check(out, lse, (dq, dk, dv))
+    assert not dq.any() and not dk.any()
+
+
+@pytest.mark.parametrize("lk", [2, 5, 30, 128, 129, 600])
+def test_gradients_of_few_states_keep_their_norm(V, lk):
+    """What roundings leave of a gradient's norm.  One to bf16 is off by 2^-8 of a value's power of two at most, evenly, so by
+    2^-8 / sqrt(3) of that in the root mean square, and that is 0.73 of the values' own: 0.0017 of a vector's norm.  dq and
+    dk have two (score gradients, result), dv two (weights, result): 0.0017 sqrt(2) = 0.0024.  D taken from a rounded
+    output is a third, as large where few states share the weight (0.0029): a third of its square at most may stay."""
+    import torch
+    c = Case(lq=[130] * 4, lk=[lk] * 4, Hq=4, Hk=4, d=128, spread=1.5)
+    d, o = c.dev, c.options()
+    out, lse = V.cross_forward(d["q"], d["k"], d["v"], return_lse=True, **o)
+    grads = V.cross_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, **o)
+    dq, dk, dv = (c.tokens(x, "tokens") for x in grads)
+    off = np.zeros((3, 2))
+    for i in range(c.n):
+        r, s = slice(c.cq[i], c.cq[i + 1]), slice(c.ck[i], c.ck[i + 1])
+        want = X.cross_sequence(c.q[r], c.k[s], c.v[s], c.seen[s], c.scale, c.do[r])[2:]
+        for x, g, w in zip(off, (dq[r], dk[s], dv[s]), want):
+            x += (np.sum((g - w) ** 2), np.sum(w ** 2))
+    assert (np.sqrt(off[:, 0] / off[:, 1]) < 0.0026).all(), np.sqrt(off[:, 0] / off[:, 1])
+
+
 def test_rows_outside_sequences_are_left(V):
     import torch
     c = Case(lq=[5, 40], lk=[70, 3], lead=4, tail=6, Hq=2, Hk=1)
