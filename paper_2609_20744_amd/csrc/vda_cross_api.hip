@@ -88,6 +88,10 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
   c.few = !backward && rows <= vda::kFewRows;
   const int tile = c.few ? vda::kFewRows : vda::kCrossRows;
   c.tiles = (int)tiles_of(p->cu_q != nullptr, p->T, p->n_seqs, group, tile);
+  // Ranges of the states, of two tiles at least, that make two workgroups a CU where there is
+  // less than one (64 rows of 40320 states of 16 heads, D = 64: 38 us, 46 us with one a CU, 40 us with
+  // four; 200 rows of 8 heads, D = 128: 59, 67 and 67 us; up to 8% behind one a CU where that fits
+  // better).  From one a CU on a join costs more than it gives (1560 x 512 of 24 heads 21 and 44 us).
   auto ranges = [&](long long groups, long long units) {
     if (groups >= cus) return 1LL;
     return std::max(1LL, std::min({(2 * cus + groups - 1) / groups, (units + 1) / 2, 64LL}));
@@ -123,8 +127,13 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     c.tiles_k = (int)tiles_of(p->cu_k != nullptr, p->S, p->n_seqs, 1, vda::kCrossRows);
     const long long most = p->cu_q ? (long long)p->T * group : rows;
     const long long groups = (long long)c.tiles_k * p->H_k;
-    const long long share = rows * groups / (3 * cus);
-    c.range = (int)std::max(groups < cus ? 64LL : 512LL, (share + 63) / 64 * 64);
+    // Rows of a workgroup of the gradient of k and v.  Fewer groups than CUs: as many ranges as
+    // make one workgroup a CU (1560 rows of 512 states of 24 heads 74 us, 100 us with the three a
+    // CU of below; 16384 of 16 heads 277 and 310 us).  Otherwise about three a CU, so that
+    // sequences of uneven length even out (16401 rows over 9 sequences 386 us, 410 us with one a
+    // CU, 420 us with six), of 512 rows at least, as each range's sums are written and added up.
+    const long long each = groups < cus ? (rows + cus / groups - 1) / (cus / groups) : std::max(512LL, rows * groups / (3 * cus));
+    c.range = (int)((std::max(each, 1LL) + 63) / 64 * 64);
     c.splits_k = (int)std::min(8LL, (most + c.range - 1) / c.range);
     c.stats = take(q_rows * 8);
     c.counts = take((size_t)p->S * 4);
@@ -158,7 +167,8 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.c = std::max((a.flip ? -p->scale : p->scale) * vda::kLog2e, 1e-37f);
   auto near = [&](const CrossStrides& s) { return (64 * s.tok + a.group * s.head) * (p->is_f32 ? 4 : 2) < (size_t)1 << 31; };
   a.near = near(a.sq) && near(a.so);
-  a.sorted = pq && pk && p->n_seqs < 64 && !c.few;
+  // With heads that share out evenly over the 8 XCDs: of 5 heads, 24 sequences of 1000 x 600 took 64 us sorted, 53 us not.
+  a.sorted = pq && pk && p->n_seqs < 64 && !c.few && (p->H_k % 8 == 0 || 8 % p->H_k == 0);
   a.tiles = c.tiles, a.splits = c.splits;
   char* w = static_cast<char*>(work);
   a.part = reinterpret_cast<float*>(w + c.part);
@@ -286,7 +296,8 @@ int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void*
   if (e == hipSuccess && c.splits > 1)
     e = vda::launch_cross_sum(
         f32, p->d, vda::CrossSum{{a.part}, nullptr, {dq}, {a.sdq}, a.cu_q, a.n, a.Lq, a.Hq, a.splits, (long long)a.T * a.Hq}, stream);
-  a.tiles = c.tiles_k, a.splits = c.splits_k;
+  // Most of these workgroups have no range and end at once: for them the order's search would cost more than it gives.
+  a.tiles = c.tiles_k, a.splits = c.splits_k, a.sorted = 0;
   if (e == hipSuccess) e = vda::launch_cross_dkv(f32, p->d, a, stream);
   if (e == hipSuccess && c.splits_k > 1)
     e = vda::launch_cross_sum(f32, p->d, vda::CrossSum{{a.part, a.part2}, a.counts, {dk, dv}, {a.sdk, a.sdv}, a.cu_k, a.n, a.Lk, a.Hk,

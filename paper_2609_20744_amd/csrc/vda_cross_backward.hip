@@ -20,7 +20,9 @@ namespace {
 // Tiles of states up to which D is summed from p dP in a pass before, in fp32.  As dout out it has
 // the rounding of out, whose part in dS is as large as the others where a few states share
 // the weight: of 4 to 60 states dq and dk were 2.8e-3 of their norm off (bf16), 2.4e-3 with this
-// pass, of 65 on 2.4e-3 without it.  A state that is seen alone leaves dS = 0, not a remainder.
+// pass, of 129 on 2.4e-3 without it (130 rows of 4 heads, D = 128, even lengths); it is two
+// products more, 382 us for 369 in a packed batch.  A state that is seen alone leaves dS = 0, not
+// a remainder; in fp32, whose error the rounding does not show in, that is all it is for.
 constexpr int kExactTiles = 2;
 
 template <bool F32, int D>
@@ -118,13 +120,18 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse));
   };
-  if (tiles <= kExactTiles && from < to) {
+  int count = 0;  // of states that are seen
+  if (tiles <= kExactTiles)
+    for (int t = 0; t < tiles; ++t) {
+      const int first = t * kCrossTile, last = s.seen - 1 - first;
+      if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
+      count += __popcll(seen_bits(last + 1, mask != nullptr, byte, lane));
+    }
+  if (from < to && (F32 ? count == 1 : count > 0)) {
     float sum = 0.f, one = 0.f;
-    int count = 0;
     for (int t = 0; t < tiles; ++t) {
       copy(t, (lds_char*)k0, (lds_char*)v0);
       const uint64_t bits = arrived(t, (lds_char*)k0, (lds_char*)v0);
-      count += __popcll(bits);
       for (int b = 0; b < 2; ++b) {
         floatx16 p, dp;
         weights((lds_char*)k0, (lds_char*)v0, b, ~bits == 0, Tile::again(offs), p, dp);

@@ -28,7 +28,9 @@ int check_channels(int C, int gate) {
 }
 
 // Tokens of a part of a sequence: a tile backward; forward a segment, so long that about
-// three workgroups of 128 channels are there for each compute unit.
+// three workgroups of 128 channels are there for each compute unit (40320 tokens of 896 channels
+// 63 us, 66 us with one and with six a unit, inputs in the last-level cache; 100000 of 128
+// channels 34, 35 and 38 us).
 int part_of(const vda_recur_problem* p, bool backward) {
   if (backward) return vda::kRecurTile;
   const long long slabs = (p->C + vda::kRecurChans - 1) / vda::kRecurChans;
