@@ -791,7 +791,10 @@ size_t vda_cross_forward_workspace(const vda_cross_problem* p);
  * out), the forward pass's inputs and its out and lse, those of q, k and v.
  * dk and dv are summed over the query heads that share a key head, and 0 for
  * states that are not seen.  dk and dv may be slices of one fused gradient
- * (equal row strides).  Otherwise as vda_cross_forward.
+ * (equal row strides).  A score's gradient is p_j (dout . v_j - D), D = sum_j p_j
+ * dout . v_j: summed so for sequences of up to 256 states (fp32 storage: where one
+ * of them is seen; dq and dk are 0 then), and else taken from the stored out, as
+ * dout . out.  Otherwise as vda_cross_forward.
  */
 int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void* q, const void* k,
                        const void* v, const void* out, const float* lse, void* dq, void* dk,

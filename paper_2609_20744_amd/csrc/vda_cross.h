@@ -50,6 +50,7 @@ struct CrossArgs {
   int Hq, Hk, group;
   uint32_t group_magic;  // x / group = x * group_magic >> 24 for x < group + 64
   float scale, c;        // c = |scale| log2 e, above 0
+  int fine;              // backward, bf16: two parts of what a short sequence's products take
   int sorted;            // tiles of packed sequences in the order of what they have to do
   int near;              // a tile's rows are within 2^31 bytes of its first, whichever their heads
   int flip;              // scale < 0: the sign of one factor of each score is changed
@@ -195,6 +196,14 @@ struct Frag<false> {
     for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(s[8 * t + 2 * e], s[8 * t + 2 * e + 1]);
     return __builtin_bit_cast(X, w);
   }
+  // What of() leaves of them.
+  static __device__ __forceinline__ X rest(const floatx16& s, int t) {
+    const u32x4 w = __builtin_bit_cast(u32x4, of(s, t));
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(s[8 * t + 2 * e] - bf16_lo(w[e]), s[8 * t + 2 * e + 1] - bf16_hi(w[e]));
+    return __builtin_bit_cast(X, r);
+  }
   static __device__ __forceinline__ X load(const void* p, size_t at) {
     return *reinterpret_cast<const bf16x8*>((const uint16_t*)p + at);
   }
@@ -217,6 +226,7 @@ struct Frag<true> {
     for (int e = 0; e < 8; ++e) x[e] = s[8 * t + e];
     return x;
   }
+  static __device__ __forceinline__ X rest(const floatx16&, int) { return zero(); }
   static __device__ __forceinline__ X load(const void* p, size_t at) {
     const floatx4* f = reinterpret_cast<const floatx4*>((const float*)p + at);
     const floatx4 a = f[0], b = f[1];

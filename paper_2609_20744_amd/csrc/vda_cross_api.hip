@@ -169,6 +169,8 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.near = near(a.sq) && near(a.so);
   // With heads that share out evenly over the 8 XCDs: of 5 heads, 24 sequences of 1000 x 600 took 64 us sorted, 53 us not.
   a.sorted = pq && pk && p->n_seqs < 64 && !c.few && (p->H_k % 8 == 0 || 8 % p->H_k == 0);
+  // Less than a workgroup a CU in the gradient of q: products are cheap then, and what roundings leave does not average out.
+  a.fine = !p->is_f32 && (long long)c.tiles * p->H_k < vda::current_device_cus();
   a.tiles = c.tiles, a.splits = c.splits;
   char* w = static_cast<char*>(work);
   a.part = reinterpret_cast<float*>(w + c.part);

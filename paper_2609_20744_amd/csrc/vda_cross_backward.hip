@@ -20,10 +20,13 @@ namespace {
 // Tiles of states up to which D is summed from p dP in a pass before, in fp32.  As dout out it has
 // the rounding of out, whose part in dS is as large as the others where a few states share
 // the weight: of 4 to 60 states dq and dk were 2.8e-3 of their norm off (bf16), 2.4e-3 with this
-// pass, of 129 on 2.4e-3 without it (130 rows of 4 heads, D = 128, even lengths); it is two
-// products more, 382 us for 369 in a packed batch.  A state that is seen alone leaves dS = 0, not
-// a remainder; in fp32, whose error the rounding does not show in, that is all it is for.
-constexpr int kExactTiles = 2;
+// pass; of 200 states 2.5e-3 and 2.4e-3, of 500 and more 2.4e-3 without it (D = 128, even lengths).
+// It is two products more where a sequence is so short.  A
+// state that is seen alone leaves dS = 0, not a remainder; in fp32, whose error the rounding
+// does not show in, that is all the pass is for.
+// Where the rows do not fill the device either (`fine`), p and dS of such sequences enter their
+// products in two parts, rounded and rest: 1.7e-3, the results' own rounding.
+constexpr int kExactTiles = 4;
 
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossArgs a) {
@@ -143,6 +146,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
     dot = count == 1 ? one : sum;
     dot += other_half(dot);
   }
+  const bool fine = a.fine && tiles <= kExactTiles;
   floatx16 dq[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dq[e] = floatx16{};
@@ -164,6 +168,12 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 #pragma unroll
         for (int e = 0; e < D / 32; ++e)
           dq[e] = Fr::mma(Tile::col_frag(kt + (32 * b + 16 * h) * Tile::kRow, e, here), x, dq[e]);
+        if (!F32 && fine) {
+          const typename Fr::X y = Fr::rest(p, h);
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e)
+            dq[e] = Fr::mma(Tile::col_frag(kt + (32 * b + 16 * h) * Tile::kRow, e, here), y, dq[e]);
+        }
       }
     }
   };
@@ -260,6 +270,7 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 
           make_uint4(0u, 0u, 0u, 0u);
   }
   lds_barrier();  // the first tile is copied over k
+  const bool fine = a.fine && s.seen <= kExactTiles * kCrossTile;
   floatx16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) dk[e] = floatx16{}, dv[e] = floatx16{};
@@ -316,6 +327,14 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 
       for (int e = 0; e < D / 32; ++e) {
         dv[e] = Fr::mma(Tile::col_frag(gt + h32 + 16 * h * Tile::kRow, e, here), x, dv[e]);
         dk[e] = Fr::mma(Tile::col_frag(qt + h32 + 16 * h * Tile::kRow, e, here), y, dk[e]);
+      }
+      if (!F32 && fine) {
+        const typename Fr::X z = Fr::rest(p, h), w = Fr::rest(dp, h);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          dv[e] = Fr::mma(Tile::col_frag(gt + h32 + 16 * h * Tile::kRow, e, here), z, dv[e]);
+          dk[e] = Fr::mma(Tile::col_frag(qt + h32 + 16 * h * Tile::kRow, e, here), w, dk[e]);
+        }
       }
     }
   };
