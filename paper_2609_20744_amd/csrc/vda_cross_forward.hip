@@ -11,8 +11,7 @@
 // more than 2^8 only: p stays below 2^8 then, where a rounding to bf16 is as good.
 //
 // Many rows: a wave has 32 rows, the four waves of a workgroup share the states'
-// tiles.  Few rows (a step, learned queries): a wave by itself, bound by the copies that it
-// has on the way.
+// tiles.  Few rows (a step): a wave by itself, bound by the copies that it has on the way.
 // Where workgroups would not fill the device, each takes a range of the states
 // and the join kernel adds their parts.
 #include "vda_cross.h"
@@ -115,6 +114,15 @@ __device__ __forceinline__ void put_rows(const CrossArgs& a, const Row& row, con
   if (lane < 32) put.stats();
 }
 
+// Many rows: 128 of them, 32 a wave, and tiles of 64 states in two places of LDS, the next one
+// copied while one is used.  q and the output go through LDS too, so that memory is asked
+// for whole rows (with 16 bytes of each of 32 rows to an instruction 264 us instead of 251).  Two
+// workgroups a CU: 237 registers a wave.  Bound by the products and the exponentials beside
+// them, in sequences of few tiles by memory too, which is hardly overlapped: 32760 x 4096 of 24
+// heads, D = 128, 1086 TFLOP/s (8192^3 by the library: 1115), 32760 x 512 247 us, 835 TFLOP/s, of
+// which about 80 us are q and the output; fp32 108 to 115 TFLOP/s (139).  Several tiles of rows
+// a workgroup, without or with q loaded ahead, and first workgroups that start at other times
+// changed nothing or spilled.
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(CrossArgs a) {
   typedef Frag<F32> Fr;
@@ -195,7 +203,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
 
 // Few rows: a wave with 32 rows takes tiles of 32 states through two places in LDS, one on
 // the way while the other is used, with no barrier.  WAVES of them share a workgroup's
-// rows, take a part of its range each and add their parts behind a barrier.
+// rows, take a part of its range each and add their parts behind a barrier.  Bound by
+// the states' bytes: 96 sequences of 8 key heads and 1130 states in the mean, D = 128, 76 us, 300 MB
+// at 3.95 TB/s (two waves that share a place and a barrier 83 us, four places of one wave 98).
 constexpr int kFewStates = 32;
 
 template <bool F32, int D, bool MASKED, int WAVES>
@@ -313,7 +323,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void cross_few_kernel(CrossArgs a) {
 }
 
 // Adds the parts of a row's splits: a wave per row, whose lanes have a split's maximum
-// and sum each, and then four channels of every 256 / D-th split; the order is fixed.
+// and sum each, and then four channels of every 256 / D-th split; the order is fixed.  A
+// launch and two waits for memory: 5 us for 2048 rows of 16 splits, D = 64 (a thread per
+// four channels 8 us).
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads) void cross_join_kernel(CrossArgs a) {
   constexpr int LANES = D / 4, SIDE = 64 / LANES;  // splits side by side

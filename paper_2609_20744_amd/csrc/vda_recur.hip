@@ -205,7 +205,8 @@ __device__ __forceinline__ void get_states(const RunStates& t, int run, float (&
   }
 }
 
-// What a segment does: a run has an equal share of its tokens, kBatch at a time.
+// What a segment does: a run has an equal share of its tokens, kBatch at a time.  40320 tokens of
+// 896 channels, log decays in fp32: 50 us, 217 MB at 4.3 TB/s.
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_segment_kernel(RecurArgs a) {
   constexpr int N = F32 || GATE == VDA_GATE_LOG ? 4 : 8;
@@ -249,6 +250,8 @@ __global__ __launch_bounds__(kThreads) void recur_segment_kernel(RecurArgs a) {
   a.A[to] = X, a.H[to] = Y;
 }
 
+// The outputs: what enters the segment from all before it, then tile after tile.  As above 49 us,
+// 289 MB at 5.9 TB/s, some of it from the last-level cache.
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
   constexpr int N = 4, kTile = kRecurRuns * N;
@@ -325,7 +328,8 @@ __global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
   if (a.S_out != nullptr && r.tile == r.last && real) a.S_out[(size_t)r.seq * a.C + chan] = h;
 }
 
-// What every tile of 64 tokens does, in both directions.
+// What every tile of 64 tokens does, in both directions.  9 sequences of 16401 tokens, 2048 channels:
+// 48 us, 202 MB at 4.2 TB/s.
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_reduce_kernel(RecurArgs a) {
   __shared__ __align__(16) RunTable table;
@@ -374,7 +378,8 @@ __global__ __launch_bounds__(kThreads) void recur_reduce_kernel(RecurArgs a) {
 }
 
 // What enters each tile of a sequence: a lane has a channel, a wave a range of the
-// tiles.  H becomes the state that enters a tile, G the E that enters at its end.
+// tiles.  H becomes the state that enters a tile, G the E that enters at its end.  As above 8 us
+// (with a tile's values kept in registers for the second way 12 us).
 constexpr int kCarryWaves = 16;
 __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs a) {
   __shared__ float sA[kCarryWaves][64], sH[kCarryWaves][64], sG[kCarryWaves][64];
@@ -431,6 +436,8 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
   }
 }
 
+// The gradients of a tile: its states and E again from what enters it.  As above 63 us, 336 MB at
+// 5.3 TB/s; runs of 4 tokens, as with 8 the registers spilled.
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
   constexpr int N = kRecurRun;
@@ -531,7 +538,7 @@ __device__ __forceinline__ floatx4 load4(const uint16_t* p) {
   return floatx4{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
 }
 
-// A lane has four channels of a sequence.
+// A lane has four channels of a sequence.  192 sequences of 2048 channels: 3 us, a launch's latency.
 template <bool F32, int GATE>
 __global__ __launch_bounds__(kThreads) void recur_step_kernel(RecurStepArgs a) {
   const unsigned per = (unsigned)a.C / 4;
