@@ -744,8 +744,8 @@ int vda_rope_backward(const void* dout, const void* x, const float* inv_freq, co
  * undefined, in the backward pass the gradients of its sequence and key head.
  * bf16 storage: products run on bf16 matrix cores with fp32 accumulation, the
  * softmax and its sums are fp32, and its weights (and the scores' gradients) are
- * rounded to bf16 once, where they enter a product.  fp32 storage: fp32
- * throughout.
+ * rounded to bf16 once, where they enter a product; few states of calls that do
+ * not fill the device enter in two parts, 16 bits.  fp32 storage: fp32 throughout.
  */
 typedef struct vda_cross_problem {
   int T, S;

@@ -427,10 +427,10 @@ __device__ __forceinline__ void cross_barrier() {
   __syncthreads();
 }
 
-// A lane's row: where its query, output and lse are.
+// A lane's row: where its query, output and lse are, and its part of a workspace.
 struct Row {
   bool real;
-  size_t q, out, dq, lse, part;
+  size_t q, out, lse, part;
 };
 __device__ __forceinline__ Row row_of(const CrossArgs& a, const CrossSeq& s, int hk, int r) {
   Row w;
@@ -440,7 +440,6 @@ __device__ __forceinline__ Row row_of(const CrossArgs& a, const CrossSeq& s, int
   const int t = r / a.group, h = hk * a.group + r - t * a.group;
   w.q = seq_base(a.sq, a.cu_q, s.q0, s.i) + (size_t)t * a.sq.tok + (size_t)h * a.sq.head;
   w.out = seq_base(a.so, a.cu_q, s.q0, s.i) + (size_t)t * a.so.tok + (size_t)h * a.so.head;
-  w.dq = seq_base(a.sdq, a.cu_q, s.q0, s.i) + (size_t)t * a.sdq.tok + (size_t)h * a.sdq.head;
   w.lse = a.cu_q != nullptr ? (size_t)h * a.T + s.q0 + t : ((size_t)s.i * a.Hq + h) * a.Lq + t;
   w.part = ((a.cu_q != nullptr ? (size_t)s.q0 : (size_t)s.i * a.Lq) + t) * a.Hq + h;
   return w;

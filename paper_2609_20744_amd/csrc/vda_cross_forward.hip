@@ -21,8 +21,9 @@ namespace {
 
 constexpr float kGrow = 8.f;  // in powers of two
 
-// The softmax's part of a tile of 32 NB states, and its product with V.
-template <bool F32, int D, int NB>
+// The softmax's part of a tile of 32 NB states, and its product with V.  FINE: p in two parts,
+// rounded and rest (bf16).
+template <bool F32, int D, int NB, bool FINE>
 __device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, const typename Frag<F32>::X (&q)[D / 16], uint64_t bits,
                                        bool all, float c, floatx16 (&o)[D / 32], float& m, float& l,
                                        const typename CrossTile<F32, D>::Lane& at) {
@@ -74,6 +75,11 @@ __device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, c
       const typename Fr::X p = Fr::of(s[b], t);
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) o[e] = Fr::mma(Tile::col_frag(vt + (32 * b + 16 * t) * Tile::kRow, e, at), p, o[e]);
+      if constexpr (FINE && !F32) {
+        const typename Fr::X y = Fr::rest(s[b], t);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = Fr::mma(Tile::col_frag(vt + (32 * b + 16 * t) * Tile::kRow, e, at), y, o[e]);
+      }
     }
 }
 
@@ -166,7 +172,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
     if (mask != nullptr && ~bits != 0) clear_copied<F32, D, kCrossTile, 4>(bits, wave, lane, vt);
     lds_barrier();
     if (t + 1 < to) copy(t + 1, next_k, next_v);
-    if (bits != 0) attend<F32, D, 2>(kt, vt, q, bits, ~bits == 0, a.c, o, m, l, offs);
+    if (bits != 0) attend<F32, D, 2, false>(kt, vt, q, bits, ~bits == 0, a.c, o, m, l, offs);
   };
   // A wave's part of two tiles' places: its q comes and its output goes through it.
   auto part = [&](lds_char* kt, lds_char* vt) { return (wave < 2 ? kt : vt) + (wave & 1) * 32 * Tile::kRow; };
@@ -203,7 +209,9 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_forward_kernel(Cr
 
 // Few rows: a wave with 32 rows takes tiles of 32 states through two places in LDS, one on
 // the way while the other is used, with no barrier.  WAVES of them share a workgroup's
-// rows, take a part of its range each and add their parts behind a barrier.  Bound by
+// rows, take a part of its range each and add their parts behind a barrier; of the few states
+// that these have p enters the product in two parts (out 1.7e-3 of its norm off instead of
+// 2.3e-3, 11.7 and 11.8 us for 512 states of 16 heads; of the long ones it would be 78 us for 76).  Bound by
 // the states' bytes: 96 sequences of 8 key heads and 1130 states in the mean, D = 128, 76 us, 300 MB
 // at 3.95 TB/s (two waves that share a place and a barrier 83 us, four places of one wave 98).
 constexpr int kFewStates = 32;
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void cross_few_kernel(CrossArgs a) {
     const bool all = bits == 0xffffffffull;
     if (bits != 0) {
       if (MASKED && !all) clear_copied<F32, D, kFewStates, 1>(bits, 0, lane, vt);
-      attend<F32, D, 1>(kt, vt, q, bits, all, a.c, o, m, l, offs);
+      attend<F32, D, 1, (WAVES > 1)>(kt, vt, q, bits, all, a.c, o, m, l, offs);
     }
     __builtin_amdgcn_sched_barrier(0);
   };

@@ -500,3 +500,18 @@ def test_refusals_of_the_binding(V):
         V.cross_step(q, k, v, slots=torch.zeros(3, dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError):
         V.cross_step(torch.cat([q, q]), k, v)  # four sequences, two slots
+
+
+@pytest.mark.parametrize("S", [2, 30, 256])
+def test_steps_over_few_states_keep_their_norm(V, S):
+    """Weights in two parts leave the output's own rounding: 0.0017 of its norm (as above), and of a sum over thousands of
+    values no more than a tenth beyond."""
+    import torch
+    rng = np.random.default_rng(S)
+    q, k, v = (torch.from_numpy(rng.standard_normal((2, n, 4, 128))).bfloat16() for n in (2, S, S))
+    got = from_device(V.cross_step(q.cuda(), k.cuda(), v.cuda()))
+    off = total = 0.0
+    for i in range(2):
+        want = X.cross_sequence(*(x[i].double().numpy() for x in (q, k, v)), np.ones(S, bool), 128 ** -0.5)[0]
+        off, total = off + np.sum((got[i] - want) ** 2), total + np.sum(want ** 2)
+    assert np.sqrt(off / total) < 0.0019
