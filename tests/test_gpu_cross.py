@@ -234,6 +234,23 @@ def test_gradients_of_few_states_keep_their_norm(V, lk):
     assert (np.sqrt(off[:, 0] / off[:, 1]) < 0.0026).all(), np.sqrt(off[:, 0] / off[:, 1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lq, lk, lens", [([70, 3, 0, 200], [90] * 4, [90, 1, 40, 65]), ([2, 9, 0, 5], [300] * 4, [0, 300, 7, 150]),
+                                          ([130] * 3, [200, 0, 61], None), ([4] * 3, [700, 1, 33], None)])
+def test_packed_on_one_side(V, lq, lk, lens, dtype):
+    """Packed queries and padded states, and the other way round."""
+    c = Case(lq=lq, lk=lk, Hq=4, Hk=2, d=64, lens=lens, mask="holes", packed=True, dtype=dtype)
+    d, o = c.dev, c.options()
+    if len(set(lk)) == 1:
+        del o["cu_k"]
+        d["k"], d["v"], o["k_mask"] = (x.unflatten(0, (len(lk), -1)) for x in (d["k"], d["v"], o["k_mask"]))
+    else:
+        del o["cu_q"]
+        d["q"], d["dout"] = (x.unflatten(0, (len(lq), -1)) for x in (d["q"], d["dout"]))
+    out, lse = V.cross_forward(d["q"], d["k"], d["v"], return_lse=True, **o)
+    c.check(out, lse, V.cross_backward(d["dout"], d["q"], d["k"], d["v"], out, lse, **o))
+
+
 def test_rows_outside_sequences_are_left(V):
     import torch
     c = Case(lq=[5, 40], lk=[70, 3], lead=4, tail=6, Hq=2, Hk=1)
