@@ -28,7 +28,7 @@ using Lds = __attribute__((address_space(3))) T;
 typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
 typedef __attribute__((address_space(1))) const void global_void;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kCrossTile = 64;   // states (or rows) of a tile in LDS
 constexpr int kCrossRows = 128;  // rows (or states) of a workgroup, 32 a wave
 constexpr int kFewRows = 32;     // rows of a workgroup whose waves share them
@@ -49,7 +49,7 @@ struct CrossArgs {
   int n, n_slots, T, S, Lq, Lk;
   int Hq, Hk, group;
   uint32_t group_magic;  // x / group = x * group_magic >> 24 for x < group + 64
-  float scale, c;        // c = |scale| log2 e, above 0
+  float scale, c, s;     // c = |scale| log2 e, s = |scale|, above 0
   int fine;              // backward, bf16: two parts of what a short sequence's products take
   int sorted;            // tiles of packed sequences in the order of what they have to do
   int near;              // a tile's rows are within 2^31 bytes of its first, whichever their heads

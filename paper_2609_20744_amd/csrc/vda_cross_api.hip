@@ -164,7 +164,7 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.group_magic = (uint32_t)(((1u << 24) + a.group - 1) / a.group);
   a.scale = p->scale, a.flip = p->scale < 0.f;
   // Above 0, so that a score of -inf has no weight; a scale of 0 is 1e-37, below what fp32 tells from it.
-  a.c = std::max((a.flip ? -p->scale : p->scale) * vda::kLog2e, 1e-37f);
+  a.s = std::max(a.flip ? -p->scale : p->scale, 1e-37f), a.c = std::max(a.s * vda::kLog2e, 1e-37f);
   auto near = [&](const CrossStrides& s) { return (64 * s.tok + a.group * s.head) * (p->is_f32 ? 4 : 2) < (size_t)1 << 31; };
   a.near = near(a.sq) && near(a.so);
   // With heads that share out evenly over the 8 XCDs: of 5 heads, 24 sequences of 1000 x 600 took 64 us sorted, 53 us not.

@@ -17,6 +17,13 @@
 namespace vda {
 namespace {
 
+// A score's weight.  lse in powers of two; in fp32 as it is kept, as its rounding in other units would
+// be one more in every weight of a row (dk and dv of 60000 states: 9e-7 of their norm off).
+template <bool F32>
+__device__ __forceinline__ float weight_of(const CrossArgs& a, float score, float lse) {
+  return __builtin_amdgcn_exp2f(F32 ? fmaf(score, a.s, -lse) * kLog2e : fmaf(score, a.c, -lse));
+}
+
 // Tiles of states up to which D is summed from p dP in a pass before, in fp32.  As dout out it has
 // the rounding of out, whose part in dS is as large as the others where a few states share
 // the weight: of 4 to 60 states dq and dk were 2.8e-3 of their norm off (bf16), 2.4e-3 with this
@@ -61,7 +68,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   auto part = [&](lds_char* kt, lds_char* vt) { return (wave < 2 ? kt : vt) + (wave & 1) * 32 * Tile::kRow; };
   const typename Tile::Lane offs = Tile::lane_of(lane);
   typename Fr::X q[D / 16], g[D / 16];
-  float dot = 0.f, lse = a.lse_in[row_of(a, s, hk, w0 + (lane & 31)).lse] * kLog2e;
+  float dot = 0.f, lse = a.lse_in[row_of(a, s, hk, w0 + (lane & 31)).lse] * (F32 ? 1.f : kLog2e);
   {
     lds_char* const q_part = part((lds_char*)k1, (lds_char*)v1);
     lds_char* const g_part = part((lds_char*)k0, (lds_char*)v0);
@@ -125,7 +132,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
       dp = Fr::mma(Tile::row_frag(vt + 32 * b * Tile::kRow, e, here), g[e], dp);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse));
+    for (int i = 0; i < 16; ++i) p[i] = weight_of<F32>(a, p[i], lse);
   };
   int count = 0;  // of states that are seen
   if (tiles <= kExactTiles)
@@ -315,14 +322,14 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 
     }
     if (!all)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = seen ? p[i] : -INFINITY;  // a.c > 0: no weight
+      for (int i = 0; i < 16; ++i) p[i] = seen ? p[i] : -INFINITY;  // no weight
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const floatx4 z = *reinterpret_cast<const floatx4*>(lse + 32 * half + 8 * i + 4 * (lane >> 5));
       const floatx4 y = *reinterpret_cast<const floatx4*>(dot + 32 * half + 8 * i + 4 * (lane >> 5));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(p[4 * i + e], a.c, -z[e]));
+        const float x = weight_of<F32>(a, p[4 * i + e], z[e]);
         p[4 * i + e] = x;
         dp[4 * i + e] = x * (dp[4 * i + e] - y[e]);
       }

@@ -83,7 +83,12 @@ __device__ __forceinline__ void attend(const lds_char* kt, const lds_char* vt, c
     }
 }
 
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2; }
+// In 64 bits, the sum's power of two apart: rounded once, where it is stored.
+__device__ __forceinline__ float lse_of(float m, float l) {
+  if (l == 0.f) return -INFINITY;
+  const double power = (double)m + __builtin_amdgcn_frexp_expf(l);
+  return (float)((power + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l))) * 0.69314718055994530942);
+}
 
 // Where a lane's row goes: to the output, or (not divided by the sum) to its split's part.
 template <bool F32, int D>
