@@ -133,8 +133,10 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     // sequences of uneven length even out (16401 rows over 9 sequences 386 us, 410 us with one a
     // CU, 420 us with six), of 512 rows at least, as each range's sums are written and added up.
     const long long each = groups < cus ? (rows + cus / groups - 1) / (cus / groups) : std::max(512LL, rows * groups / (3 * cus));
-    c.range = (int)((std::max(each, 1LL) + 63) / 64 * 64);
-    c.splits_k = (int)std::min(8LL, (most + c.range - 1) / c.range);
+    // No longer than the rows that there are, so that a range is an int where they are.
+    const long long range = (std::clamp(each, 1LL, std::max(most, 1LL)) + 63) / 64 * 64;
+    c.range = (int)range;
+    c.splits_k = (int)std::clamp((most + range - 1) / range, 1LL, 8LL);
     c.stats = take(q_rows * 8);
     c.counts = take((size_t)p->S * 4);
     const size_t a = c.splits > 1 ? c.splits * q_rows * p->d * 4 : 0;

@@ -246,7 +246,7 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 
 
   // The sequence's rows in ranges of about a.range, this workgroup's in tiles; none where no state is seen.
   const int rows = s.lq * a.group;
-  int ranges = (rows + a.range - 1) / a.range;
+  int ranges = (int)(((unsigned)rows + (unsigned)a.range - 1u) / (unsigned)a.range);
   ranges = ranges < 1 ? 1 : ranges > a.splits ? a.splits : ranges;
   if ((int)blockIdx.y >= ranges) return;
   const int tiles = j0 < s.seen ? (rows + kRows - 1) / kRows : 0, per = (tiles + ranges - 1) / ranges;
