@@ -538,6 +538,9 @@ __device__ __forceinline__ void store_states(void* to, size_t row_bytes, int row
 // Waves of a workgroup of few rows that share its range of the states; their tiles have to fit LDS.
 constexpr int few_waves(bool f32, int d) { return f32 && d == 128 ? 2 : 4; }
 
+// Waves of a workgroup of the gradients of k and v.
+constexpr int dkv_waves(bool f32) { return f32 ? 4 : 8; }
+
 // few: waves of a workgroup of few rows, 1 or few_waves(); 0: many rows
 hipError_t launch_cross_forward(bool f32, int d, int few, const CrossArgs& a, hipStream_t stream);
 hipError_t launch_cross_join(bool f32, int d, const CrossArgs& a, hipStream_t stream);

@@ -43,11 +43,13 @@ int check_problem(const vda_cross_problem* p, int n_slots, bool backward) {
   if (group > 1024) return VDA_ERR_UNSUPPORTED;
   const size_t es = p->is_f32 ? 4 : 2;
   const long long row_q = (long long)p->H_q * p->d, row_k = (long long)p->H_k * p->d;
-  // Rows and tiles are counted in 32 bits; a launch has 256 threads a tile (four lanes' channels a row).
+  // Rows and tiles are counted in 32 bits; a launch has 256 threads a tile, those of dkv_waves() a tile
+  // of states backward, and a thread for four channels of a row.
+  const long long threads_k = 64 * vda::dkv_waves(p->is_f32 != 0);
   const long long rows = (long long)p->T * group;
   if (rows + 256 > kMaxInt || (long long)p->S + 256 > kMaxInt || row_q * (long long)es >= 1 << 24) return VDA_ERR_SIZE;
   if ((rows / 32 + p->n_seqs + 1) * p->H_k + 8 > kMaxThreads / 256 ||
-      ((long long)p->S / 128 + p->n_seqs + 1) * p->H_k + 8 > kMaxThreads / 256 ||
+      ((long long)p->S / 128 + p->n_seqs + 1) * p->H_k + 8 > kMaxThreads / (backward ? threads_k : 256) ||
       ((long long)p->T * p->H_q + 64) * (p->d / 4) > kMaxThreads || ((long long)p->S * p->H_k + 64) * (p->d / 4) > kMaxThreads)
     return VDA_ERR_SIZE;
   for (int st : {check_stride(p->q_row_stride, p->layout, row_q, es), check_stride(p->k_row_stride, p->kv_layout, row_k, es),

@@ -224,7 +224,7 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 // where 4096 x 4096 of 16 heads, 4 sequences, keeps 1000 TFLOP/s of both kernels' products.
 template <bool F32>
 struct DkvShape {
-  static constexpr int kHalves = F32 ? 1 : 2, kWaves = 4 * kHalves, kRows = 32 * kHalves;  // rows of a tile
+  static constexpr int kWaves = dkv_waves(F32), kHalves = kWaves / 4, kRows = 32 * kHalves;  // rows of a tile
 };
 
 template <bool F32, int D>

@@ -42,3 +42,16 @@ def test_cross_rows_of_large_problems_are_one_range(T, S, H, packed, is_f32):
     up = lambda x: (x + 255) // 256 * 256
     assert vda.lib.vda_cross_backward_workspace(ctypes.byref(p)) == up(T * H * 8) + up(S * 4)
     assert _backward(p) == OVERLAP
+
+
+@pytest.mark.parametrize("is_f32,threads", [(0, 512), (1, 256)])
+@pytest.mark.parametrize("packed", [False, True])
+def test_cross_backward_workgroups_fit_a_launch(packed, is_f32, threads):
+    """The gradients of k and v take a workgroup for 128 states, of 512 threads in bf16 storage; a launch holds 2^32 - 1."""
+    most = (2 ** 32 - 1) // threads
+    for n, st in (((most - 16) // 2, OVERLAP), (most + 16, SIZE), (9 << 20, SIZE if is_f32 == 0 else OVERLAP), (most * 2, SIZE)):
+        p = _cross(n, n, n_seqs=n, is_f32=is_f32, cu_q=30 * BIG if packed else None, cu_k=31 * BIG if packed else None)
+        assert _backward(p) == st, n
+        assert (vda.lib.vda_cross_backward_workspace(ctypes.byref(p)) > 0) == (st == OVERLAP)
+    p = _cross(9 << 20, 9 << 20, n_seqs=9 << 20)
+    assert vda.lib.vda_cross_forward(ctypes.byref(p), BIG, 2 * BIG, 3 * BIG, BIG, None, None, None) == OVERLAP  # allowed: 256 threads
