@@ -841,7 +841,9 @@ typedef enum {
  * h_0, the tokens in order give
  *     h_t = a_t h_{t-1} + u_t,   out_t = h_t.
  *  - T, n_seqs, cu_seqlens: as in vda_delta_problem.
- *  - C >= 1 channels, a multiple of 8 (VDA_ERR_UNSUPPORTED).
+ *  - C >= 1 channels, a multiple of 8 (VDA_ERR_UNSUPPORTED), at most 8388480; in the
+ *    backward pass 4194240, but where all sequences are of equal length and that is
+ *    at most 64 tokens, or T is (VDA_ERR_SIZE).
  *  - gate: a vda_gate.
  *  - reverse: the tokens are taken from the last to the first (the states are then
  *    those behind the first token).

@@ -18,13 +18,14 @@ using vda::RecurArgs;
 using vda::round_up;
 
 constexpr long long kMaxThreads = 0xffffffffLL;  // of a launch
+constexpr int kMaxGridY = 65535;
 
 size_t gate_size(int gate, int is_f32) { return is_f32 || gate == VDA_GATE_LOG ? 4 : 2; }
 
 int check_channels(int C, int gate) {
   if (C < 1) return VDA_ERR_SIZE;
   if (C % 8 || (gate != VDA_GATE_LOG && gate != VDA_GATE_LOGIT && gate != VDA_GATE_NORM)) return VDA_ERR_UNSUPPORTED;
-  return C > 128 * 65535 ? VDA_ERR_SIZE : VDA_OK;
+  return C > 128 * kMaxGridY ? VDA_ERR_SIZE : VDA_OK;
 }
 
 // Tokens of a part of a sequence: a tile backward; forward a segment, so long that about
@@ -42,6 +43,8 @@ long long parts_of(const vda_recur_problem* p, int part) {
   const long long n = p->n_seqs, T = p->T;
   return p->cu_seqlens ? T / part + n : n * ((T / n + part - 1) / part);
 }
+
+bool carried(const vda_recur_problem* p, int part) { return (p->cu_seqlens ? p->T : p->T / p->n_seqs) > part; }
 
 int check_stride(int stride, int C, size_t es) {
   if (stride != 0 && stride < C) return VDA_ERR_SIZE;
@@ -66,10 +69,10 @@ int check_problem(const vda_recur_problem* p, bool backward) {
   if (parts_of(p, vda::kRecurTile) * slabs > kMaxThreads / 256 || (long long)p->n_seqs * 1024 > kMaxThreads ||
       (long long)p->T + vda::kRecurTile > 0x7fffffffLL)
     return VDA_ERR_SIZE;
+  // Backward, the kernel that carries states from tile to tile has 64 channels a workgroup in the grid's y.
+  if (backward && carried(p, vda::kRecurTile) && ((long long)p->C + 63) / 64 > kMaxGridY) return VDA_ERR_SIZE;
   return VDA_OK;
 }
-
-bool carried(const vda_recur_problem* p, int part) { return (p->cu_seqlens ? p->T : p->T / p->n_seqs) > part; }
 
 size_t workspace(const vda_recur_problem* p, bool backward) {
   const int part = part_of(p, backward);

@@ -55,3 +55,27 @@ def test_cross_backward_workgroups_fit_a_launch(packed, is_f32, threads):
         assert (vda.lib.vda_cross_backward_workspace(ctypes.byref(p)) > 0) == (st == OVERLAP)
     p = _cross(9 << 20, 9 << 20, n_seqs=9 << 20)
     assert vda.lib.vda_cross_forward(ctypes.byref(p), BIG, 2 * BIG, 3 * BIG, BIG, None, None, None) == OVERLAP  # allowed: 256 threads
+
+
+def _recur(T, C, n_seqs=1, cu=None):
+    return vda.VdaRecurProblem(T, n_seqs, cu, C, 1, 0, 0, 0, 0, 0, 0)
+
+
+def _recur_backward(problem):
+    """Refused for dx's place at the latest, which is that of x."""
+    x = 2 * BIG
+    return vda.lib.vda_recur_backward(ctypes.byref(problem), BIG, x, 3 * BIG, None, None, x, 4 * BIG, None, 5 * BIG, None)
+
+
+def test_recur_channels_fit_a_launch():
+    """What enters each tile is found by a workgroup for 64 channels of a sequence, the channels along the grid's second
+    dimension, of 65535 at most; a sequence of one tile (64 tokens) does without."""
+    most = 64 * 65535
+    for T, C, n, cu, st in ((65, most, 1, None, OVERLAP), (65, most + 8, 1, None, SIZE), (65, most + 64, 1, None, SIZE),
+                            (65, 128 * 65535, 1, None, SIZE), (64, most + 64, 1, None, OVERLAP), (128, most + 64, 2, None, OVERLAP),
+                            (128, most + 64, 2, 9 * BIG, SIZE), (130, most + 64, 2, None, SIZE), (64, 128 * 65535, 1, None, OVERLAP)):
+        p = _recur(T, C, n, cu)
+        assert _recur_backward(p) == st, (T, C, n, cu)
+        assert (vda.lib.vda_recur_backward_workspace(ctypes.byref(p)) > 0) == (st == OVERLAP and C <= most)
+    p = _recur(1000, 128 * 65535)
+    assert vda.lib.vda_recur_forward(ctypes.byref(p), BIG, 2 * BIG, None, BIG, None, 5 * BIG, None) == OVERLAP
