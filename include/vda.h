@@ -741,7 +741,8 @@ int vda_rope_backward(const void* dout, const void* x, const float* inv_freq, co
  *    lse is fp32, the natural logarithm: [H_q][T] with cu_q, else
  *    [n_seqs][H_q][T / n_seqs].
  * A NaN or infinity in q, or in a state that is seen, makes the rows that meet it
- * undefined, in the backward pass the gradients of its sequence and key head.
+ * undefined; in the backward pass, as one in dout, the gradients of its sequence
+ * and key head, but of states that are not seen (0, whatever q and dout hold).
  * bf16 storage: products run on bf16 matrix cores with fp32 accumulation, the
  * softmax and its sums are fp32, and its weights (and the scores' gradients) are
  * rounded to bf16 once, where they enter a product; few states of calls that do

@@ -397,6 +397,9 @@ __global__ __launch_bounds__((64 * DkvShape<F32>::kWaves), (F32 ? 1 : D == 32 ? 
   }
   const int count = s.lk - w0;  // the wave's states
   if (count <= 0) return;
+  if (!seen)  // a weight of 0 is not enough where a query or its gradient is not finite
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) dk[e] = dv[e] = floatx16{};
   if (ranges > 1) {
     const size_t first = (a.cu_k != nullptr ? (size_t)s.k0 : (size_t)s.kv * a.Lk) + w0;
     const size_t part = ((size_t)blockIdx.y * ((size_t)a.S * a.Hk) + first * a.Hk + hk) * D;
