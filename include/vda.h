@@ -793,9 +793,11 @@ size_t vda_cross_forward_workspace(const vda_cross_problem* p);
  * dk and dv are summed over the query heads that share a key head, and 0 for
  * states that are not seen.  dk and dv may be slices of one fused gradient
  * (equal row strides).  A score's gradient is p_j (dout . v_j - D), D = sum_j p_j
- * dout . v_j: summed so for sequences of up to 256 states (fp32 storage: where one
- * of them is seen; dq and dk are 0 then), and else taken from the stored out, as
- * dout . out.  Otherwise as vda_cross_forward.
+ * dout . v_j: summed so where at most 64 of a sequence's states are seen, or where
+ * those that are seen stand in at most four of its groups of 64 (so in all sequences
+ * of up to 256 states; fp32 storage: only where one state is seen), and else taken
+ * from the stored out, as dout . out.  Of a state that is seen alone, dq and dk are
+ * 0.  Otherwise as vda_cross_forward.
  */
 int vda_cross_backward(const vda_cross_problem* p, const void* dout, const void* q, const void* k,
                        const void* v, const void* out, const float* lse, void* dq, void* dk,

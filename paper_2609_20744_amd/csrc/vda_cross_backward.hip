@@ -24,17 +24,18 @@ __device__ __forceinline__ float weight_of(const CrossArgs& a, float score, floa
   return __builtin_amdgcn_exp2f(F32 ? fmaf(score, a.s, -lse) * kLog2e : fmaf(score, a.c, -lse));
 }
 
-// Tiles of states up to which D is summed from p dP in a pass before, in fp32.  As dout out it has
+// D is summed from p dP in a pass before, in fp32, where at most kExactTiles tiles have a state that is
+// seen, and of at most kExactStates wherever a mask leaves them.  As dout out it has
 // the rounding of out, whose part in dS is as large as the others where a few states share
 // the weight: of 4 to 60 states dq and dk were 2.8e-3 of their norm off (bf16), 2.4e-3 with this
 // pass; of 200 states 2.5e-3 and 2.4e-3, of 500 and more 2.4e-3 without it (D = 128, even lengths).
 // It is two products more: 1560 rows x 128 states of 24 heads 42 -> 47 us, 32760 x 226 488 -> 592 us
 // for the whole backward pass.  A state that is seen alone leaves dS = 0, not a remainder; in fp32,
 // whose error the rounding does not show in, that is all the pass is for.
-// Where the rows do not fill the device either (`fine`), p and dS of such sequences enter their
-// products in two parts, rounded and rest: 1.7e-3, the results' own rounding (300 rows x 77 states
-// of 16 heads 30 -> 32 us, 2 x 500 x 200 54 -> 58 us).
-constexpr int kExactTiles = 4;
+// Where the rows do not fill the device either (`fine`), p and dS of sequences of up to kExactTiles
+// tiles enter their products in two parts, rounded and rest: 1.7e-3, the results' own rounding (300
+// rows x 77 states of 16 heads 30 -> 32 us, 2 x 500 x 200 54 -> 58 us).
+constexpr int kExactTiles = 4, kExactStates = 64;
 
 // dq: as the forward kernel, with dP beside the scores.  9 uneven sequences of 16401 tokens, 4607
 // states and 8 key heads of 2, D = 128: 148 us, 630 TFLOP/s of its three products; fp32, 2 x 333
@@ -69,6 +70,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
   const typename Tile::Lane offs = Tile::lane_of(lane);
   typename Fr::X q[D / 16], g[D / 16];
   float dot = 0.f, lse = a.lse_in[row_of(a, s, hk, w0 + (lane & 31)).lse] * (F32 ? 1.f : kLog2e);
+  // States that are seen, and tiles that have some: of a mask counted until D is not summed from the weights.
+  constexpr int kAtOnce = 8;
+  int count = s.seen, used = tiles;
+  auto summed = [&] { return F32 ? count <= 1 : count <= kExactStates || used <= kExactTiles; };
   {
     lds_char* const q_part = part((lds_char*)k1, (lds_char*)v1);
     lds_char* const g_part = part((lds_char*)k0, (lds_char*)v0);
@@ -79,6 +84,17 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
     copy_rows<F32, D, 32, 1>(a, (const char*)a.dout + ob * Tile::kEs, a.so, r, rows - 1 - r, g_part, 0, lane);
     u32x4 o[32 * Tile::kPieces / 64];
     load_rows<F32, D>(a, (const char*)a.o + ob * Tile::kEs, a.so, r, rows - 1 - r, o, lane);
+    if (mask != nullptr) count = used = 0;
+    for (int t = 0; mask != nullptr && t < tiles && summed(); t += kAtOnce) {
+      uint8_t bytes[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) bytes[u] = mask[min((t + u) * kCrossTile + lane, s.seen - 1)];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const uint64_t bits = seen_bits(s.seen - (t + u) * kCrossTile, true, bytes[u], lane);
+        count += __popcll(bits), used += bits != 0;
+      }
+    }
     copies_landed();
 #pragma unroll
     for (int e = 0; e < D / 16; ++e) {
@@ -134,16 +150,13 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 #pragma unroll
     for (int i = 0; i < 16; ++i) p[i] = weight_of<F32>(a, p[i], lse);
   };
-  int count = 0;  // of states that are seen
-  if (tiles <= kExactTiles)
-    for (int t = 0; t < tiles; ++t) {
-      const int first = t * kCrossTile, last = s.seen - 1 - first;
-      if (mask != nullptr) byte = mask[first + (lane < last ? lane : last)];
-      count += __popcll(seen_bits(last + 1, mask != nullptr, byte, lane));
-    }
-  if (from < to && (F32 ? count == 1 : count > 0)) {
+  if (from < to && count > 0 && summed()) {
     float sum = 0.f, one = 0.f;
     for (int t = 0; t < tiles; ++t) {
+      if (mask != nullptr) {
+        const int first = t * kCrossTile;
+        if (seen_bits(s.seen - first, true, mask[min(first + lane, s.seen - 1)], lane) == 0) continue;
+      }
       copy(t, (lds_char*)k0, (lds_char*)v0);
       const uint64_t bits = arrived(t, (lds_char*)k0, (lds_char*)v0);
       for (int b = 0; b < 2; ++b) {
