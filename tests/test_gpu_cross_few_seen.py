@@ -63,7 +63,7 @@ def test_gradients_of_few_seen_states_keep_their_norm(V, lk, seen):
     """What roundings leave of a gradient's norm.  One to bf16 is off by 2^-8 of a value's power of two at most, evenly, so by
     2^-8 / sqrt(3) of that in the root mean square, and that is 0.73 of the values' own: 0.0017 of a vector's norm.  dq and
     dk have two (score gradients, result), dv two (weights, result): 0.0017 sqrt(2) = 0.0024, and of a sum over thousands of
-    values no more than a tenth beyond.  D taken from a rounded output would be a third, 0.0029."""
+    values no more than a tenth beyond.  D taken from a rounded output would be a third, larger the fewer share the weight."""
     c = Case(lq=[130] * 4, lk=[lk] * 4, Hq=4, Hk=4, d=128, spread=1.5)
     rng = np.random.default_rng(seen)
     out, lse, grads = _run(V, _see(c, np.concatenate([a + rng.permutation(lk)[:seen] for a in c.ck[:-1]])))
