@@ -932,6 +932,12 @@ def _like(t, name, shape, dtype, dev):
         raise ValueError(f"{name} shape {tuple(t.shape)} must be {tuple(shape)}")
 
 
+def _sizes32(*sizes):
+    """As _int32, of several sizes at once."""
+    if max(sizes) >= 1 << 31:
+        raise ValueError(f"sizes {sizes} do not fit 32 bits")
+
+
 def _row_stride(t, name, inner):
     """Elements between the token rows of a [..., L, `inner` dimensions] tensor, 0 where it is
     contiguous; the rows may be slices, the same stride apart over the batch and tokens."""
@@ -1002,8 +1008,7 @@ def _cross_problem(q, k, v, cu_q, cu_k, k_lens, k_mask, layout, kv_layout, out_l
     if k_mask is not None:
         _expect(k_mask, "k_mask", lead_k + (S,), torch.bool, dev)
     T, total = (L if cu_q is not None else n * L), (S if cu_k is not None else n * S)
-    for name, x in (("tokens", T), ("states", total)):
-        _int32(name, x)
+    _sizes32(T, total, n, H_q, H_k, d)
     shape = lead_q + ((H_q, L, d) if out_layout == "heads" else (L, H_q, d))
     lse = (H_q, T) if cu_q is not None else lead_q + (H_q, L)
     p = VdaCrossProblem(T, total, n, _ptr(cu_q), _ptr(cu_k), _ptr(k_lens), _ptr(k_mask), H_q, H_k, d,
@@ -1114,7 +1119,8 @@ def _cross_step_problem(q, k, v, k_lens, k_mask, slots, kv_layout, scale):
         _expect(k_mask, "k_mask", (m, S), torch.bool, dev)
     if slots is not None:
         _expect(slots, "slots", (n,), torch.int32, dev)
-    p = VdaCrossProblem(_int32("tokens", n * t), _int32("states", m * S), n, None, None, _ptr(k_lens),
+    _sizes32(n * t, m * S, n, m, H_q, H_k, d)
+    p = VdaCrossProblem(n * t, m * S, n, None, None, _ptr(k_lens),
                         _ptr(k_mask), H_q, H_k, d, LAYOUTS["tokens"], LAYOUTS[kv_layout],
                         LAYOUTS["tokens"], 0, k_stride, v_stride, 0, 0, 0, int(dt == torch.float32),
                         d ** -0.5 if scale is None else float(scale))
@@ -1172,7 +1178,8 @@ def _recur_problem(x, g, gate, cu_seqlens, reverse):
     else:
         n, states = math.prod(lead), lead + (C,)
         T = n * L
-    p = VdaRecurProblem(_int32("tokens", T), n, _ptr(cu_seqlens), _int32("channels", C), GATES[gate],
+    _sizes32(T, n, C)
+    p = VdaRecurProblem(T, n, _ptr(cu_seqlens), C, GATES[gate],
                         int(bool(reverse)), _row_stride(x, "x", 1), _row_stride(g, "g", 1), 0, 0,
                         int(dt == torch.float32))
     return p, states, dt, gt, dev
@@ -1265,6 +1272,7 @@ def recur_step(x, g, state, gate="log", slots=None, out=None, stream=None):
         raise ValueError(f"state shape {tuple(state.shape)} must be [n_slots, {C}]")
     if slots is not None:
         _expect(slots, "slots", (n,), torch.int32, dev)
+    _sizes32(n, t, C, state.shape[0])
     if out is None:
         out = _new(x.shape, dt, dev, stream)
     else:
