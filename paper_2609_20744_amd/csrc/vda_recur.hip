@@ -237,7 +237,7 @@ __global__ __launch_bounds__(kThreads) void recur_segment_kernel(RecurArgs a) {
     now = next;
   }
   put_run(table, w.run, A, H);
-  __syncthreads();
+  lds_barrier();
   const int at = threadIdx.x, chan = slab * kRecurChans + at;
   if (at >= kRecurChans || chan >= a.C) return;
   float X = 1.f, Y = 0.f;
@@ -287,9 +287,9 @@ __global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
       for (int e = 0; e < 8; ++e) H[e] = fmaf(x[e], H[e], y[e]), A[e] *= x[e];
     }
     put_run(table, w.run, A, H);
-    __syncthreads();
+    lds_barrier();
     if (carries) h = scan_runs(table, states, h, c);
-    __syncthreads();
+    lds_barrier();
   }
   auto tile = [&](int p0, auto full) {
     const int p = p0 + w.run * N;
@@ -305,9 +305,9 @@ __global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
         A[e] *= al[i][e];
       }
     put_run(table, w.run, A, H);
-    __syncthreads();
+    lds_barrier();
     if (carries) h = scan_runs(table, states, h, c);
-    __syncthreads();
+    lds_barrier();
     get_states(states, w.run, H);
     if (w.real) {
 #pragma unroll
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void recur_reduce_kernel(RecurArgs a) {
   const int c = (threadIdx.x & 15) * 8;
 #pragma unroll
   for (int e = 0; e < 8; e += 4) *reinterpret_cast<floatx4*>(&sG[w.run][c + e]) = floatx4{G[e], G[e + 1], G[e + 2], G[e + 3]};
-  __syncthreads();
+  lds_barrier();
   const int at = threadIdx.x, chan = slab * kRecurChans + at;
   if (at >= kRecurChans || chan >= a.C) return;
   float X = 1.f, Y = 0.f, Z = 0.f;
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
     A *= ta;
   }
   sA[wave][lane] = A, sH[wave][lane] = H, sG[wave][lane] = G;
-  __syncthreads();
+  lds_barrier();
   const size_t st = (size_t)seq * a.C + chan;
   float h = real && a.S_in != nullptr ? a.S_in[st] : 0.f;
   for (int w = 0; w < wave; ++w) h = fmaf(sA[w][lane], h, sH[w][lane]);
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
 #pragma unroll
   for (int e = 0; e < 8; e += 4)
     *reinterpret_cast<floatx4*>(&sG[w.run][(threadIdx.x & 15) * 8 + e]) = floatx4{G[e], G[e + 1], G[e + 2], G[e + 3]};
-  __syncthreads();
+  lds_barrier();
   if (!back) {
     scan_runs(table, states, z, c);
   } else {
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
     }
     if (a.dS_in != nullptr && r.tile == 0 && real) a.dS_in[(size_t)r.seq * a.C + chan] = z;
   }
-  __syncthreads();
+  lds_barrier();
   if (!w.real) return;
   get_states(states, w.run, H);
   get_states(grads, w.run, G);
