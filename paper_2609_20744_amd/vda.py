@@ -932,9 +932,12 @@ def _like(t, name, shape, dtype, dev):
         raise ValueError(f"{name} shape {tuple(t.shape)} must be {tuple(shape)}")
 
 
+_INT_MAX = (1 << 31) - 1
+
+
 def _sizes32(*sizes):
     """As _int32, of several sizes at once."""
-    if max(sizes) >= 1 << 31:
+    if max(sizes) > _INT_MAX:
         raise ValueError(f"sizes {sizes} do not fit 32 bits")
 
 
@@ -1272,13 +1275,15 @@ def recur_step(x, g, state, gate="log", slots=None, out=None, stream=None):
         raise ValueError(f"state shape {tuple(state.shape)} must be [n_slots, {C}]")
     if slots is not None:
         _expect(slots, "slots", (n,), torch.int32, dev)
-    _sizes32(n, t, C, state.shape[0])
+    m = state.shape[0]
+    if n > _INT_MAX or t > _INT_MAX or C > _INT_MAX or m > _INT_MAX:
+        raise ValueError(f"sizes {(n, t, C, m)} do not fit 32 bits")
     if out is None:
         out = _new(x.shape, dt, dev, stream)
     else:
         _expect(out, "out", x.shape, dt, dev)
     st = _call(lib.vda_recur_step, dev, x.data_ptr(), g.data_ptr(), n, t, C, GATES[gate],
-               int(dt == torch.float32), _ptr(slots), state.shape[0], state.data_ptr(), out.data_ptr(),
+               int(dt == torch.float32), _ptr(slots), m, state.data_ptr(), out.data_ptr(),
                _stream_ptr(dev, stream))
     _check(st, "vda_recur_step")
     return out
