@@ -877,9 +877,10 @@ typedef struct vda_recur_problem {
  *  - S_in: the states the sequences start from, [n_seqs][C] fp32, or NULL
  *    (zero).  S_out: the states that they end with, likewise, or NULL.  An empty
  *    sequence's state passes through.
- *  - work: a caller-owned DEVICE buffer of vda_recur_forward_workspace(p) bytes
- *    (may be NULL where that is 0); its contents need not be kept.  Calls that may
- *    run at the same time need buffers of their own.
+ *  - work: a caller-owned DEVICE buffer of vda_recur_forward_workspace(p) bytes,
+ *    queried with the call's device current (may be NULL where that is 0); its
+ *    contents need not be kept.  Calls that may run at the same time need buffers of
+ *    their own.
  * No sum's order depends on timing.  x, g, out, states and work 16-byte aligned,
  * cu_seqlens 4-byte; no output or work buffer may overlap an input or another
  * output.  Nothing is allocated or copied: the call can be captured into a
@@ -889,7 +890,8 @@ typedef struct vda_recur_problem {
 int vda_recur_forward(const vda_recur_problem* p, const void* x, const void* g, const float* S_in,
                       void* out, float* S_out, void* work, hipStream_t stream);
 
-/* Bytes of the work buffer of vda_recur_forward (0 also for an invalid problem). */
+/* Bytes of the work buffer of vda_recur_forward on the current device, whose
+ * compute units say how sequences are cut (0 also for an invalid problem). */
 size_t vda_recur_forward_workspace(const vda_recur_problem* p);
 
 /*

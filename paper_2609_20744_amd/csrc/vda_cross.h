@@ -107,8 +107,10 @@ __device__ __forceinline__ bool place_of(const CrossArgs& a, int& hk, int& t) {
 // places as it needs or one more, so no table is made and every place is found from the
 // offsets alone.  Both lists are loaded before either is waited for.
 // Sorted (the queries' side): up to 63 sequences packed on both sides, those with most states
-// first, so that none of their tiles is left for the end (24 uneven sequences of 16411 tokens,
-// 9601 states and 8 key heads: 101 -> 90 us; of one length 0 to 4% more for the search).  A lane
+// first, so that none of their tiles is left for the end.  24 uneven sequences of 16411 tokens and
+// 9601 states, D = 128, eight draws of lengths: with 4 key heads of 2 63 -> 49 us in the mean (0.58 to
+// 0.97 of the time), with 8 106 -> 95 (0.81 to 0.98), with 16 182 -> 178 (0.94 to 1.02); of one length the
+// search costs 6 to 11% with up to 8 heads and up to 6% with more.  A lane
 // has a sequence; its tiles begin behind those of all with more states.
 template <bool KEYS>
 __device__ __forceinline__ bool seq_of_tile(const CrossArgs& a, int per, int t, CrossSeq& s, int& tile) {

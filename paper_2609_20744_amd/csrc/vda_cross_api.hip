@@ -103,7 +103,10 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
   if (c.few && groups_q <= cus && states <= 128 * waves) {
     // A workgroup a CU, 128 states a wave: no join to launch.  One sequence of 16 heads and 512
     // states, D = 128: 11.6 us where ranges of single waves and a join took 15.5 us (captured,
-    // 9.6 and 9.8 us); of 2048 states 16 to 20 us against 10 us captured.
+    // 9.6 and 9.8 us).  Of 768 states the one launch still takes 12.6 us for 14.3, but captured 17.0
+    // for 14.7 (640: 11.6 and 14.4, captured 16.0 and 14.8; 1024: 14.8 and 14.3, captured 19.0 and 14.9;
+    // 2048: 23 and 14), and in fp32, two waves, 33 us for 25 at 384 states: so the limit is where it
+    // loses in neither.
     c.few = waves;
     c.splits = 1;
   } else if (c.few) {
@@ -134,6 +137,8 @@ CrossPlan plan_of(const vda_cross_problem* p, int n_slots, bool backward) {
     // CU of below; 16384 of 16 heads 277 and 310 us).  Otherwise about three a CU, so that
     // sequences of uneven length even out (16401 rows over 9 sequences 386 us, 410 us with one a
     // CU, 420 us with six), of 512 rows at least, as each range's sums are written and added up.
+    // Eight ranges at most bound the workspace; where the groups are fewer than an eighth of the CUs these
+    // do not fill the device.
     const long long each = groups < cus ? (rows + cus / groups - 1) / (cus / groups) : std::max(512LL, rows * groups / (3 * cus));
     // No longer than the rows that there are, so that a range is an int where they are.
     const long long range = (std::clamp(each, 1LL, std::max(most, 1LL)) + 63) / 64 * 64;
@@ -171,7 +176,8 @@ CrossArgs args_of(const vda_cross_problem* p, const CrossPlan& c, int n_slots, v
   a.s = std::max(a.flip ? -p->scale : p->scale, 1e-37f), a.c = std::max(a.s * vda::kLog2e, 1e-37f);
   auto near = [&](const CrossStrides& s) { return (64 * s.tok + a.group * s.head) * (p->is_f32 ? 4 : 2) < (size_t)1 << 31; };
   a.near = near(a.sq) && near(a.so);
-  // With heads that share out evenly over the 8 XCDs: of 5 heads, 24 sequences of 1000 x 600 took 64 us sorted, 53 us not.
+  // With heads that share out evenly over the 8 XCDs: of 5 heads, 24 sequences of 1000 x 600 took 64 us sorted, 53 us not,
+  // and uneven ones between 0.92 and 1.09 of the time; of 12 heads nothing gained.
   a.sorted = pq && pk && p->n_seqs < 64 && !c.few && (p->H_k % 8 == 0 || 8 % p->H_k == 0);
   // Less than a workgroup a CU in the gradient of q: products are cheap then, and what roundings leave does not average out.
   a.fine = !p->is_f32 && (long long)c.tiles * p->H_k < vda::current_device_cus();

@@ -27,8 +27,9 @@ __device__ __forceinline__ float weight_of(const CrossArgs& a, float score, floa
 // D is summed from p dP in a pass before, in fp32, where at most kExactTiles tiles have a state that is
 // seen, and of at most kExactStates wherever a mask leaves them.  As dout out it has
 // the rounding of out, whose part in dS is as large as the others where a few states share
-// the weight: of 4 to 60 states dq and dk were 2.8e-3 of their norm off (bf16), 2.4e-3 with this
-// pass; of 200 states 2.5e-3 and 2.4e-3, of 500 and more 2.4e-3 without it (D = 128, even lengths).
+// the weight: of 2, 5, 30 and 60 states that are seen dq and dk were 4.5, 3.1, 2.6 and 2.5e-3 of their norm
+// off (bf16, D = 128), 2.4e-3 with this pass; of 65 to 200 scattered ones 2.5e-3, of 500 and more 2.4e-3
+// without it.
 // It is two products more: 1560 rows x 128 states of 24 heads 42 -> 47 us, 32760 x 226 488 -> 592 us
 // for the whole backward pass.  A state that is seen alone leaves dS = 0, not a remainder; in fp32,
 // whose error the rounding does not show in, that is all the pass is for.
@@ -38,7 +39,7 @@ __device__ __forceinline__ float weight_of(const CrossArgs& a, float score, floa
 constexpr int kExactTiles = 4, kExactStates = 64;
 
 // dq: as the forward kernel, with dP beside the scores.  9 uneven sequences of 16401 tokens, 4607
-// states and 8 key heads of 2, D = 128: 148 us, 630 TFLOP/s of its three products; fp32, 2 x 333
+// states and 8 key heads of 2, D = 128: 152 us, 610 TFLOP/s of its three products; fp32, 2 x 333
 // rows x 77 states of 4 heads, D = 64: 14 us, two tiles of dependent fp32 products.
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossArgs a) {
@@ -231,8 +232,10 @@ __global__ __launch_bounds__(kThreads, F32 ? 1 : 2) void cross_dq_kernel(CrossAr
 // Shape of the kernel of dk and dv: 128 states a workgroup, 32 a wave.  In bf16
 // two waves have the same states and every other 32 rows, so that each SIMD has two
 // waves whose products and exponentials overlap; to leave them 256 registers, v
-// comes from LDS and k alone is held.  With four waves and both held the batch of above took
-// 735 us in all where it took 407 then.  Now 252 us of 373, 500 TFLOP/s of its four products: sequences
+// comes from LDS and k alone is held.  That is not quite enough: D = 128 spills 9 registers (22 of 512
+// in fp32), D = 32 10 of the 128 that its launch bound leaves.  With four waves and both held the batch of
+// above took 735 us in all where it took 407 then.  Now 260 us beside 152 for dq and 18 for the sums,
+// 485 TFLOP/s of its four products: sequences
 // end inside tiles of 128 states, and 3.7 rounds of workgroups of uneven work stand
 // where 4096 x 4096 of 16 heads, 4 sequences, keeps 1000 TFLOP/s of both kernels' products.
 template <bool F32>

@@ -128,10 +128,10 @@ __device__ __forceinline__ void put_rows(const CrossArgs& a, const Row& row, con
 // Many rows: 128 of them, 32 a wave, and tiles of 64 states in two places of LDS, the next one
 // copied while one is used.  q and the output go through LDS too, so that memory is asked
 // for whole rows (with 16 bytes of each of 32 rows to an instruction 264 us instead of 251).  Two
-// workgroups a CU: 237 registers a wave.  Bound by the products and the exponentials beside
+// workgroups a CU: 229 registers a wave.  Bound by the products and the exponentials beside
 // them, in sequences of few tiles by memory too, which is hardly overlapped: 32760 x 4096 of 24
-// heads, D = 128, 1086 TFLOP/s (8192^3 by the library: 1115), 32760 x 512 247 us, 835 TFLOP/s, of
-// which about 80 us are q and the output; fp32 108 to 115 TFLOP/s (139).  Several tiles of rows
+// heads, D = 128, 1086 TFLOP/s (8192^3 by the library: 1115), 32760 x 512 247 to 257 us, 835 to 800 TFLOP/s,
+// of which about 80 us are q and the output; fp32 108 to 115 TFLOP/s (139).  Several tiles of rows
 // a workgroup, without or with q loaded ahead, and first workgroups that start at other times
 // changed nothing or spilled.
 template <bool F32, int D>
