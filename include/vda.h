@@ -833,7 +833,8 @@ size_t vda_cross_step_workspace(const vda_cross_problem* p, int n_slots);
 
 /* How a token's gate g gives its decay a and what it adds, u. */
 typedef enum {
-  VDA_GATE_LOG = 0,   /* a = exp(g), u = x: g fp32, <= 0 (-inf resets the state)   */
+  VDA_GATE_LOG = 0,   /* a = exp(g), u = x: g fp32, <= 0 (-inf, or what exp takes to
+                         0, resets the state, infinities and NaN in it included) */
   VDA_GATE_LOGIT = 1, /* a = sigmoid(g), u = (1 - a) x: g in the storage type     */
   VDA_GATE_NORM = 2   /* a = sigmoid(g), u = sqrt(1 - a^2) x: likewise            */
 } vda_gate;

@@ -63,6 +63,14 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& b) {
     a = __builtin_amdgcn_rcpf(1.f + e), b = e * a;
   }
 }
+// The state h behind a token, or a stretch of tokens, of decay a that adds u.  A decay of 0 forgets h,
+// whatever it is: 0 times an infinity or NaN would keep it.
+__device__ __forceinline__ float after(float a, float h, float u) { return a == 0.f ? u : fmaf(a, h, u); }
+// ... of one token: a sigmoid is never 0.
+template <int GATE>
+__device__ __forceinline__ float after(float a, float h, float u) {
+  return GATE == VDA_GATE_LOG ? after(a, h, u) : fmaf(a, h, u);
+}
 // What x is multiplied by.
 template <int GATE>
 __device__ __forceinline__ float weight_of(float a, float b) {
@@ -191,7 +199,7 @@ __device__ __forceinline__ float scan_runs(const RunTable& t, RunStates& to, flo
 #pragma unroll
   for (int i = 0; i < kRecurRuns; ++i) {
     to[i][c] = h;
-    h = fmaf(A[i], h, H[i]);
+    h = after(A[i], h, H[i]);
   }
   return h;
 }
@@ -313,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void recur_apply_kernel(RecurArgs a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) H[e] = fmaf(al[i][e], H[e], u[i][e]);
+        for (int e = 0; e < 8; ++e) H[e] = after<GATE>(al[i][e], H[e], u[i][e]);
         if (full || p + i < end) store8<F32>(a.out, row_at(a, r, p + i) * a.C + w.chan, H);
       }
     }
@@ -416,14 +424,14 @@ __global__ __launch_bounds__(64 * kCarryWaves) void recur_carry_kernel(RecurArgs
   lds_barrier();
   const size_t st = (size_t)seq * a.C + chan;
   float h = real && a.S_in != nullptr ? a.S_in[st] : 0.f;
-  for (int w = 0; w < wave; ++w) h = fmaf(sA[w][lane], h, sH[w][lane]);
+  for (int w = 0; w < wave; ++w) h = after(sA[w][lane], h, sH[w][lane]);
   float e = real && a.dS_out != nullptr ? a.dS_out[st] : 0.f;
   for (int w = kCarryWaves - 1; w > wave; --w) e = fmaf(sA[w][lane], e, sG[w][lane]);
   if (!real) return;
 #pragma unroll 8
   for (int t = from; t < to; ++t) {
     const size_t at = base + (size_t)t * a.C;
-    const float next = fmaf(a.A[at], h, a.H[at]);
+    const float next = after(a.A[at], h, a.H[at]);
     a.H[at] = h;
     h = next;
   }
@@ -505,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
     for (int e = 0; e < 8; ++e) {
       dg[i][e] = H[e];  // the state before the token
       dx[i][e] = weight_of<GATE>(al[i][e], b[i][e]);
-      H[e] = fmaf(al[i][e], H[e], dx[i][e] * t.x.value(i, e));
+      H[e] = after<GATE>(al[i][e], H[e], dx[i][e] * t.x.value(i, e));
     }
 #pragma unroll
   for (int i = N - 1; i >= 0; --i)
@@ -514,7 +522,7 @@ __global__ __launch_bounds__(kThreads) void recur_grad_kernel(RecurArgs a) {
       const bool is = p + i < r.len;
       const float x = t.x.value(i, e), d = (is ? y.value(i, e) : 0.f) + G[e], ai = al[i][e];
       if constexpr (GATE == VDA_GATE_LOG)
-        dg[i][e] *= d * ai;
+        dg[i][e] = ai == 0.f ? 0.f : dg[i][e] * (d * ai);
       else if constexpr (GATE == VDA_GATE_LOGIT)
         dg[i][e] = d * ai * b[i][e] * (dg[i][e] - x);
       else
@@ -565,7 +573,7 @@ __global__ __launch_bounds__(kThreads) void recur_step_kernel(RecurStepArgs a) {
     for (int e = 0; e < 4; ++e) {
       float al, b;
       gate_of<GATE>(g[e], al, b);
-      h[e] = fmaf(al, h[e], weight_of<GATE>(al, b) * x[e]);
+      h[e] = after<GATE>(al, h[e], weight_of<GATE>(al, b) * x[e]);
     }
     if constexpr (F32)
       *reinterpret_cast<floatx4*>((float*)a.out + at) = h;
